@@ -1,7 +1,9 @@
-"""Build libbdcommit.so in-tree with nvcc for sm_103a.
+"""Build libbdcommit.so and libbdcache.so in-tree with nvcc for sm_103a.
 
+libbdcommit.so holds the sources of csrc/, libbdcache.so those of csrc/cache/;
+each exports the C ABI of its headers under include/ only.
 Each translation unit (CUDA .cu, host-only C++ .cpp) is compiled in
-parallel, then linked into one shared library (static CUDA runtime, no
+parallel, then linked into its shared library (static CUDA runtime, no
 link-time dependency on libcuda: the tensor-map encoder is fetched through the
 runtime's driver entry point).
 A stamp of the sources and flags skips the build when nothing changed.
@@ -23,6 +25,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libbdcommit.so")
 LIB_CHECKS = os.path.join(PKG, "libbdcommit_checks.so")
+CSRC_CACHE = os.path.join(CSRC, "cache")
+LIB_CACHE = os.path.join(PKG, "libbdcache.so")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ARCH + [
@@ -38,15 +42,15 @@ def _nvcc() -> str:
     raise RuntimeError("nvcc not found: the CUDA toolkit is required to build libbdcommit")
 
 
-def _sources():
-    return sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cu", ".cpp")))
+def _sources(src_dir=CSRC):
+    return sorted(os.path.join(src_dir, f) for f in os.listdir(src_dir) if f.endswith((".cu", ".cpp")))
 
 
-def _stamp(nvcc: str, extra) -> str:
+def _stamp(nvcc: str, extra, src_dir=CSRC) -> str:
     h = hashlib.sha256()
     h.update(" ".join([nvcc] + NVCC_FLAGS + list(extra)).encode())
-    files = _sources() + sorted(
-        os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cuh", ".h"))
+    files = _sources(src_dir) + sorted(
+        os.path.join(d, f) for d in {CSRC, src_dir} for f in os.listdir(d) if f.endswith((".cuh", ".h"))
     ) + sorted(os.path.join(INCLUDE, f) for f in os.listdir(INCLUDE) if f.endswith(".h"))
     for f in files:
         h.update(f.encode())
@@ -56,17 +60,27 @@ def _stamp(nvcc: str, extra) -> str:
 
 
 def build(verbose: bool = False, force: bool = False, extra_flags=(), checks: bool = False) -> str:
-    """Compile every source and link libbdcommit.so; returns its path.
+    """Compile every source and link libbdcommit.so and libbdcache.so; returns the path of libbdcommit.so.
 
     checks=True builds the bounds-checked variant instead (-DBD_CHECKS:
     device-side index checks that set a status bit rather than access out of
-    range) as libbdcommit_checks.so, in its own build directory."""
+    range) as libbdcommit_checks.so, in its own build directory
+    (libbdcache.so has no such variant: it checks the page numbers it is given in every build)."""
+    extra_flags = list(extra_flags)
+    if checks:
+        return _build_one(CSRC, BUILD + "_checks", LIB_CHECKS, "bd_*", verbose, force, extra_flags + ["-DBD_CHECKS"])
+    with ThreadPoolExecutor(max_workers=2) as ex:
+        libs = [ex.submit(_build_one, CSRC, BUILD, LIB, "bd_*", verbose, force, extra_flags),
+                ex.submit(_build_one, CSRC_CACHE, os.path.join(BUILD, "cache"), LIB_CACHE, "bdkv_*", verbose, force,
+                          extra_flags)]
+        return [f.result() for f in libs][0]
+
+
+def _build_one(src_dir, build_dir, lib, symbols, verbose, force, extra_flags) -> str:
     nvcc = _nvcc()
-    build_dir, lib = (BUILD + "_checks", LIB_CHECKS) if checks else (BUILD, LIB)
-    extra_flags = list(extra_flags) + (["-DBD_CHECKS"] if checks else [])
     os.makedirs(build_dir, exist_ok=True)
-    stamp_file = os.path.join(build_dir, "libbdcommit.stamp")
-    stamp = _stamp(nvcc, extra_flags)
+    stamp_file = os.path.join(build_dir, "build.stamp")
+    stamp = _stamp(nvcc, extra_flags, src_dir)
     if not force and os.path.exists(lib) and os.path.exists(stamp_file):
         with open(stamp_file) as f:
             if f.read().strip() == stamp:
@@ -82,13 +96,13 @@ def build(verbose: bool = False, force: bool = False, extra_flags=(), checks: bo
             sys.stderr.write(r.stdout + r.stderr)
         return obj
 
-    srcs = _sources()
+    srcs = _sources(src_dir)
     with ThreadPoolExecutor(max_workers=min(8, len(srcs))) as ex:
         objs = list(ex.map(compile_one, srcs))
     tmp = lib + ".tmp"
     exports = os.path.join(build_dir, "exports.map")
     with open(exports, "w") as f:
-        f.write("{ global: bd_*; local: *; };\n")  # only the C ABI is visible
+        f.write("{ global: %s; local: *; };\n" % symbols)  # only the C ABI is visible
     cmd = [nvcc] + ARCH + ["-shared", "-cudart", "static", "-Xlinker", "--version-script=" + exports,
                            "-o", tmp] + objs + ["-ldl"]  # libdl: the NVTX trace ranges load a tracer on demand
     r = subprocess.run(cmd, capture_output=True, text=True)

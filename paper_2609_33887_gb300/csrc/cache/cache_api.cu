@@ -1,0 +1,189 @@
+// The C entry points of libbdcache (bdcache.h): argument checks, workspaces,
+// kernel choice. Checks come before any CUDA call.
+#include <atomic>
+#include <climits>
+#include <cmath>
+
+#include "cache.h"
+#include "trace.h"
+
+namespace {
+
+// Compute capability and SM count of the current device, cached (0 = unknown, -1 = another device than sm_103).
+std::atomic<int> g_sms[64];
+
+int check_device(int* sms) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return BD_ERR_CUDA;
+  if (dev < 0 || dev >= 64) return BD_ERR_DEVICE;
+  int s = g_sms[dev].load(std::memory_order_relaxed);
+  if (s == 0) {
+    int maj = 0, mnr = 0, n = 0;
+    if (cudaDeviceGetAttribute(&maj, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&mnr, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+      return BD_ERR_CUDA;
+    s = maj == 10 && mnr == 3 ? n : -1;
+    g_sms[dev].store(s, std::memory_order_relaxed);
+  }
+  *sms = s;
+  return s > 0 ? BD_OK : BD_ERR_DEVICE;
+}
+
+int cuda_status(cudaError_t e) {
+  if (e == cudaSuccess) return BD_OK;
+  return e == cudaErrorNoKernelImageForDevice || e == cudaErrorInvalidDeviceFunction ? BD_ERR_DEVICE : BD_ERR_CUDA;
+}
+
+bool aligned(const void* p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+bool page_size_ok(int p) { return p == 16 || p == 32 || p == 64 || p == 128 || p == 256; }
+
+constexpr int64_t MAX_STRIDE = int64_t(1) << 40;
+
+int check_strides(const int64_t* s, int n, int64_t multiple) {
+  for (int i = 0; i < n; ++i) {
+    if (s[i] < 0 || s[i] > MAX_STRIDE) return BD_ERR_SHAPE;
+    if (s[i] % multiple != 0) return BD_ERR_ALIGN;
+  }
+  return BD_OK;
+}
+
+int check_cache(const bdkv_cache& c) {
+  if (!page_size_ok(c.page_size) || c.n_heads < 1 || c.n_heads > 1024 || c.head_dim < 16 || c.head_dim > 128 ||
+      c.head_dim % 16 != 0)
+    return BD_ERR_SHAPE;
+  if (c.n_pages < 0 || c.n_pages > INT_MAX || c.k_scale_stride < 0 || c.v_scale_stride < 0 ||
+      c.k_scale_stride > MAX_STRIDE || c.v_scale_stride > MAX_STRIDE)
+    return BD_ERR_SHAPE;
+  if (int rc = check_strides(c.k_stride, 3, 16)) return rc;
+  if (int rc = check_strides(c.v_stride, 3, 16)) return rc;
+  if (c.n_pages > 0 && (!c.k || !c.v || !c.k_scale || !c.v_scale)) return BD_ERR_NULL;
+  return aligned(c.k, 16) && aligned(c.v, 16) ? BD_OK : BD_ERR_ALIGN;
+}
+
+int check_rows(const bdkv_rows& r) {
+  if (r.dtype != BDKV_BF16 && r.dtype != BDKV_F16) return BD_ERR_DTYPE;
+  const int64_t s[2] = {r.stride_token, r.stride_head};
+  if (int rc = check_strides(s, 2, 8)) return rc;
+  return aligned(r.data, 16) ? BD_OK : BD_ERR_ALIGN;
+}
+
+}  // namespace
+
+extern "C" {
+
+int bdkv_tables(const bdkv_tables_args* args, void* stream) {
+  bd::TraceRange trace("bdkv_tables");
+  if (args == nullptr) return BD_ERR_NULL;
+  const bdkv_tables_args& a = *args;
+  if (a.n_seq < 0 || a.n_seq > bdkv::MAX_SEQ_TABLES || !page_size_ok(a.page_size) || a.max_blocks < 0 ||
+      a.max_tokens < 0 || a.table_stride < a.max_blocks || a.ring_size < 1 || a.ring_size > INT_MAX)
+    return BD_ERR_SHAPE;
+  if (!a.free_pages || !a.pool_in || !a.pool_out || !a.query_start ||
+      (a.n_seq > 0 && (!a.lens || !a.new_tokens || !a.kv_lens || !a.status || (a.max_blocks > 0 && !a.block_table))) ||
+      (a.max_tokens > 0 && (!a.slot_map || !a.positions)))
+    return BD_ERR_NULL;
+  if (a.pool_out == a.pool_in || (a.n_seq > 0 && a.kv_lens == a.lens)) return BD_ERR_ARG;
+  if (!aligned(a.pool_in, 8) || !aligned(a.pool_out, 8) || !aligned(a.slot_map, 8) || !aligned(a.positions, 4) ||
+      !aligned(a.lens, 4) || !aligned(a.new_tokens, 4) || !aligned(a.block_table, 4) || !aligned(a.free_pages, 4) ||
+      !aligned(a.kv_lens, 4) || !aligned(a.query_start, 4) || !aligned(a.status, 4))
+    return BD_ERR_ALIGN;
+  int sms = 0;
+  if (int rc = check_device(&sms)) return rc;
+  return cuda_status(bdkv::launch_tables(a, sms, static_cast<cudaStream_t>(stream)));
+}
+
+int bdkv_write(const bdkv_cache* cache, const bdkv_rows* k, const bdkv_rows* v, const int64_t* slot_map,
+               int64_t n_tokens, void* stream) {
+  bd::TraceRange trace("bdkv_write");
+  if (!cache || !k || !v) return BD_ERR_NULL;
+  if (int rc = check_cache(*cache)) return rc;
+  if (int rc = check_rows(*k)) return rc;
+  if (int rc = check_rows(*v)) return rc;
+  if (k->dtype != v->dtype) return BD_ERR_DTYPE;
+  if (n_tokens < 0 || n_tokens > INT_MAX) return BD_ERR_SHAPE;
+  if (n_tokens == 0) return BD_OK;
+  if (!k->data || !v->data || !slot_map) return BD_ERR_NULL;
+  if (!aligned(slot_map, 8)) return BD_ERR_ALIGN;
+  int sms = 0;
+  if (int rc = check_device(&sms)) return rc;
+  return cuda_status(
+      bdkv::launch_write(*cache, *k, *v, slot_map, n_tokens, sms, static_cast<cudaStream_t>(stream)));
+}
+
+}  // extern "C"
+
+namespace {
+
+int check_attention(const bdkv_cache* cache, const bdkv_attention_args* args) {
+  if (!cache || !args) return BD_ERR_NULL;
+  const bdkv_cache& c = *cache;
+  const bdkv_attention_args& a = *args;
+  if (int rc = check_cache(c)) return rc;
+  if (int rc = check_rows(a.q)) return rc;
+  if (int rc = check_rows(a.out)) return rc;
+  if (a.out.dtype != a.q.dtype) return BD_ERR_DTYPE;
+  if (a.n_seq < 0 || a.n_seq > 65535 || a.n_q_heads < 1 || a.n_q_heads % c.n_heads != 0 ||
+      a.n_q_heads / c.n_heads > 64 || a.max_q_len < 0 || a.max_kv_len < 0 || a.max_blocks < 0 ||
+      a.table_stride < a.max_blocks || a.table_stride > MAX_STRIDE ||
+      a.max_kv_len > int64_t(a.max_blocks) * c.page_size ||
+      int64_t(a.max_q_len) * (a.n_q_heads / c.n_heads) > (1 << 26))
+    return BD_ERR_SHAPE;
+  if (a.mask_block < 0 || !std::isfinite(a.scale)) return BD_ERR_ARG;
+  if (a.n_seq > 0 && a.max_q_len > 0) {
+    if (!a.q.data || !a.out.data || !a.kv_lens || !a.query_start || (a.max_blocks > 0 && !a.block_table))
+      return BD_ERR_NULL;
+    if (!aligned(a.kv_lens, 4) || !aligned(a.query_start, 4) || !aligned(a.block_table, 4) || !aligned(a.lse, 4) ||
+        !aligned(a.workspace, 256))
+      return BD_ERR_ALIGN;
+  }
+  return BD_OK;
+}
+
+bdkv::AttnArgs attn_args(const bdkv_cache& c, const bdkv_attention_args& a) {
+  bdkv::AttnArgs r = {};
+  r.k = c.k, r.v = c.v, r.ks = c.k_scale, r.vs = c.v_scale;
+  r.k_page = c.k_stride[0], r.k_tok = c.k_stride[1], r.k_head = c.k_stride[2];
+  r.v_page = c.v_stride[0], r.v_tok = c.v_stride[1], r.v_head = c.v_stride[2];
+  r.ks_page = c.k_scale_stride, r.vs_page = c.v_scale_stride;
+  r.n_pages = c.n_pages;
+  while ((1 << r.page_shift) < c.page_size) ++r.page_shift;
+  r.dim = c.head_dim, r.n_kv = c.n_heads, r.group = a.n_q_heads / c.n_heads;
+  r.q = a.q.data, r.q_tok = a.q.stride_token, r.q_head = a.q.stride_head;
+  r.out = a.out.data, r.o_tok = a.out.stride_token, r.o_head = a.out.stride_head;
+  r.lse = a.lse;
+  r.table = a.block_table, r.table_stride = a.table_stride, r.max_blocks = a.max_blocks;
+  r.kv_lens = a.kv_lens, r.q_start = a.query_start;
+  r.n_seq = a.n_seq, r.max_q = a.max_q_len, r.max_kv = a.max_kv_len, r.mask_block = a.mask_block;
+  r.coef = a.scale * bd::LOG2E;
+  r.f16 = a.q.dtype == BDKV_F16;
+  return r;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t bdkv_attention_workspace(const bdkv_cache* cache, const bdkv_attention_args* args) {
+  if (check_attention(cache, args) != BD_OK) return 0;
+  return 0;
+}
+
+int bdkv_attention(const bdkv_cache* cache, const bdkv_attention_args* args) {
+  bd::TraceRange trace("bdkv_attention");
+  if (int rc = check_attention(cache, args)) return rc;
+  if (args->n_seq == 0 || args->max_q_len == 0) return BD_OK;
+  int sms = 0;
+  if (int rc = check_device(&sms)) return rc;
+  return cuda_status(
+      bdkv::launch_attn_rows(attn_args(*cache, *args), sms, static_cast<cudaStream_t>(args->stream)));
+}
+
+int bdkv_get_device_status(void* stream) {
+  return cudaStreamSynchronize(static_cast<cudaStream_t>(stream)) == cudaSuccess ? BD_OK : BD_ERR_CUDA;
+}
+
+int bdkv_shutdown(void) { return BD_OK; }
+
+}  // extern "C"
