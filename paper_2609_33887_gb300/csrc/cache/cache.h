@@ -40,9 +40,21 @@ struct AttnArgs {
   int n_seq, max_q, max_kv, mask_block;
   float coef;  // scale * log2(e)
   bool f16;
+  // Work split along the cache: part p of n_split takes tokens [p chunk, (p + 1) chunk). A row that sees at most `chunk`
+  // tokens is written by part 0; of the others each part leaves its output (fp32, divided by its sum of weights) and
+  // log2-sum-exp in part_o [row, part, dim] and part_l [row, part], row = (seq max_q + query) n_q + head.
+  int chunk, n_split;
+  float* part_o;
+  float* part_l;
 };
 
-cudaError_t launch_attn_rows(const AttnArgs& a, int sm_count, cudaStream_t st);
+constexpr int ROWS_TILE = 16;    // rows of a CTA of the two attention kernels (the second: one or two tiles of as many)
+constexpr int TILES_TILE = 128;
+cudaError_t launch_attn_rows(const AttnArgs& a, cudaStream_t st);
+cudaError_t launch_attn_tiles(const AttnArgs& a, cudaStream_t st);
+cudaError_t launch_attn_join(const AttnArgs& a, cudaStream_t st);
+// Reads and clears the device status bits of the current device.
+cudaError_t tiles_status(cudaStream_t st, uint32_t* bits);
 
 #ifdef __CUDACC__
 // 2^k for whole k in -126..127.
@@ -77,26 +89,70 @@ struct F16 {
 };
 __device__ __forceinline__ uint32_t f16x2(float2 x) { return F16::from_float2(x); }
 
-// One request's lengths, cut to the call's bounds.
+// One request's lengths; q_len and kv_len cut to the call's bounds.
 struct Seq {
-  int q0, q_len, kv_len, shown;  // shown: kv_len - the request's whole q_len, what its first query has before it
+  int q0, q_len, kv_len;
+  int q_all, shown;  // its whole q_len, and what its first query has before it
 };
 __device__ __forceinline__ Seq load_seq(const AttnArgs& a, int s) {
   Seq r;
   r.q0 = a.q_start[s];
-  const int q_len = max(a.q_start[s + 1] - r.q0, 0);
-  r.q_len = min(q_len, a.max_q);
+  r.q_all = max(a.q_start[s + 1] - r.q0, 0);
+  r.q_len = min(r.q_all, a.max_q);
   const int kv = max(a.kv_lens[s], 0);
-  r.shown = kv - q_len;
+  r.shown = kv - r.q_all;
   r.kv_len = min(kv, a.max_kv);
   return r;
 }
-// Tokens that query i of the request sees.
-__device__ __forceinline__ int visible(const AttnArgs& a, const Seq& s, int q_len_all, int i) {
+// Tokens that query i of the request sees (no fewer for a later query).
+__device__ __forceinline__ int visible(const AttnArgs& a, const Seq& s, int i) {
   if (a.mask_block == 0) return s.kv_len;
-  const int64_t end = (static_cast<int64_t>(i) / a.mask_block + 1) * a.mask_block;
-  const int n = s.shown + static_cast<int>(end < q_len_all ? end : q_len_all);
-  return min(max(n, 0), s.kv_len);
+  const int64_t end = (static_cast<int64_t>(i / a.mask_block) + 1) * a.mask_block;
+  return min(max(s.shown + static_cast<int>(end < s.q_all ? end : s.q_all), 0), s.kv_len);
+}
+
+// Where a part's result for one row goes: the call's outputs, the workspace, or nowhere.
+struct RowOut {
+  uint16_t* out;  // null: a partial result
+  float* o;
+  float* l;  // the log-sum-exp (null: none wanted)
+};
+__device__ __forceinline__ RowOut row_out(const AttnArgs& a, const Seq& s, int seq, int part, int i, int h, int vis) {
+  RowOut r = {nullptr, nullptr, nullptr};
+  const int64_t n_q = static_cast<int64_t>(a.n_kv) * a.group, tok = static_cast<int64_t>(s.q0) + i;
+  if (vis <= a.chunk) {
+    if (part == 0) {
+      r.out = static_cast<uint16_t*>(a.out) + tok * a.o_tok + h * a.o_head;
+      if (a.lse != nullptr) r.l = a.lse + tok * n_q + h;
+    }
+  } else {
+    const int64_t at = ((static_cast<int64_t>(seq) * a.max_q + i) * n_q + h) * a.n_split + part;
+    r.o = a.part_o + at * a.dim;
+    r.l = a.part_l + at;
+  }
+  return r;
+}
+template <class T>
+__device__ __forceinline__ void store4(const RowOut& r, int d, float4 x) {
+  if (r.out != nullptr)
+    *reinterpret_cast<uint2*>(r.out + d) =
+        make_uint2(T::from_float2(make_float2(x.x, x.y)), T::from_float2(make_float2(x.z, x.w)));
+  else if (r.o != nullptr)
+    *reinterpret_cast<float4*>(r.o + d) = x;
+}
+template <class T>
+__device__ __forceinline__ void store8(const RowOut& r, int d, float4 x, float4 y) {
+  if (r.out != nullptr) {
+    *reinterpret_cast<uint4*>(r.out + d) =
+        make_uint4(T::from_float2(make_float2(x.x, x.y)), T::from_float2(make_float2(x.z, x.w)),
+                   T::from_float2(make_float2(y.x, y.y)), T::from_float2(make_float2(y.z, y.w)));
+  } else if (r.o != nullptr) {
+    *reinterpret_cast<float4*>(r.o + d) = x;
+    *reinterpret_cast<float4*>(r.o + d + 4) = y;
+  }
+}
+__device__ __forceinline__ void store_lse(const RowOut& r, float lse2) {
+  if (r.l != nullptr) *r.l = r.out != nullptr ? lse2 / bd::LOG2E : lse2;
 }
 
 // Exponent s with amax * 2^s in [2^14, 2^15), for query rows held in f16: a bf16 element keeps its eight

@@ -3,6 +3,7 @@
 #include <atomic>
 #include <climits>
 #include <cmath>
+#include <mutex>
 
 #include "cache.h"
 #include "trace.h"
@@ -163,11 +164,85 @@ bdkv::AttnArgs attn_args(const bdkv_cache& c, const bdkv_attention_args& a) {
 
 }  // namespace
 
+namespace {
+
+// How a call runs: the kernel, and its split along the cache.
+struct Plan {
+  bool tiles;
+  int chunk, n_split;
+  int64_t part_rows;  // rows of partial results
+  size_t bytes;       // of workspace
+};
+
+// The kernel: up to 16 rows per key/value head (queries times the group) fit the one tile of the row kernel.
+// The split: parts of the cache so that the CTAs fill the SMs (four times over for the row kernel, whose CTAs are
+// short; once for the other one).
+Plan make_plan(const bdkv_cache& c, const bdkv_attention_args& a, int sms) {
+  Plan p = {};
+  const int64_t rows = int64_t(a.max_q_len) * (a.n_q_heads / c.n_heads);
+  p.tiles = rows > bdkv::ROWS_TILE;
+  const int64_t tile = !p.tiles ? bdkv::ROWS_TILE : rows <= bdkv::TILES_TILE ? bdkv::TILES_TILE : 2 * bdkv::TILES_TILE;
+  const int64_t ctas = (rows + tile - 1) / tile * c.n_heads * a.n_seq;
+  const int64_t parts = p.tiles ? sms / ctas : (4 * int64_t(sms) + ctas - 1) / ctas;
+  const int64_t least = p.tiles ? 256 : 128;  // tokens
+  int64_t chunk = parts > 1 ? ((a.max_kv_len + parts - 1) / parts + 127) / 128 * 128 : a.max_kv_len;
+  if (chunk < least) chunk = least;
+  p.n_split = static_cast<int>((a.max_kv_len + chunk - 1) / chunk);
+  if (p.n_split <= 1) {
+    p.n_split = 1;
+    p.chunk = INT_MAX;
+    return p;
+  }
+  p.chunk = static_cast<int>(chunk);
+  p.part_rows = int64_t(a.n_seq) * a.max_q_len * a.n_q_heads * p.n_split;
+  p.bytes = static_cast<size_t>(p.part_rows) * (c.head_dim + 1) * sizeof(float);
+  return p;
+}
+
+// The library's own workspace of a device. Calls on different streams share it: each waits for the last one's end.
+struct Workspace {
+  void* data = nullptr;
+  size_t bytes = 0;
+  cudaEvent_t used = nullptr;
+  cudaStream_t stream = nullptr;
+};
+std::mutex g_mu;
+Workspace g_ws[64];
+
+int own_workspace(size_t bytes, cudaStream_t st, Workspace** out) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return BD_ERR_CUDA;
+  cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+  if (cudaStreamIsCapturing(st, &capture) != cudaSuccess) return BD_ERR_CUDA;
+  if (capture != cudaStreamCaptureStatusNone) return BD_ERR_WORKSPACE;
+  Workspace& w = g_ws[dev];
+  if (w.used == nullptr && cudaEventCreateWithFlags(&w.used, cudaEventDisableTiming) != cudaSuccess) return BD_ERR_CUDA;
+  if (w.bytes < bytes) {
+    if (w.data) cudaFree(w.data);  // synchronises the device: no call can still use it
+    w.data = nullptr;
+    w.bytes = 0;
+    if (cudaMalloc(&w.data, bytes) != cudaSuccess) {
+      cudaGetLastError();
+      return BD_ERR_CUDA;
+    }
+    w.bytes = bytes;
+  } else if (w.stream != st && cudaStreamWaitEvent(st, w.used) != cudaSuccess) {
+    return BD_ERR_CUDA;
+  }
+  w.stream = st;
+  *out = &w;
+  return BD_OK;
+}
+
+}  // namespace
+
 extern "C" {
 
 size_t bdkv_attention_workspace(const bdkv_cache* cache, const bdkv_attention_args* args) {
-  if (check_attention(cache, args) != BD_OK) return 0;
-  return 0;
+  int sms = 0;
+  if (check_attention(cache, args) != BD_OK || args->n_seq == 0 || args->max_q_len == 0 || check_device(&sms) != BD_OK)
+    return 0;
+  return make_plan(*cache, *args, sms).bytes;
 }
 
 int bdkv_attention(const bdkv_cache* cache, const bdkv_attention_args* args) {
@@ -176,14 +251,48 @@ int bdkv_attention(const bdkv_cache* cache, const bdkv_attention_args* args) {
   if (args->n_seq == 0 || args->max_q_len == 0) return BD_OK;
   int sms = 0;
   if (int rc = check_device(&sms)) return rc;
-  return cuda_status(
-      bdkv::launch_attn_rows(attn_args(*cache, *args), sms, static_cast<cudaStream_t>(args->stream)));
+  const cudaStream_t st = static_cast<cudaStream_t>(args->stream);
+  const Plan plan = make_plan(*cache, *args, sms);
+  bdkv::AttnArgs a = attn_args(*cache, *args);
+  a.chunk = plan.chunk;
+  a.n_split = plan.n_split;
+  const auto run = [&](void* ws) {
+    a.part_o = static_cast<float*>(ws);
+    a.part_l = a.part_o + plan.part_rows * cache->head_dim;
+    cudaError_t e = plan.tiles ? bdkv::launch_attn_tiles(a, st) : bdkv::launch_attn_rows(a, st);
+    if (e == cudaSuccess && plan.n_split > 1) e = bdkv::launch_attn_join(a, st);
+    return cuda_status(e);
+  };
+  if (plan.bytes == 0) return run(nullptr);
+  if (args->workspace != nullptr) return args->workspace_bytes < plan.bytes ? BD_ERR_WORKSPACE : run(args->workspace);
+  std::lock_guard<std::mutex> lock(g_mu);
+  Workspace* w = nullptr;
+  if (int rc = own_workspace(plan.bytes, st, &w)) return rc;
+  const int rc = run(w->data);
+  return cudaEventRecord(w->used, st) == cudaSuccess ? rc : BD_ERR_CUDA;
 }
 
 int bdkv_get_device_status(void* stream) {
-  return cudaStreamSynchronize(static_cast<cudaStream_t>(stream)) == cudaSuccess ? BD_OK : BD_ERR_CUDA;
+  int sms = 0;
+  if (int rc = check_device(&sms)) return rc;
+  uint32_t bits = 0;
+  if (bdkv::tiles_status(static_cast<cudaStream_t>(stream), &bits) != cudaSuccess) return BD_ERR_CUDA;
+  return bits ? BD_ERR_TIMEOUT : BD_OK;
 }
 
-int bdkv_shutdown(void) { return BD_OK; }
+int bdkv_shutdown(void) {
+  std::lock_guard<std::mutex> lock(g_mu);
+  int cur = 0;
+  if (cudaGetDevice(&cur) != cudaSuccess) return BD_ERR_CUDA;
+  for (int dev = 0; dev < 64; ++dev) {
+    Workspace& w = g_ws[dev];
+    if (w.used == nullptr || cudaSetDevice(dev) != cudaSuccess) continue;
+    if (w.data) cudaFree(w.data);
+    cudaEventDestroy(w.used);
+    w = Workspace();
+  }
+  cudaSetDevice(cur);
+  return BD_OK;
+}
 
 }  // extern "C"

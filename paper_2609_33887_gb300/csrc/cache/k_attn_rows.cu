@@ -59,7 +59,7 @@ constexpr size_t smem_bytes() {
   return ring > merge ? ring : merge;
 }
 
-// One CTA: 16 rows of a request's key/value head, its whole cache.
+// One CTA: 16 rows of a request's key/value head, one part of its cache.
 template <class T, int D>
 __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(AttnArgs a) {
   constexpr int CH = D / 16;  // 16-byte chunks of a token's row; also k-steps
@@ -67,11 +67,16 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(AttnArgs a) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ float sm_m[WARPS][16], sm_M[WARPS][16], sm_L[WARPS][16];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = lane >> 2, c = lane & 3;
-  const int head = blockIdx.y, seq = blockIdx.z, row0 = blockIdx.x * 16;
+  const int seq = blockIdx.z, part = blockIdx.y;
+  const int head = blockIdx.x % a.n_kv, row0 = blockIdx.x / a.n_kv * ROWS_TILE;
   const Seq sq = load_seq(a, seq);
-  const int q_all = max(a.q_start[seq + 1] - sq.q0, 0);
   const int rows = sq.q_len * a.group;
   if (row0 >= rows) return;
+  // later queries see at least as much, so the CTA's last row bounds it
+  const int begin = part * a.chunk;
+  const int end = min(visible(a, sq, (min(rows, row0 + ROWS_TILE) - 1) / a.group), begin + a.chunk);
+  if (part > 0 && end <= begin) return;
+  bd::griddep_launch_dependents();
 
   // queries as A fragments, in f16 times a power of two per row
   uint32_t qf[CH][4];
@@ -81,9 +86,9 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(AttnArgs a) {
   for (int r = 0; r < 2; ++r) {
     const int row = row0 + n + 8 * r, i = row / a.group;
     const bool live = row < rows;
-    const uint16_t* q = static_cast<const uint16_t*>(a.q) + (sq.q0 + i) * a.q_tok +
+    const uint16_t* q = static_cast<const uint16_t*>(a.q) + static_cast<int64_t>(sq.q0 + i) * a.q_tok +
                         (static_cast<int64_t>(head) * a.group + row - i * a.group) * a.q_head;
-    vis[r] = live ? visible(a, sq, q_all, i) : 0;
+    vis[r] = live ? visible(a, sq, i) : 0;
     float2 x[CH][2];
     float amax = 0.f;
 #pragma unroll
@@ -108,18 +113,14 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(AttnArgs a) {
 
   float O[VB][4] = {};
   float m[2] = {-INFINITY, -INFINITY}, M[2] = {-INFINITY, -INFINITY}, L[2] = {0.f, 0.f};
-  int end = max(vis[0], vis[1]);
-#pragma unroll
-  for (int d = 4; d < 32; d <<= 1) end = max(end, __shfl_xor_sync(~0u, end, d));
-
-  const int n_steps = (end + STEP - 1) / STEP;
+  const int n_steps = end > begin ? (end - begin + STEP - 1) / STEP : 0;
   const uint32_t ring = bd::smem_u32(smem) + warp * (STAGES * STEP * D * 2);
   int scales[STAGES];  // of the steps in flight: key byte, value byte << 8
 
   auto fetch = [&](int step, int stage) -> int {
     int got = 0;
     if (step < n_steps) {
-      const int t0 = step * STEP, col = t0 >> a.page_shift;
+      const int t0 = begin + step * STEP, col = t0 >> a.page_shift;
       const int64_t page = col < a.max_blocks ? a.table[seq * a.table_stride + col] : -1;
       const bool ok = page >= 0 && page < a.n_pages;
       const int64_t p = ok ? page : 0;
@@ -179,8 +180,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(AttnArgs a) {
       float x[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int t = step * STEP + (e >> 1) * 8 + 2 * c + (e & 1);
-        x[e] = t < vis[r] ? S[e >> 1][2 * r + (e & 1)] * f : -INFINITY;
+        const int t = begin + step * STEP + (e >> 1) * 8 + 2 * c + (e & 1);
+        x[e] = t < min(vis[r], end) ? S[e >> 1][2 * r + (e & 1)] * f : -INFINITY;
       }
       float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
       top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
@@ -276,13 +277,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(AttnArgs a) {
       o.x += x.x * f, o.y += x.y * f, o.z += x.z * f, o.w += x.w * f;
     }
     const float f = Lt == 0.f ? 0.f : bd::ex2_approx(Ms - P_SHIFT - ms) / Lt;
-    const int i = row / a.group, h = head * a.group + row - i * a.group;
-    const int64_t tok = sq.q0 + i;
-    if (d < a.dim)
-      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + tok * a.o_tok + h * a.o_head + d) =
-          make_uint2(T::from_float2(make_float2(o.x * f, o.y * f)), T::from_float2(make_float2(o.z * f, o.w * f)));
-    if (d == 0 && a.lse != nullptr)
-      a.lse[tok * (static_cast<int64_t>(a.n_kv) * a.group) + h] = Lt == 0.f ? -INFINITY : (ms + log2f(Lt)) / bd::LOG2E;
+    const int i = row / a.group;
+    const RowOut dst = row_out(a, sq, seq, part, i, head * a.group + row - i * a.group, visible(a, sq, i));
+    if (d < a.dim) store4<T>(dst, d, make_float4(o.x * f, o.y * f, o.z * f, o.w * f));
+    if (d == 0) store_lse(dst, Lt == 0.f ? -INFINITY : ms + log2f(Lt));
   }
 }
 
@@ -291,15 +289,14 @@ cudaError_t launch(const AttnArgs& a, cudaStream_t st) {
   cudaError_t e = cudaFuncSetAttribute(attn_rows_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                        smem_bytes<D>());
   if (e != cudaSuccess) return e;
-  const dim3 grid((a.max_q * a.group + 15) / 16, a.n_kv, a.n_seq);
+  const dim3 grid((a.max_q * a.group + ROWS_TILE - 1) / ROWS_TILE * a.n_kv, a.n_split, a.n_seq);
   attn_rows_kernel<T, D><<<grid, WARPS * 32, smem_bytes<D>(), st>>>(a);
   return cudaGetLastError();
 }
 
 }  // namespace
 
-cudaError_t launch_attn_rows(const AttnArgs& a, int sm_count, cudaStream_t st) {
-  (void)sm_count;
+cudaError_t launch_attn_rows(const AttnArgs& a, cudaStream_t st) {
   if (a.dim <= 64) return a.f16 ? launch<F16, 64>(a, st) : launch<Bf16, 64>(a, st);
   return a.f16 ? launch<F16, 128>(a, st) : launch<Bf16, 128>(a, st);
 }

@@ -1,0 +1,465 @@
+// bdkv_attention for many query rows per key/value head: windows of blocks,
+// prompts. tcgen05 products on tiles of 128 rows by 128 cached tokens.
+//
+// A CTA holds NM x 128 rows of a request's key/value head (queries x the
+// group's heads, so the head's cache is read once for all of them) and walks
+// the cache in tiles of 128 tokens:
+//   converter warps   codes from global memory to f16 (exact), into shared
+//                     memory in the 128-byte swizzle, double buffered; a
+//                     request's tail is zeros, so its values times zero
+//                     weights stay zero
+//   MMA warp          S = Q K^T (both operands in shared memory) and O += P V
+//                     (P in tensor memory, V read with the token index along
+//                     K); S of one half runs while the other half's softmax does
+//   softmax warps     a thread per row: running maxima, weights to f16, written
+//                     over S in tensor memory; O is rescaled only when a row's
+//                     maximum has grown by more than 2^3
+// Scales of pages come in through the exponent: w = 2^(S coef k_scale + e_v),
+// see k_attn_rows.cu; O and the sum L have a reference maximum of their own.
+#include "cache.h"
+
+namespace bdkv {
+namespace {
+
+constexpr int TILE = TILES_TILE;  // rows of an MMA, tokens of a tile
+constexpr float P_SHIFT = 12, P_SLACK = 3;
+constexpr int CONV_WARPS = 4;
+
+__device__ uint32_t g_status;  // bd::DEV_* bits
+
+struct Ctl {
+  uint64_t q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], pv_done[2], drain;
+  float ks[4][8], ve[4][8];  // page scales of a tile's eight groups of 16 tokens: factor, exponent
+  uint32_t tmem_base;
+  int abort_flag;
+};
+
+__device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+__device__ __forceinline__ void st_shared_v4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+// D[tmem] (+)= A[tmem] * B[smem], f16: row i of A in lane i, two elements per 32-bit column.
+__device__ __forceinline__ void umma_f16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
+                                            uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+// B operand stored with N contiguous (128-byte swizzle, atoms of 64 elements of
+// N by 8 of K): `lead` bytes between atoms along N, 1 KB along K.
+__device__ __forceinline__ uint64_t sw128_mnmajor_desc(uint32_t saddr, uint32_t lead) {
+  uint64_t d = 0;
+  d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
+  d |= static_cast<uint64_t>(lead >> 4) << 16;
+  d |= static_cast<uint64_t>(1024u >> 4) << 32;
+  d |= static_cast<uint64_t>(1u) << 46;
+  d |= static_cast<uint64_t>(2u) << 61;
+  return d;
+}
+constexpr uint32_t B_MN_MAJOR = 1u << 16;
+
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+      : "memory");
+}
+
+template <int NM, int D>
+constexpr size_t smem_bytes() {
+  return size_t(NM + 4) * TILE * D * 2 + sizeof(Ctl) + 1024;
+}
+
+// Sixteen codes to f16, two 16-byte chunks.
+__device__ __forceinline__ void decode16(uint4 x, uint32_t (&y)[8]) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y[2 * i] = bd::e4m3x2_to_f16x2(w[i] & 0xffffu);
+    y[2 * i + 1] = bd::e4m3x2_to_f16x2(w[i] >> 16);
+  }
+}
+
+template <class T, int NM, int D>
+__global__ void __launch_bounds__((4 * NM + CONV_WARPS + 1) * 32, 1) attn_tiles_kernel(AttnArgs a) {
+  constexpr int ATOMS = D / 64;             // 128-byte column blocks of a row
+  constexpr uint32_t ATOM = TILE * 128;     // bytes of one, 128 rows
+  constexpr uint32_t OPERAND = ATOMS * ATOM;
+  constexpr int CH = D / 16;                // 16-code chunks of a token's row
+  constexpr int O_COL = 256;                // tensor memory: S and P at 0 and 128, O behind
+  extern __shared__ uint8_t raw[];
+  const uint32_t base = (bd::smem_u32(raw) + 1023u) & ~1023u;
+  const uint32_t q_at = base, k_at = q_at + NM * OPERAND, v_at = k_at + 2 * OPERAND;
+  Ctl* ctl = reinterpret_cast<Ctl*>(raw + (v_at + 2 * OPERAND - bd::smem_u32(raw)));
+  const int tid = threadIdx.x, warp = static_cast<int>(bd::warp_uniform(tid >> 5));
+  const int n_tiles_rows = gridDim.x / a.n_kv;
+  const int head = blockIdx.x / n_tiles_rows, row0 = (n_tiles_rows - 1 - blockIdx.x % n_tiles_rows) * (NM * TILE);
+  const int seq = blockIdx.z, part = blockIdx.y;
+  const Seq sq = load_seq(a, seq);
+  const int rows = sq.q_len * a.group;
+  if (row0 >= rows) return;
+  // later queries see at least as much, so the CTA's last row bounds it
+  const int i_last = (min(rows, row0 + NM * TILE) - 1) / a.group;
+  const int begin = part * a.chunk, end = min(visible(a, sq, i_last), begin + a.chunk);
+  if (part > 0 && end <= begin) return;
+  const int n = end > begin ? (end - begin + TILE - 1) / TILE : 0;
+
+  if (tid == 0) {
+    bd::mbar_init(bd::smem_u32(&ctl->q_full), NM * TILE);
+    for (int i = 0; i < 2; ++i) {
+      bd::mbar_init(bd::smem_u32(&ctl->k_full[i]), CONV_WARPS * 32);
+      bd::mbar_init(bd::smem_u32(&ctl->v_full[i]), CONV_WARPS * 32);
+      bd::mbar_init(bd::smem_u32(&ctl->k_empty[i]), 1);
+      bd::mbar_init(bd::smem_u32(&ctl->v_empty[i]), 1);
+      bd::mbar_init(bd::smem_u32(&ctl->s_full[i]), 1);
+      bd::mbar_init(bd::smem_u32(&ctl->p_full[i]), TILE);
+      bd::mbar_init(bd::smem_u32(&ctl->pv_done[i]), 1);
+    }
+    bd::mbar_init(bd::smem_u32(&ctl->drain), 1);
+    ctl->abort_flag = 0;
+    bd::fence_mbar_init();
+  }
+  constexpr int MMA_WARP = 4 * NM + CONV_WARPS;
+  if (warp == MMA_WARP) {
+    bd::tmem_alloc(bd::smem_u32(&ctl->tmem_base), 512);
+    bd::tmem_relinquish();
+  }
+  bd::tc_fence_before();
+  __syncthreads();
+  bd::tc_fence_after();
+  const uint32_t tmem = bd::warp_uniform(ctl->tmem_base);
+  volatile int* abort_flag = &ctl->abort_flag;
+  const auto wait = [&](uint64_t& bar, int phase) {
+    return bd::mbar_wait_warp(bd::smem_u32(&bar), static_cast<uint32_t>(phase & 1), abort_flag, &g_status);
+  };
+  bd::griddep_launch_dependents();
+
+  if (warp == MMA_WARP) {
+    // ---------------------------------------------------------- MMA issuer
+    const bool leader = bd::elect_one();
+    constexpr uint32_t IDESC_S = bd::idesc_f16_f32(TILE, TILE), IDESC_O = bd::idesc_f16_f32(TILE, D) | B_MN_MAJOR;
+    const auto scores = [&](int x, int j) {  // S in slot x
+      if (leader) {
+        const uint32_t qa = q_at + (NM == 2 ? x * OPERAND : 0), kb = k_at + (j & 1) * OPERAND;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k)
+          bd::umma_bf16(tmem + x * TILE, bd::sw128_kmajor_desc(qa + (k / 4) * ATOM) + 2u * (k % 4),
+                        bd::sw128_kmajor_desc(kb + (k / 4) * ATOM) + 2u * (k % 4), IDESC_S, k != 0);
+        bd::umma_commit(bd::smem_u32(&ctl->s_full[x]));
+        if (NM == 1 || x == NM - 1) bd::umma_commit(bd::smem_u32(&ctl->k_empty[j & 1]));
+      }
+      __syncwarp();
+    };
+    bool ok = n > 0 && wait(ctl->q_full, 0);
+    bd::tc_fence_after();
+    for (int j = 0; ok && j < (NM == 1 ? min(n, 2) : 1); ++j) {
+      ok = wait(ctl->k_full[j & 1], 0);
+      bd::tc_fence_after();
+      if (ok)
+        for (int x = 0; x < NM; ++x) scores(NM == 1 ? j : x, j);
+    }
+    for (int j = 0; ok && j < n; ++j) {
+      for (int x = 0; x < NM; ++x) {
+        const int slot = NM == 1 ? j & 1 : x;
+        ok = ok && wait(ctl->p_full[slot], NM == 1 ? j >> 1 : j);
+        if (x == 0) ok = ok && wait(ctl->v_full[j & 1], j >> 1);
+        if (!ok) break;
+        bd::tc_fence_after();
+        if (leader) {
+          const uint32_t vb = v_at + (j & 1) * OPERAND;
+#pragma unroll
+          for (int k = 0; k < TILE / 16; ++k)
+            umma_f16_ta(tmem + O_COL + x * TILE, tmem + slot * TILE + k * 8,
+                        sw128_mnmajor_desc(vb + k * 2048, ATOM), IDESC_O, (j | k) != 0);
+          bd::umma_commit(bd::smem_u32(&ctl->pv_done[x]));
+          if (x == NM - 1) bd::umma_commit(bd::smem_u32(&ctl->v_empty[j & 1]));
+        }
+        __syncwarp();
+        const int next = NM == 1 ? j + 2 : j + 1;
+        if (next < n) {
+          if (x == 0) ok = wait(ctl->k_full[next & 1], next >> 1);
+          if (!ok) break;
+          bd::tc_fence_after();
+          scores(slot, next);
+        }
+      }
+    }
+    if (leader) {  // all MMAs issued have completed once `drain` flips
+      bd::umma_commit(bd::smem_u32(&ctl->drain));
+      bd::mbar_drain(bd::smem_u32(&ctl->drain), 0);
+    }
+    __syncwarp();
+  } else if (warp >= 4 * NM) {
+    // ---------------------------------------------------------- converters
+    const int ct = tid - 4 * NM * 32;
+    constexpr int PER = TILE * CH / (CONV_WARPS * 32);  // chunks of a thread and tile
+    constexpr int STEP = CONV_WARPS * 32 / CH;          // rows between them
+    const int sub = ct % CH, mine = ct / CH;
+    const int64_t row_k = a.k_tok, row_v = a.v_tok;
+    const uint8_t* kp = a.k + head * a.k_head + sub * 16;
+    const uint8_t* vp = a.v + head * a.v_head + sub * 16;
+    const int32_t* table = a.table + seq * a.table_stride;
+    const int mask = (1 << a.page_shift) - 1;
+    uint4 kx[PER], vx[PER];
+    const auto load = [&](const uint8_t* p, int64_t page_stride, int64_t tok_stride, int j, uint4 (&x)[PER]) {
+#pragma unroll
+      for (int u = 0; u < PER; ++u) {
+        const int t = begin + j * TILE + mine + u * STEP, col = t >> a.page_shift;
+        x[u] = make_uint4(0, 0, 0, 0);
+        if (t < end && sub * 16 < a.dim) {
+          const int64_t page = col < a.max_blocks ? table[col] : -1;
+          if (page >= 0 && page < a.n_pages)
+            x[u] = *reinterpret_cast<const uint4*>(p + page * page_stride + (t & mask) * tok_stride);
+        }
+      }
+    };
+    const auto store = [&](uint32_t at, const uint4 (&x)[PER]) {
+#pragma unroll
+      for (int u = 0; u < PER; ++u) {
+        const int r = mine + u * STEP;
+        uint32_t y[8];
+        decode16(x[u], y);
+        const uint32_t rowp = at + (sub / 4) * ATOM + r * 128;
+        // the lanes of the second atom store their second chunk first: the two atoms' lanes meet in different banks
+        const bool flip = sub >= 4;
+        const int c0 = (sub % 4) * 2 + flip;
+        st_shared_v4(rowp + ((c0 ^ (r & 7)) << 4), flip ? y[4] : y[0], flip ? y[5] : y[1], flip ? y[6] : y[2],
+                     flip ? y[7] : y[3]);
+        st_shared_v4(rowp + (((c0 ^ 1) ^ (r & 7)) << 4), flip ? y[0] : y[4], flip ? y[1] : y[5], flip ? y[2] : y[6],
+                     flip ? y[3] : y[7]);
+      }
+    };
+    if (n > 0) {
+      load(kp, a.k_page, row_k, 0, kx);
+      load(vp, a.v_page, row_v, 0, vx);
+    }
+    bool ok = true;
+    for (int j = 0; j < n; ++j) {
+      ok = wait(ctl->k_empty[j & 1], (j >> 1) + 1);
+      if (!ok) break;
+      if (ct < 8) {
+        const int t = begin + j * TILE + ct * 16, col = t >> a.page_shift;
+        const int64_t page = t < end && col < a.max_blocks ? table[col] : -1;
+        const bool in = page >= 0 && page < a.n_pages;
+        ctl->ks[j & 3][ct] = in ? pow2i(a.ks[page * a.ks_page + head] - 127) : 1.f;
+        ctl->ve[j & 3][ct] = in ? static_cast<float>(a.vs[page * a.vs_page + head] - 127) : 0.f;
+      }
+      store(k_at + (j & 1) * OPERAND, kx);
+      fence_proxy_async();
+      bd::mbar_arrive(bd::smem_u32(&ctl->k_full[j & 1]));
+      if (j + 1 < n) load(kp, a.k_page, row_k, j + 1, kx);
+      ok = wait(ctl->v_empty[j & 1], (j >> 1) + 1);
+      if (!ok) break;
+      store(v_at + (j & 1) * OPERAND, vx);
+      fence_proxy_async();
+      bd::mbar_arrive(bd::smem_u32(&ctl->v_full[j & 1]));
+      if (j + 1 < n) load(vp, a.v_page, row_v, j + 1, vx);
+    }
+  } else {
+    // ------------------------------------------------------------- softmax
+    const int x = NM == 2 ? warp >> 2 : 0;  // half
+    const int r = tid & 127, row = row0 + x * TILE + r, i = row / a.group;
+    const bool live = row < rows;
+    const int h = head * a.group + row - i * a.group;
+    const int vis = live ? min(visible(a, sq, i), end) : 0;
+    float coef = 0.f;
+    if (n > 0) {
+      // the row in f16 times a power of two, with the sign of the scale
+      const uint16_t* q = static_cast<const uint16_t*>(a.q) + static_cast<int64_t>(sq.q0 + i) * a.q_tok + h * a.q_head;
+      uint4 w[D / 8];
+      float amax = 0.f;
+#pragma unroll
+      for (int c = 0; c < D / 8; ++c) {
+        w[c] = make_uint4(0, 0, 0, 0);
+        if (live && c * 8 < a.dim) w[c] = *reinterpret_cast<const uint4*>(q + c * 8);
+        const uint32_t ww[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const float2 f = T::to_float2(ww[u]);
+          amax = bd::max3(amax, fabsf(f.x), fabsf(f.y));
+        }
+      }
+      const int s = row_shift(amax);
+      const float f = a.coef < 0.f ? -pow2i(s) : pow2i(s);
+      coef = fabsf(a.coef) * pow2i(-s);
+#pragma unroll
+      for (int c = 0; c < D / 8; ++c) {
+        const uint32_t ww[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
+        uint32_t y[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const float2 v = T::to_float2(ww[u]);
+          y[u] = f16x2(make_float2(v.x * f, v.y * f));
+        }
+        st_shared_v4(q_at + x * OPERAND + (c / 8) * ATOM + r * 128 + (((c % 8) ^ (r & 7)) << 4), y[0], y[1], y[2], y[3]);
+      }
+      fence_proxy_async();
+      bd::mbar_arrive(bd::smem_u32(&ctl->q_full));
+    }
+
+    const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t o_at = tmem + lanes + O_COL + x * TILE;
+    const bool any_live = __any_sync(~0u, live);
+    float m = -INFINITY, M = -INFINITY, L = 0.f;
+    bool ok = true;
+    for (int j = 0; j < n; ++j) {
+      const int slot = NM == 1 ? j & 1 : x;
+      ok = wait(ctl->s_full[slot], NM == 1 ? j >> 1 : j);
+      if (!ok) break;
+      bd::tc_fence_after();
+      if (any_live) {
+        const uint32_t s_at = tmem + lanes + slot * TILE;
+        const int left = vis - (begin + j * TILE);  // columns this row sees
+        const bool cut = __any_sync(~0u, left < TILE);
+        const float* ks = ctl->ks[j & 3];
+        const float* ve = ctl->ve[j & 3];
+        float s_top = -INFINITY, u_top = -INFINITY;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          float v[32];
+          bd::tmem_ld32(s_at + c * 32, v);
+          if (cut)
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+              if (c * 32 + e >= left) v[e] = -INFINITY;
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            float t = v[b * 16];
+#pragma unroll
+            for (int e = 1; e < 15; e += 2) t = bd::max3(t, v[b * 16 + e], v[b * 16 + e + 1]);
+            t = fmaxf(t, v[b * 16 + 15]);
+            const float s2 = t == -INFINITY ? t : t * (coef * ks[c * 2 + b]);
+            s_top = fmaxf(s_top, s2);
+            u_top = fmaxf(u_top, s2 + ve[c * 2 + b]);
+          }
+        }
+        if (s_top > m) {
+          L *= bd::ex2_approx(m - s_top);
+          m = s_top;
+        }
+        const bool grow = u_top > M + P_SLACK || (M == -INFINITY && u_top > M);
+        if (__any_sync(~0u, grow)) {
+          if (j > 0) {
+            ok = wait(ctl->pv_done[x], j - 1);
+            if (!ok) break;
+            bd::tc_fence_after();
+            const float f = grow ? bd::ex2_approx(M - u_top) : 1.f;
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+              float v[32];
+              bd::tmem_ld32(o_at + c * 32, v);
+              uint32_t y[32];
+#pragma unroll
+              for (int e = 0; e < 32; ++e) y[e] = __float_as_uint(v[e] * f);
+              bd::tmem_st32(o_at + c * 32, y);
+            }
+          }
+          if (grow) M = u_top;
+        }
+        const float ms = m == -INFINITY ? 0.f : m, Ms = M == -INFINITY ? 0.f : M;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          float v[32];
+          bd::tmem_ld32(s_at + c * 32, v);
+          uint32_t p[16];
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            const float f = coef * ks[c * 2 + b], ref = Ms - ve[c * 2 + b] - P_SHIFT;
+            float2 sum = {0.f, 0.f};
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+              const float2 y = bd::fma2(make_float2(v[b * 16 + e], v[b * 16 + e + 1]), make_float2(f, f),
+                                        make_float2(-ref, -ref));
+              float2 w = make_float2(bd::ex2_approx(y.x), bd::ex2_approx(y.y));
+              if (cut) {
+                if (c * 32 + b * 16 + e >= left) w.x = 0.f;
+                if (c * 32 + b * 16 + e + 1 >= left) w.y = 0.f;
+              }
+              sum = bd::add2(sum, w);
+              p[b * 8 + e / 2] = f16x2(w);
+            }
+            L += (sum.x + sum.y) * bd::ex2_approx(ref - ms);
+          }
+          tmem_st16(s_at + c * 16, p);
+        }
+        bd::tmem_st_wait();
+      }
+      bd::tc_fence_before();
+      bd::mbar_arrive(bd::smem_u32(&ctl->p_full[slot]));
+    }
+
+    if (n > 0 && ok) ok = wait(ctl->pv_done[x], n - 1);
+    bd::tc_fence_after();
+    const float ms = m == -INFINITY ? 0.f : m, Ms = M == -INFINITY ? 0.f : M;
+    const float f = L == 0.f ? 0.f : bd::ex2_approx(Ms - P_SHIFT - ms) / L;
+    const float lse2 = L == 0.f ? -INFINITY : ms + log2f(L);
+    RowOut o = {nullptr, nullptr, nullptr};
+    if (live) o = row_out(a, sq, seq, part, i, h, visible(a, sq, i));
+    if (any_live) {
+#pragma unroll 1
+      for (int c = 0; c < D / 32; ++c) {
+        float v[32];
+        if (n > 0)
+          bd::tmem_ld32(o_at + c * 32, v);
+        else
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 32; e += 8)
+          if (c * 32 + e < a.dim)
+            store8<T>(o, c * 32 + e, make_float4(v[e] * f, v[e + 1] * f, v[e + 2] * f, v[e + 3] * f),
+                      make_float4(v[e + 4] * f, v[e + 5] * f, v[e + 6] * f, v[e + 7] * f));
+      }
+      if (live) store_lse(o, lse2);
+    }
+  }
+
+  __syncwarp();
+  bd::tc_fence_before();
+  __syncthreads();
+  bd::tc_fence_after();
+  if (warp == MMA_WARP) bd::tmem_dealloc(tmem, 512);
+}
+
+template <class T, int NM, int D>
+cudaError_t launch(const AttnArgs& a, cudaStream_t st) {
+  cudaError_t e = cudaFuncSetAttribute(attn_tiles_kernel<T, NM, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       smem_bytes<NM, D>());
+  if (e != cudaSuccess) return e;
+  const int tiles = (a.max_q * a.group + NM * TILE - 1) / (NM * TILE);
+  const dim3 grid(tiles * a.n_kv, a.n_split, a.n_seq);
+  attn_tiles_kernel<T, NM, D><<<grid, (4 * NM + CONV_WARPS + 1) * 32, smem_bytes<NM, D>(), st>>>(a);
+  return cudaGetLastError();
+}
+
+template <class T>
+cudaError_t launch_type(const AttnArgs& a, cudaStream_t st) {
+  const bool one = a.max_q * a.group <= TILE;
+  if (a.dim <= 64) return one ? launch<T, 1, 64>(a, st) : launch<T, 2, 64>(a, st);
+  return one ? launch<T, 1, 128>(a, st) : launch<T, 2, 128>(a, st);
+}
+
+}  // namespace
+
+cudaError_t launch_attn_tiles(const AttnArgs& a, cudaStream_t st) {
+  return a.f16 ? launch_type<F16>(a, st) : launch_type<Bf16>(a, st);
+}
+
+cudaError_t tiles_status(cudaStream_t st, uint32_t* bits) {
+  cudaError_t e = cudaMemcpyFromSymbolAsync(bits, g_status, sizeof *bits, 0, cudaMemcpyDeviceToHost, st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  if (e != cudaSuccess || *bits == 0) return e;
+  const uint32_t zero = 0;
+  e = cudaMemcpyToSymbolAsync(g_status, &zero, sizeof zero, 0, cudaMemcpyHostToDevice, st);
+  return e == cudaSuccess ? cudaStreamSynchronize(st) : e;
+}
+
+}  // namespace bdkv
