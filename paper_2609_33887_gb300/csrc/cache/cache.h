@@ -2,6 +2,7 @@
 // the kernel translation units, and the device helpers they share.
 #pragma once
 
+#include <atomic>
 #include <cstddef>
 #include <cstdint>
 #include <cuda_runtime.h>
@@ -57,6 +58,17 @@ cudaError_t launch_attn_join(const AttnArgs& a, cudaStream_t st);
 cudaError_t tiles_status(cudaStream_t st, uint32_t* bits);
 
 #ifdef __CUDACC__
+// Lets `kernel` use `bytes` of dynamic shared memory on the current device, once per device.
+template <class K>
+cudaError_t allow_smem(K kernel, size_t bytes, std::atomic<bool> (&ready)[64]) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || ready[dev].load(std::memory_order_relaxed)) return e;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+  if (e == cudaSuccess) ready[dev].store(true, std::memory_order_relaxed);
+  return e;
+}
+
 // 2^k for whole k in -126..127.
 __device__ __forceinline__ float pow2i(int k) { return __int_as_float((k + 127) << 23); }
 

@@ -286,9 +286,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(AttnArgs a) {
 
 template <class T, int D>
 cudaError_t launch(const AttnArgs& a, cudaStream_t st) {
-  cudaError_t e = cudaFuncSetAttribute(attn_rows_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       smem_bytes<D>());
-  if (e != cudaSuccess) return e;
+  static std::atomic<bool> ready[64];  // by device
+  if (cudaError_t e = allow_smem(attn_rows_kernel<T, D>, smem_bytes<D>(), ready); e != cudaSuccess) return e;
   const dim3 grid((a.max_q * a.group + ROWS_TILE - 1) / ROWS_TILE * a.n_kv, a.n_split, a.n_seq);
   attn_rows_kernel<T, D><<<grid, WARPS * 32, smem_bytes<D>(), st>>>(a);
   return cudaGetLastError();

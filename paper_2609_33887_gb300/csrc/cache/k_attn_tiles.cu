@@ -24,6 +24,10 @@ namespace {
 constexpr int TILE = TILES_TILE;  // rows of an MMA, tokens of a tile
 constexpr float P_SHIFT = 12, P_SLACK = 3;
 constexpr int CONV_WARPS = 4;
+// Warps of a CTA: 4 for each half's softmax, 4 converters, 4 of which one issues the MMAs: warpgroups, so that registers
+// can be moved between them. With two halves, 512 threads start with 128 each: 2 x 128 x 184 (a row's 128 scores stay in
+// registers) + 128 x 104 + 128 x 40 = 65536; with one, 384 threads with 168.
+constexpr int threads(int nm) { return (nm + 2) * 128; }
 
 __device__ uint32_t g_status;  // bd::DEV_* bits
 
@@ -73,6 +77,77 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
       : "memory");
 }
 
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
+      : "memory");
+}
+
+// All 128 columns of a tile for this thread's lane.
+__device__ __forceinline__ void tmem_ld128(uint32_t taddr, float (&v)[128]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
+      "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
+      "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
+      "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%128];\n\t"
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
+      "%64, %65, %66, %67, %68, %69, %70, %71, %72, %73, %74, %75, %76, %77, %78, %79, "
+      "%80, %81, %82, %83, %84, %85, %86, %87, %88, %89, %90, %91, %92, %93, %94, %95, "
+      "%96, %97, %98, %99, %100, %101, %102, %103, %104, %105, %106, %107, %108, %109, %110, %111, "
+      "%112, %113, %114, %115, %116, %117, %118, %119, %120, %121, %122, %123, %124, %125, %126, %127}, [%129];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]),
+        "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
+        "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]),
+        "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]),
+        "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]),
+        "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]),
+        "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]),
+        "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31]),
+        "=f"(v[32]), "=f"(v[33]), "=f"(v[34]), "=f"(v[35]),
+        "=f"(v[36]), "=f"(v[37]), "=f"(v[38]), "=f"(v[39]),
+        "=f"(v[40]), "=f"(v[41]), "=f"(v[42]), "=f"(v[43]),
+        "=f"(v[44]), "=f"(v[45]), "=f"(v[46]), "=f"(v[47]),
+        "=f"(v[48]), "=f"(v[49]), "=f"(v[50]), "=f"(v[51]),
+        "=f"(v[52]), "=f"(v[53]), "=f"(v[54]), "=f"(v[55]),
+        "=f"(v[56]), "=f"(v[57]), "=f"(v[58]), "=f"(v[59]),
+        "=f"(v[60]), "=f"(v[61]), "=f"(v[62]), "=f"(v[63]),
+        "=f"(v[64]), "=f"(v[65]), "=f"(v[66]), "=f"(v[67]),
+        "=f"(v[68]), "=f"(v[69]), "=f"(v[70]), "=f"(v[71]),
+        "=f"(v[72]), "=f"(v[73]), "=f"(v[74]), "=f"(v[75]),
+        "=f"(v[76]), "=f"(v[77]), "=f"(v[78]), "=f"(v[79]),
+        "=f"(v[80]), "=f"(v[81]), "=f"(v[82]), "=f"(v[83]),
+        "=f"(v[84]), "=f"(v[85]), "=f"(v[86]), "=f"(v[87]),
+        "=f"(v[88]), "=f"(v[89]), "=f"(v[90]), "=f"(v[91]),
+        "=f"(v[92]), "=f"(v[93]), "=f"(v[94]), "=f"(v[95]),
+        "=f"(v[96]), "=f"(v[97]), "=f"(v[98]), "=f"(v[99]),
+        "=f"(v[100]), "=f"(v[101]), "=f"(v[102]), "=f"(v[103]),
+        "=f"(v[104]), "=f"(v[105]), "=f"(v[106]), "=f"(v[107]),
+        "=f"(v[108]), "=f"(v[109]), "=f"(v[110]), "=f"(v[111]),
+        "=f"(v[112]), "=f"(v[113]), "=f"(v[114]), "=f"(v[115]),
+        "=f"(v[116]), "=f"(v[117]), "=f"(v[118]), "=f"(v[119]),
+        "=f"(v[120]), "=f"(v[121]), "=f"(v[122]), "=f"(v[123]),
+        "=f"(v[124]), "=f"(v[125]), "=f"(v[126]), "=f"(v[127])
+      : "r"(taddr), "r"(taddr + 64)
+      : "memory");
+}
+
+// Moves registers between the warpgroups (all four warps execute it).
+template <int N>
+__device__ __forceinline__ void take_registers() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void give_registers() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+
 template <int NM, int D>
 constexpr size_t smem_bytes() {
   return size_t(NM + 4) * TILE * D * 2 + sizeof(Ctl) + 1024;
@@ -89,7 +164,7 @@ __device__ __forceinline__ void decode16(uint4 x, uint32_t (&y)[8]) {
 }
 
 template <class T, int NM, int D>
-__global__ void __launch_bounds__((4 * NM + CONV_WARPS + 1) * 32, 1) attn_tiles_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) {
   constexpr int ATOMS = D / 64;             // 128-byte column blocks of a row
   constexpr uint32_t ATOM = TILE * 128;     // bytes of one, 128 rows
   constexpr uint32_t OPERAND = ATOMS * ATOM;
@@ -142,8 +217,10 @@ __global__ void __launch_bounds__((4 * NM + CONV_WARPS + 1) * 32, 1) attn_tiles_
   };
   bd::griddep_launch_dependents();
 
-  if (warp == MMA_WARP) {
+  if (warp >= MMA_WARP) {
     // ---------------------------------------------------------- MMA issuer
+    give_registers<40>();
+    if (warp == MMA_WARP) {
     const bool leader = bd::elect_one();
     constexpr uint32_t IDESC_S = bd::idesc_f16_f32(TILE, TILE), IDESC_O = bd::idesc_f16_f32(TILE, D) | B_MN_MAJOR;
     const auto scores = [&](int x, int j) {  // S in slot x
@@ -196,9 +273,11 @@ __global__ void __launch_bounds__((4 * NM + CONV_WARPS + 1) * 32, 1) attn_tiles_
       bd::umma_commit(bd::smem_u32(&ctl->drain));
       bd::mbar_drain(bd::smem_u32(&ctl->drain), 0);
     }
+    }
     __syncwarp();
   } else if (warp >= 4 * NM) {
     // ---------------------------------------------------------- converters
+    give_registers<104>();
     const int ct = tid - 4 * NM * 32;
     constexpr int PER = TILE * CH / (CONV_WARPS * 32);  // chunks of a thread and tile
     constexpr int STEP = CONV_WARPS * 32 / CH;          // rows between them
@@ -265,6 +344,7 @@ __global__ void __launch_bounds__((4 * NM + CONV_WARPS + 1) * 32, 1) attn_tiles_
     }
   } else {
     // ------------------------------------------------------------- softmax
+    take_registers<184>();
     const int x = NM == 2 ? warp >> 2 : 0;  // half
     const int r = tid & 127, row = row0 + x * TILE + r, i = row / a.group;
     const bool live = row < rows;
@@ -310,92 +390,98 @@ __global__ void __launch_bounds__((4 * NM + CONV_WARPS + 1) * 32, 1) attn_tiles_
     const bool any_live = __any_sync(~0u, live);
     float m = -INFINITY, M = -INFINITY, L = 0.f;
     bool ok = true;
+    // One tile: the row's scores become weights, over themselves in tensor memory. CUT: some row of the warp does not see
+    // all 128 tokens.
+    const auto softmax = [&](auto cut, int slot, int j, int left) -> bool {
+      constexpr bool CUT = decltype(cut)::value;
+      const uint32_t s_at = tmem + lanes + slot * TILE;
+      const float* ks = ctl->ks[j & 3];
+      const float* ve = ctl->ve[j & 3];
+      float v[TILE];
+      __syncwarp();
+      tmem_ld128(s_at, v);
+      float s_top = -INFINITY, u_top = -INFINITY;
+#pragma unroll
+      for (int b = 0; b < 8; ++b) {
+        if (CUT)
+#pragma unroll
+          for (int e = b * 16; e < b * 16 + 16; ++e)
+            if (e >= left) v[e] = -INFINITY;
+        float t = v[b * 16];
+#pragma unroll
+        for (int e = 1; e < 15; e += 2) t = bd::max3(t, v[b * 16 + e], v[b * 16 + e + 1]);
+        t = fmaxf(t, v[b * 16 + 15]);
+        const float s2 = CUT && t == -INFINITY ? t : t * (coef * ks[b]);
+        s_top = fmaxf(s_top, s2);
+        u_top = fmaxf(u_top, s2 + ve[b]);
+      }
+      const float m_new = fmaxf(m, s_top);
+      L *= m_new == m ? 1.f : bd::ex2_approx(m - m_new);
+      m = m_new;
+      const bool grow = u_top > M + P_SLACK || (M == -INFINITY && u_top > M);
+      if (__any_sync(~0u, grow)) {
+        if (j > 0) {
+          if (!wait(ctl->pv_done[x], j - 1)) return false;
+          bd::tc_fence_after();
+          const float f = grow ? bd::ex2_approx(M - u_top) : 1.f;
+          __syncwarp();  // tensor-memory accesses take the whole warp at once
+#pragma unroll 1
+          for (int c = 0; c < D / 16; ++c) {
+            uint32_t o[16];
+            tmem_ld16(o_at + c * 16, o);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+            tmem_st16(o_at + c * 16, o);
+          }
+        }
+        M = grow ? u_top : M;
+      }
+      __syncwarp();
+      const float ms = m == -INFINITY ? 0.f : m, Ms = M == -INFINITY ? 0.f : M;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t p[16];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const float f = coef * ks[c * 2 + b], ref = Ms - ve[c * 2 + b] - P_SHIFT;
+          float2 sum = {0.f, 0.f};
+#pragma unroll
+          for (int e = 0; e < 16; e += 2) {
+            const int col = c * 32 + b * 16 + e;
+            const float2 y = bd::fma2(make_float2(v[col], v[col + 1]), make_float2(f, f), make_float2(-ref, -ref));
+            float2 w = make_float2(bd::ex2_approx(y.x), bd::ex2_approx(y.y));
+            if (CUT) {
+              if (col >= left) w.x = 0.f;
+              if (col + 1 >= left) w.y = 0.f;
+            }
+            sum = bd::add2(sum, w);
+            p[b * 8 + e / 2] = f16x2(w);
+          }
+          L += (sum.x + sum.y) * bd::ex2_approx(ref - ms);
+        }
+        tmem_st16(s_at + c * 16, p);
+      }
+      bd::tmem_st_wait();
+      return true;
+    };
+
     for (int j = 0; j < n; ++j) {
       const int slot = NM == 1 ? j & 1 : x;
       ok = wait(ctl->s_full[slot], NM == 1 ? j >> 1 : j);
       if (!ok) break;
       bd::tc_fence_after();
       if (any_live) {
-        const uint32_t s_at = tmem + lanes + slot * TILE;
         const int left = vis - (begin + j * TILE);  // columns this row sees
-        const bool cut = __any_sync(~0u, left < TILE);
-        const float* ks = ctl->ks[j & 3];
-        const float* ve = ctl->ve[j & 3];
-        float s_top = -INFINITY, u_top = -INFINITY;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          float v[32];
-          bd::tmem_ld32(s_at + c * 32, v);
-          if (cut)
-#pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (c * 32 + e >= left) v[e] = -INFINITY;
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            float t = v[b * 16];
-#pragma unroll
-            for (int e = 1; e < 15; e += 2) t = bd::max3(t, v[b * 16 + e], v[b * 16 + e + 1]);
-            t = fmaxf(t, v[b * 16 + 15]);
-            const float s2 = t == -INFINITY ? t : t * (coef * ks[c * 2 + b]);
-            s_top = fmaxf(s_top, s2);
-            u_top = fmaxf(u_top, s2 + ve[c * 2 + b]);
-          }
-        }
-        if (s_top > m) {
-          L *= bd::ex2_approx(m - s_top);
-          m = s_top;
-        }
-        const bool grow = u_top > M + P_SLACK || (M == -INFINITY && u_top > M);
-        if (__any_sync(~0u, grow)) {
-          if (j > 0) {
-            ok = wait(ctl->pv_done[x], j - 1);
-            if (!ok) break;
-            bd::tc_fence_after();
-            const float f = grow ? bd::ex2_approx(M - u_top) : 1.f;
-#pragma unroll 1
-            for (int c = 0; c < D / 32; ++c) {
-              float v[32];
-              bd::tmem_ld32(o_at + c * 32, v);
-              uint32_t y[32];
-#pragma unroll
-              for (int e = 0; e < 32; ++e) y[e] = __float_as_uint(v[e] * f);
-              bd::tmem_st32(o_at + c * 32, y);
-            }
-          }
-          if (grow) M = u_top;
-        }
-        const float ms = m == -INFINITY ? 0.f : m, Ms = M == -INFINITY ? 0.f : M;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          float v[32];
-          bd::tmem_ld32(s_at + c * 32, v);
-          uint32_t p[16];
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            const float f = coef * ks[c * 2 + b], ref = Ms - ve[c * 2 + b] - P_SHIFT;
-            float2 sum = {0.f, 0.f};
-#pragma unroll
-            for (int e = 0; e < 16; e += 2) {
-              const float2 y = bd::fma2(make_float2(v[b * 16 + e], v[b * 16 + e + 1]), make_float2(f, f),
-                                        make_float2(-ref, -ref));
-              float2 w = make_float2(bd::ex2_approx(y.x), bd::ex2_approx(y.y));
-              if (cut) {
-                if (c * 32 + b * 16 + e >= left) w.x = 0.f;
-                if (c * 32 + b * 16 + e + 1 >= left) w.y = 0.f;
-              }
-              sum = bd::add2(sum, w);
-              p[b * 8 + e / 2] = f16x2(w);
-            }
-            L += (sum.x + sum.y) * bd::ex2_approx(ref - ms);
-          }
-          tmem_st16(s_at + c * 16, p);
-        }
-        bd::tmem_st_wait();
+        ok = __any_sync(~0u, left < TILE) ? softmax(std::true_type(), slot, j, left) : softmax(std::false_type(), slot, j, left);
+        if (!ok) break;
       }
       bd::tc_fence_before();
       bd::mbar_arrive(bd::smem_u32(&ctl->p_full[slot]));
     }
 
+    // The last tile's scores follow O's product of two tiles before it (NM == 1), so that is as far as O is known to be: a
+    // parity wait must not skip a phase.
+    if (NM == 1 && n > 1 && ok) ok = wait(ctl->pv_done[x], n - 2);
     if (n > 0 && ok) ok = wait(ctl->pv_done[x], n - 1);
     bd::tc_fence_after();
     const float ms = m == -INFINITY ? 0.f : m, Ms = M == -INFINITY ? 0.f : M;
@@ -431,12 +517,11 @@ __global__ void __launch_bounds__((4 * NM + CONV_WARPS + 1) * 32, 1) attn_tiles_
 
 template <class T, int NM, int D>
 cudaError_t launch(const AttnArgs& a, cudaStream_t st) {
-  cudaError_t e = cudaFuncSetAttribute(attn_tiles_kernel<T, NM, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       smem_bytes<NM, D>());
-  if (e != cudaSuccess) return e;
+  static std::atomic<bool> ready[64];  // by device
+  if (cudaError_t e = allow_smem(attn_tiles_kernel<T, NM, D>, smem_bytes<NM, D>(), ready); e != cudaSuccess) return e;
   const int tiles = (a.max_q * a.group + NM * TILE - 1) / (NM * TILE);
   const dim3 grid(tiles * a.n_kv, a.n_split, a.n_seq);
-  attn_tiles_kernel<T, NM, D><<<grid, (4 * NM + CONV_WARPS + 1) * 32, smem_bytes<NM, D>(), st>>>(a);
+  attn_tiles_kernel<T, NM, D><<<grid, threads(NM), smem_bytes<NM, D>(), st>>>(a);
   return cudaGetLastError();
 }
 

@@ -375,6 +375,25 @@ def test_bounds_above_the_lengths_change_nothing(q_len):
     assert torch.allclose(a.float(), b.float(), atol=2 ** -6)
 
 
+@pytest.mark.parametrize("q_len,g,total", [(1, 4, 700), (20, 4, 300), (20, 4, 900), (31, 1, 513), (70, 4, 1300)])
+def test_repeated_calls_give_the_same_bits(q_len, g, total):
+    """Also the first one, whose warps run apart (their code and data come from memory), in cleared and in used scratch."""
+    n_seq, n_kv, dim = 30, 2, 128
+    c = random_cache([total] * n_seq, 16, n_kv, dim, seed=3)
+    gen = torch.Generator(device="cuda").manual_seed(q_len)
+    args = (torch.randn(n_seq * q_len, n_kv * g, dim, generator=gen, device="cuda").to(torch.bfloat16), gpu_cache(c),
+            torch.from_numpy(c.table).cuda(), torch.from_numpy(c.kv_lens).cuda(),
+            torch.arange(0, (n_seq + 1) * q_len, q_len, dtype=torch.int32, device="cuda"))
+    bounds = dict(max_q_len=q_len, max_kv_len=total)
+    need = bdc.kv_attention_workspace(*args, **bounds)
+    raw = torch.full((need + 256,), 0xFF, dtype=torch.uint8, device="cuda")  # NaN
+    ws = raw[-raw.data_ptr() % 256:][:need] if need else None
+    torch.cuda.synchronize()
+    first = bdc.kv_attention(*args, **bounds, workspace=ws)
+    for i in range(100):
+        assert torch.equal(bdc.kv_attention(*args, **bounds, workspace=ws if i % 2 else None), first), i
+
+
 def test_page_numbers_out_of_range_are_not_read():
     c = random_cache([64, 64], 16, 1, 32, seed=10)
     c.table[1, 1], c.table[1, 2] = -1, 2 ** 31 - 1
