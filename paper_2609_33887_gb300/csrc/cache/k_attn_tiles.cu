@@ -44,14 +44,32 @@ __device__ __forceinline__ void st_shared_v4(uint32_t addr, uint32_t a, uint32_t
   asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
-// D[tmem] (+)= A[tmem] * B[smem], f16: row i of A in lane i, two elements per 32-bit column.
-__device__ __forceinline__ void umma_f16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
-                                            uint32_t accumulate) {
+// The MMA warp issues in the elected lane by predicate, not by branch: its addresses and descriptors then stay in uniform
+// registers. D[tmem] (+)= A[smem] * B[smem]^T, f16.
+__device__ __forceinline__ void mma_ss(uint32_t issue, uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
+                                       uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(issue)
+      : "memory");
+}
+// D[tmem] (+)= A[tmem] * B[smem], f16: row i of A in lane i, two elements per 32-bit column.
+__device__ __forceinline__ void mma_ts(uint32_t issue, uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
+                                       uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(issue)
+      : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t issue, uint32_t bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar),
+      "r"(issue)
       : "memory");
 }
 
@@ -153,6 +171,29 @@ constexpr size_t smem_bytes() {
   return size_t(NM + 4) * TILE * D * 2 + sizeof(Ctl) + 1024;
 }
 
+// Loads that happen where `live` says so, without a branch that would hold up the loads behind them.
+__device__ __forceinline__ int ld_global_if(const int32_t* p, bool live, int other) {
+  int x = other;
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\t@p ld.global.b32 %0, [%1];\n\t}"
+               : "+r"(x)
+               : "l"(p), "r"(static_cast<int>(live)));
+  return x;
+}
+__device__ __forceinline__ int ld_global_byte_if(const uint8_t* p, bool live) {
+  int x = 0;
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\t@p ld.global.u8 %0, [%1];\n\t}"
+               : "+r"(x)
+               : "l"(p), "r"(static_cast<int>(live)));
+  return x;
+}
+__device__ __forceinline__ uint4 ld_global_if(const uint8_t* p, bool live) {
+  uint4 x = {0, 0, 0, 0};
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %5, 0;\n\t@p ld.global.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
+               : "+r"(x.x), "+r"(x.y), "+r"(x.z), "+r"(x.w)
+               : "l"(p), "r"(static_cast<int>(live)));
+  return x;
+}
+
 // Sixteen codes to f16, two 16-byte chunks.
 __device__ __forceinline__ void decode16(uint4 x, uint32_t (&y)[8]) {
   const uint32_t w[4] = {x.x, x.y, x.z, x.w};
@@ -221,58 +262,54 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
     // ---------------------------------------------------------- MMA issuer
     give_registers<40>();
     if (warp == MMA_WARP) {
-    const bool leader = bd::elect_one();
-    constexpr uint32_t IDESC_S = bd::idesc_f16_f32(TILE, TILE), IDESC_O = bd::idesc_f16_f32(TILE, D) | B_MN_MAJOR;
-    const auto scores = [&](int x, int j) {  // S in slot x
-      if (leader) {
-        const uint32_t qa = q_at + (NM == 2 ? x * OPERAND : 0), kb = k_at + (j & 1) * OPERAND;
+      const uint32_t issue = bd::elect_one();
+      constexpr uint32_t IDESC_S = bd::idesc_f16_f32(TILE, TILE), IDESC_O = bd::idesc_f16_f32(TILE, D) | B_MN_MAJOR;
+      const uint64_t q_desc = bd::sw128_kmajor_desc(q_at), k_desc = bd::sw128_kmajor_desc(k_at);
+      const uint64_t v_desc = sw128_mnmajor_desc(v_at, ATOM);
+      const auto scores = [&](int x, int j) {  // S in slot x; addresses in descriptors count 16 bytes
+        const uint64_t qd = q_desc + (NM == 2 ? x * (OPERAND >> 4) : 0u), kd = k_desc + (j & 1) * (OPERAND >> 4);
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k)
-          bd::umma_bf16(tmem + x * TILE, bd::sw128_kmajor_desc(qa + (k / 4) * ATOM) + 2u * (k % 4),
-                        bd::sw128_kmajor_desc(kb + (k / 4) * ATOM) + 2u * (k % 4), IDESC_S, k != 0);
-        bd::umma_commit(bd::smem_u32(&ctl->s_full[x]));
-        if (NM == 1 || x == NM - 1) bd::umma_commit(bd::smem_u32(&ctl->k_empty[j & 1]));
-      }
-      __syncwarp();
-    };
-    bool ok = n > 0 && wait(ctl->q_full, 0);
-    bd::tc_fence_after();
-    for (int j = 0; ok && j < (NM == 1 ? min(n, 2) : 1); ++j) {
-      ok = wait(ctl->k_full[j & 1], 0);
-      bd::tc_fence_after();
-      if (ok)
-        for (int x = 0; x < NM; ++x) scores(NM == 1 ? j : x, j);
-    }
-    for (int j = 0; ok && j < n; ++j) {
-      for (int x = 0; x < NM; ++x) {
-        const int slot = NM == 1 ? j & 1 : x;
-        ok = ok && wait(ctl->p_full[slot], NM == 1 ? j >> 1 : j);
-        if (x == 0) ok = ok && wait(ctl->v_full[j & 1], j >> 1);
-        if (!ok) break;
-        bd::tc_fence_after();
-        if (leader) {
-          const uint32_t vb = v_at + (j & 1) * OPERAND;
-#pragma unroll
-          for (int k = 0; k < TILE / 16; ++k)
-            umma_f16_ta(tmem + O_COL + x * TILE, tmem + slot * TILE + k * 8,
-                        sw128_mnmajor_desc(vb + k * 2048, ATOM), IDESC_O, (j | k) != 0);
-          bd::umma_commit(bd::smem_u32(&ctl->pv_done[x]));
-          if (x == NM - 1) bd::umma_commit(bd::smem_u32(&ctl->v_empty[j & 1]));
+        for (int k = 0; k < D / 16; ++k) {
+          const uint32_t at = (k / 4) * (ATOM >> 4) + 2u * (k % 4);
+          mma_ss(issue, tmem + x * TILE, qd + at, kd + at, IDESC_S, k != 0);
         }
-        __syncwarp();
-        const int next = NM == 1 ? j + 2 : j + 1;
-        if (next < n) {
-          if (x == 0) ok = wait(ctl->k_full[next & 1], next >> 1);
+        mma_commit(issue, bd::smem_u32(&ctl->s_full[x]));
+        if (NM == 1 || x == NM - 1) mma_commit(issue, bd::smem_u32(&ctl->k_empty[j & 1]));
+      };
+      bool ok = n > 0 && wait(ctl->q_full, 0);
+      for (int j = 0; ok && j < (NM == 1 ? min(n, 2) : 1); ++j) {
+        ok = wait(ctl->k_full[j & 1], 0);
+        bd::tc_fence_after();
+        if (ok)
+          for (int x = 0; x < NM; ++x) scores(NM == 1 ? j : x, j);
+      }
+      for (int j = 0; ok && j < n; ++j) {
+#pragma unroll
+        for (int x = 0; x < NM; ++x) {
+          const int slot = NM == 1 ? j & 1 : x;
+          ok = ok && wait(ctl->p_full[slot], NM == 1 ? j >> 1 : j);
+          if (x == 0) ok = ok && wait(ctl->v_full[j & 1], j >> 1);
           if (!ok) break;
           bd::tc_fence_after();
-          scores(slot, next);
+          const uint64_t vd = v_desc + (j & 1) * (OPERAND >> 4);
+#pragma unroll
+          for (int k = 0; k < TILE / 16; ++k)
+            mma_ts(issue, tmem + O_COL + x * TILE, tmem + slot * TILE + k * 8, vd + k * (2048u >> 4), IDESC_O,
+                   (j | k) != 0);
+          mma_commit(issue, bd::smem_u32(&ctl->pv_done[x]));
+          if (x == NM - 1) mma_commit(issue, bd::smem_u32(&ctl->v_empty[j & 1]));
+          const int next = NM == 1 ? j + 2 : j + 1;
+          if (next < n) {
+            if (x == 0) ok = wait(ctl->k_full[next & 1], next >> 1);
+            if (!ok) break;
+            bd::tc_fence_after();
+            scores(slot, next);
+          }
         }
       }
-    }
-    if (leader) {  // all MMAs issued have completed once `drain` flips
-      bd::umma_commit(bd::smem_u32(&ctl->drain));
+      mma_commit(issue, bd::smem_u32(&ctl->drain));  // all MMAs issued have completed once it flips
+      __syncwarp();
       bd::mbar_drain(bd::smem_u32(&ctl->drain), 0);
-    }
     }
     __syncwarp();
   } else if (warp >= 4 * NM) {
@@ -288,16 +325,20 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
     const int32_t* table = a.table + seq * a.table_stride;
     const int mask = (1 << a.page_shift) - 1;
     uint4 kx[PER], vx[PER];
+    int pages[PER];  // of the tile to be loaded next (-1: nothing to read)
+    const auto find = [&](int j) {
+#pragma unroll
+      for (int u = 0; u < PER; ++u) {
+        const int t = begin + j * TILE + mine + u * STEP;
+        pages[u] = ld_global_if(table + (t >> a.page_shift), t < end && (t >> a.page_shift) < a.max_blocks, -1);
+      }
+    };
     const auto load = [&](const uint8_t* p, int64_t page_stride, int64_t tok_stride, int j, uint4 (&x)[PER]) {
 #pragma unroll
       for (int u = 0; u < PER; ++u) {
-        const int t = begin + j * TILE + mine + u * STEP, col = t >> a.page_shift;
-        x[u] = make_uint4(0, 0, 0, 0);
-        if (t < end && sub * 16 < a.dim) {
-          const int64_t page = col < a.max_blocks ? table[col] : -1;
-          if (page >= 0 && page < a.n_pages)
-            x[u] = *reinterpret_cast<const uint4*>(p + page * page_stride + (t & mask) * tok_stride);
-        }
+        const int t = begin + j * TILE + mine + u * STEP;
+        x[u] = ld_global_if(p + pages[u] * page_stride + (t & mask) * tok_stride,
+                            pages[u] >= 0 && pages[u] < a.n_pages && sub * 16 < a.dim);
       }
     };
     const auto store = [&](uint32_t at, const uint4 (&x)[PER]) {
@@ -316,21 +357,36 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
                      flip ? y[3] : y[7]);
       }
     };
+    // a lane of the first eight has a tile's group of 16 tokens: its page and, one tile ahead, its scales
+    int group_page = -1, ks_byte = 0, vs_byte = 0;
+    bool group_in = false;
+    const auto find_group = [&](int j) {
+      const int t = begin + j * TILE + ct * 16;
+      group_page = ld_global_if(table + (t >> a.page_shift), ct < 8 && t < end && (t >> a.page_shift) < a.max_blocks, -1);
+    };
+    const auto find_scales = [&](int j) {  // of tile j, whose pages find_group has looked up; then the pages of the next
+      group_in = group_page >= 0 && group_page < a.n_pages;
+      ks_byte = ld_global_byte_if(a.ks + group_page * a.ks_page + head, group_in);
+      vs_byte = ld_global_byte_if(a.vs + group_page * a.vs_page + head, group_in);
+      find_group(j + 1);
+    };
     if (n > 0) {
+      find_group(0);
+      find_scales(0);
+      find(0);
       load(kp, a.k_page, row_k, 0, kx);
       load(vp, a.v_page, row_v, 0, vx);
     }
     bool ok = true;
     for (int j = 0; j < n; ++j) {
+      find(j + 1);
       ok = wait(ctl->k_empty[j & 1], (j >> 1) + 1);
       if (!ok) break;
       if (ct < 8) {
-        const int t = begin + j * TILE + ct * 16, col = t >> a.page_shift;
-        const int64_t page = t < end && col < a.max_blocks ? table[col] : -1;
-        const bool in = page >= 0 && page < a.n_pages;
-        ctl->ks[j & 3][ct] = in ? pow2i(a.ks[page * a.ks_page + head] - 127) : 1.f;
-        ctl->ve[j & 3][ct] = in ? static_cast<float>(a.vs[page * a.vs_page + head] - 127) : 0.f;
+        ctl->ks[j & 3][ct] = group_in ? pow2i(ks_byte - 127) : 1.f;
+        ctl->ve[j & 3][ct] = group_in ? static_cast<float>(vs_byte - 127) : 0.f;
       }
+      find_scales(j + 1);
       store(k_at + (j & 1) * OPERAND, kx);
       fence_proxy_async();
       bd::mbar_arrive(bd::smem_u32(&ctl->k_full[j & 1]));
