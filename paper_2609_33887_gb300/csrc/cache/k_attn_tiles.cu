@@ -1,19 +1,20 @@
 // bdkv_attention for many query rows per key/value head: windows of blocks,
-// prompts. tcgen05 products on tiles of 128 rows by 128 cached tokens.
+// prompts. tcgen05 products on tiles of 128 rows by 64 cached tokens.
 //
 // A CTA holds NM x 128 rows of a request's key/value head (queries x the
 // group's heads, so the head's cache is read once for all of them) and walks
-// the cache in tiles of 128 tokens:
+// the cache in tiles of 64 tokens:
 //   converter warps   codes from global memory to f16 (exact), into shared
-//                     memory in the 128-byte swizzle, double buffered; a
-//                     request's tail is zeros, so its values times zero
-//                     weights stay zero
+//                     memory in the 128-byte swizzle, four stages; a request's
+//                     tail is zeros, so its values times zero weights stay zero
 //   MMA warp          S = Q K^T (both operands in shared memory) and O += P V
 //                     (P in tensor memory, V read with the token index along
-//                     K); S of one half runs while the other half's softmax does
+//                     K); S of the next two tiles is ready before its softmax
+//                     begins, so the softmax warps never wait for a product of
+//                     their own last weights
 //   softmax warps     a thread per row: running maxima, weights to f16, written
 //                     over S in tensor memory; O is rescaled only when a row's
-//                     maximum has grown by more than 2^3
+//                     maximum has grown by more than 2^7
 // Scales of pages come in through the exponent: w = 2^(S coef k_scale + e_v),
 // see k_attn_rows.cu; O and the sum L have a reference maximum of their own.
 #include "cache.h"
@@ -21,19 +22,25 @@
 namespace bdkv {
 namespace {
 
-constexpr int TILE = TILES_TILE;  // rows of an MMA, tokens of a tile
-constexpr float P_SHIFT = 12, P_SLACK = 3;
-constexpr int CONV_WARPS = 4;
-// Warps of a CTA: 4 for each half's softmax, 4 converters, 4 of which one issues the MMAs: warpgroups, so that registers
-// can be moved between them. With two halves, 512 threads start with 128 each: 2 x 128 x 184 (a row's 128 scores stay in
-// registers) + 128 x 104 + 128 x 40 = 65536; with one, 384 threads with 168.
-constexpr int threads(int nm) { return (nm + 2) * 128; }
+constexpr int TILE = TILES_TILE;  // rows of an MMA
+constexpr int TOK = 64;           // tokens of a tile
+constexpr int STAGES = 4;         // tiles of keys and of values in shared memory
+constexpr int GROUPS = TOK / 16;  // scales of a tile
+// Weights are held as f16 times 2^8, with 11 bits down to 2^-22 of the reference, and may exceed it by 2^7 before O is
+// rescaled (2^15 < 65504): a rescale costs a warp about as much as a tile.
+constexpr float P_SHIFT = 8, P_SLACK = 7;
+constexpr int CONV_WARPS = 8;
+// Warps of a CTA: 4 for each half's softmax, 8 converters, 4 of which one issues the MMAs: warpgroups, so that registers
+// can be moved between them. With two halves 640 threads start with 96 each: 2 x 128 x 128 (a row's 64 scores and 32
+// words of weights) + 256 x 80 + 128 x 56 <= 61440; with one, 512 threads with 128.
+constexpr int threads(int nm) { return (4 * nm + CONV_WARPS + 4) * 32; }
 
 __device__ uint32_t g_status;  // bd::DEV_* bits
 
 struct Ctl {
-  uint64_t q_full, k_full[2], k_empty[2], v_full[2], v_empty[2], s_full[2], p_full[2], pv_done[2], drain;
-  float ks[4][8], ve[4][8];  // page scales of a tile's eight groups of 16 tokens: factor, exponent
+  uint64_t q_full, k_full[STAGES], k_empty[STAGES], v_full[STAGES], v_empty[STAGES];
+  uint64_t s_full[2][2], p_full[2][2], pv_done[2], o_done[2], drain;  // by half (and parity of the tile)
+  float ks[8][GROUPS], ve[8][GROUPS];  // page scales of a tile's groups of 16 tokens: factor, exponent
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -95,30 +102,14 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
       : "memory");
 }
 
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
-      "tcgen05.wait::ld.sync.aligned;"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr)
-      : "memory");
-}
-
-// All 128 columns of a tile for this thread's lane.
-__device__ __forceinline__ void tmem_ld128(uint32_t taddr, float (&v)[128]) {
+// The 64 columns of a tile for this thread's lane.
+__device__ __forceinline__ void tmem_ld64(uint32_t taddr, float (&v)[64]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
       "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
       "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, "
       "%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47, "
-      "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%128];\n\t"
-      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
-      "%64, %65, %66, %67, %68, %69, %70, %71, %72, %73, %74, %75, %76, %77, %78, %79, "
-      "%80, %81, %82, %83, %84, %85, %86, %87, %88, %89, %90, %91, %92, %93, %94, %95, "
-      "%96, %97, %98, %99, %100, %101, %102, %103, %104, %105, %106, %107, %108, %109, %110, %111, "
-      "%112, %113, %114, %115, %116, %117, %118, %119, %120, %121, %122, %123, %124, %125, %126, %127}, [%129];\n\t"
+      "%48, %49, %50, %51, %52, %53, %54, %55, %56, %57, %58, %59, %60, %61, %62, %63}, [%64];\n\t"
       "tcgen05.wait::ld.sync.aligned;"
       : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]),
         "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]),
@@ -135,24 +126,8 @@ __device__ __forceinline__ void tmem_ld128(uint32_t taddr, float (&v)[128]) {
         "=f"(v[48]), "=f"(v[49]), "=f"(v[50]), "=f"(v[51]),
         "=f"(v[52]), "=f"(v[53]), "=f"(v[54]), "=f"(v[55]),
         "=f"(v[56]), "=f"(v[57]), "=f"(v[58]), "=f"(v[59]),
-        "=f"(v[60]), "=f"(v[61]), "=f"(v[62]), "=f"(v[63]),
-        "=f"(v[64]), "=f"(v[65]), "=f"(v[66]), "=f"(v[67]),
-        "=f"(v[68]), "=f"(v[69]), "=f"(v[70]), "=f"(v[71]),
-        "=f"(v[72]), "=f"(v[73]), "=f"(v[74]), "=f"(v[75]),
-        "=f"(v[76]), "=f"(v[77]), "=f"(v[78]), "=f"(v[79]),
-        "=f"(v[80]), "=f"(v[81]), "=f"(v[82]), "=f"(v[83]),
-        "=f"(v[84]), "=f"(v[85]), "=f"(v[86]), "=f"(v[87]),
-        "=f"(v[88]), "=f"(v[89]), "=f"(v[90]), "=f"(v[91]),
-        "=f"(v[92]), "=f"(v[93]), "=f"(v[94]), "=f"(v[95]),
-        "=f"(v[96]), "=f"(v[97]), "=f"(v[98]), "=f"(v[99]),
-        "=f"(v[100]), "=f"(v[101]), "=f"(v[102]), "=f"(v[103]),
-        "=f"(v[104]), "=f"(v[105]), "=f"(v[106]), "=f"(v[107]),
-        "=f"(v[108]), "=f"(v[109]), "=f"(v[110]), "=f"(v[111]),
-        "=f"(v[112]), "=f"(v[113]), "=f"(v[114]), "=f"(v[115]),
-        "=f"(v[116]), "=f"(v[117]), "=f"(v[118]), "=f"(v[119]),
-        "=f"(v[120]), "=f"(v[121]), "=f"(v[122]), "=f"(v[123]),
-        "=f"(v[124]), "=f"(v[125]), "=f"(v[126]), "=f"(v[127])
-      : "r"(taddr), "r"(taddr + 64)
+        "=f"(v[60]), "=f"(v[61]), "=f"(v[62]), "=f"(v[63])
+      : "r"(taddr)
       : "memory");
 }
 
@@ -168,7 +143,7 @@ __device__ __forceinline__ void give_registers() {
 
 template <int NM, int D>
 constexpr size_t smem_bytes() {
-  return size_t(NM + 4) * TILE * D * 2 + sizeof(Ctl) + 1024;
+  return size_t(NM * TILE + 2 * STAGES * TOK) * D * 2 + sizeof(Ctl) + 1024;
 }
 
 // Loads that happen where `live` says so, without a branch that would hold up the loads behind them.
@@ -206,15 +181,15 @@ __device__ __forceinline__ void decode16(uint4 x, uint32_t (&y)[8]) {
 
 template <class T, int NM, int D>
 __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) {
-  constexpr int ATOMS = D / 64;             // 128-byte column blocks of a row
-  constexpr uint32_t ATOM = TILE * 128;     // bytes of one, 128 rows
-  constexpr uint32_t OPERAND = ATOMS * ATOM;
-  constexpr int CH = D / 16;                // 16-code chunks of a token's row
-  constexpr int O_COL = 256;                // tensor memory: S and P at 0 and 128, O behind
+  constexpr int ATOMS = D / 64;                // 128-byte column blocks of a row
+  constexpr uint32_t Q_ATOM = TILE * 128, KV_ATOM = TOK * 128;  // bytes of one
+  constexpr uint32_t Q_HALF = ATOMS * Q_ATOM, KV_TILE = ATOMS * KV_ATOM;
+  constexpr int CH = D / 16;                   // 16-code chunks of a token's row
+  constexpr int O_COL = 256;                   // tensor memory: S and P of half x, parity b at 128 x + 64 b; O behind
   extern __shared__ uint8_t raw[];
   const uint32_t base = (bd::smem_u32(raw) + 1023u) & ~1023u;
-  const uint32_t q_at = base, k_at = q_at + NM * OPERAND, v_at = k_at + 2 * OPERAND;
-  Ctl* ctl = reinterpret_cast<Ctl*>(raw + (v_at + 2 * OPERAND - bd::smem_u32(raw)));
+  const uint32_t q_at = base, k_at = q_at + NM * Q_HALF, v_at = k_at + STAGES * KV_TILE;
+  Ctl* ctl = reinterpret_cast<Ctl*>(raw + (v_at + STAGES * KV_TILE - bd::smem_u32(raw)));
   const int tid = threadIdx.x, warp = static_cast<int>(bd::warp_uniform(tid >> 5));
   const int n_tiles_rows = gridDim.x / a.n_kv;
   const int head = blockIdx.x / n_tiles_rows, row0 = (n_tiles_rows - 1 - blockIdx.x % n_tiles_rows) * (NM * TILE);
@@ -226,18 +201,23 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
   const int i_last = (min(rows, row0 + NM * TILE) - 1) / a.group;
   const int begin = part * a.chunk, end = min(visible(a, sq, i_last), begin + a.chunk);
   if (part > 0 && end <= begin) return;
-  const int n = end > begin ? (end - begin + TILE - 1) / TILE : 0;
+  const int n = end > begin ? (end - begin + TOK - 1) / TOK : 0;
 
   if (tid == 0) {
     bd::mbar_init(bd::smem_u32(&ctl->q_full), NM * TILE);
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < STAGES; ++i) {
       bd::mbar_init(bd::smem_u32(&ctl->k_full[i]), CONV_WARPS * 32);
       bd::mbar_init(bd::smem_u32(&ctl->v_full[i]), CONV_WARPS * 32);
       bd::mbar_init(bd::smem_u32(&ctl->k_empty[i]), 1);
       bd::mbar_init(bd::smem_u32(&ctl->v_empty[i]), 1);
-      bd::mbar_init(bd::smem_u32(&ctl->s_full[i]), 1);
-      bd::mbar_init(bd::smem_u32(&ctl->p_full[i]), TILE);
-      bd::mbar_init(bd::smem_u32(&ctl->pv_done[i]), 1);
+    }
+    for (int x = 0; x < 2; ++x) {
+      for (int b = 0; b < 2; ++b) {
+        bd::mbar_init(bd::smem_u32(&ctl->s_full[x][b]), 1);
+        bd::mbar_init(bd::smem_u32(&ctl->p_full[x][b]), TILE);
+      }
+      bd::mbar_init(bd::smem_u32(&ctl->pv_done[x]), 1);
+      bd::mbar_init(bd::smem_u32(&ctl->o_done[x]), 1);
     }
     bd::mbar_init(bd::smem_u32(&ctl->drain), 1);
     ctl->abort_flag = 0;
@@ -260,50 +240,47 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
 
   if (warp >= MMA_WARP) {
     // ---------------------------------------------------------- MMA issuer
-    give_registers<40>();
+    give_registers<56>();
     if (warp == MMA_WARP) {
       const uint32_t issue = bd::elect_one();
-      constexpr uint32_t IDESC_S = bd::idesc_f16_f32(TILE, TILE), IDESC_O = bd::idesc_f16_f32(TILE, D) | B_MN_MAJOR;
+      constexpr uint32_t IDESC_S = bd::idesc_f16_f32(TILE, TOK), IDESC_O = bd::idesc_f16_f32(TILE, D) | B_MN_MAJOR;
       const uint64_t q_desc = bd::sw128_kmajor_desc(q_at), k_desc = bd::sw128_kmajor_desc(k_at);
-      const uint64_t v_desc = sw128_mnmajor_desc(v_at, ATOM);
-      const auto scores = [&](int x, int j) {  // S in slot x; addresses in descriptors count 16 bytes
-        const uint64_t qd = q_desc + (NM == 2 ? x * (OPERAND >> 4) : 0u), kd = k_desc + (j & 1) * (OPERAND >> 4);
+      const uint64_t v_desc = sw128_mnmajor_desc(v_at, KV_ATOM);
+      const auto scores = [&](int x, int j) {  // S of half x, tile j; addresses in descriptors count 16 bytes
+        const uint64_t qd = q_desc + x * (Q_HALF >> 4), kd = k_desc + (j % STAGES) * (KV_TILE >> 4);
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          const uint32_t at = (k / 4) * (ATOM >> 4) + 2u * (k % 4);
-          mma_ss(issue, tmem + x * TILE, qd + at, kd + at, IDESC_S, k != 0);
-        }
-        mma_commit(issue, bd::smem_u32(&ctl->s_full[x]));
-        if (NM == 1 || x == NM - 1) mma_commit(issue, bd::smem_u32(&ctl->k_empty[j & 1]));
+        for (int k = 0; k < D / 16; ++k)
+          mma_ss(issue, tmem + x * TILE + (j & 1) * TOK, qd + (k / 4) * (Q_ATOM >> 4) + 2u * (k % 4),
+                 kd + (k / 4) * (KV_ATOM >> 4) + 2u * (k % 4), IDESC_S, k != 0);
+        mma_commit(issue, bd::smem_u32(&ctl->s_full[x][j & 1]));
+        if (x == NM - 1) mma_commit(issue, bd::smem_u32(&ctl->k_empty[j % STAGES]));
       };
       bool ok = n > 0 && wait(ctl->q_full, 0);
-      for (int j = 0; ok && j < (NM == 1 ? min(n, 2) : 1); ++j) {
-        ok = wait(ctl->k_full[j & 1], 0);
+      for (int j = 0; ok && j < min(n, 2); ++j) {
+        ok = wait(ctl->k_full[j], 0);
         bd::tc_fence_after();
         if (ok)
-          for (int x = 0; x < NM; ++x) scores(NM == 1 ? j : x, j);
+          for (int x = 0; x < NM; ++x) scores(x, j);
       }
       for (int j = 0; ok && j < n; ++j) {
 #pragma unroll
         for (int x = 0; x < NM; ++x) {
-          const int slot = NM == 1 ? j & 1 : x;
-          ok = ok && wait(ctl->p_full[slot], NM == 1 ? j >> 1 : j);
-          if (x == 0) ok = ok && wait(ctl->v_full[j & 1], j >> 1);
+          ok = ok && wait(ctl->p_full[x][j & 1], j >> 1);
+          if (x == 0) ok = ok && wait(ctl->v_full[j % STAGES], j / STAGES);
           if (!ok) break;
           bd::tc_fence_after();
-          const uint64_t vd = v_desc + (j & 1) * (OPERAND >> 4);
+          const uint64_t vd = v_desc + (j % STAGES) * (KV_TILE >> 4);
 #pragma unroll
-          for (int k = 0; k < TILE / 16; ++k)
-            mma_ts(issue, tmem + O_COL + x * TILE, tmem + slot * TILE + k * 8, vd + k * (2048u >> 4), IDESC_O,
-                   (j | k) != 0);
-          mma_commit(issue, bd::smem_u32(&ctl->pv_done[x]));
-          if (x == NM - 1) mma_commit(issue, bd::smem_u32(&ctl->v_empty[j & 1]));
-          const int next = NM == 1 ? j + 2 : j + 1;
-          if (next < n) {
-            if (x == 0) ok = wait(ctl->k_full[next & 1], next >> 1);
+          for (int k = 0; k < TOK / 16; ++k)
+            mma_ts(issue, tmem + O_COL + x * TILE, tmem + x * TILE + (j & 1) * TOK + k * 8, vd + k * (2048u >> 4),
+                   IDESC_O, (j | k) != 0);
+          mma_commit(issue, bd::smem_u32(j + 1 < n ? &ctl->pv_done[x] : &ctl->o_done[x]));
+          if (x == NM - 1) mma_commit(issue, bd::smem_u32(&ctl->v_empty[j % STAGES]));
+          if (j + 2 < n) {  // over the weights that the products above read: the tensor pipe takes them in order
+            if (x == 0) ok = wait(ctl->k_full[(j + 2) % STAGES], (j + 2) / STAGES);
             if (!ok) break;
             bd::tc_fence_after();
-            scores(slot, next);
+            scores(x, j + 2);
           }
         }
       }
@@ -314,11 +291,12 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
     __syncwarp();
   } else if (warp >= 4 * NM) {
     // ---------------------------------------------------------- converters
-    give_registers<104>();
+    give_registers<80>();
     const int ct = tid - 4 * NM * 32;
-    constexpr int PER = TILE * CH / (CONV_WARPS * 32);  // chunks of a thread and tile
-    constexpr int STEP = CONV_WARPS * 32 / CH;          // rows between them
-    const int sub = ct % CH, mine = ct / CH;
+    constexpr int PER = TOK * CH / (CONV_WARPS * 32);  // chunks of a thread and tile
+    constexpr int STEP = CONV_WARPS * 32 / CH;         // rows between them
+    // eight lanes take four chunks each of two rows, which the swizzle puts into different banks
+    const int sub = (ct & 3) | (CH == 8 ? (ct >> 1) & 4 : 0), mine = ct / (2 * CH) * 2 + ((ct >> 2) & 1);
     const int64_t row_k = a.k_tok, row_v = a.v_tok;
     const uint8_t* kp = a.k + head * a.k_head + sub * 16;
     const uint8_t* vp = a.v + head * a.v_head + sub * 16;
@@ -329,14 +307,14 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
     const auto find = [&](int j) {
 #pragma unroll
       for (int u = 0; u < PER; ++u) {
-        const int t = begin + j * TILE + mine + u * STEP;
+        const int t = begin + j * TOK + mine + u * STEP;
         pages[u] = ld_global_if(table + (t >> a.page_shift), t < end && (t >> a.page_shift) < a.max_blocks, -1);
       }
     };
     const auto load = [&](const uint8_t* p, int64_t page_stride, int64_t tok_stride, int j, uint4 (&x)[PER]) {
 #pragma unroll
       for (int u = 0; u < PER; ++u) {
-        const int t = begin + j * TILE + mine + u * STEP;
+        const int t = begin + j * TOK + mine + u * STEP;
         x[u] = ld_global_if(p + pages[u] * page_stride + (t & mask) * tok_stride,
                             pages[u] >= 0 && pages[u] < a.n_pages && sub * 16 < a.dim);
       }
@@ -347,22 +325,17 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
         const int r = mine + u * STEP;
         uint32_t y[8];
         decode16(x[u], y);
-        const uint32_t rowp = at + (sub / 4) * ATOM + r * 128;
-        // the lanes of the second atom store their second chunk first: the two atoms' lanes meet in different banks
-        const bool flip = sub >= 4;
-        const int c0 = (sub % 4) * 2 + flip;
-        st_shared_v4(rowp + ((c0 ^ (r & 7)) << 4), flip ? y[4] : y[0], flip ? y[5] : y[1], flip ? y[6] : y[2],
-                     flip ? y[7] : y[3]);
-        st_shared_v4(rowp + (((c0 ^ 1) ^ (r & 7)) << 4), flip ? y[0] : y[4], flip ? y[1] : y[5], flip ? y[2] : y[6],
-                     flip ? y[3] : y[7]);
+        const uint32_t rowp = at + (sub / 4) * KV_ATOM + r * 128, c0 = (sub % 4) * 2;
+        st_shared_v4(rowp + ((c0 ^ (r & 7)) << 4), y[0], y[1], y[2], y[3]);
+        st_shared_v4(rowp + (((c0 + 1) ^ (r & 7)) << 4), y[4], y[5], y[6], y[7]);
       }
     };
-    // a lane of the first eight has a tile's group of 16 tokens: its page and, one tile ahead, its scales
+    // a lane of the first few has a tile's group of 16 tokens: its page and, one tile ahead, its scales
     int group_page = -1, ks_byte = 0, vs_byte = 0;
     bool group_in = false;
     const auto find_group = [&](int j) {
-      const int t = begin + j * TILE + ct * 16;
-      group_page = ld_global_if(table + (t >> a.page_shift), ct < 8 && t < end && (t >> a.page_shift) < a.max_blocks, -1);
+      const int t = begin + j * TOK + ct * 16;
+      group_page = ld_global_if(table + (t >> a.page_shift), ct < GROUPS && t < end && (t >> a.page_shift) < a.max_blocks, -1);
     };
     const auto find_scales = [&](int j) {  // of tile j, whose pages find_group has looked up; then the pages of the next
       group_in = group_page >= 0 && group_page < a.n_pages;
@@ -380,27 +353,27 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
     bool ok = true;
     for (int j = 0; j < n; ++j) {
       find(j + 1);
-      ok = wait(ctl->k_empty[j & 1], (j >> 1) + 1);
+      ok = wait(ctl->k_empty[j % STAGES], j / STAGES + 1);
       if (!ok) break;
-      if (ct < 8) {
-        ctl->ks[j & 3][ct] = group_in ? pow2i(ks_byte - 127) : 1.f;
-        ctl->ve[j & 3][ct] = group_in ? static_cast<float>(vs_byte - 127) : 0.f;
+      if (ct < GROUPS) {
+        ctl->ks[j & 7][ct] = group_in ? pow2i(ks_byte - 127) : 1.f;
+        ctl->ve[j & 7][ct] = group_in ? static_cast<float>(vs_byte - 127) : 0.f;
       }
       find_scales(j + 1);
-      store(k_at + (j & 1) * OPERAND, kx);
+      store(k_at + (j % STAGES) * KV_TILE, kx);
       fence_proxy_async();
-      bd::mbar_arrive(bd::smem_u32(&ctl->k_full[j & 1]));
-      if (j + 1 < n) load(kp, a.k_page, row_k, j + 1, kx);
-      ok = wait(ctl->v_empty[j & 1], (j >> 1) + 1);
+      bd::mbar_arrive(bd::smem_u32(&ctl->k_full[j % STAGES]));
+      load(kp, a.k_page, row_k, j + 1, kx);
+      ok = wait(ctl->v_empty[j % STAGES], j / STAGES + 1);
       if (!ok) break;
-      store(v_at + (j & 1) * OPERAND, vx);
+      store(v_at + (j % STAGES) * KV_TILE, vx);
       fence_proxy_async();
-      bd::mbar_arrive(bd::smem_u32(&ctl->v_full[j & 1]));
-      if (j + 1 < n) load(vp, a.v_page, row_v, j + 1, vx);
+      bd::mbar_arrive(bd::smem_u32(&ctl->v_full[j % STAGES]));
+      load(vp, a.v_page, row_v, j + 1, vx);
     }
   } else {
     // ------------------------------------------------------------- softmax
-    take_registers<184>();
+    if constexpr (NM == 2) take_registers<128>();
     const int x = NM == 2 ? warp >> 2 : 0;  // half
     const int r = tid & 127, row = row0 + x * TILE + r, i = row / a.group;
     const bool live = row < rows;
@@ -435,7 +408,7 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
           const float2 v = T::to_float2(ww[u]);
           y[u] = f16x2(make_float2(v.x * f, v.y * f));
         }
-        st_shared_v4(q_at + x * OPERAND + (c / 8) * ATOM + r * 128 + (((c % 8) ^ (r & 7)) << 4), y[0], y[1], y[2], y[3]);
+        st_shared_v4(q_at + x * Q_HALF + (c / 8) * Q_ATOM + r * 128 + (((c % 8) ^ (r & 7)) << 4), y[0], y[1], y[2], y[3]);
       }
       fence_proxy_async();
       bd::mbar_arrive(bd::smem_u32(&ctl->q_full));
@@ -447,18 +420,18 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
     float m = -INFINITY, M = -INFINITY, L = 0.f;
     bool ok = true;
     // One tile: the row's scores become weights, over themselves in tensor memory. CUT: some row of the warp does not see
-    // all 128 tokens.
-    const auto softmax = [&](auto cut, int slot, int j, int left) -> bool {
+    // all of its tokens.
+    const auto softmax = [&](auto cut, int j, int left) -> bool {
       constexpr bool CUT = decltype(cut)::value;
-      const uint32_t s_at = tmem + lanes + slot * TILE;
-      const float* ks = ctl->ks[j & 3];
-      const float* ve = ctl->ve[j & 3];
-      float v[TILE];
+      const uint32_t s_at = tmem + lanes + x * TILE + (j & 1) * TOK;
+      const float* ks = ctl->ks[j & 7];
+      const float* ve = ctl->ve[j & 7];
+      float v[TOK];
       __syncwarp();
-      tmem_ld128(s_at, v);
+      tmem_ld64(s_at, v);
       float s_top = -INFINITY, u_top = -INFINITY;
 #pragma unroll
-      for (int b = 0; b < 8; ++b) {
+      for (int b = 0; b < GROUPS; ++b) {
         if (CUT)
 #pragma unroll
           for (int e = b * 16; e < b * 16 + 16; ++e)
@@ -477,17 +450,19 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
       const bool grow = u_top > M + P_SLACK || (M == -INFINITY && u_top > M);
       if (__any_sync(~0u, grow)) {
         if (j > 0) {
+          // (this tile's scores followed O's product of two tiles ago, so no phase is skipped, and none is ahead)
           if (!wait(ctl->pv_done[x], j - 1)) return false;
           bd::tc_fence_after();
           const float f = grow ? bd::ex2_approx(M - u_top) : 1.f;
           __syncwarp();  // tensor-memory accesses take the whole warp at once
 #pragma unroll 1
-          for (int c = 0; c < D / 16; ++c) {
-            uint32_t o[16];
-            tmem_ld16(o_at + c * 16, o);
+          for (int c = 0; c < D / 32; ++c) {
+            float o[32];
+            bd::tmem_ld32(o_at + c * 32, o);
+            uint32_t y[32];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-            tmem_st16(o_at + c * 16, o);
+            for (int e = 0; e < 32; ++e) y[e] = __float_as_uint(o[e] * f);
+            bd::tmem_st32(o_at + c * 32, y);
           }
         }
         M = grow ? u_top : M;
@@ -495,7 +470,7 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
       __syncwarp();
       const float ms = m == -INFINITY ? 0.f : m, Ms = M == -INFINITY ? 0.f : M;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
+      for (int c = 0; c < TOK / 32; ++c) {
         uint32_t p[16];
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
@@ -522,23 +497,19 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
     };
 
     for (int j = 0; j < n; ++j) {
-      const int slot = NM == 1 ? j & 1 : x;
-      ok = wait(ctl->s_full[slot], NM == 1 ? j >> 1 : j);
+      ok = wait(ctl->s_full[x][j & 1], j >> 1);
       if (!ok) break;
       bd::tc_fence_after();
       if (any_live) {
-        const int left = vis - (begin + j * TILE);  // columns this row sees
-        ok = __any_sync(~0u, left < TILE) ? softmax(std::true_type(), slot, j, left) : softmax(std::false_type(), slot, j, left);
+        const int left = vis - (begin + j * TOK);  // columns this row sees
+        ok = __any_sync(~0u, left < TOK) ? softmax(std::true_type(), j, left) : softmax(std::false_type(), j, left);
         if (!ok) break;
       }
       bd::tc_fence_before();
-      bd::mbar_arrive(bd::smem_u32(&ctl->p_full[slot]));
+      bd::mbar_arrive(bd::smem_u32(&ctl->p_full[x][j & 1]));
     }
 
-    // The last tile's scores follow O's product of two tiles before it (NM == 1), so that is as far as O is known to be: a
-    // parity wait must not skip a phase.
-    if (NM == 1 && n > 1 && ok) ok = wait(ctl->pv_done[x], n - 2);
-    if (n > 0 && ok) ok = wait(ctl->pv_done[x], n - 1);
+    if (n > 0 && ok) ok = wait(ctl->o_done[x], 0);
     bd::tc_fence_after();
     const float ms = m == -INFINITY ? 0.f : m, Ms = M == -INFINITY ? 0.f : M;
     const float f = L == 0.f ? 0.f : bd::ex2_approx(Ms - P_SHIFT - ms) / L;
