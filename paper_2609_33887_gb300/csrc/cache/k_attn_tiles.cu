@@ -51,25 +51,28 @@ __device__ __forceinline__ void st_shared_v4(uint32_t addr, uint32_t a, uint32_t
   asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
-// The MMA warp issues in the elected lane by predicate, not by branch: its addresses and descriptors then stay in uniform
-// registers. D[tmem] (+)= A[smem] * B[smem]^T, f16.
-__device__ __forceinline__ void mma_ss(uint32_t issue, uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc,
-                                       uint32_t accumulate) {
+// The MMA warp issues in the elected lane by predicate, not by branch, and its descriptors' low words come through
+// warp_uniform: they then stay in uniform registers. D[tmem] (+)= A[smem] * B[smem]^T, f16; `hi` is the upper word of both
+// descriptors.
+__device__ __forceinline__ void mma_ss(uint32_t issue, uint32_t d_tmem, uint32_t a, uint32_t b, uint32_t hi,
+                                       uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
+      "{\n\t.reg .pred p, q;\n\t.reg .b64 da, db;\n\t"
+      "mov.b64 da, {%1, %6};\n\tmov.b64 db, {%2, %6};\n\t"
       "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
-      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(issue)
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "r"(issue), "r"(hi)
       : "memory");
 }
 // D[tmem] (+)= A[tmem] * B[smem], f16: row i of A in lane i, two elements per 32-bit column.
-__device__ __forceinline__ void mma_ts(uint32_t issue, uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc,
-                                       uint32_t accumulate) {
+__device__ __forceinline__ void mma_ts(uint32_t issue, uint32_t d_tmem, uint32_t a_tmem, uint32_t b, uint32_t hi,
+                                       uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
+      "{\n\t.reg .pred p, q;\n\t.reg .b64 db;\n\t"
+      "mov.b64 db, {%2, %6};\n\t"
       "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
-      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate), "r"(issue)
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "r"(b), "r"(idesc), "r"(accumulate), "r"(issue), "r"(hi)
       : "memory");
 }
 __device__ __forceinline__ void mma_commit(uint32_t issue, uint32_t bar) {
@@ -246,12 +249,15 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
       constexpr uint32_t IDESC_S = bd::idesc_f16_f32(TILE, TOK), IDESC_O = bd::idesc_f16_f32(TILE, D) | B_MN_MAJOR;
       const uint64_t q_desc = bd::sw128_kmajor_desc(q_at), k_desc = bd::sw128_kmajor_desc(k_at);
       const uint64_t v_desc = sw128_mnmajor_desc(v_at, KV_ATOM);
+      constexpr uint32_t HI = (1024u >> 4) | (1u << 14) | (2u << 29);  // of all three: 1 KB stride, version, swizzle
       const auto scores = [&](int x, int j) {  // S of half x, tile j; addresses in descriptors count 16 bytes
-        const uint64_t qd = q_desc + x * (Q_HALF >> 4), kd = k_desc + (j % STAGES) * (KV_TILE >> 4);
+        const uint32_t qd = bd::warp_uniform(static_cast<uint32_t>(q_desc) + x * (Q_HALF >> 4));
+        const uint32_t kd = bd::warp_uniform(static_cast<uint32_t>(k_desc) + (j % STAGES) * (KV_TILE >> 4));
+        const uint32_t sd = bd::warp_uniform(tmem + x * TILE + (j & 1) * TOK);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k)
-          mma_ss(issue, tmem + x * TILE + (j & 1) * TOK, qd + (k / 4) * (Q_ATOM >> 4) + 2u * (k % 4),
-                 kd + (k / 4) * (KV_ATOM >> 4) + 2u * (k % 4), IDESC_S, k != 0);
+          mma_ss(issue, sd, qd + (k / 4) * (Q_ATOM >> 4) + 2u * (k % 4), kd + (k / 4) * (KV_ATOM >> 4) + 2u * (k % 4),
+                 HI, IDESC_S, k != 0);
         mma_commit(issue, bd::smem_u32(&ctl->s_full[x][j & 1]));
         if (x == NM - 1) mma_commit(issue, bd::smem_u32(&ctl->k_empty[j % STAGES]));
       };
@@ -269,11 +275,11 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
           if (x == 0) ok = ok && wait(ctl->v_full[j % STAGES], j / STAGES);
           if (!ok) break;
           bd::tc_fence_after();
-          const uint64_t vd = v_desc + (j % STAGES) * (KV_TILE >> 4);
+          const uint32_t vd = bd::warp_uniform(static_cast<uint32_t>(v_desc) + (j % STAGES) * (KV_TILE >> 4));
+          const uint32_t pd = bd::warp_uniform(tmem + x * TILE + (j & 1) * TOK);
 #pragma unroll
           for (int k = 0; k < TOK / 16; ++k)
-            mma_ts(issue, tmem + O_COL + x * TILE, tmem + x * TILE + (j & 1) * TOK + k * 8, vd + k * (2048u >> 4),
-                   IDESC_O, (j | k) != 0);
+            mma_ts(issue, tmem + O_COL + x * TILE, pd + k * 8, vd + k * (2048u >> 4), HI, IDESC_O, (j | k) != 0);
           mma_commit(issue, bd::smem_u32(j + 1 < n ? &ctl->pv_done[x] : &ctl->o_done[x]));
           if (x == NM - 1) mma_commit(issue, bd::smem_u32(&ctl->v_empty[j % STAGES]));
           if (j + 2 < n) {  // over the weights that the products above read: the tensor pipe takes them in order
