@@ -152,17 +152,6 @@ __device__ __forceinline__ void store4(const RowOut& r, int d, float4 x) {
   else if (r.o != nullptr)
     *reinterpret_cast<float4*>(r.o + d) = x;
 }
-template <class T>
-__device__ __forceinline__ void store8(const RowOut& r, int d, float4 x, float4 y) {
-  if (r.out != nullptr) {
-    *reinterpret_cast<uint4*>(r.out + d) =
-        make_uint4(T::from_float2(make_float2(x.x, x.y)), T::from_float2(make_float2(x.z, x.w)),
-                   T::from_float2(make_float2(y.x, y.y)), T::from_float2(make_float2(y.z, y.w)));
-  } else if (r.o != nullptr) {
-    *reinterpret_cast<float4*>(r.o + d) = x;
-    *reinterpret_cast<float4*>(r.o + d + 4) = y;
-  }
-}
 __device__ __forceinline__ void store_lse(const RowOut& r, float lse2) {
   if (r.l != nullptr) *r.l = r.out != nullptr ? lse2 / bd::LOG2E : lse2;
 }

@@ -25,7 +25,6 @@ namespace {
 constexpr int TILE = TILES_TILE;  // rows of an MMA
 constexpr int TOK = 64;           // tokens of a tile
 constexpr int STAGES = 4;         // tiles of keys and of values in shared memory
-constexpr int GROUPS = TOK / 16;  // scales of a tile
 // Weights are held as f16 times 2^8, with 11 bits down to 2^-22 of the reference, and may exceed it by 2^7 before O is
 // rescaled (2^15 < 65504): a rescale costs a warp about as much as a tile.
 constexpr float P_SHIFT = 8, P_SLACK = 7;
@@ -40,7 +39,7 @@ __device__ uint32_t g_status;  // bd::DEV_* bits
 struct Ctl {
   uint64_t q_full, k_full[STAGES], k_empty[STAGES], v_full[STAGES], v_empty[STAGES];
   uint64_t s_full[2][2], p_full[2][2], pv_done[2], o_done[2], drain;  // by half (and parity of the tile)
-  float ks[8][GROUPS], ve[8][GROUPS];  // page scales of a tile's groups of 16 tokens: factor, exponent
+  float ks[8][TOK / 16], ve[8][TOK / 16];  // page scales of a tile's groups of tokens: factor, exponent
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -158,7 +157,7 @@ __device__ __forceinline__ int ld_global_if(const int32_t* p, bool live, int oth
   return x;
 }
 __device__ __forceinline__ int ld_global_byte_if(const uint8_t* p, bool live) {
-  int x = 0;
+  int x = 127;  // a scale of 1
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %2, 0;\n\t@p ld.global.u8 %0, [%1];\n\t}"
                : "+r"(x)
                : "l"(p), "r"(static_cast<int>(live)));
@@ -182,7 +181,8 @@ __device__ __forceinline__ void decode16(uint4 x, uint32_t (&y)[8]) {
   }
 }
 
-template <class T, int NM, int D>
+// GROUPS: runs of tokens in a tile that share a page, 1 (pages of 64 tokens and more) or 4 (16 and 32).
+template <int NM, int D, int GROUPS>
 __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) {
   constexpr int ATOMS = D / 64;                // 128-byte column blocks of a row
   constexpr uint32_t Q_ATOM = TILE * 128, KV_ATOM = TOK * 128;  // bytes of one
@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
   const uint32_t base = (bd::smem_u32(raw) + 1023u) & ~1023u;
   const uint32_t q_at = base, k_at = q_at + NM * Q_HALF, v_at = k_at + STAGES * KV_TILE;
   Ctl* ctl = reinterpret_cast<Ctl*>(raw + (v_at + STAGES * KV_TILE - bd::smem_u32(raw)));
-  const int tid = threadIdx.x, warp = static_cast<int>(bd::warp_uniform(tid >> 5));
+  const int tid = threadIdx.x, lane = tid & 31, warp = static_cast<int>(bd::warp_uniform(tid >> 5));
   const int n_tiles_rows = gridDim.x / a.n_kv;
   const int head = blockIdx.x / n_tiles_rows, row0 = (n_tiles_rows - 1 - blockIdx.x % n_tiles_rows) * (NM * TILE);
   const int seq = blockIdx.z, part = blockIdx.y;
@@ -309,20 +309,24 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
     const int32_t* table = a.table + seq * a.table_stride;
     const int mask = (1 << a.page_shift) - 1;
     uint4 kx[PER], vx[PER];
-    int pages[PER];  // of the tile to be loaded next (-1: nothing to read)
+    constexpr int PAGES = GROUPS == 1 ? 1 : PER;
+    int pages[PAGES];  // of the tile to be loaded next (-1: nothing to read)
     const auto find = [&](int j) {
 #pragma unroll
-      for (int u = 0; u < PER; ++u) {
-        const int t = begin + j * TOK + mine + u * STEP;
+      for (int u = 0; u < PAGES; ++u) {
+        const int t = begin + j * TOK + (GROUPS == 1 ? 0 : mine + u * STEP);
         pages[u] = ld_global_if(table + (t >> a.page_shift), t < end && (t >> a.page_shift) < a.max_blocks, -1);
+        if (pages[u] >= a.n_pages) pages[u] = -1;
       }
     };
     const auto load = [&](const uint8_t* p, int64_t page_stride, int64_t tok_stride, int j, uint4 (&x)[PER]) {
+      const uint8_t* at[PAGES];
+#pragma unroll
+      for (int u = 0; u < PAGES; ++u) at[u] = p + pages[u] * page_stride;
 #pragma unroll
       for (int u = 0; u < PER; ++u) {
-        const int t = begin + j * TOK + mine + u * STEP;
-        x[u] = ld_global_if(p + pages[u] * page_stride + (t & mask) * tok_stride,
-                            pages[u] >= 0 && pages[u] < a.n_pages && sub * 16 < a.dim);
+        const int t = begin + j * TOK + mine + u * STEP, v = GROUPS == 1 ? 0 : u;
+        x[u] = ld_global_if(at[v] + (t & mask) * tok_stride, pages[v] >= 0 && t < end && sub * 16 < a.dim);
       }
     };
     const auto store = [&](uint32_t at, const uint4 (&x)[PER]) {
@@ -336,22 +340,25 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
         st_shared_v4(rowp + (((c0 + 1) ^ (r & 7)) << 4), y[4], y[5], y[6], y[7]);
       }
     };
-    // a lane of the first few has a tile's group of 16 tokens: its page and, one tile ahead, its scales
-    int group_page = -1, ks_byte = 0, vs_byte = 0;
-    bool group_in = false;
+    // The first warp looks up the scales: a lane has a group's page and, a tile ahead, its scales.
+    const bool scales = ct < 32;
+    int group_page = -1, ks_byte = 127, vs_byte = 127;
     const auto find_group = [&](int j) {
-      const int t = begin + j * TOK + ct * 16;
-      group_page = ld_global_if(table + (t >> a.page_shift), ct < GROUPS && t < end && (t >> a.page_shift) < a.max_blocks, -1);
+      const int t = begin + j * TOK + ct * (TOK / GROUPS);
+      group_page =
+          ld_global_if(table + (t >> a.page_shift), ct < GROUPS && t < end && (t >> a.page_shift) < a.max_blocks, -1);
     };
     const auto find_scales = [&](int j) {  // of tile j, whose pages find_group has looked up; then the pages of the next
-      group_in = group_page >= 0 && group_page < a.n_pages;
-      ks_byte = ld_global_byte_if(a.ks + group_page * a.ks_page + head, group_in);
-      vs_byte = ld_global_byte_if(a.vs + group_page * a.vs_page + head, group_in);
+      const bool in = group_page >= 0 && group_page < a.n_pages;
+      ks_byte = ld_global_byte_if(a.ks + group_page * a.ks_page + head, in);
+      vs_byte = ld_global_byte_if(a.vs + group_page * a.vs_page + head, in);
       find_group(j + 1);
     };
     if (n > 0) {
-      find_group(0);
-      find_scales(0);
+      if (scales) {
+        find_group(0);
+        find_scales(0);
+      }
       find(0);
       load(kp, a.k_page, row_k, 0, kx);
       load(vp, a.v_page, row_v, 0, vx);
@@ -361,11 +368,13 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
       find(j + 1);
       ok = wait(ctl->k_empty[j % STAGES], j / STAGES + 1);
       if (!ok) break;
-      if (ct < GROUPS) {
-        ctl->ks[j & 7][ct] = group_in ? pow2i(ks_byte - 127) : 1.f;
-        ctl->ve[j & 7][ct] = group_in ? static_cast<float>(vs_byte - 127) : 0.f;
+      if (scales) {
+        if (ct < GROUPS) {
+          ctl->ks[j & 7][ct] = pow2i(ks_byte - 127);
+          ctl->ve[j & 7][ct] = static_cast<float>(vs_byte - 127);
+        }
+        find_scales(j + 1);
       }
-      find_scales(j + 1);
       store(k_at + (j % STAGES) * KV_TILE, kx);
       fence_proxy_async();
       bd::mbar_arrive(bd::smem_u32(&ctl->k_full[j % STAGES]));
@@ -386,36 +395,48 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
     const int h = head * a.group + row - i * a.group;
     const int vis = live ? min(visible(a, sq, i), end) : 0;
     float coef = 0.f;
+    // A warp moves its 32 rows together, LANES lanes to a row (16 bytes each): queries in, results out.
+    constexpr int LANES = D / 8, ROWS = 32 / LANES;
+    const int my_c = lane % LANES, my_r = lane / LANES, warp_row = (warp & 3) * 32;
     if (n > 0) {
-      // the row in f16 times a power of two, with the sign of the scale
+      // rows in f16 times a power of two each, with the sign of the scale
       const uint16_t* q = static_cast<const uint16_t*>(a.q) + static_cast<int64_t>(sq.q0 + i) * a.q_tok + h * a.q_head;
-      uint4 w[D / 8];
-      float amax = 0.f;
+      const float sign = a.coef < 0.f ? -1.f : 1.f;
+      int shift = 0;
 #pragma unroll
-      for (int c = 0; c < D / 8; ++c) {
-        w[c] = make_uint4(0, 0, 0, 0);
-        if (live && c * 8 < a.dim) w[c] = *reinterpret_cast<const uint4*>(q + c * 8);
-        const uint32_t ww[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
+      for (int half = 0; half < 32 / ROWS; half += 8) {
+        uint4 w[8];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const float2 f = T::to_float2(ww[u]);
-          amax = bd::max3(amax, fabsf(f.x), fabsf(f.y));
+        for (int u = 0; u < 8; ++u) {
+          const int rr = (half + u) * ROWS + my_r;
+          const uint64_t src = __shfl_sync(~0u, reinterpret_cast<uint64_t>(q), rr);
+          w[u] = ld_global_if(reinterpret_cast<const uint8_t*>(src) + my_c * 16, row - lane + rr < rows && my_c * 8 < a.dim);
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const int rr = warp_row + (half + u) * ROWS + my_r;
+          const uint32_t ww[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
+          float2 g[4];
+          float amax = 0.f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            g[e] = a.f16 ? F16::to_float2(ww[e]) : Bf16::to_float2(ww[e]);
+            amax = bd::max3(amax, fabsf(g[e].x), fabsf(g[e].y));
+          }
+#pragma unroll
+          for (int d = 1; d < LANES; d <<= 1) amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, d));
+          const int s = row_shift(amax);
+          const float f = sign * pow2i(s);
+          uint32_t y[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = f16x2(make_float2(g[e].x * f, g[e].y * f));
+          st_shared_v4(q_at + x * Q_HALF + (my_c / 8) * Q_ATOM + rr * 128 + (((my_c % 8) ^ (rr & 7)) << 4), y[0], y[1],
+                       y[2], y[3]);
+          const int given = __shfl_sync(~0u, s, (lane % ROWS) * LANES);  // to the row's own lane
+          if (lane / ROWS == half + u) shift = given;
         }
       }
-      const int s = row_shift(amax);
-      const float f = a.coef < 0.f ? -pow2i(s) : pow2i(s);
-      coef = fabsf(a.coef) * pow2i(-s);
-#pragma unroll
-      for (int c = 0; c < D / 8; ++c) {
-        const uint32_t ww[4] = {w[c].x, w[c].y, w[c].z, w[c].w};
-        uint32_t y[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const float2 v = T::to_float2(ww[u]);
-          y[u] = f16x2(make_float2(v.x * f, v.y * f));
-        }
-        st_shared_v4(q_at + x * Q_HALF + (c / 8) * Q_ATOM + r * 128 + (((c % 8) ^ (r & 7)) << 4), y[0], y[1], y[2], y[3]);
-      }
+      coef = fabsf(a.coef) * pow2i(-shift);
       fence_proxy_async();
       bd::mbar_arrive(bd::smem_u32(&ctl->q_full));
     }
@@ -436,16 +457,20 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
       __syncwarp();
       tmem_ld64(s_at, v);
       float s_top = -INFINITY, u_top = -INFINITY;
+      constexpr int W = TOK / GROUPS;  // columns of a group
 #pragma unroll
       for (int b = 0; b < GROUPS; ++b) {
-        if (CUT)
+        float t = -INFINITY, t1 = -INFINITY;
 #pragma unroll
-          for (int e = b * 16; e < b * 16 + 16; ++e)
-            if (e >= left) v[e] = -INFINITY;
-        float t = v[b * 16];
+        for (int e = b * W; e < b * W + W; e += 4) {
+          if (CUT)
 #pragma unroll
-        for (int e = 1; e < 15; e += 2) t = bd::max3(t, v[b * 16 + e], v[b * 16 + e + 1]);
-        t = fmaxf(t, v[b * 16 + 15]);
+            for (int c = e; c < e + 4; ++c)
+              if (c >= left) v[c] = -INFINITY;
+          t = bd::max3(t, v[e], v[e + 1]);
+          t1 = bd::max3(t1, v[e + 2], v[e + 3]);
+        }
+        t = fmaxf(t, t1);
         const float s2 = CUT && t == -INFINITY ? t : t * (coef * ks[b]);
         s_top = fmaxf(s_top, s2);
         u_top = fmaxf(u_top, s2 + ve[b]);
@@ -475,28 +500,25 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
       }
       __syncwarp();
       const float ms = m == -INFINITY ? 0.f : m, Ms = M == -INFINITY ? 0.f : M;
+      uint32_t p[16];
 #pragma unroll
-      for (int c = 0; c < TOK / 32; ++c) {
-        uint32_t p[16];
+      for (int b = 0; b < GROUPS; ++b) {
+        const float f = coef * ks[b], ref = Ms - ve[b] - P_SHIFT;
+        float2 sum[2] = {{0.f, 0.f}, {0.f, 0.f}};
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const float f = coef * ks[c * 2 + b], ref = Ms - ve[c * 2 + b] - P_SHIFT;
-          float2 sum = {0.f, 0.f};
-#pragma unroll
-          for (int e = 0; e < 16; e += 2) {
-            const int col = c * 32 + b * 16 + e;
-            const float2 y = bd::fma2(make_float2(v[col], v[col + 1]), make_float2(f, f), make_float2(-ref, -ref));
-            float2 w = make_float2(bd::ex2_approx(y.x), bd::ex2_approx(y.y));
-            if (CUT) {
-              if (col >= left) w.x = 0.f;
-              if (col + 1 >= left) w.y = 0.f;
-            }
-            sum = bd::add2(sum, w);
-            p[b * 8 + e / 2] = f16x2(w);
+        for (int col = b * W; col < b * W + W; col += 2) {
+          const float2 y = bd::fma2(make_float2(v[col], v[col + 1]), make_float2(f, f), make_float2(-ref, -ref));
+          float2 w = make_float2(bd::ex2_approx(y.x), bd::ex2_approx(y.y));
+          if (CUT) {
+            if (col >= left) w.x = 0.f;
+            if (col + 1 >= left) w.y = 0.f;
           }
-          L += (sum.x + sum.y) * bd::ex2_approx(ref - ms);
+          sum[col / 2 & 1] = bd::add2(sum[col / 2 & 1], w);
+          p[col / 2 % 16] = f16x2(w);
+          if (col % 32 == 30) tmem_st16(s_at + col / 32 * 16, p);
         }
-        tmem_st16(s_at + c * 16, p);
+        sum[0] = bd::add2(sum[0], sum[1]);
+        L += (sum[0].x + sum[0].y) * bd::ex2_approx(ref - ms);
       }
       bd::tmem_st_wait();
       return true;
@@ -522,23 +544,65 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
     const float lse2 = L == 0.f ? -INFINITY : ms + log2f(L);
     RowOut o = {nullptr, nullptr, nullptr};
     if (live) o = row_out(a, sq, seq, part, i, h, visible(a, sq, i));
-    if (any_live) {
+    // Through the half's part of the queries' shared memory, which no product reads any more: lanes write their rows,
+    // the warp stores them row by row.
+    const uint32_t stage = q_at + x * Q_HALF + warp_row * (D * 2);
+    const auto give = [&](const void* mine, bool there) {  // a row's D * 2 bytes to where its lane says
+#pragma unroll 4
+      for (int u = 0; u < 32 / ROWS; ++u) {
+        const int rr = u * ROWS + my_r;
+        const uint64_t dst = __shfl_sync(~0u, reinterpret_cast<uint64_t>(mine), rr);
+        const uint4 w = bd::ld_shared_v4(stage + rr * (D * 2) + ((my_c ^ (rr & 7)) << 4));
+        if (dst != 0 && there) *reinterpret_cast<uint4*>(dst + my_c * 16) = w;
+      }
+    };
+    const auto take = [&](int c, float (&v)[32]) {  // 32 elements of the lane's row
+      if (n > 0)
+        bd::tmem_ld32(o_at + c * 32, v);
+      else
+#pragma unroll
+        for (int e = 0; e < 32; ++e) v[e] = 0.f;
+#pragma unroll
+      for (int e = 0; e < 32; ++e) v[e] *= f;
+    };
+    if (__any_sync(~0u, o.out != nullptr)) {
 #pragma unroll 1
       for (int c = 0; c < D / 32; ++c) {
         float v[32];
-        if (n > 0)
-          bd::tmem_ld32(o_at + c * 32, v);
-        else
+        take(c, v);
 #pragma unroll
-          for (int e = 0; e < 32; ++e) v[e] = 0.f;
+        for (int e = 0; e < 4; ++e) {
+          uint32_t y[4];
 #pragma unroll
-        for (int e = 0; e < 32; e += 8)
-          if (c * 32 + e < a.dim)
-            store8<T>(o, c * 32 + e, make_float4(v[e] * f, v[e + 1] * f, v[e + 2] * f, v[e + 3] * f),
-                      make_float4(v[e + 4] * f, v[e + 5] * f, v[e + 6] * f, v[e + 7] * f));
+          for (int u = 0; u < 4; ++u) {
+            const float2 g = make_float2(v[e * 8 + u * 2], v[e * 8 + u * 2 + 1]);
+            y[u] = a.f16 ? F16::from_float2(g) : Bf16::from_float2(g);
+          }
+          st_shared_v4(stage + lane * (D * 2) + (((c * 4 + e) ^ (lane & 7)) << 4), y[0], y[1], y[2], y[3]);
+        }
       }
-      if (live) store_lse(o, lse2);
+      __syncwarp();
+      give(o.out, my_c * 8 < a.dim);
+      __syncwarp();
     }
+    if (__any_sync(~0u, o.o != nullptr)) {  // fp32: half of the elements at a time
+#pragma unroll 1
+      for (int c = 0; c < D / 32; ++c) {
+        float v[32];
+        take(c, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          st_shared_v4(stage + lane * (D * 2) + (((c * 8 + e) % LANES ^ (lane & 7)) << 4), __float_as_uint(v[e * 4]),
+                       __float_as_uint(v[e * 4 + 1]), __float_as_uint(v[e * 4 + 2]), __float_as_uint(v[e * 4 + 3]));
+        if ((c + 1) % (D / 64) == 0) {
+          const int d = (c * 32 + 32) / (D / 2) * (D / 2) - D / 2;  // the half's first element
+          __syncwarp();
+          give(o.o == nullptr ? nullptr : o.o + d, d + my_c * 4 < a.dim);
+          __syncwarp();
+        }
+      }
+    }
+    if (live) store_lse(o, lse2);
   }
 
   __syncwarp();
@@ -548,27 +612,28 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
   if (warp == MMA_WARP) bd::tmem_dealloc(tmem, 512);
 }
 
-template <class T, int NM, int D>
+template <int NM, int D, int GROUPS>
 cudaError_t launch(const AttnArgs& a, cudaStream_t st) {
   static std::atomic<bool> ready[64];  // by device
-  if (cudaError_t e = allow_smem(attn_tiles_kernel<T, NM, D>, smem_bytes<NM, D>(), ready); e != cudaSuccess) return e;
+  const auto kernel = attn_tiles_kernel<NM, D, GROUPS>;
+  if (cudaError_t e = allow_smem(kernel, smem_bytes<NM, D>(), ready); e != cudaSuccess) return e;
   const int tiles = (a.max_q * a.group + NM * TILE - 1) / (NM * TILE);
   const dim3 grid(tiles * a.n_kv, a.n_split, a.n_seq);
-  attn_tiles_kernel<T, NM, D><<<grid, threads(NM), smem_bytes<NM, D>(), st>>>(a);
+  kernel<<<grid, threads(NM), smem_bytes<NM, D>(), st>>>(a);
   return cudaGetLastError();
 }
 
-template <class T>
-cudaError_t launch_type(const AttnArgs& a, cudaStream_t st) {
-  const bool one = a.max_q * a.group <= TILE;
-  if (a.dim <= 64) return one ? launch<T, 1, 64>(a, st) : launch<T, 2, 64>(a, st);
-  return one ? launch<T, 1, 128>(a, st) : launch<T, 2, 128>(a, st);
+template <int NM, int D>
+cudaError_t launch_pages(const AttnArgs& a, cudaStream_t st) {
+  return (1 << a.page_shift) >= TOK ? launch<NM, D, 1>(a, st) : launch<NM, D, 4>(a, st);
 }
 
 }  // namespace
 
 cudaError_t launch_attn_tiles(const AttnArgs& a, cudaStream_t st) {
-  return a.f16 ? launch_type<F16>(a, st) : launch_type<Bf16>(a, st);
+  const bool one = a.max_q * a.group <= TILE;
+  if (a.dim <= 64) return one ? launch_pages<1, 64>(a, st) : launch_pages<2, 64>(a, st);
+  return one ? launch_pages<1, 128>(a, st) : launch_pages<2, 128>(a, st);
 }
 
 cudaError_t tiles_status(cudaStream_t st, uint32_t* bits) {
