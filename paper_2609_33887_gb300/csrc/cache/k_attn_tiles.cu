@@ -37,8 +37,9 @@ constexpr int threads(int nm) { return (4 * nm + CONV_WARPS + 4) * 32; }
 __device__ uint32_t g_status;  // bd::DEV_* bits
 
 struct Ctl {
-  uint64_t q_full, k_full[STAGES], k_empty[STAGES], v_full[STAGES], v_empty[STAGES];
-  uint64_t s_full[2][2], p_full[2][2], pv_done[2], o_done[2], drain;  // by half (and parity of the tile)
+  uint64_t q_full, kv_full[STAGES], kv_empty[STAGES];
+  uint64_t s_full[2][2], p_full[2][2];   // by half and parity of the tile
+  uint64_t o_before[2], o_done[2], drain;  // by half: O without, and with its last product
   float ks[8][TOK / 16], ve[8][TOK / 16];  // page scales of a tile's groups of tokens: factor, exponent
   uint32_t tmem_base;
   int abort_flag;
@@ -209,17 +210,15 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
   if (tid == 0) {
     bd::mbar_init(bd::smem_u32(&ctl->q_full), NM * TILE);
     for (int i = 0; i < STAGES; ++i) {
-      bd::mbar_init(bd::smem_u32(&ctl->k_full[i]), CONV_WARPS * 32);
-      bd::mbar_init(bd::smem_u32(&ctl->v_full[i]), CONV_WARPS * 32);
-      bd::mbar_init(bd::smem_u32(&ctl->k_empty[i]), 1);
-      bd::mbar_init(bd::smem_u32(&ctl->v_empty[i]), 1);
+      bd::mbar_init(bd::smem_u32(&ctl->kv_full[i]), CONV_WARPS * 32);
+      bd::mbar_init(bd::smem_u32(&ctl->kv_empty[i]), 1);
     }
     for (int x = 0; x < 2; ++x) {
       for (int b = 0; b < 2; ++b) {
         bd::mbar_init(bd::smem_u32(&ctl->s_full[x][b]), 1);
         bd::mbar_init(bd::smem_u32(&ctl->p_full[x][b]), TILE);
       }
-      bd::mbar_init(bd::smem_u32(&ctl->pv_done[x]), 1);
+      bd::mbar_init(bd::smem_u32(&ctl->o_before[x]), 1);
       bd::mbar_init(bd::smem_u32(&ctl->o_done[x]), 1);
     }
     bd::mbar_init(bd::smem_u32(&ctl->drain), 1);
@@ -247,46 +246,49 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
     if (warp == MMA_WARP) {
       const uint32_t issue = bd::elect_one();
       constexpr uint32_t IDESC_S = bd::idesc_f16_f32(TILE, TOK), IDESC_O = bd::idesc_f16_f32(TILE, D) | B_MN_MAJOR;
-      const uint64_t q_desc = bd::sw128_kmajor_desc(q_at), k_desc = bd::sw128_kmajor_desc(k_at);
-      const uint64_t v_desc = sw128_mnmajor_desc(v_at, KV_ATOM);
-      constexpr uint32_t HI = (1024u >> 4) | (1u << 14) | (2u << 29);  // of all three: 1 KB stride, version, swizzle
-      const auto scores = [&](int x, int j) {  // S of half x, tile j; addresses in descriptors count 16 bytes
-        const uint32_t qd = bd::warp_uniform(static_cast<uint32_t>(q_desc) + x * (Q_HALF >> 4));
-        const uint32_t kd = bd::warp_uniform(static_cast<uint32_t>(k_desc) + (j % STAGES) * (KV_TILE >> 4));
-        const uint32_t sd = bd::warp_uniform(tmem + x * TILE + (j & 1) * TOK);
+      // low words of the descriptors (addresses count 16 bytes) and their common upper word: 1 KB stride, version, swizzle
+      const uint32_t q_lo = bd::warp_uniform(static_cast<uint32_t>(bd::sw128_kmajor_desc(q_at)));
+      const uint32_t k_lo = bd::warp_uniform(static_cast<uint32_t>(bd::sw128_kmajor_desc(k_at)));
+      const uint32_t v_lo = bd::warp_uniform(static_cast<uint32_t>(sw128_mnmajor_desc(v_at, KV_ATOM)));
+      constexpr uint32_t HI = (1024u >> 4) | (1u << 14) | (2u << 29);
+      const auto scores = [&](int x, int u) {  // S of half x, a tile of stage u
 #pragma unroll
         for (int k = 0; k < D / 16; ++k)
-          mma_ss(issue, sd, qd + (k / 4) * (Q_ATOM >> 4) + 2u * (k % 4), kd + (k / 4) * (KV_ATOM >> 4) + 2u * (k % 4),
-                 HI, IDESC_S, k != 0);
-        mma_commit(issue, bd::smem_u32(&ctl->s_full[x][j & 1]));
-        if (x == NM - 1) mma_commit(issue, bd::smem_u32(&ctl->k_empty[j % STAGES]));
+          mma_ss(issue, tmem + x * TILE + (u & 1) * TOK, q_lo + x * (Q_HALF >> 4) + (k / 4) * (Q_ATOM >> 4) + 2u * (k % 4),
+                 k_lo + u * (KV_TILE >> 4) + (k / 4) * (KV_ATOM >> 4) + 2u * (k % 4), HI, IDESC_S, k != 0);
+        mma_commit(issue, bd::smem_u32(&ctl->s_full[x][u & 1]));
       };
       bool ok = n > 0 && wait(ctl->q_full, 0);
-      for (int j = 0; ok && j < min(n, 2); ++j) {
-        ok = wait(ctl->k_full[j], 0);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        if (!ok || u >= n) break;
+        ok = wait(ctl->kv_full[u], 0);
+        if (!ok) break;
         bd::tc_fence_after();
-        if (ok)
-          for (int x = 0; x < NM; ++x) scores(x, j);
+#pragma unroll
+        for (int x = 0; x < NM; ++x) scores(x, u);
       }
-      for (int j = 0; ok && j < n; ++j) {
+      for (int j0 = 0; ok && j0 < n; j0 += STAGES) {
 #pragma unroll
-        for (int x = 0; x < NM; ++x) {
-          ok = ok && wait(ctl->p_full[x][j & 1], j >> 1);
-          if (x == 0) ok = ok && wait(ctl->v_full[j % STAGES], j / STAGES);
-          if (!ok) break;
-          bd::tc_fence_after();
-          const uint32_t vd = bd::warp_uniform(static_cast<uint32_t>(v_desc) + (j % STAGES) * (KV_TILE >> 4));
-          const uint32_t pd = bd::warp_uniform(tmem + x * TILE + (j & 1) * TOK);
+        for (int u = 0; u < STAGES; ++u) {  // stages by number: every address is a constant away from its base
+          const int j = j0 + u;
+          if (!ok || j >= n) break;
 #pragma unroll
-          for (int k = 0; k < TOK / 16; ++k)
-            mma_ts(issue, tmem + O_COL + x * TILE, pd + k * 8, vd + k * (2048u >> 4), HI, IDESC_O, (j | k) != 0);
-          mma_commit(issue, bd::smem_u32(j + 1 < n ? &ctl->pv_done[x] : &ctl->o_done[x]));
-          if (x == NM - 1) mma_commit(issue, bd::smem_u32(&ctl->v_empty[j % STAGES]));
-          if (j + 2 < n) {  // over the weights that the products above read: the tensor pipe takes them in order
-            if (x == 0) ok = wait(ctl->k_full[(j + 2) % STAGES], (j + 2) / STAGES);
-            if (!ok) break;
+          for (int x = 0; x < NM; ++x) {
+            if (!ok || !(ok = wait(ctl->p_full[x][u & 1], j >> 1))) break;
             bd::tc_fence_after();
-            scores(x, j + 2);
+#pragma unroll
+            for (int k = 0; k < TOK / 16; ++k)
+              mma_ts(issue, tmem + O_COL + x * TILE, tmem + x * TILE + (u & 1) * TOK + k * 8,
+                     v_lo + u * (KV_TILE >> 4) + k * (2048u >> 4), HI, IDESC_O, (j | k) != 0);
+            if (x == NM - 1) mma_commit(issue, bd::smem_u32(&ctl->kv_empty[u]));
+            if (j + 2 < n) {  // over the weights that the products above read: the tensor pipe takes them in order
+              if (x == 0 && !(ok = wait(ctl->kv_full[(u + 2) % STAGES], (j + 2) / STAGES))) break;
+              bd::tc_fence_after();
+              scores(x, (u + 2) % STAGES);
+            } else {
+              mma_commit(issue, bd::smem_u32(j + 1 < n ? &ctl->o_before[x] : &ctl->o_done[x]));
+            }
           }
         }
       }
@@ -366,7 +368,7 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
     bool ok = true;
     for (int j = 0; j < n; ++j) {
       find(j + 1);
-      ok = wait(ctl->k_empty[j % STAGES], j / STAGES + 1);
+      ok = wait(ctl->kv_empty[j % STAGES], j / STAGES + 1);
       if (!ok) break;
       if (scales) {
         if (ct < GROUPS) {
@@ -376,15 +378,11 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
         find_scales(j + 1);
       }
       store(k_at + (j % STAGES) * KV_TILE, kx);
-      fence_proxy_async();
-      bd::mbar_arrive(bd::smem_u32(&ctl->k_full[j % STAGES]));
       load(kp, a.k_page, row_k, j + 1, kx);
-      ok = wait(ctl->v_empty[j % STAGES], j / STAGES + 1);
-      if (!ok) break;
       store(v_at + (j % STAGES) * KV_TILE, vx);
-      fence_proxy_async();
-      bd::mbar_arrive(bd::smem_u32(&ctl->v_full[j % STAGES]));
       load(vp, a.v_page, row_v, j + 1, vx);
+      fence_proxy_async();
+      bd::mbar_arrive(bd::smem_u32(&ctl->kv_full[j % STAGES]));
     }
   } else {
     // ------------------------------------------------------------- softmax
@@ -399,42 +397,41 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
     constexpr int LANES = D / 8, ROWS = 32 / LANES;
     const int my_c = lane % LANES, my_r = lane / LANES, warp_row = (warp & 3) * 32;
     if (n > 0) {
-      // rows in f16 times a power of two each, with the sign of the scale
+      // Rows in f16, with the sign of the scale; bf16 ones times a power of two that brings the largest finite element of
+      // the warp's rows into [2^14, 2^15): elements down to 2^-32 of it keep their eight bits.
       const uint16_t* q = static_cast<const uint16_t*>(a.q) + static_cast<int64_t>(sq.q0 + i) * a.q_tok + h * a.q_head;
-      const float sign = a.coef < 0.f ? -1.f : 1.f;
+      uint4 w[32 / ROWS];
+#pragma unroll
+      for (int u = 0; u < 32 / ROWS; ++u) {
+        const int rr = u * ROWS + my_r;
+        const uint64_t src = __shfl_sync(~0u, reinterpret_cast<uint64_t>(q), rr);
+        w[u] = ld_global_if(reinterpret_cast<const uint8_t*>(src) + my_c * 16, row - lane + rr < rows && my_c * 8 < a.dim);
+      }
       int shift = 0;
+      if (!a.f16) {
+        uint32_t most = 0;  // magnitudes' patterns, two to a word
 #pragma unroll
-      for (int half = 0; half < 32 / ROWS; half += 8) {
-        uint4 w[8];
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          const int rr = (half + u) * ROWS + my_r;
-          const uint64_t src = __shfl_sync(~0u, reinterpret_cast<uint64_t>(q), rr);
-          w[u] = ld_global_if(reinterpret_cast<const uint8_t*>(src) + my_c * 16, row - lane + rr < rows && my_c * 8 < a.dim);
+        for (int u = 0; u < 32 / ROWS; ++u) {
+          const uint32_t t = __vmaxu2(__vmaxu2(w[u].x & 0x7fff7fffu, w[u].y & 0x7fff7fffu),
+                                      __vmaxu2(w[u].z & 0x7fff7fffu, w[u].w & 0x7fff7fffu));
+          if ((t & 0xffffu) < 0x7f80u && t < 0x7f800000u) most = __vmaxu2(most, t);
         }
+        most = __reduce_max_sync(~0u, max(most & 0xffffu, most >> 16));
+        shift = row_shift(__uint_as_float(most << 16));
+      }
+      const float f = a.coef < 0.f ? -pow2i(shift) : pow2i(shift);
+      const uint32_t flip = a.coef < 0.f ? 0x80008000u : 0u;
 #pragma unroll
-        for (int u = 0; u < 8; ++u) {
-          const int rr = warp_row + (half + u) * ROWS + my_r;
-          const uint32_t ww[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
-          float2 g[4];
-          float amax = 0.f;
+      for (int u = 0; u < 32 / ROWS; ++u) {
+        const int rr = warp_row + u * ROWS + my_r;
+        uint32_t y[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            g[e] = a.f16 ? F16::to_float2(ww[e]) : Bf16::to_float2(ww[e]);
-            amax = bd::max3(amax, fabsf(g[e].x), fabsf(g[e].y));
-          }
-#pragma unroll
-          for (int d = 1; d < LANES; d <<= 1) amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, d));
-          const int s = row_shift(amax);
-          const float f = sign * pow2i(s);
-          uint32_t y[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) y[e] = f16x2(make_float2(g[e].x * f, g[e].y * f));
-          st_shared_v4(q_at + x * Q_HALF + (my_c / 8) * Q_ATOM + rr * 128 + (((my_c % 8) ^ (rr & 7)) << 4), y[0], y[1],
-                       y[2], y[3]);
-          const int given = __shfl_sync(~0u, s, (lane % ROWS) * LANES);  // to the row's own lane
-          if (lane / ROWS == half + u) shift = given;
+        for (int e = 0; e < 4; ++e) {
+          const float2 g = Bf16::to_float2(y[e]);
+          y[e] = a.f16 ? y[e] ^ flip : f16x2(make_float2(g.x * f, g.y * f));
         }
+        st_shared_v4(q_at + x * Q_HALF + (my_c / 8) * Q_ATOM + rr * 128 + (((my_c % 8) ^ (rr & 7)) << 4), y[0], y[1], y[2],
+                     y[3]);
       }
       coef = fabsf(a.coef) * pow2i(-shift);
       fence_proxy_async();
@@ -481,8 +478,8 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
       const bool grow = u_top > M + P_SLACK || (M == -INFINITY && u_top > M);
       if (__any_sync(~0u, grow)) {
         if (j > 0) {
-          // (this tile's scores followed O's product of two tiles ago, so no phase is skipped, and none is ahead)
-          if (!wait(ctl->pv_done[x], j - 1)) return false;
+          // O's product of the tile before is done where the next tile's scores, issued behind it, are
+          if (!(j + 1 < n ? wait(ctl->s_full[x][(j + 1) & 1], (j + 1) >> 1) : wait(ctl->o_before[x], 0))) return false;
           bd::tc_fence_after();
           const float f = grow ? bd::ex2_approx(M - u_top) : 1.f;
           __syncwarp();  // tensor-memory accesses take the whole warp at once
