@@ -310,25 +310,24 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
     const uint8_t* vp = a.v + head * a.v_head + sub * 16;
     const int32_t* table = a.table + seq * a.table_stride;
     const int mask = (1 << a.page_shift) - 1;
-    uint4 kx[PER], vx[PER];
+    // Two tiles of codes are on their way in registers, and the page numbers of the one behind them.
+    uint4 kx[2][PER], vx[2][PER];
     constexpr int PAGES = GROUPS == 1 ? 1 : PER;
-    int pages[PAGES];  // of the tile to be loaded next (-1: nothing to read)
+    int pages[PAGES];  // -1: nothing to read
     const auto find = [&](int j) {
 #pragma unroll
       for (int u = 0; u < PAGES; ++u) {
         const int t = begin + j * TOK + (GROUPS == 1 ? 0 : mine + u * STEP);
         pages[u] = ld_global_if(table + (t >> a.page_shift), t < end && (t >> a.page_shift) < a.max_blocks, -1);
-        if (pages[u] >= a.n_pages) pages[u] = -1;
       }
     };
-    const auto load = [&](const uint8_t* p, int64_t page_stride, int64_t tok_stride, int j, uint4 (&x)[PER]) {
-      const uint8_t* at[PAGES];
-#pragma unroll
-      for (int u = 0; u < PAGES; ++u) at[u] = p + pages[u] * page_stride;
+    const auto load = [&](int j, uint4 (&k)[PER], uint4 (&v)[PER]) {  // of tile j, whose pages were found
 #pragma unroll
       for (int u = 0; u < PER; ++u) {
-        const int t = begin + j * TOK + mine + u * STEP, v = GROUPS == 1 ? 0 : u;
-        x[u] = ld_global_if(at[v] + (t & mask) * tok_stride, pages[v] >= 0 && t < end && sub * 16 < a.dim);
+        const int t = begin + j * TOK + mine + u * STEP, page = pages[GROUPS == 1 ? 0 : u];
+        const bool live = page >= 0 && page < a.n_pages && t < end && sub * 16 < a.dim;
+        k[u] = ld_global_if(kp + page * a.k_page + (t & mask) * row_k, live);
+        v[u] = ld_global_if(vp + page * a.v_page + (t & mask) * row_v, live);
       }
     };
     const auto store = [&](uint32_t at, const uint4 (&x)[PER]) {
@@ -362,27 +361,31 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
         find_scales(0);
       }
       find(0);
-      load(kp, a.k_page, row_k, 0, kx);
-      load(vp, a.v_page, row_v, 0, vx);
+      load(0, kx[0], vx[0]);
+      find(1);
+      load(1, kx[1], vx[1]);
+      find(2);
     }
     bool ok = true;
-    for (int j = 0; j < n; ++j) {
-      find(j + 1);
-      ok = wait(ctl->kv_empty[j % STAGES], j / STAGES + 1);
-      if (!ok) break;
-      if (scales) {
-        if (ct < GROUPS) {
-          ctl->ks[j & 7][ct] = pow2i(ks_byte - 127);
-          ctl->ve[j & 7][ct] = static_cast<float>(vs_byte - 127);
+    for (int j0 = 0; ok && j0 < n; j0 += 2) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int j = j0 + b;
+        if (j >= n || !(ok = wait(ctl->kv_empty[j % STAGES], j / STAGES + 1))) break;
+        if (scales) {
+          if (ct < GROUPS) {
+            ctl->ks[j & 7][ct] = pow2i(ks_byte - 127);
+            ctl->ve[j & 7][ct] = static_cast<float>(vs_byte - 127);
+          }
+          find_scales(j + 1);
         }
-        find_scales(j + 1);
+        store(k_at + (j % STAGES) * KV_TILE, kx[b]);
+        store(v_at + (j % STAGES) * KV_TILE, vx[b]);
+        fence_proxy_async();
+        bd::mbar_arrive(bd::smem_u32(&ctl->kv_full[j % STAGES]));
+        load(j + 2, kx[b], vx[b]);
+        find(j + 3);
       }
-      store(k_at + (j % STAGES) * KV_TILE, kx);
-      load(kp, a.k_page, row_k, j + 1, kx);
-      store(v_at + (j % STAGES) * KV_TILE, vx);
-      load(vp, a.v_page, row_v, j + 1, vx);
-      fence_proxy_async();
-      bd::mbar_arrive(bd::smem_u32(&ctl->kv_full[j % STAGES]));
     }
   } else {
     // ------------------------------------------------------------- softmax
