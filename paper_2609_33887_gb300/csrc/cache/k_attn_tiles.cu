@@ -46,7 +46,7 @@ struct Shape {
 __device__ uint32_t g_status;  // bd::DEV_* bits
 
 struct Ctl {
-  uint64_t q_full, kv_full[4], kv_empty[4];
+  uint64_t q_full, k_full[4], k_empty[4], v_full[4], v_empty[4];
   uint64_t s_full[2][2], p_full[2][2];     // by half and parity of the tile
   uint64_t o_before[2], o_done[2], drain;  // by half: O without (AHEAD = 2), and with its last product
   float ks[8][8], ve[8][8];                // page scales of a tile's groups of 16 tokens: factor, exponent
@@ -141,12 +141,10 @@ __device__ __forceinline__ int ld_global_byte_if(const uint8_t* p, bool live) {
                : "l"(p), "r"(static_cast<int>(live)));
   return x;
 }
-__device__ __forceinline__ uint4 ld_global_if(const uint8_t* p, bool live) {
-  uint4 x = {0, 0, 0, 0};
+__device__ __forceinline__ void ld_global_over(uint4& x, const uint8_t* p, bool live) {
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %5, 0;\n\t@p ld.global.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
                : "+r"(x.x), "+r"(x.y), "+r"(x.z), "+r"(x.w)
                : "l"(p), "r"(static_cast<int>(live)));
-  return x;
 }
 
 // Sixteen codes to f16, two 16-byte chunks.
@@ -206,8 +204,10 @@ __global__ void __launch_bounds__(Shape<NM>::THREADS, 1) attn_tiles_kernel(AttnA
   if (tid == 0) {
     bd::mbar_init(bd::smem_u32(&ctl->q_full), Sh::SOFT_WARPS);  // a warp's arrival, like that of every barrier with warps
     for (int i = 0; i < STAGES; ++i) {
-      bd::mbar_init(bd::smem_u32(&ctl->kv_full[i]), CONV_WARPS + 1);
-      bd::mbar_init(bd::smem_u32(&ctl->kv_empty[i]), 1);
+      bd::mbar_init(bd::smem_u32(&ctl->k_full[i]), CONV_WARPS + 1);
+      bd::mbar_init(bd::smem_u32(&ctl->v_full[i]), CONV_WARPS);
+      bd::mbar_init(bd::smem_u32(&ctl->k_empty[i]), 1);
+      bd::mbar_init(bd::smem_u32(&ctl->v_empty[i]), 1);
     }
     for (int x = 0; x < 2; ++x) {
       for (int b = 0; b < 2; ++b) {
@@ -257,12 +257,13 @@ __global__ void __launch_bounds__(Shape<NM>::THREADS, 1) attn_tiles_kernel(AttnA
           mma_ss(issue, tmem + x * TILE + u % AHEAD * TOK, q_lo + x * (Q_HALF >> 4) + (k / 4) * (Q_ATOM >> 4) + 2u * (k % 4),
                  k_lo + u * (KV_TILE >> 4) + (k / 4) * (KV_ATOM >> 4) + 2u * (k % 4), HI, IDESC_S, k != 0);
         mma_commit(issue, bd::smem_u32(&ctl->s_full[x][u % AHEAD]));
+        if (x == NM - 1) mma_commit(issue, bd::smem_u32(&ctl->k_empty[u]));
       };
       bool ok = n > 0 && wait(ctl->q_full, 0);
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) {
         if (!ok || u >= n) break;
-        ok = wait(ctl->kv_full[u], 0);
+        ok = wait(ctl->k_full[u], 0);
         if (!ok) break;
         bd::tc_fence_after();
 #pragma unroll
@@ -276,15 +277,16 @@ __global__ void __launch_bounds__(Shape<NM>::THREADS, 1) attn_tiles_kernel(AttnA
 #pragma unroll
           for (int x = 0; x < NM; ++x) {
             if (!ok || !(ok = wait(ctl->p_full[x][u % AHEAD], j / AHEAD))) break;
+            if (x == 0 && !(ok = wait(ctl->v_full[u], j / STAGES))) break;
             bd::tc_fence_after();
 #pragma unroll
             for (int k = 0; k < TOK / 16; ++k)  // a side's weights lie over the first half of its scores
               mma_ts(issue, tmem + O_COL + x * TILE,
                      tmem + x * TILE + u % AHEAD * TOK + k * 16 / W * W + k * 16 % W / 2,
                      v_lo + u * (KV_TILE >> 4) + k * (2048u >> 4), HI, IDESC_O, (j | k) != 0);
-            if (x == NM - 1) mma_commit(issue, bd::smem_u32(&ctl->kv_empty[u]));
+            if (x == NM - 1) mma_commit(issue, bd::smem_u32(&ctl->v_empty[u]));
             if (j + AHEAD < n) {  // over the weights that the products above read: the tensor pipe takes them in order
-              if (x == 0 && !(ok = wait(ctl->kv_full[(u + AHEAD) % STAGES], (j + AHEAD) / STAGES))) break;
+              if (x == 0 && !(ok = wait(ctl->k_full[(u + AHEAD) % STAGES], (j + AHEAD) / STAGES))) break;
               bd::tc_fence_after();
               scores(x, (u + AHEAD) % STAGES);
             } else {
@@ -315,12 +317,12 @@ __global__ void __launch_bounds__(Shape<NM>::THREADS, 1) attn_tiles_kernel(AttnA
         find_page(0);
         find_scales(0);
       }
-      for (int j = 0; j < n && wait(ctl->kv_empty[j % STAGES], j / STAGES + 1); ++j) {
+      for (int j = 0; j < n && wait(ctl->k_empty[j % STAGES], j / STAGES + 1); ++j) {
         if (lane < TOK / 16) {
           ctl->ks[j & 7][lane] = pow2i(ks_byte - 127);
           ctl->ve[j & 7][lane] = static_cast<float>(vs_byte - 127);
         }
-        arrive(ctl->kv_full[j % STAGES]);
+        arrive(ctl->k_full[j % STAGES]);
         find_scales(j + 1);
       }
     }
@@ -334,12 +336,12 @@ __global__ void __launch_bounds__(Shape<NM>::THREADS, 1) attn_tiles_kernel(AttnA
     constexpr int DEPTH = NM == 2 ? 1 : 2;             // tiles on their way in registers
     // eight lanes take four chunks each of two rows, which the swizzle puts into different banks
     const int sub = (ct & 3) | (CH == 8 ? (ct >> 1) & 4 : 0), mine = ct / (2 * CH) * 2 + ((ct >> 2) & 1);
-    const int64_t row_k = a.k_tok, row_v = a.v_tok;
-    const uint8_t* kp = a.k + head * a.k_head + sub * 16;
-    const uint8_t* vp = a.v + head * a.v_head + sub * 16;
     const int32_t* table = a.table + seq * a.table_stride;
-    const int mask = (1 << a.page_shift) - 1;
-    uint4 kx[DEPTH][PER], vx[DEPTH][PER];
+    const int mask = (1 << a.page_shift) - 1, n_pages = static_cast<int>(a.n_pages);
+    const uint8_t* k0 = a.k + head * a.k_head + mine * a.k_tok + sub * 16;
+    const uint8_t* v0 = a.v + head * a.v_head + mine * a.v_tok + sub * 16;
+    const bool in_row = sub * 16 < a.dim;
+    uint4 kx[DEPTH][PER] = {}, vx[DEPTH][PER] = {};
     constexpr int PAGES = BIG ? TOK / 64 : PER;
     int pages[PAGES];  // of the tile to be loaded next (-1: nothing to read)
     const auto find = [&](int j) {
@@ -347,15 +349,31 @@ __global__ void __launch_bounds__(Shape<NM>::THREADS, 1) attn_tiles_kernel(AttnA
       for (int u = 0; u < PAGES; ++u) {
         const int t = begin + j * TOK + (BIG ? u * 64 : mine + u * STEP);
         pages[u] = ld_global_if(table + (t >> a.page_shift), t < end && (t >> a.page_shift) < a.max_blocks, -1);
+        if (pages[u] >= n_pages) pages[u] = -1;
       }
     };
-    const auto load = [&](int j, uint4 (&k)[PER], uint4 (&v)[PER]) {  // of tile j, whose pages were found
+    // One of keys and values of tile j, whose pages were found. Lanes past a row's end keep the zeros they began with; what
+    // is not there in a tile (past the last token, on no page of the cache) becomes zeros.
+    const auto load = [&](const uint8_t* p, int64_t page_stride, int64_t tok_stride, int j, uint4 (&x)[PER]) {
+      const int t0 = begin + j * TOK;
+      bool whole = t0 + TOK <= end;
 #pragma unroll
-      for (int u = 0; u < PER; ++u) {
-        const int t = begin + j * TOK + mine + u * STEP, page = pages[BIG ? u * STEP / 64 : u];
-        const bool live = page >= 0 && page < a.n_pages && t < end && sub * 16 < a.dim;
-        k[u] = ld_global_if(kp + page * a.k_page + (t & mask) * row_k, live);
-        v[u] = ld_global_if(vp + page * a.v_page + (t & mask) * row_v, live);
+      for (int u = 0; u < PAGES; ++u) whole = whole && pages[u] >= 0;
+      if (BIG && whole) {
+#pragma unroll
+        for (int g = 0; g < PAGES; ++g) {
+          const uint8_t* at = p + pages[g] * page_stride + ((t0 + g * 64) & mask) * tok_stride;
+#pragma unroll
+          for (int u = 0; u < PER / PAGES; ++u) ld_global_over(x[g * (PER / PAGES) + u], at + u * STEP * tok_stride, in_row);
+        }
+      } else {
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+          const int page = pages[BIG ? u * STEP / 64 : u], t = t0 + u * STEP;
+          const int in = ((t + mine) & mask) - mine;  // tokens from this thread's first to its chunk's in the page
+          x[u] = make_uint4(0, 0, 0, 0);
+          ld_global_over(x[u], p + page * page_stride + in * tok_stride, in_row && page >= 0 && t + mine < end);
+        }
       }
     };
     const auto store = [&](uint32_t at, const uint4 (&x)[PER]) {
@@ -373,7 +391,8 @@ __global__ void __launch_bounds__(Shape<NM>::THREADS, 1) attn_tiles_kernel(AttnA
 #pragma unroll
       for (int b = 0; b < DEPTH; ++b) {
         find(b);
-        load(b, kx[b], vx[b]);
+        load(k0, a.k_page, a.k_tok, b, kx[b]);
+        load(v0, a.v_page, a.v_tok, b, vx[b]);
       }
       find(DEPTH);
     }
@@ -382,12 +401,16 @@ __global__ void __launch_bounds__(Shape<NM>::THREADS, 1) attn_tiles_kernel(AttnA
 #pragma unroll
       for (int b = 0; b < DEPTH; ++b) {
         const int j = j0 + b;
-        if (j >= n || !(ok = wait(ctl->kv_empty[j % STAGES], j / STAGES + 1))) break;
+        if (j >= n || !(ok = wait(ctl->k_empty[j % STAGES], j / STAGES + 1))) break;
         store(k_at + (j % STAGES) * KV_TILE, kx[b]);
+        fence_proxy_async();
+        arrive(ctl->k_full[j % STAGES]);
+        load(k0, a.k_page, a.k_tok, j + DEPTH, kx[b]);
+        if (!(ok = wait(ctl->v_empty[j % STAGES], j / STAGES + 1))) break;
         store(v_at + (j % STAGES) * KV_TILE, vx[b]);
         fence_proxy_async();
-        arrive(ctl->kv_full[j % STAGES]);
-        load(j + DEPTH, kx[b], vx[b]);
+        arrive(ctl->v_full[j % STAGES]);
+        load(v0, a.v_page, a.v_tok, j + DEPTH, vx[b]);
         find(j + DEPTH + 1);
       }
     }
@@ -408,12 +431,12 @@ __global__ void __launch_bounds__(Shape<NM>::THREADS, 1) attn_tiles_kernel(AttnA
       constexpr int LANES = D / 8, ROWS = 32 / LANES;
       const int my_c = lane % LANES, my_r = lane / LANES;
       const uint16_t* q = static_cast<const uint16_t*>(a.q) + static_cast<int64_t>(sq.q0 + i) * a.q_tok + h * a.q_head;
-      uint4 w[16 / ROWS];
+      uint4 w[16 / ROWS] = {};
 #pragma unroll
       for (int u = 0; u < 16 / ROWS; ++u) {
         const int rr = side * 16 + u * ROWS + my_r;
         const uint64_t src = __shfl_sync(~0u, reinterpret_cast<uint64_t>(q), rr);
-        w[u] = ld_global_if(reinterpret_cast<const uint8_t*>(src) + my_c * 16, row - lane + rr < rows && my_c * 8 < a.dim);
+        ld_global_over(w[u], reinterpret_cast<const uint8_t*>(src) + my_c * 16, row - lane + rr < rows && my_c * 8 < a.dim);
       }
       int shift = 0;
       if (!a.f16) {
