@@ -80,6 +80,14 @@ __device__ __forceinline__ int scale_byte(float amax) {
   return min(max(e, E_MIN), E_MAX);
 }
 
+// Four E4M3 codes of a word to f16, two words.
+__device__ __forceinline__ void decode4(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\t"
+      "cvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+      : "=r"(lo), "=r"(hi)
+      : "r"(w));
+}
+
 // The 16-bit element types of rows.
 struct Bf16 {
   static __device__ __forceinline__ float2 to_float2(uint32_t x) {

@@ -175,15 +175,15 @@ struct Plan {
 };
 
 // The kernel: up to 16 rows per key/value head (queries times the group) fit the one tile of the row kernel.
-// The split: parts of the cache so that the CTAs fill the SMs (four times over for the row kernel, whose CTAs are
-// short; once for the other one).
+// The split: parts of the cache so that the CTAs fill the SMs (eight to an SM for the row kernel, of which two run at
+// once; one to an SM for the other one).
 Plan make_plan(const bdkv_cache& c, const bdkv_attention_args& a, int sms) {
   Plan p = {};
   const int64_t rows = int64_t(a.max_q_len) * (a.n_q_heads / c.n_heads);
   p.tiles = rows > bdkv::ROWS_TILE;
   const int64_t tile = !p.tiles ? bdkv::ROWS_TILE : rows <= bdkv::TILES_TILE ? bdkv::TILES_TILE : 2 * bdkv::TILES_TILE;
   const int64_t ctas = (rows + tile - 1) / tile * c.n_heads * a.n_seq;
-  const int64_t parts = p.tiles ? sms / ctas : (4 * int64_t(sms) + ctas - 1) / ctas;
+  const int64_t parts = p.tiles ? sms / ctas : (8 * int64_t(sms) + ctas - 1) / ctas;
   const int64_t least = p.tiles ? 256 : 128;  // tokens
   int64_t chunk = parts > 1 ? ((a.max_kv_len + parts - 1) / parts + 127) / 128 * 128 : a.max_kv_len;
   if (chunk < least) chunk = least;

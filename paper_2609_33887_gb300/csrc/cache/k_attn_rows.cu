@@ -15,9 +15,9 @@
 namespace bdkv {
 namespace {
 
-constexpr int WARPS = 8;
-constexpr int STAGES = 4;
-constexpr int STEP = 16;       // tokens a warp takes at once
+constexpr int WARPS = 4;       // two CTAs to an SM: one's start and merge run beside the other's products
+constexpr int STAGES = 3;
+constexpr int STEP = 32;       // tokens a warp takes at once
 constexpr float P_SHIFT = 12;  // weights are held as f16 times 2^12: 11 bits down to 2^-26 of the largest
 constexpr float P_SLACK = 3;   // ... and may exceed it by 2^3 before O is rescaled (2^15 < 65504)
 
@@ -59,11 +59,14 @@ constexpr size_t smem_bytes() {
   return ring > merge ? ring : merge;
 }
 
-// One CTA: 16 rows of a request's key/value head, one part of its cache.
-template <class T, int D>
-__global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(AttnArgs a) {
+// One CTA: 16 rows of a request's key/value head (R = 1: at most 8 of them exist), one part of its cache. BIG: a step's
+// tokens share a page (pages of 32 and more).
+template <class T, int D, int R, bool BIG>
+__global__ void __launch_bounds__(WARPS * 32, 2) attn_rows_kernel(AttnArgs a) {
   constexpr int CH = D / 16;  // 16-byte chunks of a token's row; also k-steps
   constexpr int VB = D / 8;   // bytes of a value row a lane reads; also n-tiles of O
+  constexpr int STAGE = STEP * D * 2;
+  constexpr int GROUPS = BIG ? 1 : 2;  // pages of a step
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ float sm_m[WARPS][16], sm_M[WARPS][16], sm_L[WARPS][16];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = lane >> 2, c = lane & 3;
@@ -77,28 +80,82 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(AttnArgs a) {
   const int end = min(visible(a, sq, (min(rows, row0 + ROWS_TILE) - 1) / a.group), begin + a.chunk);
   if (part > 0 && end <= begin) return;
   bd::griddep_launch_dependents();
+  const int n_steps = end > begin ? (end - begin + STEP - 1) / STEP : 0;
+
+  // Copies: a lane has a 16-byte chunk of every (32 / CH)-th token of a step. What is not there (past the last token, past
+  // the row's end, on no page of the cache) is filled with zeros.
+  const int my_t = lane / CH, my_ch = lane % CH;
+  const bool in_row = my_ch * 16 < a.dim;
+  const uint32_t ring = bd::smem_u32(smem) + warp * (STAGES * STAGE);
+  const int32_t* table = a.table + seq * a.table_stride;
+  const uint8_t* k0 = a.k + head * a.k_head + my_t * a.k_tok + my_ch * 16;
+  const uint8_t* v0 = a.v + head * a.v_head + my_t * a.v_tok + my_ch * 16;
+  const int mask = (1 << a.page_shift) - 1, n_pages = static_cast<int>(a.n_pages);
+  int pages[GROUPS];  // of the step to be fetched next (-1: nothing to read)
+  const auto find = [&](int step) {
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+      const int t = begin + step * STEP + g * 16, col = t >> a.page_shift;
+      pages[g] = t < end && col < a.max_blocks ? table[col] : -1;
+    }
+  };
+  const auto fetch = [&](int step, int stage, int (&ks)[GROUPS], int (&vs)[GROUPS]) {
+    const int t0 = begin + step * STEP;
+    const uint32_t dst = ring + stage * STAGE;
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+      const bool ok = pages[g] >= 0 && pages[g] < n_pages;
+      const int64_t page = ok ? pages[g] : 0;
+      ks[g] = vs[g] = 127;
+      if (ok) {
+        ks[g] = a.ks[page * a.ks_page + head];
+        vs[g] = a.vs[page * a.vs_page + head];
+      }
+      const int in = (t0 + g * 16) & mask;
+      const uint8_t* k = k0 + page * a.k_page + in * a.k_tok;
+      const uint8_t* v = v0 + page * a.v_page + in * a.v_tok;
+      if (step < n_steps) {
+#pragma unroll
+        for (int u = 0; u < STEP * CH / 32 / GROUPS; ++u) {
+          const int t = u * (32 / CH) + my_t;  // of the group's tokens
+          const bool live = ok && in_row && t0 + g * 16 + t < end;
+          cp_async16(dst + ((g * 16 + t) * CH + k_chunk<D>(t, my_ch)) * 16, live ? k + u * (32 / CH) * a.k_tok : a.k, live);
+          cp_async16(dst + STEP * D + ((g * 16 + t) * CH + v_chunk<D>(t, my_ch)) * 16,
+                     live ? v + u * (32 / CH) * a.v_tok : a.v, live);
+        }
+      }
+    }
+    cp_async_commit();
+    find(step + WARPS);
+  };
+  int ks[STAGES][GROUPS], vs[STAGES][GROUPS];
+  find(warp);
+#pragma unroll
+  for (int s = 0; s < STAGES - 1; ++s) fetch(warp + s * WARPS, s, ks[s], vs[s]);
 
   // queries as A fragments, in f16 times a power of two per row
-  uint32_t qf[CH][4];
-  float coef[2];
-  int vis[2];
+  uint32_t qf[CH][4] = {};
+  float coef[R];
+  int vis[R];
 #pragma unroll
-  for (int r = 0; r < 2; ++r) {
+  for (int r = 0; r < R; ++r) {
     const int row = row0 + n + 8 * r, i = row / a.group;
     const bool live = row < rows;
     const uint16_t* q = static_cast<const uint16_t*>(a.q) + static_cast<int64_t>(sq.q0 + i) * a.q_tok +
                         (static_cast<int64_t>(head) * a.group + row - i * a.group) * a.q_head;
-    vis[r] = live ? visible(a, sq, i) : 0;
-    float2 x[CH][2];
+    vis[r] = live ? min(visible(a, sq, i), end) : 0;
+    uint2 w[CH];
     float amax = 0.f;
 #pragma unroll
     for (int j = 0; j < CH; ++j) {
       const int d = (j / 4) * 64 + c * 16 + (j % 4) * 4;
-      uint2 w = {0, 0};
-      if (live && d < a.dim) w = *reinterpret_cast<const uint2*>(q + d);
-      x[j][0] = T::to_float2(w.x);
-      x[j][1] = T::to_float2(w.y);
-      amax = fmaxf(amax, fmaxf(fmaxf(fabsf(x[j][0].x), fabsf(x[j][0].y)), fmaxf(fabsf(x[j][1].x), fabsf(x[j][1].y))));
+      w[j] = make_uint2(0, 0);
+      if (live && d < a.dim) w[j] = *reinterpret_cast<const uint2*>(q + d);
+    }
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+      const float2 x = T::to_float2(w[j].x), y = T::to_float2(w[j].y);
+      amax = bd::max3(bd::max3(amax, fabsf(x.x), fabsf(x.y)), fabsf(y.x), fabsf(y.y));
     }
     amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 1));
     amax = fmaxf(amax, __shfl_xor_sync(~0u, amax, 2));
@@ -106,137 +163,138 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(AttnArgs a) {
     const float f = pow2i(s);
     coef[r] = a.coef * pow2i(-s);
 #pragma unroll
-    for (int j = 0; j < CH; ++j)
-#pragma unroll
-      for (int p = 0; p < 2; ++p) qf[j][r + 2 * p] = f16x2(make_float2(x[j][p].x * f, x[j][p].y * f));
+    for (int j = 0; j < CH; ++j) {
+      const float2 x = T::to_float2(w[j].x), y = T::to_float2(w[j].y);
+      qf[j][r] = f16x2(make_float2(x.x * f, x.y * f));
+      qf[j][r + 2] = f16x2(make_float2(y.x * f, y.y * f));
+    }
   }
 
   float O[VB][4] = {};
-  float m[2] = {-INFINITY, -INFINITY}, M[2] = {-INFINITY, -INFINITY}, L[2] = {0.f, 0.f};
-  const int n_steps = end > begin ? (end - begin + STEP - 1) / STEP : 0;
-  const uint32_t ring = bd::smem_u32(smem) + warp * (STAGES * STEP * D * 2);
-  int scales[STAGES];  // of the steps in flight: key byte, value byte << 8
+  float m[R], M[R], L[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) m[r] = M[r] = -INFINITY, L[r] = 0.f;
 
-  auto fetch = [&](int step, int stage) -> int {
-    int got = 0;
-    if (step < n_steps) {
-      const int t0 = begin + step * STEP, col = t0 >> a.page_shift;
-      const int64_t page = col < a.max_blocks ? a.table[seq * a.table_stride + col] : -1;
-      const bool ok = page >= 0 && page < a.n_pages;
-      const int64_t p = ok ? page : 0;
-      got = ok ? a.ks[p * a.ks_page + head] | (a.vs[p * a.vs_page + head] << 8) : 127 | (127 << 8);
-      const uint8_t* k = a.k + p * a.k_page + head * a.k_head;
-      const uint8_t* v = a.v + p * a.v_page + head * a.v_head;
-      const int in = t0 & ((1 << a.page_shift) - 1);
-      const uint32_t dst = ring + stage * (STEP * D * 2);
+  for (int step0 = warp; step0 < n_steps; step0 += STAGES * WARPS) {
 #pragma unroll
-      for (int u = 0; u < STEP * CH / 32; ++u) {
-        const int t = (u * 32 + lane) / CH, ch = (u * 32 + lane) % CH;
-        const bool live = ok && t0 + t < end && ch * 16 < a.dim;
-        const int64_t ko = live ? (in + t) * a.k_tok + ch * 16 : 0, vo = live ? (in + t) * a.v_tok + ch * 16 : 0;
-        cp_async16(dst + (t * CH + k_chunk<D>(t, ch)) * 16, k + ko, live);
-        cp_async16(dst + STEP * D + (t * CH + v_chunk<D>(t, ch)) * 16, v + vo, live);
-      }
-    }
-    cp_async_commit();
-    return got;
-  };
-#pragma unroll
-  for (int s = 0; s < STAGES - 1; ++s) scales[s] = fetch(warp + s * WARPS, s);
+    for (int stage = 0; stage < STAGES; ++stage) {
+      const int step = step0 + stage * WARPS;
+      if (step >= n_steps) break;
+      cp_async_wait<STAGES - 2>();
+      __syncwarp();
+      constexpr int AHEAD = STAGES - 1;
+      fetch(step + AHEAD * WARPS, (stage + AHEAD) % STAGES, ks[(stage + AHEAD) % STAGES], vs[(stage + AHEAD) % STAGES]);
+      const uint32_t kb = ring + stage * STAGE, vb = kb + STEP * D;
+      const int t0 = begin + step * STEP;
 
-  int stage = 0;
-  for (int step = warp; step < n_steps; step += WARPS) {
-    cp_async_wait<STAGES - 2>();
-    __syncwarp();
-    const int sc = scales[0];
+      float S[4][4] = {};
 #pragma unroll
-    for (int s = 0; s < STAGES - 2; ++s) scales[s] = scales[s + 1];
-    scales[STAGES - 2] = fetch(step + (STAGES - 1) * WARPS, (stage + STAGES - 1) % STAGES);
-    const uint32_t kb = ring + stage * (STEP * D * 2), vb = kb + STEP * D;
-    stage = (stage + 1) % STAGES;
-
-    float S[2][4] = {};
+      for (int nt = 0; nt < 4; ++nt) {
+        const int t = nt * 8 + n;
 #pragma unroll
-    for (int nt = 0; nt < 2; ++nt) {
-      const int t = nt * 8 + n;
+        for (int q4 = 0; q4 < CH / 4; ++q4) {
+          const uint4 w = bd::ld_shared_v4(kb + (t * CH + k_chunk<D>(t, q4 * 4 + c)) * 16);
+          const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-      for (int q4 = 0; q4 < CH / 4; ++q4) {
-        const uint4 w = bd::ld_shared_v4(kb + (t * CH + k_chunk<D>(t, q4 * 4 + c)) * 16);
-        const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          mma_f16(S[nt], qf[q4 * 4 + j], bd::e4m3x2_to_f16x2(ww[j] & 0xffffu), bd::e4m3x2_to_f16x2(ww[j] >> 16));
-      }
-    }
-
-    const float ks = pow2i((sc & 255) - 127);
-    const float ve = static_cast<float>((sc >> 8) - 127);
-    uint32_t pf[4];
-    bool grown = false;
-    float newM[2];
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      const float f = coef[r] * ks;
-      float x[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int t = begin + step * STEP + (e >> 1) * 8 + 2 * c + (e & 1);
-        x[e] = t < min(vis[r], end) ? S[e >> 1][2 * r + (e & 1)] * f : -INFINITY;
-      }
-      float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3]));
-      top = fmaxf(top, __shfl_xor_sync(~0u, top, 1));
-      top = fmaxf(top, __shfl_xor_sync(~0u, top, 2));
-      if (top > m[r]) {
-        L[r] *= bd::ex2_approx(m[r] - top);  // m = -inf: L is 0
-        m[r] = top;
-      }
-      newM[r] = top + ve > M[r] + P_SLACK || M[r] == -INFINITY ? top + ve : M[r];
-      grown |= newM[r] != M[r];
-      const float mr = m[r] == -INFINITY ? 0.f : m[r];
-      const float Mr = (newM[r] == -INFINITY ? 0.f : newM[r]) - ve - P_SHIFT;
-      float w[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        L[r] += bd::ex2_approx(x[e] - mr);
-        w[e] = bd::ex2_approx(x[e] - Mr);
-      }
-      pf[r] = f16x2(make_float2(w[0], w[1]));
-      pf[r + 2] = f16x2(make_float2(w[2], w[3]));
-    }
-    if (__any_sync(~0u, grown)) {
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        const float f = newM[r] == M[r] ? 1.f : bd::ex2_approx(M[r] - newM[r]);
-        M[r] = newM[r];
-#pragma unroll
-        for (int j = 0; j < VB; ++j) {
-          O[j][2 * r] *= f;
-          O[j][2 * r + 1] *= f;
+          for (int j = 0; j < 4; ++j) {
+            uint32_t b0, b1;
+            decode4(ww[j], b0, b1);
+            mma_f16(S[nt], qf[q4 * 4 + j], b0, b1);
+          }
         }
       }
-    }
 
-    // values: this lane's bytes n * VB .. of tokens 2c, 2c + 1, 8 + 2c, 9 + 2c
-    uint32_t w[4][VB / 4];
+      uint32_t pf[2][4] = {};  // weights as A fragments of two products
+      float newM[R];
+      bool grown = false;
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int t = (u >> 1) * 8 + 2 * c + (u & 1);
-      if constexpr (D == 128) {
-        const uint4 x = bd::ld_shared_v4(vb + (t * CH + v_chunk<D>(t, n)) * 16);
-        w[u][0] = x.x, w[u][1] = x.y, w[u][2] = x.z, w[u][3] = x.w;
-      } else {
-        const uint2 x = ld_shared_v2(vb + (t * CH + v_chunk<D>(t, n >> 1)) * 16 + (n & 1) * 8);
-        w[u][0] = x.x, w[u][1] = x.y;
+      for (int r = 0; r < R; ++r) {
+        float x[8];
+        float s_top = -INFINITY, u_top = -INFINITY;
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+          const float f = coef[r] * pow2i(ks[stage][g] - 127);
+          constexpr int E = 8 / GROUPS;
+          float top = -INFINITY;
+#pragma unroll
+          for (int e = g * E; e < g * E + E; ++e) x[e] = S[e >> 1][2 * r + (e & 1)] * f;
+          if (t0 + STEP > vis[r])
+#pragma unroll
+            for (int e = g * E; e < g * E + E; ++e)
+              if (t0 + (e >> 1) * 8 + 2 * c + (e & 1) >= vis[r]) x[e] = -INFINITY;
+#pragma unroll
+          for (int e = g * E; e < g * E + E; e += 2) top = bd::max3(top, x[e], x[e + 1]);
+          s_top = fmaxf(s_top, top);
+          u_top = fmaxf(u_top, top + static_cast<float>(vs[stage][g] - 127));
+        }
+        if (GROUPS > 1) {
+          s_top = fmaxf(s_top, __shfl_xor_sync(~0u, s_top, 1));
+          s_top = fmaxf(s_top, __shfl_xor_sync(~0u, s_top, 2));
+        }
+        u_top = fmaxf(u_top, __shfl_xor_sync(~0u, u_top, 1));
+        u_top = fmaxf(u_top, __shfl_xor_sync(~0u, u_top, 2));
+        if (GROUPS == 1) s_top = u_top - static_cast<float>(vs[stage][0] - 127);
+        const float m_new = fmaxf(m[r], s_top);
+        L[r] *= m_new == m[r] ? 1.f : bd::ex2_approx(m[r] - m_new);
+        m[r] = m_new;
+        newM[r] = u_top > M[r] + P_SLACK || (M[r] == -INFINITY && u_top > M[r]) ? u_top : M[r];
+        grown |= newM[r] != M[r];
+        const float mr = m_new == -INFINITY ? 0.f : m_new;
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float ve = static_cast<float>(vs[stage][e / (8 / GROUPS)] - 127);
+          const float Mr = (newM[r] == -INFINITY ? 0.f : newM[r]) - ve - P_SHIFT;
+          L[r] += bd::ex2_approx(x[e] - mr);
+          w[e] = bd::ex2_approx(x[e] - Mr);
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          pf[k][r] = f16x2(make_float2(w[4 * k], w[4 * k + 1]));
+          pf[k][r + 2] = f16x2(make_float2(w[4 * k + 2], w[4 * k + 3]));
+        }
       }
-    }
+      if (__any_sync(~0u, grown)) {
 #pragma unroll
-    for (int j = 0; j < VB / 4; ++j) {
-      const uint32_t a0 = __byte_perm(w[0][j], w[1][j], 0x5140), a1 = __byte_perm(w[0][j], w[1][j], 0x7362);
-      const uint32_t b0 = __byte_perm(w[2][j], w[3][j], 0x5140), b1 = __byte_perm(w[2][j], w[3][j], 0x7362);
-      mma_f16(O[4 * j], pf, bd::e4m3x2_to_f16x2(a0 & 0xffffu), bd::e4m3x2_to_f16x2(b0 & 0xffffu));
-      mma_f16(O[4 * j + 1], pf, bd::e4m3x2_to_f16x2(a0 >> 16), bd::e4m3x2_to_f16x2(b0 >> 16));
-      mma_f16(O[4 * j + 2], pf, bd::e4m3x2_to_f16x2(a1 & 0xffffu), bd::e4m3x2_to_f16x2(b1 & 0xffffu));
-      mma_f16(O[4 * j + 3], pf, bd::e4m3x2_to_f16x2(a1 >> 16), bd::e4m3x2_to_f16x2(b1 >> 16));
+        for (int r = 0; r < R; ++r) {
+          const float f = newM[r] == M[r] ? 1.f : bd::ex2_approx(M[r] - newM[r]);
+          M[r] = newM[r];
+#pragma unroll
+          for (int j = 0; j < VB; ++j) {
+            O[j][2 * r] *= f;
+            O[j][2 * r + 1] *= f;
+          }
+        }
+      }
+
+      // values: this lane's bytes n * VB .. of tokens 2c, 2c + 1, 8 + 2c, 9 + 2c of each half of the step
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        uint32_t w[4][VB / 4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int t = k * 16 + (u >> 1) * 8 + 2 * c + (u & 1);
+          if constexpr (D == 128) {
+            const uint4 x = bd::ld_shared_v4(vb + (t * CH + v_chunk<D>(t, n)) * 16);
+            w[u][0] = x.x, w[u][1] = x.y, w[u][2] = x.z, w[u][3] = x.w;
+          } else {
+            const uint2 x = ld_shared_v2(vb + (t * CH + v_chunk<D>(t, n >> 1)) * 16 + (n & 1) * 8);
+            w[u][0] = x.x, w[u][1] = x.y;
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < VB / 4; ++j) {
+          uint32_t a0, a1, a2, a3, b0, b1, b2, b3;
+          decode4(__byte_perm(w[0][j], w[1][j], 0x5140), a0, a1);
+          decode4(__byte_perm(w[0][j], w[1][j], 0x7362), a2, a3);
+          decode4(__byte_perm(w[2][j], w[3][j], 0x5140), b0, b1);
+          decode4(__byte_perm(w[2][j], w[3][j], 0x7362), b2, b3);
+          mma_f16(O[4 * j], pf[k], a0, b0);
+          mma_f16(O[4 * j + 1], pf[k], a1, b1);
+          mma_f16(O[4 * j + 2], pf[k], a2, b2);
+          mma_f16(O[4 * j + 3], pf[k], a3, b3);
+        }
+      }
     }
   }
   cp_async_wait<0>();
@@ -245,7 +303,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(AttnArgs a) {
   constexpr int LD = D + 4;
   float* acc = reinterpret_cast<float*>(smem);
 #pragma unroll
-  for (int r = 0; r < 2; ++r) {
+  for (int r = 0; r < R; ++r) {
     L[r] += __shfl_xor_sync(~0u, L[r], 1);
     L[r] += __shfl_xor_sync(~0u, L[r], 2);
     if (c == 0) {
@@ -260,7 +318,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(AttnArgs a) {
         acc[(warp * 16 + n + 8 * r) * LD + (2 * c + e) * VB + j] = O[j][2 * r + e];
   }
   __syncthreads();
-  for (int u = tid; u < 16 * D / 4; u += WARPS * 32) {
+  for (int u = tid; u < 8 * R * D / 4; u += WARPS * 32) {
     const int r = u / (D / 4), d = u % (D / 4) * 4, row = row0 + r;
     if (row >= rows) continue;
     float mt = -INFINITY, Mt = -INFINITY, Lt = 0.f;
@@ -284,20 +342,28 @@ __global__ void __launch_bounds__(WARPS * 32, 1) attn_rows_kernel(AttnArgs a) {
   }
 }
 
-template <class T, int D>
+template <class T, int D, int R, bool BIG>
 cudaError_t launch(const AttnArgs& a, cudaStream_t st) {
   static std::atomic<bool> ready[64];  // by device
-  if (cudaError_t e = allow_smem(attn_rows_kernel<T, D>, smem_bytes<D>(), ready); e != cudaSuccess) return e;
+  const auto kernel = attn_rows_kernel<T, D, R, BIG>;
+  if (cudaError_t e = allow_smem(kernel, smem_bytes<D>(), ready); e != cudaSuccess) return e;
   const dim3 grid((a.max_q * a.group + ROWS_TILE - 1) / ROWS_TILE * a.n_kv, a.n_split, a.n_seq);
-  attn_rows_kernel<T, D><<<grid, WARPS * 32, smem_bytes<D>(), st>>>(a);
+  kernel<<<grid, WARPS * 32, smem_bytes<D>(), st>>>(a);
   return cudaGetLastError();
+}
+
+template <class T, int D>
+cudaError_t launch_rows(const AttnArgs& a, cudaStream_t st) {
+  const bool big = (1 << a.page_shift) >= STEP;
+  if (a.max_q * a.group <= 8) return big ? launch<T, D, 1, true>(a, st) : launch<T, D, 1, false>(a, st);
+  return big ? launch<T, D, 2, true>(a, st) : launch<T, D, 2, false>(a, st);
 }
 
 }  // namespace
 
 cudaError_t launch_attn_rows(const AttnArgs& a, cudaStream_t st) {
-  if (a.dim <= 64) return a.f16 ? launch<F16, 64>(a, st) : launch<Bf16, 64>(a, st);
-  return a.f16 ? launch<F16, 128>(a, st) : launch<Bf16, 128>(a, st);
+  if (a.dim <= 64) return a.f16 ? launch_rows<F16, 64>(a, st) : launch_rows<Bf16, 64>(a, st);
+  return a.f16 ? launch_rows<F16, 128>(a, st) : launch_rows<Bf16, 128>(a, st);
 }
 
 }  // namespace bdkv

@@ -147,16 +147,6 @@ __device__ __forceinline__ void ld_global_over(uint4& x, const uint8_t* p, bool 
                : "l"(p), "r"(static_cast<int>(live)));
 }
 
-// Sixteen codes to f16, two 16-byte chunks.
-__device__ __forceinline__ void decode16(uint4 x, uint32_t (&y)[8]) {
-  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    y[2 * i] = bd::e4m3x2_to_f16x2(w[i] & 0xffffu);
-    y[2 * i + 1] = bd::e4m3x2_to_f16x2(w[i] >> 16);
-  }
-}
-
 // A barrier of the two warps that share 32 rows, which tells both whether some thread of either says so.
 __device__ __forceinline__ bool pair_any(int id, bool says) {
   uint32_t any;
@@ -381,7 +371,10 @@ __global__ void __launch_bounds__(Shape<NM>::THREADS, 1) attn_tiles_kernel(AttnA
       for (int u = 0; u < PER; ++u) {
         const int r = mine + u * STEP;
         uint32_t y[8];
-        decode16(x[u], y);
+        decode4(x[u].x, y[0], y[1]);
+        decode4(x[u].y, y[2], y[3]);
+        decode4(x[u].z, y[4], y[5]);
+        decode4(x[u].w, y[6], y[7]);
         const uint32_t rowp = at + (sub / 4) * KV_ATOM + r * 128, c0 = (sub % 4) * 2;
         st_shared_v4(rowp + ((c0 ^ (r & 7)) << 4), y[0], y[1], y[2], y[3]);
         st_shared_v4(rowp + (((c0 + 1) ^ (r & 7)) << 4), y[4], y[5], y[6], y[7]);
