@@ -175,15 +175,18 @@ struct Plan {
 };
 
 // The kernel: up to 16 rows per key/value head (queries times the group) fit the one tile of the row kernel.
-// The split: parts of the cache so that the CTAs fill the SMs (eight to an SM for the row kernel, of which two run at
-// once; one to an SM for the other one).
+// The split along the cache. Row kernel, two CTAs to an SM: one wave for very few rows' work (one or two requests: two
+// caches of 131071 tokens 49 us, 68 in four waves), else four waves, since the host does not know how the lengths
+// differ (64 requests of 57 to 8189 tokens 103 us, 120 in one wave). Tile kernel: one CTA to an SM.
 Plan make_plan(const bdkv_cache& c, const bdkv_attention_args& a, int sms) {
   Plan p = {};
   const int64_t rows = int64_t(a.max_q_len) * (a.n_q_heads / c.n_heads);
   p.tiles = rows > bdkv::ROWS_TILE;
   const int64_t tile = !p.tiles ? bdkv::ROWS_TILE : rows <= bdkv::TILES_TILE ? bdkv::TILES_TILE : 2 * bdkv::TILES_TILE;
   const int64_t ctas = (rows + tile - 1) / tile * c.n_heads * a.n_seq;
-  const int64_t parts = p.tiles ? sms / ctas : (8 * int64_t(sms) + ctas - 1) / ctas;
+  const int64_t parts = p.tiles            ? sms / ctas
+                        : ctas <= sms / 8 ? 2 * int64_t(sms) / ctas
+                                          : (8 * int64_t(sms) + ctas - 1) / ctas;
   const int64_t least = p.tiles ? 256 : 128;  // tokens
   int64_t chunk = parts > 1 ? ((a.max_kv_len + parts - 1) / parts + 127) / 128 * 128 : a.max_kv_len;
   if (chunk < least) chunk = least;
