@@ -4,10 +4,11 @@
 // Every output follows from three prefix sums over the requests (tokens added,
 // pages needed, pages given back). They are a few thousand additions, so every
 // CTA computes all of them for itself in shared memory, which takes one launch
-// and no waiting between CTAs; the added tokens are then divided evenly among
-// the CTAs and the page lists among their warps. A page just taken is read
-// from the ring again where its token's slot is written, so no CTA depends on
-// another's block-table stores.
+// and no waiting between CTAs; added tokens and pages that change hands are
+// then divided evenly among all threads, which find their request by bisection.
+// A page just taken is read from the ring again where its token's slot is
+// written, so no thread depends on another's block-table stores. Bound by
+// latency: two trips to memory and two scans (8 requests 5 us).
 #include "cache.h"
 
 namespace bdkv {
@@ -50,18 +51,31 @@ __device__ __forceinline__ Sums warp_scan(Sums v, int lane) {
   return v;
 }
 
-// Shared memory: starts[n_seq + 1] (tokens before a request), first[n_seq]
-// (index of its first new page behind the ring's head, -1: not served).
+// The last of n entries of `before` (ascending) that is at most i.
+template <class F>
+__device__ __forceinline__ int last_at_most(F before, int n, int i) {
+  int lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (before(mid) <= i) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+
+// Shared memory: starts[n_seq + 1] (tokens added before a request), taken_at[n_seq] (pages needed before it; ~that where it
+// is not served), given_at[n_seq] (pages given back before it).
 __global__ void __launch_bounds__(THREADS) tables_kernel(bdkv_tables_args a, int shift) {
   extern __shared__ int sh[];
   int* starts = sh;
-  int* first = sh + a.n_seq + 1;
+  int* taken_at = sh + a.n_seq + 1;
+  int* given_at = taken_at + a.n_seq;
   __shared__ Sums warp_sum[THREADS / 32];
-  __shared__ int taken;
+  __shared__ int taken_sh;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int64_t head = a.pool_in[0], tail = a.pool_in[1];
-  const int64_t avail = tail - head;
-  if (tid == 0) taken = 0;
+  const int R = static_cast<int>(a.ring_size);
+  const int64_t avail = min(tail - head, a.ring_size);
+  if (tid == 0) taken_sh = 0;
 
   Sums base = {0, 0, 0};
   for (int s0 = 0; s0 < a.n_seq; s0 += THREADS) {
@@ -82,49 +96,55 @@ __global__ void __launch_bounds__(THREADS) tables_kernel(bdkv_tables_args a, int
     if (s < a.n_seq) {
       const bool ok = r.fits && (r.need == 0 || inc.need <= avail);
       starts[s] = inc.add - r.add;
-      first[s] = ok ? inc.need - r.need : -1;
-      if (ok && r.need > 0) atomicMax(&taken, inc.need);
+      taken_at[s] = ok ? inc.need - r.need : ~(inc.need - r.need);
+      given_at[s] = inc.give - r.give;
+      if (ok && r.need > 0) atomicMax(&taken_sh, inc.need);
       if (blockIdx.x == 0) {
         a.kv_lens[s] = ok ? r.want : r.old;
         a.query_start[s] = inc.add - r.add;
         a.status[s] = ok ? 0 : r.fits ? 1 : 2;
       }
-      // pages that change hands, a request per thread of one CTA in turn
-      if (s % gridDim.x == blockIdx.x) {
-        int32_t* row = a.block_table + s * a.table_stride;
-        if (ok)
-          for (int j = 0; j < r.need; ++j)
-            row[r.held + j] = a.free_pages[(head + inc.need - r.need + j) % a.ring_size];
-        for (int j = 0; j < r.give; ++j)
-          a.free_pages[(tail + inc.give - r.give + j) % a.ring_size] = row[r.want_pages + j];
-      }
     }
   }
-  const int total = base.add;
-  if (tid == 0) starts[a.n_seq] = total;
+  const int total = base.add, given = base.give;
   __syncthreads();
+  const int taken = taken_sh;
   if (blockIdx.x == 0 && tid == 0) {
     a.query_start[a.n_seq] = total;
     a.pool_out[0] = head + taken;
-    a.pool_out[1] = tail + base.give;
+    a.pool_out[1] = tail + given;
   }
+  // ring indices by one remainder each (heads of either sign)
+  const int head_at = static_cast<int>((head % R + R) % R), tail_at = static_cast<int>((tail % R + R) % R);
+  const auto ring = [&](int at, int i) {  // 0 <= i < R
+    const int64_t x = static_cast<int64_t>(at) + i;
+    return a.free_pages + (x >= R ? x - R : x);
+  };
+  const auto pages = [&](int n) { return static_cast<int>((static_cast<uint32_t>(n) + a.page_size - 1) >> shift); };
+  const auto taken_before = [&](int s) { return taken_at[s] < 0 ? ~taken_at[s] : taken_at[s]; };
+  const int64_t gtid = static_cast<int64_t>(blockIdx.x) * THREADS + tid, threads = static_cast<int64_t>(gridDim.x) * THREADS;
 
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * THREADS + tid; i < a.max_tokens;
-       i += static_cast<int64_t>(gridDim.x) * THREADS) {
+  for (int64_t i = gtid; i < static_cast<int64_t>(taken) + given; i += threads) {
+    if (i < taken) {
+      const int p = static_cast<int>(i), s = last_at_most(taken_before, a.n_seq, p);
+      a.block_table[s * a.table_stride + pages(max(a.lens[s], 0)) + p - taken_before(s)] = *ring(head_at, p);
+    } else {
+      const int p = static_cast<int>(i - taken), s = last_at_most([&](int k) { return given_at[k]; }, a.n_seq, p);
+      const int old = max(a.lens[s], 0), n = a.new_tokens[s];
+      const int left = n == INT32_MIN || -n >= old ? 0 : old + n;  // tokens it keeps
+      *ring(tail_at, p % R) = a.block_table[s * a.table_stride + pages(left) + p - given_at[s]];
+    }
+  }
+  for (int64_t i = gtid; i < a.max_tokens; i += threads) {
     int64_t slot = -1;
     int pos = -1;
     if (i < total) {
-      int lo = 0, hi = a.n_seq - 1;  // the last request whose tokens start at or before i
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (starts[mid] <= i) lo = mid; else hi = mid - 1;
-      }
-      const int old = max(a.lens[lo], 0);
-      pos = old + static_cast<int>(i) - starts[lo];
-      if (first[lo] >= 0) {
-        const int held = static_cast<int>((static_cast<uint32_t>(old) + a.page_size - 1) >> shift), j = pos >> shift;
-        const int page = j < held ? a.block_table[lo * a.table_stride + j]
-                                  : a.free_pages[(head + first[lo] + j - held) % a.ring_size];
+      const int s = last_at_most([&](int k) { return starts[k]; }, a.n_seq, static_cast<int>(i));
+      const int old = max(a.lens[s], 0);
+      pos = old + static_cast<int>(i) - starts[s];
+      if (taken_at[s] >= 0) {
+        const int held = pages(old), j = pos >> shift;
+        const int page = j < held ? a.block_table[s * a.table_stride + j] : *ring(head_at, taken_at[s] + j - held);
         slot = (static_cast<int64_t>(page) << shift) + (pos & (a.page_size - 1));
       }
     }
@@ -142,12 +162,11 @@ cudaError_t launch_tables(const bdkv_tables_args& a, int sm_count, cudaStream_t 
   int64_t grid = (work + THREADS - 1) / THREADS;
   if (grid < 1) grid = 1;
   if (grid > sm_count) grid = sm_count;
-  const size_t smem = (2 * static_cast<size_t>(a.n_seq) + 1) * sizeof(int);
-  if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(tables_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               (2 * MAX_SEQ_TABLES + 1) * sizeof(int));
-    if (e != cudaSuccess) return e;
-  }
+  const size_t smem = (3 * static_cast<size_t>(a.n_seq) + 1) * sizeof(int);
+  static std::atomic<bool> ready[64];  // by device
+  if (smem > 40 * 1024)
+    if (cudaError_t e = allow_smem(tables_kernel, (3 * MAX_SEQ_TABLES + 1) * sizeof(int), ready); e != cudaSuccess)
+      return e;
   tables_kernel<<<static_cast<unsigned>(grid), THREADS, smem, st>>>(a, shift);
   return cudaGetLastError();
 }
