@@ -198,7 +198,7 @@ def kv_attention(q: torch.Tensor, cache: KvCache, block_table: torch.Tensor, kv_
     mask_block: 0 = no mask, 1 = causal, B = causal by blocks of B queries (a window of block slots). scale defaults to
     head_dim^-0.5. Returns out (q's shape and type), or (out, lse float32 [tokens, n_q_heads])."""
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     elif out.shape != q.shape or out.dtype != q.dtype:
         raise ValueError("out must have q's shape and type")
     lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if return_lse else None

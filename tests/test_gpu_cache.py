@@ -249,9 +249,9 @@ def test_a_page_written_token_by_token_equals_its_scales_history():
 
 # --------------------------------------------------------------- attention --
 def attention_bounds(out, lse, spread, work, dtype, v_max):
-    """How far a result may be off. The output is rounded once: 2^-8 of it in bf16 (8 significant bits, half a unit in the
-    last), 2^-11 in f16. Weights are rounded to f16: 2^-11 of each, or 2^-37 of the largest one for weights that small
-    (and 2^15 such tokens at most). A score is a sum of up to 128 exact products kept in fp32 by a tree whose nodes may
+    """How far a result may be off. The output is rounded once: 2^-8 of it in bf16 (8 significant bits, half a unit in
+    the last), 2^-11 in f16. Weights are rounded to f16: 2^-11 of each, or 2^-37 of the largest one for weights that
+    small (and 2^15 such tokens at most). A score is a sum of up to 128 exact products kept in fp32 by a tree whose nodes may
     drop 2^-22 of the largest partial sum each: 2^-15 of the sum of their magnitudes, which moves a weight, and the
     log-sum-exp, by as much (twice, for numerator and normaliser); exp2 and the sums of weights add 2^-19."""
     u = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11}[dtype]
@@ -377,7 +377,7 @@ def test_bounds_above_the_lengths_change_nothing(q_len):
 
 @pytest.mark.parametrize("q_len,g,total", [(1, 4, 700), (20, 4, 300), (20, 4, 900), (31, 1, 513), (70, 4, 1300)])
 def test_repeated_calls_give_the_same_bits(q_len, g, total):
-    """Also the first one, whose warps run apart (their code and data come from memory), in cleared and in used scratch."""
+    """Also the first one, whose warps run apart (code and data come from memory), in filled and in used scratch."""
     n_seq, n_kv, dim = 30, 2, 128
     c = random_cache([total] * n_seq, 16, n_kv, dim, seed=3)
     gen = torch.Generator(device="cuda").manual_seed(q_len)
@@ -432,3 +432,91 @@ def test_long_caches_with_offsets_past_32_bits():
     bdc.kv_write(x, x, torch.arange((far + 7) * page, (far + 7) * page + 3, device="cuda"), cache)
     bdc.kv_write(x, x, torch.arange(7 * page, 7 * page + 3, device="cuda"), cache)
     assert torch.equal(k[far + 7, :3], k[7, :3]) and torch.equal(s[far + 7], s[7])
+
+
+# ------------------------------------------------- streams, graphs, workspaces --
+def attention_case(q_len, n_seq=6, total=900):
+    c = random_cache([total] * n_seq, 64, 2, 128, seed=11)
+    gen = torch.Generator(device="cuda").manual_seed(q_len)
+    q = torch.randn(n_seq * q_len, 8, 128, generator=gen, device="cuda").to(torch.bfloat16)
+    args = (q, gpu_cache(c), torch.from_numpy(c.table).cuda(), torch.from_numpy(c.kv_lens).cuda(),
+            torch.arange(0, (n_seq + 1) * q_len, q_len, dtype=torch.int32, device="cuda"))
+    return args, dict(max_q_len=q_len, max_kv_len=total)
+
+
+@pytest.mark.parametrize("q_len", [1, 20, 64])
+def test_streams_share_the_librarys_workspace(q_len):
+    args, bounds = attention_case(q_len)
+    assert bdc.kv_attention_workspace(*args, **bounds) > 0
+    ref = bdc.kv_attention(*args, **bounds)
+    outs = [torch.empty_like(ref) for _ in range(24)]
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    for i, out in enumerate(outs):  # calls in flight at once, each in the one workspace
+        bdc.kv_attention(*args, **bounds, out=out, stream=streams[i % 3])
+    torch.cuda.synchronize()
+    assert all(torch.equal(out, ref) for out in outs)
+
+
+@pytest.mark.parametrize("q_len", [1, 64])
+def test_a_forward_replays_from_a_graph(q_len):
+    args, bounds = attention_case(q_len)
+    q, cache, table, lens, starts = args
+    need = bdc.kv_attention_workspace(*args, **bounds)
+    raw = torch.empty(need + 256, dtype=torch.uint8, device="cuda")
+    ws = raw[-raw.data_ptr() % 256:][:need]
+    before = lens - q_len
+    new = torch.full_like(lens, q_len)
+    # free: the pages that the requests do not hold without the new tokens (their tables' last ones are taken again)
+    held = -(-(900 - q_len) // 64)
+    ring = torch.full((cache.k.shape[0],), -1, dtype=torch.int32, device="cuda")
+    spare = table[:, held:15].reshape(-1)
+    ring[:spare.numel()] = spare
+    pool = torch.tensor([0, spare.numel()], dtype=torch.int64, device="cuda")
+    k = torch.randn(6 * q_len, 2, 128, device="cuda").to(torch.bfloat16)
+
+    def forward():
+        t = bdc.kv_tables(before, new, table, ring, pool, page_size=64, max_tokens=6 * q_len)
+        bdc.kv_write(k, k, t.slot_map, cache)
+        return bdc.kv_attention(q, cache, table, t.kv_lens, t.query_start, workspace=ws, **bounds)
+
+    ref = forward()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = forward()
+    k.mul_(2)
+    out.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert not torch.equal(out, ref)  # the new keys and values
+    assert torch.equal(out, forward())
+
+
+def test_a_capture_without_a_workspace_is_refused():
+    args, bounds = attention_case(1)
+    graph = torch.cuda.CUDAGraph()
+    with pytest.raises(bdc.BdError) as e, torch.cuda.graph(graph):
+        bdc.kv_attention(*args, **bounds)
+    assert e.value.status == bdc.bdcommit.BD_ERR_WORKSPACE
+
+
+def test_a_small_workspace_is_refused_and_shutdown_frees():
+    args, bounds = attention_case(1)
+    need = bdc.kv_attention_workspace(*args, **bounds)
+    ws = torch.empty(need + 256, dtype=torch.uint8, device="cuda")
+    ws = ws[-ws.data_ptr() % 256:]
+    with pytest.raises(bdc.BdError) as e:
+        bdc.kv_attention(*args, **bounds, workspace=ws[:need - 1])
+    assert e.value.status == bdc.bdcommit.BD_ERR_WORKSPACE
+    ref = bdc.kv_attention(*args, **bounds, workspace=ws[:need])
+    torch.cuda.synchronize()
+    assert bdc.kvcache.kv_shutdown() == 0
+    assert torch.equal(bdc.kv_attention(*args, **bounds), ref)
+
+
+def test_negative_and_zero_scales():
+    c = random_cache([200, 77], 32, 2, 64, seed=12)
+    for q_len in (1, 60):
+        for scale in (-0.125, 0.0):
+            assert_attention(c, [q_len] * 2, 4, scale=scale)
