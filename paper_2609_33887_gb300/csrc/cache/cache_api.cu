@@ -1,5 +1,6 @@
 // The C entry points of libbdcache (bdcache.h): argument checks, workspaces,
 // kernel choice. Checks come before any CUDA call.
+#include <algorithm>
 #include <atomic>
 #include <climits>
 #include <cmath>
@@ -174,19 +175,27 @@ struct Plan {
   size_t bytes;       // of workspace
 };
 
-// The kernel: up to 16 rows per key/value head (queries times the group) fit the one tile of the row kernel.
-// The split along the cache. Row kernel, two CTAs to an SM: one wave for very few rows' work (one or two requests: two
-// caches of 131071 tokens 49 us, 68 in four waves), else four waves, since the host does not know how the lengths
-// differ (64 requests of 57 to 8189 tokens 103 us, 120 in one wave). Tile kernel: one CTA to an SM.
+// The kernel: up to 32 rows per key/value head (queries times the group) are one or two tiles of the row kernel (64
+// requests of 300 to 4001 tokens: 20 rows 75 us, 94 in the tile kernel; 32 rows 131 and 136; 48 rows 102 and 96).
+// The split along the cache. The host does not know how the lengths differ: one or two requests are split into one wave of
+// CTAs (two to an SM for the row kernel, one for the other), more requests into finer parts, which even out. Row kernel:
+// two caches of 131071 tokens 49 us in one wave, 68 in four; 64 requests of 57 to 8189 tokens 120 and 103. Tile kernel,
+// parts of 2048 tokens or more (a part costs its rows' fp32 results): 2 x 64 queries over 20000 to 30000 tokens 72 us in
+// one wave, 92 in three; 8 x 9 queries over 300 to 30001 tokens 231 and 132.
 Plan make_plan(const bdkv_cache& c, const bdkv_attention_args& a, int sms) {
   Plan p = {};
   const int64_t rows = int64_t(a.max_q_len) * (a.n_q_heads / c.n_heads);
-  p.tiles = rows > bdkv::ROWS_TILE;
+  p.tiles = rows > 2 * bdkv::ROWS_TILE;
   const int64_t tile = !p.tiles ? bdkv::ROWS_TILE : rows <= bdkv::TILES_TILE ? bdkv::TILES_TILE : 2 * bdkv::TILES_TILE;
   const int64_t ctas = (rows + tile - 1) / tile * c.n_heads * a.n_seq;
-  const int64_t parts = p.tiles            ? sms / ctas
-                        : ctas <= sms / 8 ? 2 * int64_t(sms) / ctas
-                                          : (8 * int64_t(sms) + ctas - 1) / ctas;
+  const bool few = a.n_seq <= 2;
+  int64_t parts;
+  if (p.tiles) {
+    const int64_t finer = std::min<int64_t>((3 * int64_t(sms) + ctas - 1) / ctas, a.max_kv_len / 2048);
+    parts = few || ctas >= sms ? sms / ctas : std::max<int64_t>(sms / ctas, finer);
+  } else {
+    parts = few ? 2 * int64_t(sms) / ctas : (8 * int64_t(sms) + ctas - 1) / ctas;
+  }
   const int64_t least = p.tiles ? 256 : 128;  // tokens
   int64_t chunk = parts > 1 ? ((a.max_kv_len + parts - 1) / parts + 127) / 128 * 128 : a.max_kv_len;
   if (chunk < least) chunk = least;

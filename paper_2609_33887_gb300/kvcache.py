@@ -112,23 +112,26 @@ def _cache_fields(c: KvCache) -> bytes:
 
 
 def _rows_fields(x: torch.Tensor, name: str) -> tuple:
-    if x.dim() != 3 or x.stride(2) != 1:
+    strides = x.stride()
+    if len(strides) != 3 or strides[2] != 1:
         raise ValueError(f"{name} must be [tokens, heads, head_dim] with head_dim contiguous")
-    if x.dtype not in _DT:
+    dtype = _DT.get(x.dtype)
+    if dtype is None:
         raise ValueError(f"{name} must be bfloat16 or float16")
-    return x.data_ptr(), _DT[x.dtype], x.stride(0), x.stride(1)
+    return x.data_ptr(), dtype, strides[0], strides[1]
 
 
 def _vector(t: torch.Tensor, dtype, n: Optional[int], name: str) -> int:
-    if t.dtype != dtype or not t.is_contiguous() or (n is not None and t.numel() != n):
+    if t.dtype is not dtype or not t.is_contiguous() or (n is not None and t.numel() != n):
         raise ValueError(f"{name} must be a contiguous {dtype} tensor" + ("" if n is None else f" of {n}"))
     return t.data_ptr()
 
 
 def _table(t: torch.Tensor, n_seq: int) -> tuple:
-    if t.dtype != torch.int32 or t.dim() != 2 or t.shape[0] != n_seq or (t.shape[1] > 1 and t.stride(1) != 1):
+    shape, strides = t.shape, t.stride()
+    if t.dtype is not torch.int32 or len(shape) != 2 or shape[0] != n_seq or (shape[1] > 1 and strides[1] != 1):
         raise ValueError(f"block_table must be int32 [{n_seq}, blocks] with contiguous rows")
-    return t.data_ptr(), max(t.stride(0), t.shape[1]), t.shape[1]
+    return t.data_ptr(), max(strides[0], shape[1]), shape[1]
 
 
 def kv_tables(lens: torch.Tensor, new_tokens: torch.Tensor, block_table: torch.Tensor, free_pages: torch.Tensor,
@@ -138,22 +141,23 @@ def kv_tables(lens: torch.Tensor, new_tokens: torch.Tensor, block_table: torch.T
     lens, new_tokens int32 [n_seq]; block_table int32 [n_seq, max_blocks] and free_pages int32 [ring] are updated in
     place; pool int64 [2] is the ring's (head, tail), not written. max_tokens: entries of slot_map and positions, at
     least the tokens added (entries behind them are -1)."""
-    n_seq, dev = lens.numel(), lens.device
-
-    def empty(n, dtype=torch.int32):
-        return torch.empty(n, dtype=dtype, device=dev)
-
-    out = KvTables(empty(n_seq), empty(n_seq + 1), empty(max_tokens, torch.int64), empty(max_tokens), empty(n_seq),
-                   empty(2, torch.int64))
+    n_seq, i32, i64 = lens.numel(), torch.int32, torch.int64
+    kv_lens = lens.new_empty(n_seq)
+    query_start = lens.new_empty(n_seq + 1)
+    slot_map = pool.new_empty(max_tokens)
+    positions = lens.new_empty(max_tokens)
+    status = lens.new_empty(n_seq)
+    pool_out = pool.new_empty(2)
     table, stride, cols = _table(block_table, n_seq)
     args = TABLES_FIELDS.pack(
-        n_seq, page_size, cols, max_tokens, stride, free_pages.numel(), _vector(lens, torch.int32, n_seq, "lens"),
-        _vector(new_tokens, torch.int32, n_seq, "new_tokens"), table,
-        _vector(free_pages, torch.int32, None, "free_pages"), _vector(pool, torch.int64, 2, "pool"),
-        out.pool.data_ptr(), out.kv_lens.data_ptr(), out.query_start.data_ptr(), out.slot_map.data_ptr(),
-        out.positions.data_ptr(), out.status.data_ptr())
-    _check(load_library().bdkv_tables(args, _stream_handle(stream)), "bdkv_tables")
-    return out
+        n_seq, page_size, cols, max_tokens, stride, free_pages.numel(), _vector(lens, i32, n_seq, "lens"),
+        _vector(new_tokens, i32, n_seq, "new_tokens"), table, _vector(free_pages, i32, None, "free_pages"),
+        _vector(pool, i64, 2, "pool"), pool_out.data_ptr(), kv_lens.data_ptr(), query_start.data_ptr(),
+        slot_map.data_ptr(), positions.data_ptr(), status.data_ptr())
+    rc = load_library().bdkv_tables(args, _stream_handle(stream))
+    if rc != BD_OK:
+        raise BdError(rc, "bdkv_tables")
+    return KvTables(kv_lens, query_start, slot_map, positions, status, pool_out)
 
 
 def kv_write(k: torch.Tensor, v: torch.Tensor, slot_map: torch.Tensor, cache: KvCache, *, stream=None) -> None:
