@@ -1,20 +1,23 @@
 // bdkv_attention for many query rows per key/value head: windows of blocks,
 // prompts. tcgen05 products on tiles of 128 rows by 64 cached tokens.
 //
-// A CTA holds NM x 128 rows of a request's key/value head (queries x the
-// group's heads, so the head's cache is read once for all of them) and walks
-// the cache in tiles of 64 tokens:
+// A CTA walks a request's key/value head (whose cache is read once for all of
+// the group's heads) in tiles of 64 tokens, with two streams of products:
+//   NM = 2   256 rows (queries x heads): each half of them sees every tile
+//   NM = 1   up to 128 rows: one stream takes the even tiles, one the odd ones,
+//            and the two results are joined at the end
+// and with warps for each part of the work:
 //   converter warps   codes from global memory to f16 (exact), into shared
-//                     memory in the 128-byte swizzle, four stages; a request's
+//                     memory in the 128-byte swizzle, in stages; a request's
 //                     tail is zeros, so its values times zero weights stay zero
 //   MMA warp          S = Q K^T (both operands in shared memory) and O += P V
 //                     (P in tensor memory, V read with the token index along
-//                     K); S of the next two tiles is ready before its softmax
-//                     begins, so the softmax warps never wait for a product of
-//                     their own last weights
-//   softmax warps     a thread per row: running maxima, weights to f16, written
-//                     over S in tensor memory; O is rescaled only when a row's
-//                     maximum has grown by more than 2^7
+//                     K); a stream's S of the next tile is ready before its
+//                     softmax begins, so the softmax warps never wait for a
+//                     product of their own last weights
+//   softmax warps     a thread per row and stream: running maxima, weights to
+//                     f16, written over S in tensor memory; O is rescaled only
+//                     when a row's maximum has grown by more than 2^7
 // Scales of pages come in through the exponent: w = 2^(S coef k_scale + e_v),
 // see k_attn_rows.cu; O and the sum L have a reference maximum of their own.
 #include "cache.h"
@@ -24,25 +27,25 @@ namespace {
 
 constexpr int TILE = TILES_TILE;  // rows of an MMA
 constexpr int TOK = 64;           // tokens of a tile
-constexpr int STAGES = 4;         // tiles of keys and of values in shared memory
 // Weights are held as f16 times 2^8, with 11 bits down to 2^-22 of the reference, and may exceed it by 2^7 before O is
 // rescaled (2^15 < 65504): a rescale costs a warp about as much as a tile.
 constexpr float P_SHIFT = 8, P_SLACK = 7;
-// Warps of a CTA: 4 for each half's softmax, the converters, and 4 of which one issues the MMAs and one looks up page
-// scales: warpgroups, so that registers can be moved between them. Two halves leave few issue slots, and four converter
-// warps disturb their softmax least (32 windows of 8 x 64 tokens 524 us, 540 with eight): 512 threads start with 128
-// registers, 256 x 144 (a row's 64 scores and their weights) + 128 x 112 + 128 x 56 <= 65536. One half waits for the codes
-// (64 x 5 drafts 95 us with eight converter warps, 101 with four): 512 threads with 128.
+constexpr int stages(int nm) { return nm == 2 ? 4 : 6; }  // tiles of keys and of values in shared memory
+// Warps of a CTA: 4 for each stream's softmax, the converters, and 4 of which one issues the MMAs and one looks up page
+// scales: warpgroups, so that registers can be moved between them (a row's 64 scores and their weights stay in 128 or more).
+// 256 rows leave few issue slots, and four converter warps disturb their softmax least (32 windows of 8 x 64 tokens 524 us,
+// 540 with eight): 512 threads start with 128 registers, 256 x 144 + 128 x 112 + 128 x 56 <= 65536. Few rows wait for the
+// codes: eight converter warps, 640 threads with 96, 256 x 128 + 256 x 80 + 128 x 56 <= 61440.
 constexpr int conv_warps(int nm) { return nm == 2 ? 4 : 8; }
-constexpr int threads(int nm) { return (4 * nm + conv_warps(nm) + 4) * 32; }
+constexpr int threads(int nm) { return (8 + conv_warps(nm) + 4) * 32; }
 
 __device__ uint32_t g_status;  // bd::DEV_* bits
 
 struct Ctl {
-  uint64_t q_full, kv_full[STAGES], kv_empty[STAGES];
-  uint64_t s_full[2][2], p_full[2][2];   // by half and parity of the tile
-  uint64_t o_before[2], o_done[2], drain;  // by half: O without, and with its last product
-  float ks[8][TOK / 16], ve[8][TOK / 16];  // page scales of a tile's groups of tokens: factor, exponent
+  uint64_t q_full, kv_full[6], kv_empty[6];
+  uint64_t s_full[2][2], p_full[2][2];             // by stream and parity of its tile
+  uint64_t o_before[2], o_done[2], joined, drain;  // by stream: O without, and with its last product
+  float ks[8][TOK / 16], ve[8][TOK / 16];          // page scales of a tile's groups of tokens: factor, exponent
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -136,6 +139,21 @@ __device__ __forceinline__ void tmem_ld64(uint32_t taddr, float (&v)[64]) {
       : "memory");
 }
 
+// Three words of this thread's lane, in four columns.
+__device__ __forceinline__ void tmem_st4(uint32_t taddr, float a, float b, float c) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %3};" ::"r"(taddr), "f"(a), "f"(b), "f"(c)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_ld4(uint32_t taddr, float& a, float& b, float& c) {
+  float d;
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=f"(a), "=f"(b), "=f"(c), "=f"(d)
+      : "r"(taddr)
+      : "memory");
+}
+
 // Moves registers between the warpgroups (all four warps execute it).
 template <int N>
 __device__ __forceinline__ void take_registers() {
@@ -148,7 +166,7 @@ __device__ __forceinline__ void give_registers() {
 
 template <int NM, int D>
 constexpr size_t smem_bytes() {
-  return size_t(NM * TILE + 2 * STAGES * TOK) * D * 2 + sizeof(Ctl) + 1024;
+  return size_t(NM * TILE + 2 * stages(NM) * TOK) * D * 2 + sizeof(Ctl) + 1024;
 }
 
 // Loads that happen where `live` says so, without a branch that would hold up the loads behind them.
@@ -181,8 +199,8 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
   constexpr uint32_t Q_ATOM = TILE * 128, KV_ATOM = TOK * 128;  // bytes of one
   constexpr uint32_t Q_HALF = ATOMS * Q_ATOM, KV_TILE = ATOMS * KV_ATOM;
   constexpr int CH = D / 16;                   // 16-code chunks of a token's row
-  constexpr int CONV = conv_warps(NM);
-  constexpr int O_COL = 256;                   // tensor memory: S and P of half x, parity b at 128 x + 64 b; O behind
+  constexpr int CONV = conv_warps(NM), STAGES = stages(NM);
+  constexpr int O_COL = 256;                   // tensor memory: S and P of stream x, parity b at 128 x + 64 b; O behind
   extern __shared__ uint8_t raw[];
   const uint32_t base = (bd::smem_u32(raw) + 1023u) & ~1023u;
   const uint32_t q_at = base, k_at = q_at + NM * Q_HALF, v_at = k_at + STAGES * KV_TILE;
@@ -202,6 +220,7 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
 
   if (tid == 0) {
     bd::mbar_init(bd::smem_u32(&ctl->q_full), NM * TILE);
+    bd::mbar_init(bd::smem_u32(&ctl->joined), 2 * TILE);
     for (int i = 0; i < STAGES; ++i) {
       bd::mbar_init(bd::smem_u32(&ctl->kv_full[i]), CONV * 32 + 32);
       bd::mbar_init(bd::smem_u32(&ctl->kv_empty[i]), 1);
@@ -218,7 +237,10 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
     ctl->abort_flag = 0;
     bd::fence_mbar_init();
   }
-  constexpr int MMA_WARP = 4 * NM + CONV;
+  constexpr int MMA_WARP = 8 + CONV;
+  // A stream's j-th tile is the request's tile j (NM = 2) or 2 j + x.
+  const auto tile_of = [](int x, int j) { return NM == 2 ? j : 2 * j + x; };
+  const auto tiles_of = [&](int x) { return NM == 2 ? n : (n + 1 - x) / 2; };
   if (warp == MMA_WARP) {
     bd::tmem_alloc(bd::smem_u32(&ctl->tmem_base), 512);
     bd::tmem_relinquish();
@@ -235,7 +257,7 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
 
   if (warp >= MMA_WARP) {
     // ---------------------------------------------------------- MMA issuer
-    if constexpr (NM == 2) give_registers<56>();
+    give_registers<56>();
     if (warp == MMA_WARP) {
       const uint32_t issue = bd::elect_one();
       constexpr uint32_t IDESC_S = bd::idesc_f16_f32(TILE, TOK), IDESC_O = bd::idesc_f16_f32(TILE, D) | B_MN_MAJOR;
@@ -244,45 +266,48 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
       const uint32_t k_lo = bd::warp_uniform(static_cast<uint32_t>(bd::sw128_kmajor_desc(k_at)));
       const uint32_t v_lo = bd::warp_uniform(static_cast<uint32_t>(sw128_mnmajor_desc(v_at, KV_ATOM)));
       constexpr uint32_t HI = (1024u >> 4) | (1u << 14) | (2u << 29);
-      const auto scores = [&](int x, int u) {  // S of half x, a tile of stage u
+      const auto scores = [&](int x, int parity, int stage) {
+        const uint32_t kd = bd::warp_uniform(k_lo + stage * (KV_TILE >> 4));
+        const uint32_t qd = bd::warp_uniform(q_lo + (NM == 2 ? x * (Q_HALF >> 4) : 0u));
+        const uint32_t sd = bd::warp_uniform(tmem + x * TILE + parity * TOK);
 #pragma unroll
         for (int k = 0; k < D / 16; ++k)
-          mma_ss(issue, tmem + x * TILE + (u & 1) * TOK, q_lo + x * (Q_HALF >> 4) + (k / 4) * (Q_ATOM >> 4) + 2u * (k % 4),
-                 k_lo + u * (KV_TILE >> 4) + (k / 4) * (KV_ATOM >> 4) + 2u * (k % 4), HI, IDESC_S, k != 0);
-        mma_commit(issue, bd::smem_u32(&ctl->s_full[x][u & 1]));
+          mma_ss(issue, sd, qd + (k / 4) * (Q_ATOM >> 4) + 2u * (k % 4), kd + (k / 4) * (KV_ATOM >> 4) + 2u * (k % 4), HI,
+                 IDESC_S, k != 0);
+        mma_commit(issue, bd::smem_u32(&ctl->s_full[x][parity]));
       };
+      // Products in the order of the request's tiles, S four of them ahead (two of a stream).
+      const int total = tiles_of(0) + tiles_of(1);
       bool ok = n > 0 && wait(ctl->q_full, 0);
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        if (!ok || u >= n) break;
-        ok = wait(ctl->kv_full[u], 0);
+      for (int k = 0; ok && k < min(total, 4); ++k) {
+        const int x = k & 1, t = tile_of(x, k >> 1);
+        if (NM == 1 || x == 0) ok = wait(ctl->kv_full[t], 0);
         if (!ok) break;
         bd::tc_fence_after();
-#pragma unroll
-        for (int x = 0; x < NM; ++x) scores(x, u);
+        scores(x, k >> 1, t);
       }
-      for (int j0 = 0; ok && j0 < n; j0 += STAGES) {
-#pragma unroll 1  // (unrolled, the four stages' code took issue slots from the others: 541 us unrolled once, 556 four times)
-        for (int u = 0; u < STAGES; ++u) {
-          const int j = j0 + u;
-          if (!ok || j >= n) break;
+      int stage = 0, ahead = NM == 2 ? 2 : 4, ahead_phase = 0;  // of the tile of k and of k + 4
+      for (int k = 0; ok && k < total; ++k) {
+        const int x = k & 1, j = k >> 1, parity = j & 1;
+        if (!(ok = wait(ctl->p_full[x][parity], j >> 1))) break;
+        bd::tc_fence_after();
+        const uint32_t vd = bd::warp_uniform(v_lo + stage * (KV_TILE >> 4));
+        const uint32_t pd = bd::warp_uniform(tmem + x * TILE + parity * TOK), od = bd::warp_uniform(tmem + O_COL + x * TILE);
 #pragma unroll
-          for (int x = 0; x < NM; ++x) {
-            if (!ok || !(ok = wait(ctl->p_full[x][u & 1], j >> 1))) break;
-            bd::tc_fence_after();
-#pragma unroll
-            for (int k = 0; k < TOK / 16; ++k)
-              mma_ts(issue, tmem + O_COL + x * TILE, tmem + x * TILE + (u & 1) * TOK + k * 8,
-                     v_lo + u * (KV_TILE >> 4) + k * (2048u >> 4), HI, IDESC_O, (j | k) != 0);
-            if (x == NM - 1) mma_commit(issue, bd::smem_u32(&ctl->kv_empty[u]));
-            if (j + 2 < n) {  // over the weights that the products above read: the tensor pipe takes them in order
-              if (x == 0 && !(ok = wait(ctl->kv_full[(u + 2) % STAGES], (j + 2) / STAGES))) break;
-              bd::tc_fence_after();
-              scores(x, (u + 2) % STAGES);
-            } else {
-              mma_commit(issue, bd::smem_u32(j + 1 < n ? &ctl->o_before[x] : &ctl->o_done[x]));
-            }
-          }
+        for (int i = 0; i < TOK / 16; ++i)
+          mma_ts(issue, od, pd + i * 8, vd + i * (2048u >> 4), HI, IDESC_O, (j | i) != 0);
+        if (NM == 1 || x == 1) {
+          mma_commit(issue, bd::smem_u32(&ctl->kv_empty[stage]));
+          stage = stage + 1 == STAGES ? 0 : stage + 1;
+        }
+        if (k + 4 < total) {  // over the weights that the products above read: the tensor pipe takes them in order
+          if ((NM == 1 || x == 0) && !(ok = wait(ctl->kv_full[ahead], ahead_phase))) break;
+          bd::tc_fence_after();
+          scores(x, parity, ahead);
+          if (NM == 1 || x == 1)
+            if (++ahead == STAGES) ahead = 0, ahead_phase ^= 1;
+        } else {
+          mma_commit(issue, bd::smem_u32(k + 2 < total ? &ctl->o_before[x] : &ctl->o_done[x]));
         }
       }
       mma_commit(issue, bd::smem_u32(&ctl->drain));  // all MMAs issued have completed once it flips
@@ -317,10 +342,10 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
       }
     }
     __syncwarp();
-  } else if (warp >= 4 * NM) {
+  } else if (warp >= 8) {
     // ---------------------------------------------------------- converters
-    if constexpr (NM == 2) give_registers<112>();
-    const int ct = tid - 4 * NM * 32;
+    give_registers<NM == 2 ? 112 : 80>();
+    const int ct = tid - 256;
     constexpr int PER = TOK * CH / (CONV * 32);  // chunks of a thread and tile
     constexpr int STEP = CONV * 32 / CH;         // rows between them
     // eight lanes take four chunks each of two rows, which the swizzle puts into different banks
@@ -387,9 +412,9 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
     }
   } else {
     // ------------------------------------------------------------- softmax
-    if constexpr (NM == 2) take_registers<144>();
-    const int x = NM == 2 ? warp >> 2 : 0;  // half
-    const int r = tid & 127, row = row0 + x * TILE + r, i = row / a.group;
+    take_registers<NM == 2 ? 144 : 128>();
+    const int x = warp >> 2, mine = tiles_of(x);  // stream and its tiles
+    const int r = tid & 127, row = row0 + (NM == 2 ? x * TILE : 0) + r, i = row / a.group;
     const bool live = row < rows;
     const int h = head * a.group + row - i * a.group;
     const int vis = live ? min(visible(a, sq, i), end) : 0;
@@ -431,12 +456,13 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
           const float2 g = Bf16::to_float2(y[e]);
           y[e] = a.f16 ? y[e] ^ flip : f16x2(make_float2(g.x * f, g.y * f));
         }
-        st_shared_v4(q_at + x * Q_HALF + (my_c / 8) * Q_ATOM + rr * 128 + (((my_c % 8) ^ (rr & 7)) << 4), y[0], y[1], y[2],
-                     y[3]);
+        if (NM == 2 || x == 0)  // (both streams of NM = 1 read the rows: they need the shift)
+          st_shared_v4(q_at + (NM == 2 ? x * Q_HALF : 0u) + (my_c / 8) * Q_ATOM + rr * 128 + (((my_c % 8) ^ (rr & 7)) << 4),
+                       y[0], y[1], y[2], y[3]);
       }
       coef = fabsf(a.coef) * pow2i(-shift);
       fence_proxy_async();
-      bd::mbar_arrive(bd::smem_u32(&ctl->q_full));
+      if (NM == 2 || x == 0) bd::mbar_arrive(bd::smem_u32(&ctl->q_full));
     }
 
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
@@ -449,8 +475,8 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
     const auto softmax = [&](auto cut, int j, int left) -> bool {
       constexpr bool CUT = decltype(cut)::value;
       const uint32_t s_at = tmem + lanes + x * TILE + (j & 1) * TOK;
-      const float* ks = ctl->ks[j & 7];
-      const float* ve = ctl->ve[j & 7];
+      const float* ks = ctl->ks[tile_of(x, j) & 7];
+      const float* ve = ctl->ve[tile_of(x, j) & 7];
       float v[TOK];
       __syncwarp();
       tmem_ld64(s_at, v);
@@ -481,7 +507,7 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
       if (__any_sync(~0u, grow)) {
         if (j > 0) {
           // O's product of the tile before is done where the next tile's scores, issued behind it, are
-          if (!(j + 1 < n ? wait(ctl->s_full[x][(j + 1) & 1], (j + 1) >> 1) : wait(ctl->o_before[x], 0))) return false;
+          if (!(j + 1 < mine ? wait(ctl->s_full[x][(j + 1) & 1], (j + 1) >> 1) : wait(ctl->o_before[x], 0))) return false;
           bd::tc_fence_after();
           const float f = grow ? bd::ex2_approx(M - u_top) : 1.f;
           __syncwarp();  // tensor-memory accesses take the whole warp at once
@@ -526,12 +552,12 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
       return true;
     };
 
-    for (int j = 0; j < n; ++j) {
+    for (int j = 0; j < mine; ++j) {
       ok = wait(ctl->s_full[x][j & 1], j >> 1);
       if (!ok) break;
       bd::tc_fence_after();
       if (any_live) {
-        const int left = vis - (begin + j * TOK);  // columns this row sees
+        const int left = vis - (begin + tile_of(x, j) * TOK);  // columns this row sees
         ok = __any_sync(~0u, left < TOK) ? softmax(std::true_type(), j, left) : softmax(std::false_type(), j, left);
         if (!ok) break;
       }
@@ -539,15 +565,40 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
       bd::mbar_arrive(bd::smem_u32(&ctl->p_full[x][j & 1]));
     }
 
-    if (n > 0 && ok) ok = wait(ctl->o_done[x], 0);
+    if (mine > 0 && ok) ok = wait(ctl->o_done[x], 0);
+    float f[2] = {0.f, 0.f};  // what O of this stream, and with NM = 1 of the other one, is multiplied by
+    float lse2;
+    if constexpr (NM == 2) {
+      const float ms = m == -INFINITY ? 0.f : m, Ms = M == -INFINITY ? 0.f : M;
+      f[0] = L == 0.f ? 0.f : bd::ex2_approx(Ms - P_SHIFT - ms) / L;
+      lse2 = L == 0.f ? -INFINITY : ms + log2f(L);
+    } else {
+      // the streams tell each other m, M and L through tensor memory, over their last scores (shared memory is full)
+      __syncwarp();
+      bd::tc_fence_after();
+      tmem_st4(tmem + lanes + x * TILE, m, M, L);
+      bd::tmem_st_wait();
+      bd::tc_fence_before();
+      bd::mbar_arrive(bd::smem_u32(&ctl->joined));
+      wait(ctl->joined, 0);  // both streams' sums, and both O
+      bd::tc_fence_after();
+      float m2, M2, L2;
+      tmem_ld4(tmem + lanes + (x ^ 1) * TILE, m2, M2, L2);
+      const float mt = fmaxf(m, m2), ms = mt == -INFINITY ? 0.f : mt;
+      const float total = L * bd::ex2_approx(m - ms) + L2 * bd::ex2_approx(m2 - ms);
+      if (total != 0.f) {
+        f[0] = bd::ex2_approx(M - P_SHIFT - ms) / total;  // (M is -inf where the stream's tiles hold nothing for the row)
+        f[1] = bd::ex2_approx(M2 - P_SHIFT - ms) / total;
+      }
+      lse2 = total == 0.f ? -INFINITY : ms + log2f(total);
+    }
     bd::tc_fence_after();
-    const float ms = m == -INFINITY ? 0.f : m, Ms = M == -INFINITY ? 0.f : M;
-    const float f = L == 0.f ? 0.f : bd::ex2_approx(Ms - P_SHIFT - ms) / L;
-    const float lse2 = L == 0.f ? -INFINITY : ms + log2f(L);
     RowOut o = {nullptr, nullptr, nullptr};
     if (live) o = row_out(a, sq, seq, part, i, h, visible(a, sq, i));
-    // Through the half's part of the queries' shared memory, which no product reads any more: lanes write their rows,
-    // the warp stores them row by row.
+    // Through shared memory that no product reads any more (the queries', for the odd stream of NM = 1 the keys'): lanes
+    // write their rows, the warp stores them row by row. The streams of NM = 1 share the rows: each has half of the columns.
+    const int c0 = NM == 2 ? 0 : x * (D / 64), c1 = NM == 2 ? D / 32 : c0 + D / 64;
+    const auto in_half = [&](int d) { return NM == 2 || d / (D / 2) == x; };
     const uint32_t stage = q_at + x * Q_HALF + warp_row * (D * 2);
     const auto give = [&](const void* mine, bool there) {  // a row's D * 2 bytes to where its lane says
 #pragma unroll 4
@@ -559,17 +610,23 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
       }
     };
     const auto take = [&](int c, float (&v)[32]) {  // 32 elements of the lane's row
-      if (n > 0)
+      if (mine > 0)
         bd::tmem_ld32(o_at + c * 32, v);
       else
 #pragma unroll
         for (int e = 0; e < 32; ++e) v[e] = 0.f;
 #pragma unroll
-      for (int e = 0; e < 32; ++e) v[e] *= f;
+      for (int e = 0; e < 32; ++e) v[e] *= f[0];
+      if (NM == 1 && tiles_of(x ^ 1) > 0) {
+        float w[32];
+        bd::tmem_ld32(tmem + lanes + O_COL + (x ^ 1) * TILE + c * 32, w);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) v[e] = fmaf(w[e], f[1], v[e]);
+      }
     };
     if (__any_sync(~0u, o.out != nullptr)) {
 #pragma unroll 1
-      for (int c = 0; c < D / 32; ++c) {
+      for (int c = c0; c < c1; ++c) {
         float v[32];
         take(c, v);
 #pragma unroll
@@ -584,12 +641,12 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
         }
       }
       __syncwarp();
-      give(o.out, my_c * 8 < a.dim);
+      give(o.out, my_c * 8 < a.dim && in_half(my_c * 8));
       __syncwarp();
     }
     if (__any_sync(~0u, o.o != nullptr)) {  // fp32: half of the elements at a time
 #pragma unroll 1
-      for (int c = 0; c < D / 32; ++c) {
+      for (int c = c0; c < c1; ++c) {
         float v[32];
         take(c, v);
 #pragma unroll
@@ -604,7 +661,7 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
         }
       }
     }
-    if (live) store_lse(o, lse2);
+    if (live && (NM == 2 || x == 0)) store_lse(o, lse2);
   }
 
   __syncwarp();
