@@ -39,6 +39,7 @@ struct AttnArgs {
   const int32_t* kv_lens;
   const int32_t* q_start;
   int n_seq, max_q, max_kv, mask_block;
+  bool longest_first;  // CTAs take the requests in that order (see pick_seq)
   float coef;  // scale * log2(e)
   bool f16;
   // Work split along the cache: part p of n_split takes tokens [p chunk, (p + 1) chunk). A row that sees at most `chunk`
@@ -114,15 +115,58 @@ struct Seq {
   int q0, q_len, kv_len;
   int q_all, shown;  // its whole q_len, and what its first query has before it
 };
-__device__ __forceinline__ Seq load_seq(const AttnArgs& a, int s) {
+__device__ __forceinline__ Seq make_seq(const AttnArgs& a, int q0, int q1, int kv) {
   Seq r;
-  r.q0 = a.q_start[s];
-  r.q_all = max(a.q_start[s + 1] - r.q0, 0);
+  r.q0 = q0;
+  r.q_all = max(q1 - q0, 0);
   r.q_len = min(r.q_all, a.max_q);
-  const int kv = max(a.kv_lens[s], 0);
-  r.shown = kv - r.q_all;
-  r.kv_len = min(kv, a.max_kv);
+  r.shown = max(kv, 0) - r.q_all;
+  r.kv_len = min(max(kv, 0), a.max_kv);
   return r;
+}
+__device__ __forceinline__ Seq load_seq(const AttnArgs& a, int s) {
+  return make_seq(a, a.q_start[s], a.q_start[s + 1], a.kv_lens[s]);
+}
+// A CTA's request: the nth one, or the one with the nth longest cache (equal ones in their order). With more CTAs than the
+// device runs at once, the long ones then start first and the short ones fill up the end. The host does not know the
+// lengths, so each CTA ranks them itself, in `lens`, shared memory of MAX_ORDERED + 4 words, free again afterwards.
+constexpr int MAX_ORDERED = 256;
+template <int THREADS>
+__device__ __forceinline__ Seq pick_seq(const AttnArgs& a, int n, int* lens, int& seq) {
+  seq = n;
+  if (!a.longest_first) return load_seq(a, n);
+  constexpr int PER = (MAX_ORDERED + THREADS - 1) / THREADS;
+  const int n4 = (a.n_seq + 3) / 4 * 4;
+  int q0[PER], q1[PER], kv[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int t = threadIdx.x + i * THREADS;
+    q0[i] = q1[i] = kv[i] = -1;
+    if (t < a.n_seq) {
+      kv[i] = max(a.kv_lens[t], 0);
+      q0[i] = a.q_start[t];
+      q1[i] = a.q_start[t + 1];
+    }
+    if (t < n4) lens[t] = kv[i];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int t = threadIdx.x + i * THREADS;
+    if (t >= a.n_seq) break;
+    int rank = 0;
+    for (int u = 0; u < n4; u += 4) {
+      const int4 x = *reinterpret_cast<const int4*>(lens + u);
+      rank += (x.x > kv[i] - (u < t)) + (x.y > kv[i] - (u + 1 < t)) + (x.z > kv[i] - (u + 2 < t)) +
+              (x.w > kv[i] - (u + 3 < t));
+    }
+    if (rank == n) *reinterpret_cast<int4*>(lens + MAX_ORDERED) = make_int4(t, q0[i], q1[i], kv[i]);
+  }
+  __syncthreads();
+  const int4 x = *reinterpret_cast<const int4*>(lens + MAX_ORDERED);
+  __syncthreads();
+  seq = x.x;
+  return make_seq(a, x.y, x.z, x.w);
 }
 // Tokens that query i of the request sees (no fewer for a later query).
 __device__ __forceinline__ int visible(const AttnArgs& a, const Seq& s, int i) {

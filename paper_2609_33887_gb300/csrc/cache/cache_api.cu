@@ -169,19 +169,21 @@ namespace {
 
 // How a call runs: the kernel, and its split along the cache.
 struct Plan {
-  bool tiles;
+  bool tiles, longest_first;
   int chunk, n_split;
   int64_t part_rows;  // rows of partial results
   size_t bytes;       // of workspace
 };
 
 // The kernel: up to 32 rows per key/value head (queries times the group) are one or two tiles of the row kernel (64
-// requests of 300 to 4001 tokens: 20 rows 75 us, 94 in the tile kernel; 32 rows 131 and 136; 48 rows 102 and 96).
+// requests of 300 to 4001 tokens: 20 rows 56 us, 64 in the tile kernel; 32 rows 56 and 62; 48 rows 82 and 66).
 // The split along the cache. The host does not know how the lengths differ: one or two requests are split into one wave of
 // CTAs (two to an SM for the row kernel, one for the other), more requests into finer parts, which even out. Row kernel:
-// two caches of 131071 tokens 49 us in one wave, 68 in four; 64 requests of 57 to 8189 tokens 120 and 103. Tile kernel,
-// parts of 2048 tokens or more (a part costs its rows' fp32 results): 2 x 64 queries over 20000 to 30000 tokens 72 us in
-// one wave, 92 in three; 8 x 9 queries over 300 to 30001 tokens 231 and 132.
+// two caches of 131071 tokens 49 us in one wave, 68 in four; 16 requests of 57 to 60000 tokens 192 us in parts for 2 CTAs
+// per SM, 161 for 3, 207 for 4. Tile kernel, parts of 2048 tokens or more (a part costs its rows' fp32 results): 2 x 64
+// queries over 20000 to 30000 tokens 72 us in one wave, 92 in three; 8 x 9 queries over 300 to 30001 tokens 151 and 127.
+// More CTAs than run at once take the requests longest first: 64 requests x 35 rows over 300 to 4001 tokens 92 us in the
+// requests' order and 65 so; 512 CTAs of equal lengths, where the order is for nothing, 232 and 234.
 Plan make_plan(const bdkv_cache& c, const bdkv_attention_args& a, int sms) {
   Plan p = {};
   const int64_t rows = int64_t(a.max_q_len) * (a.n_q_heads / c.n_heads);
@@ -194,12 +196,13 @@ Plan make_plan(const bdkv_cache& c, const bdkv_attention_args& a, int sms) {
     const int64_t finer = std::min<int64_t>((3 * int64_t(sms) + ctas - 1) / ctas, a.max_kv_len / 2048);
     parts = few || ctas >= sms ? sms / ctas : std::max<int64_t>(sms / ctas, finer);
   } else {
-    parts = few ? 2 * int64_t(sms) / ctas : (8 * int64_t(sms) + ctas - 1) / ctas;
+    parts = few ? 2 * int64_t(sms) / ctas : (3 * int64_t(sms) + ctas - 1) / ctas;
   }
   const int64_t least = p.tiles ? 256 : 128;  // tokens
   int64_t chunk = parts > 1 ? ((a.max_kv_len + parts - 1) / parts + 127) / 128 * 128 : a.max_kv_len;
   if (chunk < least) chunk = least;
   p.n_split = static_cast<int>((a.max_kv_len + chunk - 1) / chunk);
+  p.longest_first = !few && a.n_seq <= bdkv::MAX_ORDERED && ctas * p.n_split > (p.tiles ? sms : 2 * sms);
   if (p.n_split <= 1) {
     p.n_split = 1;
     p.chunk = INT_MAX;
@@ -268,6 +271,7 @@ int bdkv_attention(const bdkv_cache* cache, const bdkv_attention_args* args) {
   bdkv::AttnArgs a = attn_args(*cache, *args);
   a.chunk = plan.chunk;
   a.n_split = plan.n_split;
+  a.longest_first = plan.longest_first;
   const auto run = [&](void* ws) {
     a.part_o = static_cast<float*>(ws);
     a.part_l = a.part_o + plan.part_rows * cache->head_dim;

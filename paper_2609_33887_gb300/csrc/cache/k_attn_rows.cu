@@ -70,9 +70,10 @@ __global__ void __launch_bounds__(WARPS * 32, 2) attn_rows_kernel(AttnArgs a) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ float sm_m[WARPS][16], sm_M[WARPS][16], sm_L[WARPS][16];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = lane >> 2, c = lane & 3;
-  const int seq = blockIdx.z, part = blockIdx.y;
+  int seq;
+  const Seq sq = pick_seq<WARPS * 32>(a, blockIdx.z, reinterpret_cast<int*>(smem), seq);
+  const int part = blockIdx.y;
   const int head = blockIdx.x % a.n_kv, row0 = blockIdx.x / a.n_kv * ROWS_TILE;
-  const Seq sq = load_seq(a, seq);
   const int rows = sq.q_len * a.group;
   if (row0 >= rows) return;
   // later queries see at least as much, so the CTA's last row bounds it

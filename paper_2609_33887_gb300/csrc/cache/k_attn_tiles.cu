@@ -201,15 +201,16 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
   constexpr int CH = D / 16;                   // 16-code chunks of a token's row
   constexpr int CONV = conv_warps(NM), STAGES = stages(NM);
   constexpr int O_COL = 256;                   // tensor memory: S and P of stream x, parity b at 128 x + 64 b; O behind
-  extern __shared__ uint8_t raw[];
+  extern __shared__ __align__(16) uint8_t raw[];
   const uint32_t base = (bd::smem_u32(raw) + 1023u) & ~1023u;
   const uint32_t q_at = base, k_at = q_at + NM * Q_HALF, v_at = k_at + STAGES * KV_TILE;
   Ctl* ctl = reinterpret_cast<Ctl*>(raw + (v_at + STAGES * KV_TILE - bd::smem_u32(raw)));
   const int tid = threadIdx.x, lane = tid & 31, warp = static_cast<int>(bd::warp_uniform(tid >> 5));
   const int n_tiles_rows = gridDim.x / a.n_kv;
   const int head = blockIdx.x / n_tiles_rows, row0 = (n_tiles_rows - 1 - blockIdx.x % n_tiles_rows) * (NM * TILE);
-  const int seq = blockIdx.z, part = blockIdx.y;
-  const Seq sq = load_seq(a, seq);
+  int seq;
+  const Seq sq = pick_seq<threads(NM)>(a, blockIdx.z, reinterpret_cast<int*>(raw), seq);
+  const int part = blockIdx.y;
   const int rows = sq.q_len * a.group;
   if (row0 >= rows) return;
   // later queries see at least as much, so the CTA's last row bounds it
