@@ -39,7 +39,7 @@ struct AttnArgs {
   const int32_t* kv_lens;
   const int32_t* q_start;
   int n_seq, max_q, max_kv, mask_block;
-  bool longest_first;  // CTAs take the requests in that order (see pick_seq)
+  bool longest_first;  // CTAs take the requests in that order (see ranked_seq)
   float coef;  // scale * log2(e)
   bool f16;
   // Work split along the cache: part p of n_split takes tokens [p chunk, (p + 1) chunk). A row that sees at most `chunk`
@@ -127,14 +127,12 @@ __device__ __forceinline__ Seq make_seq(const AttnArgs& a, int q0, int q1, int k
 __device__ __forceinline__ Seq load_seq(const AttnArgs& a, int s) {
   return make_seq(a, a.q_start[s], a.q_start[s + 1], a.kv_lens[s]);
 }
-// A CTA's request: the nth one, or the one with the nth longest cache (equal ones in their order). With more CTAs than the
-// device runs at once, the long ones then start first and the short ones fill up the end. The host does not know the
-// lengths, so each CTA ranks them itself, in `lens`, shared memory of MAX_ORDERED + 4 words, free again afterwards.
+// The request with the nth longest cache (equal ones in their order). With more CTAs than the device runs at once, the
+// long ones then start first and the short ones fill up the end. The host does not know the lengths, so each CTA ranks
+// them itself, in `lens`, shared memory of MAX_ORDERED + 4 words, free again afterwards.
 constexpr int MAX_ORDERED = 256;
 template <int THREADS>
-__device__ __forceinline__ Seq pick_seq(const AttnArgs& a, int n, int* lens, int& seq) {
-  seq = n;
-  if (!a.longest_first) return load_seq(a, n);
+__device__ __forceinline__ Seq ranked_seq(const AttnArgs& a, int n, int* lens, int& seq) {
   constexpr int PER = (MAX_ORDERED + THREADS - 1) / THREADS;
   const int n4 = (a.n_seq + 3) / 4 * 4;
   int q0[PER], q1[PER], kv[PER];

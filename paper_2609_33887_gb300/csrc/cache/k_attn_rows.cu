@@ -60,8 +60,9 @@ constexpr size_t smem_bytes() {
 }
 
 // One CTA: 16 rows of a request's key/value head (R = 1: at most 8 of them exist), one part of its cache. BIG: a step's
-// tokens share a page (pages of 32 and more).
-template <class T, int D, int R, bool BIG>
+// tokens share a page (pages of 32 and more). ORDERED: the longest caches first; a kernel of its own, since the code for it,
+// even where it is not taken, costs a call of one request 1.7 of 8.6 us.
+template <class T, int D, int R, bool BIG, bool ORDERED>
 __global__ void __launch_bounds__(WARPS * 32, 2) attn_rows_kernel(AttnArgs a) {
   constexpr int CH = D / 16;  // 16-byte chunks of a token's row; also k-steps
   constexpr int VB = D / 8;   // bytes of a value row a lane reads; also n-tiles of O
@@ -70,8 +71,12 @@ __global__ void __launch_bounds__(WARPS * 32, 2) attn_rows_kernel(AttnArgs a) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ float sm_m[WARPS][16], sm_M[WARPS][16], sm_L[WARPS][16];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = lane >> 2, c = lane & 3;
-  int seq;
-  const Seq sq = pick_seq<WARPS * 32>(a, blockIdx.z, reinterpret_cast<int*>(smem), seq);
+  int seq = blockIdx.z;
+  Seq sq;
+  if constexpr (ORDERED)
+    sq = ranked_seq<WARPS * 32>(a, blockIdx.z, reinterpret_cast<int*>(smem), seq);
+  else
+    sq = load_seq(a, seq);
   const int part = blockIdx.y;
   const int head = blockIdx.x % a.n_kv, row0 = blockIdx.x / a.n_kv * ROWS_TILE;
   const int rows = sq.q_len * a.group;
@@ -343,21 +348,25 @@ __global__ void __launch_bounds__(WARPS * 32, 2) attn_rows_kernel(AttnArgs a) {
   }
 }
 
-template <class T, int D, int R, bool BIG>
+template <class T, int D, int R, bool BIG, bool ORDERED>
 cudaError_t launch(const AttnArgs& a, cudaStream_t st) {
   static std::atomic<bool> ready[64];  // by device
-  const auto kernel = attn_rows_kernel<T, D, R, BIG>;
+  const auto kernel = attn_rows_kernel<T, D, R, BIG, ORDERED>;
   if (cudaError_t e = allow_smem(kernel, smem_bytes<D>(), ready); e != cudaSuccess) return e;
   const dim3 grid((a.max_q * a.group + ROWS_TILE - 1) / ROWS_TILE * a.n_kv, a.n_split, a.n_seq);
   kernel<<<grid, WARPS * 32, smem_bytes<D>(), st>>>(a);
   return cudaGetLastError();
 }
 
+template <class T, int D, int R>
+cudaError_t launch_pages(const AttnArgs& a, cudaStream_t st) {
+  if ((1 << a.page_shift) >= STEP) return a.longest_first ? launch<T, D, R, true, true>(a, st) : launch<T, D, R, true, false>(a, st);
+  return a.longest_first ? launch<T, D, R, false, true>(a, st) : launch<T, D, R, false, false>(a, st);
+}
+
 template <class T, int D>
 cudaError_t launch_rows(const AttnArgs& a, cudaStream_t st) {
-  const bool big = (1 << a.page_shift) >= STEP;
-  if (a.max_q * a.group <= 8) return big ? launch<T, D, 1, true>(a, st) : launch<T, D, 1, false>(a, st);
-  return big ? launch<T, D, 2, true>(a, st) : launch<T, D, 2, false>(a, st);
+  return a.max_q * a.group <= 8 ? launch_pages<T, D, 1>(a, st) : launch_pages<T, D, 2>(a, st);
 }
 
 }  // namespace

@@ -145,7 +145,7 @@ __device__ __forceinline__ void tmem_st4(uint32_t taddr, float a, float b, float
                : "memory");
 }
 __device__ __forceinline__ void tmem_ld4(uint32_t taddr, float& a, float& b, float& c) {
-  float d;
+  [[maybe_unused]] float d;
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];\n\t"
       "tcgen05.wait::ld.sync.aligned;"
@@ -208,8 +208,8 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
   const int tid = threadIdx.x, lane = tid & 31, warp = static_cast<int>(bd::warp_uniform(tid >> 5));
   const int n_tiles_rows = gridDim.x / a.n_kv;
   const int head = blockIdx.x / n_tiles_rows, row0 = (n_tiles_rows - 1 - blockIdx.x % n_tiles_rows) * (NM * TILE);
-  int seq;
-  const Seq sq = pick_seq<threads(NM)>(a, blockIdx.z, reinterpret_cast<int*>(raw), seq);
+  int seq = blockIdx.z;
+  const Seq sq = a.longest_first ? ranked_seq<threads(NM)>(a, blockIdx.z, reinterpret_cast<int*>(raw), seq) : load_seq(a, seq);
   const int part = blockIdx.y;
   const int rows = sq.q_len * a.group;
   if (row0 >= rows) return;

@@ -394,6 +394,17 @@ def test_repeated_calls_give_the_same_bits(q_len, g, total):
         assert torch.equal(bdc.kv_attention(*args, **bounds, workspace=ws if i % 2 else None), first), i
 
 
+@pytest.mark.parametrize("q_len", [1, 4, 12])
+@pytest.mark.parametrize("n_seq", [103, 256, 257])
+def test_many_requests_of_any_lengths(n_seq, q_len):
+    rng = np.random.default_rng(n_seq + q_len)
+    lens = rng.integers(0, 180, n_seq)
+    lens[rng.random(n_seq) < 0.3] = 64  # ranked by length, these are equals
+    lens[rng.random(n_seq) < 0.05] = 700
+    q_lens = np.minimum(rng.integers(0, q_len + 1, n_seq), lens)
+    assert_attention(random_cache(lens, 16, 3, 64, seed=8), q_lens.tolist(), 12, "bf16", 1)
+
+
 def test_page_numbers_out_of_range_are_not_read():
     c = random_cache([64, 64], 16, 1, 32, seed=10)
     c.table[1, 1], c.table[1, 2] = -1, 2 ** 31 - 1
