@@ -39,6 +39,7 @@ struct AttnArgs {
   const int32_t* kv_lens;
   const int32_t* q_start;
   int n_seq, max_q, max_kv, mask_block;
+  bool one_tile;       // of rows to a CTA of the tile kernel
   bool longest_first;  // CTAs take the requests in that order (see ranked_seq)
   float coef;  // scale * log2(e)
   bool f16;

@@ -169,7 +169,7 @@ namespace {
 
 // How a call runs: the kernel, and its split along the cache.
 struct Plan {
-  bool tiles, longest_first;
+  bool tiles, one_tile, longest_first;
   int chunk, n_split;
   int64_t part_rows;  // rows of partial results
   size_t bytes;       // of workspace
@@ -177,6 +177,9 @@ struct Plan {
 
 // The kernel: up to 32 rows per key/value head (queries times the group) are one or two tiles of the row kernel (64
 // requests of 300 to 4001 tokens: 20 rows 56 us, 64 in the tile kernel; 32 rows 56 and 62; 48 rows 82 and 66).
+// Two tiles of 128 rows to a CTA read the cache once for both; one where that still runs in one wave and the
+// caches are too short to fill the device by a split (8 x 512 rows over 200 to 1400 tokens 23 us, 31 with two; 32 x 256
+// rows, two waves, 129 and 82; 2 x 256 rows over 20000 to 30000 tokens 108 and 76).
 // The split along the cache. The host does not know how the lengths differ: one or two requests are split into one wave of
 // CTAs (two to an SM for the row kernel, one for the other), more requests into finer parts, which even out. Row kernel:
 // two caches of 131071 tokens 49 us in one wave, 68 in four; 16 requests of 57 to 60000 tokens 192 us in parts for 2 CTAs
@@ -188,8 +191,11 @@ Plan make_plan(const bdkv_cache& c, const bdkv_attention_args& a, int sms) {
   Plan p = {};
   const int64_t rows = int64_t(a.max_q_len) * (a.n_q_heads / c.n_heads);
   p.tiles = rows > 2 * bdkv::ROWS_TILE;
-  const int64_t tile = !p.tiles ? bdkv::ROWS_TILE : rows <= bdkv::TILES_TILE ? bdkv::TILES_TILE : 2 * bdkv::TILES_TILE;
-  const int64_t ctas = (rows + tile - 1) / tile * c.n_heads * a.n_seq;
+  const int64_t pairs = int64_t(c.n_heads) * a.n_seq;
+  const int64_t one_tile_ctas = (rows + bdkv::TILES_TILE - 1) / bdkv::TILES_TILE * pairs;
+  p.one_tile = rows <= bdkv::TILES_TILE || (one_tile_ctas <= sms && a.max_kv_len <= 4096);
+  const int64_t tile = !p.tiles ? bdkv::ROWS_TILE : p.one_tile ? bdkv::TILES_TILE : 2 * bdkv::TILES_TILE;
+  const int64_t ctas = (rows + tile - 1) / tile * pairs;
   const bool few = a.n_seq <= 2;
   int64_t parts;
   if (p.tiles) {
@@ -271,6 +277,7 @@ int bdkv_attention(const bdkv_cache* cache, const bdkv_attention_args* args) {
   bdkv::AttnArgs a = attn_args(*cache, *args);
   a.chunk = plan.chunk;
   a.n_split = plan.n_split;
+  a.one_tile = plan.one_tile;
   a.longest_first = plan.longest_first;
   const auto run = [&](void* ws) {
     a.part_o = static_cast<float*>(ws);

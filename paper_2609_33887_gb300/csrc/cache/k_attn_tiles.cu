@@ -692,9 +692,8 @@ cudaError_t launch_pages(const AttnArgs& a, cudaStream_t st) {
 }  // namespace
 
 cudaError_t launch_attn_tiles(const AttnArgs& a, cudaStream_t st) {
-  const bool one = a.max_q * a.group <= TILE;
-  if (a.dim <= 64) return one ? launch_pages<1, 64>(a, st) : launch_pages<2, 64>(a, st);
-  return one ? launch_pages<1, 128>(a, st) : launch_pages<2, 128>(a, st);
+  if (a.dim <= 64) return a.one_tile ? launch_pages<1, 64>(a, st) : launch_pages<2, 64>(a, st);
+  return a.one_tile ? launch_pages<1, 128>(a, st) : launch_pages<2, 128>(a, st);
 }
 
 cudaError_t tiles_status(cudaStream_t st, uint32_t* bits) {

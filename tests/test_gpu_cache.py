@@ -394,6 +394,27 @@ def test_repeated_calls_give_the_same_bits(q_len, g, total):
         assert torch.equal(bdc.kv_attention(*args, **bounds, workspace=ws if i % 2 else None), first), i
 
 
+# More than 128 rows to a key/value head: two tiles to a CTA, unless all CTAs of one tile run at once and no length may
+# pass 4096.
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("mask_block", [0, 1, 32])
+@pytest.mark.parametrize("page,n_kv,g,dim", [(16, 1, 3, 128), (64, 2, 4, 64), (32, 1, 5, 80), (128, 1, 2, 16)])
+def test_windows_under_a_long_bound(page, n_kv, g, dim, mask_block, dtype):
+    c = random_cache([77, 900, 129, 0, 70], page, n_kv, dim, seed=12, extra_cols=5000 // page)
+    assert_attention(c, [77, 110, 65, 0, 70], n_kv * g, dtype, mask_block, max_q=130, max_kv=5000)
+    c = random_cache([400, 170], page, n_kv, dim, seed=13, k_exp=(-16, -6), v_exp=(-60, 40), extra_cols=5000 // page)
+    assert_attention(c, [130, 66], n_kv * g, "bf16", mask_block, max_kv=4097)  # results up to 2^48: none in f16
+
+
+@pytest.mark.parametrize("page,n_kv,g,dim,n_seq", [(16, 2, 2, 64, 80), (64, 1, 3, 96, 160)])
+@pytest.mark.parametrize("mask_block", [0, 1, 20])
+def test_many_windows(page, n_kv, g, dim, n_seq, mask_block):
+    rng = np.random.default_rng(n_seq + mask_block)
+    lens = rng.integers(-2, 330, n_seq)
+    q_lens = np.minimum(rng.integers(0, 100, n_seq), np.maximum(lens, 0))
+    assert_attention(random_cache(lens, page, n_kv, dim, seed=14), q_lens.tolist(), n_kv * g, "bf16", mask_block)
+
+
 @pytest.mark.parametrize("q_len", [1, 4, 12])
 @pytest.mark.parametrize("n_seq", [103, 256, 257])
 def test_many_requests_of_any_lengths(n_seq, q_len):
