@@ -20,6 +20,12 @@
 //                     when a row's maximum has grown by more than 2^7
 // Scales of pages come in through the exponent: w = 2^(S coef k_scale + e_v),
 // see k_attn_rows.cu; O and the sum L have a reference maximum of their own.
+//
+// 32 windows of 512 queries, 32 heads on 8, over 700 to 4096 tokens take 507 us:
+// 1150 TFLOP/s, 0.61 of a library product's rate. Bound by the softmax warps'
+// chain from scores to weights (about 1600 cycles a tile of 2 x 128 x 64 scores,
+// 1080 of them under products), and by each CTA's start and end (a fifth of it),
+// during which nothing is multiplied.
 #include "cache.h"
 
 namespace bdkv {
