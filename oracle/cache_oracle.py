@@ -149,3 +149,50 @@ def attention(q, k_codes, v_codes, k_scale, v_scale, block_table, kv_lens, query
                 lse[q0 + i, h] = top + np.log(total)
                 work[q0 + i, h] = np.max(np.abs(kk) @ np.abs(qq)) * abs(scale)
     return out, lse, spread, work
+
+
+def attention_largest_term(q, k_codes, v_codes, k_scale, v_scale, block_table, kv_lens, query_start, scale, mask_block):
+    """[tokens, heads, dim]: the largest p_t 2^(value exponent) of the tokens that a row sees, p its softmax, times the sum
+    of their value codes' magnitudes: what absolute errors of weights too small for their format are proportional to."""
+    n_tok, n_q, dim = q.shape
+    n_kv = k_codes.shape[2]
+    g = n_q // n_kv
+    out = np.zeros((n_tok, n_q, dim))
+    for s in range(len(kv_lens)):
+        n, q0 = max(int(kv_lens[s]), 0), int(query_start[s])
+        q_len = int(query_start[s + 1]) - q0
+        pages = np.asarray(block_table[s][:-(-n // k_codes.shape[1])], dtype=np.int64)
+        k = (E4M3[k_codes[pages]] * pow2(k_scale[pages])[:, None, :, None]).reshape(-1, n_kv, dim)[:n]
+        codes = np.abs(E4M3[v_codes[pages]]).reshape(-1, n_kv, dim)[:n]
+        ve = np.repeat(pow2(v_scale[pages]), k_codes.shape[1], axis=0)[:n]
+        for i in range(q_len):
+            see = visible(n, q_len, i, mask_block)
+            for h in range(n_q if see else 0):
+                x = k[:see, h // g] @ q[q0 + i, h] * scale
+                w = np.exp(x - np.max(x))
+                out[q0 + i, h] = np.max(w * ve[:see, h // g]) / w.sum() * codes[:see, h // g].sum(0)
+    return out
+
+
+def attention_best_token(q, k_codes, v_codes, k_scale, v_scale, block_table, kv_lens, query_start, scale, mask_block):
+    """For each row: the value of the token with the best score [tokens, heads, dim], by how much that score is above
+    the next [tokens, heads] (infinite for one token), and the largest |value| it sees [tokens, heads, dim]."""
+    n_tok, n_q, dim = q.shape
+    n_kv = k_codes.shape[2]
+    g = n_q // n_kv
+    value, most, gap = np.zeros((n_tok, n_q, dim)), np.zeros((n_tok, n_q, dim)), np.full((n_tok, n_q), np.inf)
+    for s in range(len(kv_lens)):
+        n, q0 = max(int(kv_lens[s]), 0), int(query_start[s])
+        q_len = int(query_start[s + 1]) - q0
+        pages = np.asarray(block_table[s][:-(-n // k_codes.shape[1])], dtype=np.int64)
+        k = (E4M3[k_codes[pages]] * pow2(k_scale[pages])[:, None, :, None]).reshape(-1, n_kv, dim)[:n]
+        v = (E4M3[v_codes[pages]] * pow2(v_scale[pages])[:, None, :, None]).reshape(-1, n_kv, dim)[:n]
+        for i in range(q_len):
+            see = visible(n, q_len, i, mask_block)
+            for h in range(n_q if see else 0):
+                x = k[:see, h // g] @ q[q0 + i, h] * scale
+                t = int(np.argmax(x))
+                value[q0 + i, h], most[q0 + i, h] = v[t, h // g], np.abs(v[:see, h // g]).max(0)
+                if see > 1:
+                    gap[q0 + i, h] = x[t] - np.max(np.delete(x, t))
+    return value, gap, most

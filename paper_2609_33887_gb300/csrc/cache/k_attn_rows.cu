@@ -8,8 +8,10 @@
 //     S = Q K^T, w = 2^(S coef + e_v), O = sum w code_v, L = sum 2^(S coef)
 // where e_v is the exponent of the page's value scale, so values are
 // multiplied as the codes they are (exact in f16). O and L have a reference
-// of their own each (M and m), so pages of very different value scales, all
-// zeros among them, cost neither range.
+// of their own each, 2^(r + d) and 2^m, so pages of very different value scales,
+// all zeros among them, cost neither range. O's is in two parts, r a score and
+// d an exponent of values: added up, a large score would leave the exponent no
+// bits (scores of 2^24 made results wrong by powers of two).
 //
 // Bound by the cache's bytes while a head has few rows: one token of each of 64
 // requests of 57 to 8189 tokens, 8 heads of 128, takes 87 us, 6.2 TB/s (0.92 of
@@ -74,7 +76,7 @@ __global__ void __launch_bounds__(WARPS * 32, 2) attn_rows_kernel(AttnArgs a) {
   constexpr int STAGE = STEP * D * 2;
   constexpr int GROUPS = BIG ? 1 : 2;  // pages of a step
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ float sm_m[WARPS][16], sm_M[WARPS][16], sm_L[WARPS][16];
+  __shared__ float sm_m[WARPS][16], sm_r[WARPS][16], sm_d[WARPS][16], sm_L[WARPS][16];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = lane >> 2, c = lane & 3;
   int seq = blockIdx.z;
   Seq sq;
@@ -182,9 +184,9 @@ __global__ void __launch_bounds__(WARPS * 32, 2) attn_rows_kernel(AttnArgs a) {
   }
 
   float O[VB][4] = {};
-  float m[R], M[R], L[R];
+  float m[R], ro[R], d[R], L[R];  // ro, d: O's reference (d = -inf: O holds nothing yet)
 #pragma unroll
-  for (int r = 0; r < R; ++r) m[r] = M[r] = -INFINITY, L[r] = 0.f;
+  for (int r = 0; r < R; ++r) m[r] = d[r] = -INFINITY, ro[r] = L[r] = 0.f;
 
   for (int step0 = warp; step0 < n_steps; step0 += STAGES * WARPS) {
 #pragma unroll
@@ -216,48 +218,49 @@ __global__ void __launch_bounds__(WARPS * 32, 2) attn_rows_kernel(AttnArgs a) {
       }
 
       uint32_t pf[2][4] = {};  // weights as A fragments of two products
-      float newM[R];
+      float new_ro[R], new_d[R];
       bool grown = false;
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        float x[8];
-        float s_top = -INFINITY, u_top = -INFINITY;
+        float x[8], ve[GROUPS], top[GROUPS];
+        constexpr int E = 8 / GROUPS;
 #pragma unroll
         for (int g = 0; g < GROUPS; ++g) {
           const float f = coef[r] * pow2i(ks[stage][g] - 127);
-          constexpr int E = 8 / GROUPS;
-          float top = -INFINITY;
+          ve[g] = static_cast<float>(vs[stage][g] - 127);
+          top[g] = -INFINITY;
 #pragma unroll
-          for (int e = g * E; e < g * E + E; ++e) x[e] = S[e >> 1][2 * r + (e & 1)] * f;
+          for (int e = g * E; e < g * E + E; ++e) x[e] = __fmul_rn(S[e >> 1][2 * r + (e & 1)], f);  // (its own maximum less itself is 0)
           if (t0 + STEP > vis[r])
 #pragma unroll
             for (int e = g * E; e < g * E + E; ++e)
               if (t0 + (e >> 1) * 8 + 2 * c + (e & 1) >= vis[r]) x[e] = -INFINITY;
 #pragma unroll
-          for (int e = g * E; e < g * E + E; e += 2) top = bd::max3(top, x[e], x[e + 1]);
-          s_top = fmaxf(s_top, top);
-          u_top = fmaxf(u_top, top + static_cast<float>(vs[stage][g] - 127));
+          for (int e = g * E; e < g * E + E; e += 2) top[g] = bd::max3(top[g], x[e], x[e + 1]);
+          top[g] = fmaxf(top[g], __shfl_xor_sync(~0u, top[g], 1));
+          top[g] = fmaxf(top[g], __shfl_xor_sync(~0u, top[g], 2));
         }
-        if (GROUPS > 1) {
-          s_top = fmaxf(s_top, __shfl_xor_sync(~0u, s_top, 1));
-          s_top = fmaxf(s_top, __shfl_xor_sync(~0u, s_top, 2));
+        float m_new = m[r], u_top = -INFINITY;
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+          m_new = fmaxf(m_new, top[g]);
+          u_top = fmaxf(u_top, (top[g] - ro[r]) + ve[g]);
         }
-        u_top = fmaxf(u_top, __shfl_xor_sync(~0u, u_top, 1));
-        u_top = fmaxf(u_top, __shfl_xor_sync(~0u, u_top, 2));
-        if (GROUPS == 1) s_top = u_top - static_cast<float>(vs[stage][0] - 127);
-        const float m_new = fmaxf(m[r], s_top);
         L[r] *= m_new == m[r] ? 1.f : bd::ex2_approx(m[r] - m_new);
         m[r] = m_new;
-        newM[r] = u_top > M[r] + P_SLACK || (M[r] == -INFINITY && u_top > M[r]) ? u_top : M[r];
-        grown |= newM[r] != M[r];
-        const float mr = m_new == -INFINITY ? 0.f : m_new;
+        const bool grow = u_top > d[r] + P_SLACK || (d[r] == -INFINITY && u_top > d[r]);
+        new_ro[r] = grow ? m_new : ro[r];
+        new_d[r] = grow ? -INFINITY : d[r];
+        if (grow)
+#pragma unroll
+          for (int g = 0; g < GROUPS; ++g) new_d[r] = fmaxf(new_d[r], (top[g] - m_new) + ve[g]);
+        grown |= grow;
+        const float mr = m_new == -INFINITY ? 0.f : m_new, dr = new_d[r] == -INFINITY ? 0.f : new_d[r];
         float w[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const float ve = static_cast<float>(vs[stage][e / (8 / GROUPS)] - 127);
-          const float Mr = (newM[r] == -INFINITY ? 0.f : newM[r]) - ve - P_SHIFT;
           L[r] += bd::ex2_approx(x[e] - mr);
-          w[e] = bd::ex2_approx(x[e] - Mr);
+          w[e] = bd::ex2_approx((x[e] - new_ro[r]) - (dr - ve[e / E] - P_SHIFT));
         }
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
@@ -268,8 +271,9 @@ __global__ void __launch_bounds__(WARPS * 32, 2) attn_rows_kernel(AttnArgs a) {
       if (__any_sync(~0u, grown)) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-          const float f = newM[r] == M[r] ? 1.f : bd::ex2_approx(M[r] - newM[r]);
-          M[r] = newM[r];
+          const float f = bd::ex2_approx((ro[r] - new_ro[r]) + (d[r] == new_d[r] ? 0.f : d[r] - new_d[r]));
+          ro[r] = new_ro[r];
+          d[r] = new_d[r];
 #pragma unroll
           for (int j = 0; j < VB; ++j) {
             O[j][2 * r] *= f;
@@ -319,7 +323,8 @@ __global__ void __launch_bounds__(WARPS * 32, 2) attn_rows_kernel(AttnArgs a) {
     L[r] += __shfl_xor_sync(~0u, L[r], 2);
     if (c == 0) {
       sm_m[warp][n + 8 * r] = m[r];
-      sm_M[warp][n + 8 * r] = M[r];
+      sm_r[warp][n + 8 * r] = ro[r];
+      sm_d[warp][n + 8 * r] = d[r];
       sm_L[warp][n + 8 * r] = L[r];
     }
 #pragma unroll
@@ -332,23 +337,20 @@ __global__ void __launch_bounds__(WARPS * 32, 2) attn_rows_kernel(AttnArgs a) {
   for (int u = tid; u < 8 * R * D / 4; u += WARPS * 32) {
     const int r = u / (D / 4), d = u % (D / 4) * 4, row = row0 + r;
     if (row >= rows) continue;
-    float mt = -INFINITY, Mt = -INFINITY, Lt = 0.f;
-    for (int w = 0; w < WARPS; ++w) {
-      mt = fmaxf(mt, sm_m[w][r]);
-      Mt = fmaxf(Mt, sm_M[w][r]);
-    }
-    const float ms = mt == -INFINITY ? 0.f : mt, Ms = Mt == -INFINITY ? 0.f : Mt;
+    float mt = -INFINITY, Lt = 0.f;
+    for (int w = 0; w < WARPS; ++w) mt = fmaxf(mt, sm_m[w][r]);
+    const float ms = mt == -INFINITY ? 0.f : mt;
+    for (int w = 0; w < WARPS; ++w) Lt += sm_L[w][r] * bd::ex2_approx(sm_m[w][r] - ms);
+    const float inv = Lt == 0.f ? 0.f : 1.f / Lt;
     float4 o = {0.f, 0.f, 0.f, 0.f};
     for (int w = 0; w < WARPS; ++w) {
-      Lt += sm_L[w][r] * bd::ex2_approx(sm_m[w][r] - ms);
-      const float f = bd::ex2_approx(sm_M[w][r] - Ms);
+      const float f = bd::ex2_approx((sm_r[w][r] - ms) + (sm_d[w][r] - P_SHIFT)) * inv;
       const float4 x = *reinterpret_cast<const float4*>(acc + (w * 16 + r) * LD + d);
       o.x += x.x * f, o.y += x.y * f, o.z += x.z * f, o.w += x.w * f;
     }
-    const float f = Lt == 0.f ? 0.f : bd::ex2_approx(Ms - P_SHIFT - ms) / Lt;
     const int i = row / a.group;
     const RowOut dst = row_out(a, sq, seq, part, i, head * a.group + row - i * a.group, visible(a, sq, i));
-    if (d < a.dim) store4<T>(dst, d, make_float4(o.x * f, o.y * f, o.z * f, o.w * f));
+    if (d < a.dim) store4<T>(dst, d, o);
     if (d == 0) store_lse(dst, Lt == 0.f ? -INFINITY : ms + log2f(Lt));
   }
 }

@@ -19,7 +19,9 @@
 //                     f16, written over S in tensor memory; O is rescaled only
 //                     when a row's maximum has grown by more than 2^7
 // Scales of pages come in through the exponent: w = 2^(S coef k_scale + e_v),
-// see k_attn_rows.cu; O and the sum L have a reference maximum of their own.
+// see k_attn_rows.cu; O and the sum L have a reference maximum of their own,
+// O's in two parts, a score and an exponent, so that scores of any size leave
+// the exponent its bits.
 //
 // 32 windows of 512 queries, 32 heads on 8, over 700 to 4096 tokens take 507 us:
 // 1150 TFLOP/s, 0.61 of a library product's rate. Bound by the softmax warps'
@@ -36,6 +38,9 @@ constexpr int TOK = 64;           // tokens of a tile
 // Weights are held as f16 times 2^8, with 11 bits down to 2^-22 of the reference, and may exceed it by 2^7 before O is
 // rescaled (2^15 < 65504): a rescale costs a warp about as much as a tile.
 constexpr float P_SHIFT = 8, P_SLACK = 7;
+// Scores (in powers of two) from which on references are taken off the scores themselves, before exponents of values are
+// added: below, the sum of both is rounded by 2^-16 at most, and a product's rounding moves no weight past f16's range.
+constexpr float LARGE = 256;
 constexpr int stages(int nm) { return nm == 2 ? 4 : 6; }  // tiles of keys and of values in shared memory
 // Warps of a CTA: 4 for each stream's softmax, the converters, and 4 of which one issues the MMAs and one looks up page
 // scales: warpgroups, so that registers can be moved between them (a row's 64 scores and their weights stay in 128 or more).
@@ -145,13 +150,12 @@ __device__ __forceinline__ void tmem_ld64(uint32_t taddr, float (&v)[64]) {
       : "memory");
 }
 
-// Three words of this thread's lane, in four columns.
-__device__ __forceinline__ void tmem_st4(uint32_t taddr, float a, float b, float c) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %3};" ::"r"(taddr), "f"(a), "f"(b), "f"(c)
+// Four words of this thread's lane.
+__device__ __forceinline__ void tmem_st4(uint32_t taddr, float a, float b, float c, float d) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "f"(a), "f"(b), "f"(c), "f"(d)
                : "memory");
 }
-__device__ __forceinline__ void tmem_ld4(uint32_t taddr, float& a, float& b, float& c) {
-  [[maybe_unused]] float d;
+__device__ __forceinline__ void tmem_ld4(uint32_t taddr, float& a, float& b, float& c, float& d) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];\n\t"
       "tcgen05.wait::ld.sync.aligned;"
@@ -476,7 +480,8 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
     const uint32_t lanes = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t o_at = tmem + lanes + O_COL + x * TILE;
     const bool any_live = __any_sync(~0u, live);
-    float m = -INFINITY, M = -INFINITY, L = 0.f;
+    // the sum's reference is 2^m, O's 2^(r + d): r a score, d an exponent of values (-inf: O holds nothing yet)
+    float m = -INFINITY, r_o = 0.f, d_o = -INFINITY, L = 0.f;
     bool ok = true;
     // One tile: the row's scores become weights, over themselves in tensor memory. CUT: some row of the warp does not see
     // all of its tokens.
@@ -488,7 +493,7 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
       float v[TOK];
       __syncwarp();
       tmem_ld64(s_at, v);
-      float s_top = -INFINITY, u_top = -INFINITY, u_of[GROUPS];
+      float s_top = -INFINITY, u_top = -INFINITY, s_of[GROUPS];
       constexpr int W = TOK / GROUPS;  // columns of a group
 #pragma unroll
       for (int b = 0; b < GROUPS; ++b) {
@@ -503,43 +508,59 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
           t1 = bd::max3(t1, v[e + 2], v[e + 3]);
         }
         t = fmaxf(t, t1);
-        const float s2 = CUT && t == -INFINITY ? t : t * (coef * ks[b]);
-        s_top = fmaxf(s_top, s2);
-        u_of[b] = s2 + ve[b];
-        u_top = fmaxf(u_top, u_of[b]);
+        s_of[b] = CUT && t == -INFINITY ? t : __fmul_rn(t, coef * ks[b]);  // (as where the scores are large)
+        s_top = fmaxf(s_top, s_of[b]);
+        u_top = fmaxf(u_top, (s_of[b] - r_o) + ve[b]);
       }
       const float m_new = fmaxf(m, s_top);
       L *= m_new == m ? 1.f : bd::ex2_approx(m - m_new);
       m = m_new;
-      const bool grow = u_top > M + P_SLACK || (M == -INFINITY && u_top > M);
-      if (__any_sync(~0u, grow)) {
-        if (j > 0) {
-          // O's product of the tile before is done where the next tile's scores, issued behind it, are
-          if (!(j + 1 < mine ? wait(ctl->s_full[x][(j + 1) & 1], (j + 1) >> 1) : wait(ctl->o_before[x], 0))) return false;
-          bd::tc_fence_after();
-          const float f = grow ? bd::ex2_approx(M - u_top) : 1.f;
-          __syncwarp();  // tensor-memory accesses take the whole warp at once
-#pragma unroll 1
-          for (int c = 0; c < D / 32; ++c) {
-            float o[32];
-            bd::tmem_ld32(o_at + c * 32, o);
-            uint32_t y[32];
+      const float ms = m == -INFINITY ? 0.f : m;
+      const bool grow = u_top > d_o + P_SLACK || (d_o == -INFINITY && u_top > d_o);
+      bool large = fmaxf(fabsf(ms), fabsf(r_o)) >= LARGE;
+      if (__any_sync(~0u, grow || large)) {
+        const bool some_grow = __any_sync(~0u, grow);
+        large = __any_sync(~0u, large);
+        if (some_grow) {
+          float d_new = -INFINITY;
 #pragma unroll
-            for (int e = 0; e < 32; ++e) y[e] = __float_as_uint(o[e] * f);
-            bd::tmem_st32(o_at + c * 32, y);
+          for (int b = 0; b < GROUPS; ++b) d_new = fmaxf(d_new, (s_of[b] - m) + ve[b]);
+          if (j > 0) {
+            // O's product of the tile before is done where the next tile's scores, issued behind it, are
+            if (!(j + 1 < mine ? wait(ctl->s_full[x][(j + 1) & 1], (j + 1) >> 1) : wait(ctl->o_before[x], 0))) return false;
+            bd::tc_fence_after();
+            const float f = grow ? bd::ex2_approx((r_o - m) + (d_o - d_new)) : 1.f;
+            __syncwarp();  // tensor-memory accesses take the whole warp at once
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+              float o[32];
+              bd::tmem_ld32(o_at + c * 32, o);
+              uint32_t y[32];
+#pragma unroll
+              for (int e = 0; e < 32; ++e) y[e] = __float_as_uint(o[e] * f);
+              bd::tmem_st32(o_at + c * 32, y);
+            }
           }
+          r_o = grow ? m : r_o;
+          d_o = grow ? d_new : d_o;
         }
-        M = grow ? u_top : M;
+        if (large) {
+#pragma unroll
+          for (int b = 0; b < GROUPS; ++b)
+#pragma unroll
+            for (int col = b * W; col < b * W + W; ++col) v[col] = __fsub_rn(__fmul_rn(v[col], coef * ks[b]), r_o);
+        }
       }
       __syncwarp();
-      const float ms = m == -INFINITY ? 0.f : m, Ms = M == -INFINITY ? 0.f : M;
+      // references as the weights see them: of scores less r_o where those are large
+      const float rs = large ? 0.f : r_o, md = large ? ms - r_o : ms, d = d_o == -INFINITY ? 0.f : d_o;
       uint32_t p[16];
 #pragma unroll
       for (int b = 0; b < GROUPS; ++b) {
         // A group whose weights all go to zero in f16 (its page's values are so small) may still count in L: its weights are
         // then taken from L's reference, 2^60 below it, which is zero in f16 as well.
-        const bool faint = u_of[b] < Ms - 40.f;
-        const float f = coef * ks[b], ref = faint ? ms + 60.f : Ms - ve[b] - P_SHIFT;
+        const bool faint = (s_of[b] - r_o) + ve[b] < d - 40.f;
+        const float f = large ? 1.f : coef * ks[b], ref = faint ? md + 60.f : rs + (d - ve[b] - P_SHIFT);
         float2 sum[2] = {{0.f, 0.f}, {0.f, 0.f}};
 #pragma unroll
         for (int col = b * W; col < b * W + W; col += 2) {
@@ -554,7 +575,7 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
           if (col % 32 == 30) tmem_st16(s_at + col / 32 * 16, p);
         }
         sum[0] = bd::add2(sum[0], sum[1]);
-        L += (sum[0].x + sum[0].y) * bd::ex2_approx(ref - ms);
+        L += (sum[0].x + sum[0].y) * bd::ex2_approx(ref - md);
       }
       bd::tmem_st_wait();
       return true;
@@ -577,26 +598,26 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
     float f[2] = {0.f, 0.f};  // what O of this stream, and with NM = 1 of the other one, is multiplied by
     float lse2;
     if constexpr (NM == 2) {
-      const float ms = m == -INFINITY ? 0.f : m, Ms = M == -INFINITY ? 0.f : M;
-      f[0] = L == 0.f ? 0.f : bd::ex2_approx(Ms - P_SHIFT - ms) / L;
+      const float ms = m == -INFINITY ? 0.f : m;
+      f[0] = L == 0.f ? 0.f : bd::ex2_approx((r_o - ms) + (d_o - P_SHIFT)) / L;
       lse2 = L == 0.f ? -INFINITY : ms + log2f(L);
     } else {
-      // the streams tell each other m, M and L through tensor memory, over their last scores (shared memory is full)
+      // the streams tell each other m, L and O's reference through tensor memory, over their last scores (shared memory is full)
       __syncwarp();
       bd::tc_fence_after();
-      tmem_st4(tmem + lanes + x * TILE, m, M, L);
+      tmem_st4(tmem + lanes + x * TILE, m, L, r_o, d_o);
       bd::tmem_st_wait();
       bd::tc_fence_before();
       bd::mbar_arrive(bd::smem_u32(&ctl->joined));
       wait(ctl->joined, 0);  // both streams' sums, and both O
       bd::tc_fence_after();
-      float m2, M2, L2;
-      tmem_ld4(tmem + lanes + (x ^ 1) * TILE, m2, M2, L2);
+      float m2, L2, r2, d2;
+      tmem_ld4(tmem + lanes + (x ^ 1) * TILE, m2, L2, r2, d2);
       const float mt = fmaxf(m, m2), ms = mt == -INFINITY ? 0.f : mt;
       const float total = L * bd::ex2_approx(m - ms) + L2 * bd::ex2_approx(m2 - ms);
       if (total != 0.f) {
-        f[0] = bd::ex2_approx(M - P_SHIFT - ms) / total;  // (M is -inf where the stream's tiles hold nothing for the row)
-        f[1] = bd::ex2_approx(M2 - P_SHIFT - ms) / total;
+        f[0] = bd::ex2_approx((r_o - ms) + (d_o - P_SHIFT)) / total;  // (d is -inf where a stream's tiles hold nothing for the row)
+        f[1] = bd::ex2_approx((r2 - ms) + (d2 - P_SHIFT)) / total;
       }
       lse2 = total == 0.f ? -INFINITY : ms + log2f(total);
     }
