@@ -435,8 +435,8 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
     constexpr int LANES = D / 8, ROWS = 32 / LANES;
     const int my_c = lane % LANES, my_r = lane / LANES, warp_row = (warp & 3) * 32;
     if (n > 0) {
-      // Rows in f16, with the sign of the scale; bf16 ones times a power of two that brings the largest finite element of
-      // the warp's rows into [2^14, 2^15): elements down to 2^-32 of it keep their eight bits.
+      // Rows in f16, with the sign of the scale; bf16 ones times a power of two each that brings the row's largest element
+      // into [2^14, 2^15): elements down to 2^-32 of it keep their eight bits.
       const uint16_t* q = static_cast<const uint16_t*>(a.q) + static_cast<int64_t>(sq.q0 + i) * a.q_tok + h * a.q_head;
       uint4 w[32 / ROWS];
 #pragma unroll
@@ -445,28 +445,42 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
         const uint64_t src = __shfl_sync(~0u, reinterpret_cast<uint64_t>(q), rr);
         w[u] = ld_global_if(reinterpret_cast<const uint8_t*>(src) + my_c * 16, row - lane + rr < rows && my_c * 8 < a.dim);
       }
-      int shift = 0;
+      int shift = 0, held = 0;  // of the lane's row, and of row my_c * ROWS + my_r
       if (!a.f16) {
-        uint32_t most = 0;  // magnitudes' patterns, two to a word
+        static_assert(LANES == 32 / ROWS, "a lane ends up with the maximum of one row");
+        uint32_t most[LANES];  // magnitudes' patterns; halved and exchanged until the lane has row my_c * ROWS + my_r
 #pragma unroll
-        for (int u = 0; u < 32 / ROWS; ++u) {
+        for (int u = 0; u < LANES; ++u) {
           const uint32_t t = __vmaxu2(__vmaxu2(w[u].x & 0x7fff7fffu, w[u].y & 0x7fff7fffu),
                                       __vmaxu2(w[u].z & 0x7fff7fffu, w[u].w & 0x7fff7fffu));
-          if ((t & 0xffffu) < 0x7f80u && t < 0x7f800000u) most = __vmaxu2(most, t);
+          most[u] = max(t & 0xffffu, t >> 16);
         }
-        most = __reduce_max_sync(~0u, max(most & 0xffffu, most >> 16));
-        shift = row_shift(__uint_as_float(most << 16));
+        const auto exchange = [&](auto lanes) {
+          constexpr int HALF = decltype(lanes)::value;
+          const bool upper = my_c & HALF;
+#pragma unroll
+          for (int u = 0; u < HALF; ++u) {
+            const uint32_t other = __shfl_xor_sync(~0u, upper ? most[u] : most[u + HALF], HALF);
+            most[u] = max(upper ? most[u + HALF] : most[u], other);
+          }
+        };
+        if constexpr (LANES == 16) exchange(std::integral_constant<int, 8>());
+        exchange(std::integral_constant<int, 4>());
+        exchange(std::integral_constant<int, 2>());
+        exchange(std::integral_constant<int, 1>());
+        held = row_shift(__uint_as_float(most[0] << 16));
+        shift = __shfl_sync(~0u, held, lane % ROWS * LANES + lane / ROWS);
       }
-      const float f = a.coef < 0.f ? -pow2i(shift) : pow2i(shift);
       const uint32_t flip = a.coef < 0.f ? 0x80008000u : 0u;
 #pragma unroll
       for (int u = 0; u < 32 / ROWS; ++u) {
         const int rr = warp_row + u * ROWS + my_r;
+        const float f = pow2i(__shfl_sync(~0u, held, my_r * LANES + u));
         uint32_t y[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float2 g = Bf16::to_float2(y[e]);
-          y[e] = a.f16 ? y[e] ^ flip : f16x2(make_float2(g.x * f, g.y * f));
+          y[e] = (a.f16 ? y[e] : f16x2(make_float2(g.x * f, g.y * f))) ^ flip;
         }
         if (NM == 2 || x == 0)  // (both streams of NM = 1 read the rows: they need the shift)
           st_shared_v4(q_at + (NM == 2 ? x * Q_HALF : 0u) + (my_c / 8) * Q_ATOM + rr * 128 + (((my_c % 8) ^ (rr & 7)) << 4),

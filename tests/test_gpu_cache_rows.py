@@ -1,4 +1,5 @@
-"""Every row of kv_attention by its own measure: scores of any size, pages of very different scales. Bounds are those of test_gpu_cache.attention_bounds, but for weights that are too
+"""Every row of kv_attention by its own measure: scores of any size, rows of very different magnitude in one
+call, pages of very different scales. Bounds are those of test_gpu_cache.attention_bounds, but for weights that are too
 small for f16: they are held times 2^8 or more against a reference that is at most the largest weight of a token that
 the row itself sees, so each is off by at most 2^-33 of that (half a subnormal step, 2^-25, over 2^8)."""
 
@@ -77,6 +78,26 @@ def test_scores_of_any_size(k, q_len, page, dim, v_exp):
         assert sure.mean() > 0.9
     if k <= 10:
         assert_rows(c, q, starts, 1, 5000 if q_len == 70 else None)
+
+
+# rows of a key/value head: 4 and 32 (16-row tiles), 36 (one tile of 128), 280 (two to a CTA, under a long bound)
+@pytest.mark.parametrize("q_len", [1, 8, 9, 70])
+@pytest.mark.parametrize("k", [31, 36, 40, 90, -40, -90])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_a_row_far_above_or_below_its_neighbours(q_len, k, dim):
+    c = random_cache([q_len + 150, q_len + 33], 16, 2, dim, seed=21, extra_cols=330)
+    q, starts = queries([q_len] * 2, 8, dim, 5)
+    q[q_len // 2, 1] *= 2.0 ** k  # exact: whole powers of two
+    q[-1, 6] *= 2.0 ** k
+    assert_rows(c, q, starts, max_kv=5000 if q_len == 70 else None)
+
+
+@pytest.mark.parametrize("q_len", [8, 9, 70])
+def test_rows_of_all_magnitudes_in_one_call(q_len):
+    c = random_cache([q_len + 90], 32, 1, 80, seed=22, extra_cols=160)
+    q, starts = queries([q_len], 4, 80, 6)
+    q *= torch.exp2(torch.arange(q.shape[0] * 4) % 41 * 5.0 - 100).view(-1, 4, 1).to(q.dtype)
+    assert_rows(c, q, starts, max_kv=5000 if q_len == 70 else None)
 
 
 @pytest.mark.parametrize("q_len", [1, 8, 100, 150])
