@@ -153,12 +153,12 @@ int bdkv_write(const bdkv_cache* cache, const bdkv_rows* k, const bdkv_rows* v, 
  *       visible(i) = kv_len - q_len + min(q_len, (i / B + 1) * B);
  *     B = 1 is causal, B = the engine's block length its block-causal mask.
  * A query that sees no token (an empty cache, or kv_len < q_len) gives 0 and
- * lse -inf. Products of 16-bit by decoded 8-bit elements are exact (of bf16
- * queries: elements down to 2^-31 of their row's largest; smaller ones are off
- * by at most 2^-39 of it) and summed
- * in fp32; statistics are fp32; the softmax weights are rounded to f16, scaled
- * so that weights down to 2^-22 of a row's largest keep 11 bits (smaller ones
- * 2^-33 of it).
+ * lse -inf; one whose scores are all -inf (an infinity in q) gives NaN and lse
+ * -inf, as the formula does. Products of 16-bit by decoded 8-bit elements are
+ * exact (of bf16 queries: elements down to 2^-31 of their row's largest;
+ * smaller ones are off by at most 2^-39 of it) and summed in fp32; statistics
+ * are fp32; the softmax weights are rounded to f16, scaled so that weights down
+ * to 2^-22 of a row's largest keep 11 bits (smaller ones 2^-33 of it).
  *   max_q_len, max_kv_len  upper bounds of the q_len and kv_lens (a longer one
  *                   is cut there); max_kv_len <= max_blocks * page_size.
  *                   They size the launch: tight bounds launch less.

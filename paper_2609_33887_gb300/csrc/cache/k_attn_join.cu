@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(WARPS * 32) attn_join_kernel(AttnArgs a, int p
     }
   }
   if (!mine) return;
-  const float f = total == 0.f ? 0.f : 1.f / total;
+  const float f = 1.f / total;  // (0 * inf, NaN, where all scores of the row are -inf)
   const int64_t tok = static_cast<int64_t>(sq.q0) + i;
   const RowOut dst = {static_cast<uint16_t*>(a.out) + tok * a.o_tok + h * a.o_head, nullptr,
                       a.lse == nullptr ? nullptr : a.lse + tok * n_q + h};

@@ -341,15 +341,16 @@ __global__ void __launch_bounds__(WARPS * 32, 2) attn_rows_kernel(AttnArgs a) {
     for (int w = 0; w < WARPS; ++w) mt = fmaxf(mt, sm_m[w][r]);
     const float ms = mt == -INFINITY ? 0.f : mt;
     for (int w = 0; w < WARPS; ++w) Lt += sm_L[w][r] * bd::ex2_approx(sm_m[w][r] - ms);
-    const float inv = Lt == 0.f ? 0.f : 1.f / Lt;
+    const int i = row / a.group, see = visible(a, sq, i);
+    const RowOut dst = row_out(a, sq, seq, part, i, head * a.group + row - i * a.group, see);
+    // a row's whole result: 0 where it sees nothing, NaN where all of its scores are -inf (a part may well hold nothing)
+    const float inv = Lt != 0.f ? 1.f / Lt : dst.out != nullptr && see > 0 ? NAN : 0.f;
     float4 o = {0.f, 0.f, 0.f, 0.f};
     for (int w = 0; w < WARPS; ++w) {
       const float f = bd::ex2_approx((sm_r[w][r] - ms) + (sm_d[w][r] - P_SHIFT)) * inv;
       const float4 x = *reinterpret_cast<const float4*>(acc + (w * 16 + r) * LD + d);
       o.x += x.x * f, o.y += x.y * f, o.z += x.z * f, o.w += x.w * f;
     }
-    const int i = row / a.group;
-    const RowOut dst = row_out(a, sq, seq, part, i, head * a.group + row - i * a.group, visible(a, sq, i));
     if (d < a.dim) store4<T>(dst, d, o);
     if (d == 0) store_lse(dst, Lt == 0.f ? -INFINITY : ms + log2f(Lt));
   }

@@ -609,11 +609,15 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
     }
 
     if (mine > 0 && ok) ok = wait(ctl->o_done[x], 0);
-    float f[2] = {0.f, 0.f};  // what O of this stream, and with NM = 1 of the other one, is multiplied by
+    float f[2];  // what O of this stream, and with NM = 1 of the other one, is multiplied by
     float lse2;
+    RowOut o = {nullptr, nullptr, nullptr};
+    if (live) o = row_out(a, sq, seq, part, i, h, visible(a, sq, i));
+    // a row's whole result: 0 where it sees nothing, NaN where all of its scores are -inf (a part may well hold nothing)
+    const float none = o.out != nullptr && vis > 0 ? NAN : 0.f;
     if constexpr (NM == 2) {
       const float ms = m == -INFINITY ? 0.f : m;
-      f[0] = L == 0.f ? 0.f : bd::ex2_approx((r_o - ms) + (d_o - P_SHIFT)) / L;
+      f[0] = L == 0.f ? none : bd::ex2_approx((r_o - ms) + (d_o - P_SHIFT)) / L;
       lse2 = L == 0.f ? -INFINITY : ms + log2f(L);
     } else {
       // the streams tell each other m, L and O's reference through tensor memory, over their last scores (shared memory is full)
@@ -629,6 +633,7 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
       tmem_ld4(tmem + lanes + (x ^ 1) * TILE, m2, L2, r2, d2);
       const float mt = fmaxf(m, m2), ms = mt == -INFINITY ? 0.f : mt;
       const float total = L * bd::ex2_approx(m - ms) + L2 * bd::ex2_approx(m2 - ms);
+      f[0] = none, f[1] = 0.f;
       if (total != 0.f) {
         f[0] = bd::ex2_approx((r_o - ms) + (d_o - P_SHIFT)) / total;  // (d is -inf where a stream's tiles hold nothing for the row)
         f[1] = bd::ex2_approx((r2 - ms) + (d2 - P_SHIFT)) / total;
@@ -636,8 +641,6 @@ __global__ void __launch_bounds__(threads(NM), 1) attn_tiles_kernel(AttnArgs a) 
       lse2 = total == 0.f ? -INFINITY : ms + log2f(total);
     }
     bd::tc_fence_after();
-    RowOut o = {nullptr, nullptr, nullptr};
-    if (live) o = row_out(a, sq, seq, part, i, h, visible(a, sq, i));
     // Through shared memory that no product reads any more (the queries', for the odd stream of NM = 1 the keys'): lanes
     // write their rows, the warp stores them row by row. The streams of NM = 1 share the rows: each has half of the columns.
     const int c0 = NM == 2 ? 0 : x * (D / 64), c1 = NM == 2 ? D / 32 : c0 + D / 64;

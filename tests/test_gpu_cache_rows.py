@@ -1,7 +1,10 @@
-"""Every row of kv_attention by its own measure: scores of any size, rows of very different magnitude in one
-call, pages of very different scales. Bounds are those of test_gpu_cache.attention_bounds, but for weights that are too
-small for f16: they are held times 2^8 or more against a reference that is at most the largest weight of a token that
-the row itself sees, so each is off by at most 2^-33 of that (half a subnormal step, 2^-25, over 2^8)."""
+"""Every row of kv_attention by its own measure: scores of any size, rows of very different magnitude in one call,
+pages of very different scales, queries that are not finite. Bounds are those of test_gpu_cache.attention_bounds, but
+for weights that are too small for f16: they are held times 2^8 or more against a reference that is at most the largest
+weight of a token that the row itself sees, so each is off by at most 2^-33 of that (half a subnormal step, 2^-25, over
+2^8)."""
+
+import math
 
 import numpy as np
 import pytest
@@ -109,3 +112,23 @@ def test_pages_of_very_different_scales_by_each_rows_own(q_len, page, mask_block
     assert_rows(c, q, starts, mask_block)
     if q_len == 150:
         assert_rows(c, q, starts, mask_block, max_kv=5000)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("q_len", [1, 8, 9, 70])
+@pytest.mark.parametrize("total", [90, 2000])  # in one part, in several
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_queries_that_are_not_finite(bad, total, q_len, dtype):
+    """A softmax of scores that are all -inf, or hold +inf or NaN, is NaN, for that row alone."""
+    c = random_cache([total, total - 7], 16, 2, 64, seed=23)
+    c.k[c.k != 0x7F] &= 0x7F  # keys of one sign, none of them zero: scores of an infinity are infinities of one sign
+    c.k[c.k == 0] = 1
+    q, starts = queries([q_len] * 2, 8, 64, 8, dtype)
+    q[q_len // 2, 1, 5] = bad
+    got, lse = attention(c, q, starts, 0)
+    want = np.zeros(got.shape[:2], dtype=bool)
+    want[q_len // 2, 1] = True
+    assert np.array_equal(np.isnan(got), np.repeat(want[..., None], 64, 2))
+    assert np.all(np.isfinite(lse[~want]))
+    if bad == -math.inf:
+        assert lse[q_len // 2, 1] == -math.inf
