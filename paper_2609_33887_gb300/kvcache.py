@@ -131,7 +131,10 @@ def _table(t: torch.Tensor, n_seq: int) -> tuple:
     shape, strides = t.shape, t.stride()
     if t.dtype is not torch.int32 or len(shape) != 2 or shape[0] != n_seq or (shape[1] > 1 and strides[1] != 1):
         raise ValueError(f"block_table must be int32 [{n_seq}, blocks] with contiguous rows")
-    return t.data_ptr(), max(strides[0], shape[1]), shape[1]
+    if n_seq > 1 and strides[0] < shape[1]:
+        raise ValueError("the rows of block_table must not overlap (an expanded one: call contiguous() first)")
+    # (a single row's stride may be anything)
+    return t.data_ptr(), strides[0] if n_seq > 1 else max(strides[0], shape[1]), shape[1]
 
 
 def kv_tables(lens: torch.Tensor, new_tokens: torch.Tensor, block_table: torch.Tensor, free_pages: torch.Tensor,
