@@ -220,12 +220,12 @@ Plan make_plan(const bdkv_cache& c, const bdkv_attention_args& a, int sms) {
   return p;
 }
 
-// The library's own workspace of a device. Calls on different streams share it: each waits for the last one's end.
+// The library's own workspace of a device. All calls share it: each waits for the last one's end, also on what looks like
+// the same stream (a handle may be a destroyed stream's, or the per-thread default stream's of another thread).
 struct Workspace {
   void* data = nullptr;
   size_t bytes = 0;
   cudaEvent_t used = nullptr;
-  cudaStream_t stream = nullptr;
 };
 std::mutex g_mu;
 Workspace g_ws[64];
@@ -247,10 +247,9 @@ int own_workspace(size_t bytes, cudaStream_t st, Workspace** out) {
       return BD_ERR_CUDA;
     }
     w.bytes = bytes;
-  } else if (w.stream != st && cudaStreamWaitEvent(st, w.used) != cudaSuccess) {
+  } else if (cudaStreamWaitEvent(st, w.used) != cudaSuccess) {
     return BD_ERR_CUDA;
   }
-  w.stream = st;
   *out = &w;
   return BD_OK;
 }
