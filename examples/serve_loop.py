@@ -4,6 +4,7 @@ Every forward runs the committed blocks that are not in the cache yet and the wi
 (kv_tables, kv_write, kv_attention with the engine's block-causal mask), reads the LM head at the window's masked
 positions (commit_step), and moves the window on (commit_sweep). The window's own keys and values are written for the
 forward and given back after it; committed blocks are computed once more with their final tokens and stay ("one-step cache writes").
+A request whose table has no room for the next forward stands still from then on, with all that it has committed.
 Nothing waits for the GPU inside the loop.
 
     python examples/serve_loop.py [steps]
@@ -71,7 +72,7 @@ class Server:
         inside = o >= kept[s]
         token = torch.where(inside, self.tokens.view(self.n_seq, W)[s, (o - kept[s]).clamp(0, W - 1)],
                             self.blocks[s, o.clamp(0, W - 1)])
-        x = m.embed[token] + m.place[t.positions.clamp(min=0)]
+        x = m.embed[token] + m.place[t.positions.clamp(0, len(m.place) - 1)]
         qkv = (x @ m.qkv.T).view(most, -1, m.dim)
         q, k, v = qkv.split([m.n_q, m.n_kv, m.n_kv], 1)
         bdc.kv_write(k, v, t.slot_map, self.cache)
@@ -86,12 +87,16 @@ class Server:
         hidden = self.forward()
         tokens, _, commit, _ = bdc.commit_step(hidden, self.m.head, self.masked, self.flags, self.n_seq, self.B, self.L,
                                                self.tau)
+        # a request that got no pages was computed over the wrong tokens: its commits are dropped, its window stays
+        served = self.t.status == 0
+        commit = torch.where(served[:, None], commit.view(self.n_seq, self.W), 0).view(-1)
         blocks, done, resolved = bdc.commit_sweep(
             self.tokens, self.masked, self.flags, self.n_seq, self.B, self.L, tokens, commit, 0,
             mask_token_id=self.m.vocab, options=bdc.BD_SWEEP_ADMIT | bdc.BD_SWEEP_ELIGIBLE_OLDEST)
         # the window's pages go back; the blocks that this forward computed with their final tokens stay
-        self.lens = self.tables(self.t.kv_lens, torch.full_like(self.lens, -self.W), 0).kv_lens
-        self.blocks, self.pending = blocks.view(self.n_seq, self.W), done
+        self.lens = self.tables(self.t.kv_lens, torch.where(served, -self.W, 0).int(), 0).kv_lens
+        self.blocks = torch.where(served[:, None], blocks.view(self.n_seq, self.W), self.blocks)
+        self.pending = torch.where(served, done, self.pending)
         return done, resolved
 
 
