@@ -38,14 +38,14 @@ class Model:
 class Server:
     def __init__(self, model, n_seq=6, n_slots=3, block_len=16, page=32, max_len=768, tau=0.3):
         self.m, self.n_seq, self.B, self.L, self.page, self.tau = model, n_seq, n_slots, block_len, page, [tau]
-        self.W, self.max_len = n_slots * block_len, max_len
-        n_pages = n_seq * (-(-max_len // page))
+        self.W, self.max_len = n_slots * block_len, -(-max_len // page) * page  # as many tokens as its table's pages hold
+        n_pages = n_seq * (self.max_len // page)
         self.cache = bdc.kv_cache(n_pages, page, model.n_kv, model.dim)
 
         def ints(*shape, fill=0, dtype=torch.int32):
             return torch.full(shape, fill, dtype=dtype, device="cuda")
 
-        self.table = ints(n_seq, -(-max_len // page), fill=-1)
+        self.table = ints(n_seq, self.max_len // page, fill=-1)
         self.free = torch.randperm(n_pages, device="cuda").to(torch.int32)
         self.pool = torch.tensor([0, n_pages], dtype=torch.int64, device="cuda")
         self.lens = ints(n_seq)        # tokens that stay in the cache

@@ -68,3 +68,14 @@ def test_requests_that_fill_their_tables_lose_nothing(loop, max_len, page):
     assert stopped == 3  # all of them came to their tables' end, and stayed there
     assert int(server.lens.max()) <= server.table.shape[1] * page
     assert bdc.kvcache.kv_device_status() == 0 and bdc.bd_get_device_status() == 0
+
+
+def test_forwards_of_full_tables_see_all_of_their_tokens(loop):
+    """max_len need not be a whole number of pages: a table's last page may be filled all the same."""
+    server = loop.Server(loop.Model(), n_seq=1, n_slots=1, block_len=16, page=64, max_len=70)
+    most = 0
+    for _ in range(120):
+        server.step()
+        most = max(most, int(server.t.kv_lens.max()))
+    assert most > 70
+    assert server.max_len >= most
