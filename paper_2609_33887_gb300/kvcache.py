@@ -94,6 +94,17 @@ def _check(rc: int, where: str) -> None:
         raise BdError(rc, where)
 
 
+def _same_gpu(*tensors) -> None:
+    """The library is given addresses and launches on the current device, so all of them have to be there."""
+    device = tensors[0].get_device()  # -1: the host
+    same = device >= 0 and device == torch._C._cuda_getDevice()
+    for t in tensors:
+        if t.get_device() != device:
+            same = False
+    if not same:
+        raise ValueError("all tensors must be on the current GPU")
+
+
 def _cache_fields(c: KvCache) -> bytes:
     k, v, ks, vs = c
     n_pages, page_size, n_heads, dim = k.shape
@@ -157,6 +168,7 @@ def kv_tables(lens: torch.Tensor, new_tokens: torch.Tensor, block_table: torch.T
         _vector(new_tokens, i32, n_seq, "new_tokens"), table, _vector(free_pages, i32, None, "free_pages"),
         _vector(pool, i64, 2, "pool"), pool_out.data_ptr(), kv_lens.data_ptr(), query_start.data_ptr(),
         slot_map.data_ptr(), positions.data_ptr(), status.data_ptr())
+    _same_gpu(lens, new_tokens, block_table, free_pages, pool)
     rc = load_library().bdkv_tables(args, _stream_handle(stream))
     if rc != BD_OK:
         raise BdError(rc, "bdkv_tables")
@@ -170,8 +182,9 @@ def kv_write(k: torch.Tensor, v: torch.Tensor, slot_map: torch.Tensor, cache: Kv
     if k.shape != v.shape or k.shape[2:] != cache.k.shape[3:] or k.shape[1] != cache.k.shape[2] or k.shape[0] < n:
         raise ValueError("k and v must be [tokens, n_heads, head_dim] of the cache, a row for each slot")
     kf, vf = ROWS_FIELDS.pack(*_rows_fields(k, "k")), ROWS_FIELDS.pack(*_rows_fields(v, "v"))
-    _check(load_library().bdkv_write(_cache_fields(cache), kf, vf, _vector(slot_map, torch.int64, None, "slot_map"), n,
-                                     _stream_handle(stream)), "bdkv_write")
+    fields, slots = _cache_fields(cache), _vector(slot_map, torch.int64, None, "slot_map")
+    _same_gpu(k, v, slot_map, *cache)
+    _check(load_library().bdkv_write(fields, kf, vf, slots, n, _stream_handle(stream)), "bdkv_write")
 
 
 def _attn_fields(q, out, lse, cache, block_table, kv_lens, query_start, max_q_len, max_kv_len, scale, mask_block,
@@ -211,7 +224,9 @@ def kv_attention(q: torch.Tensor, cache: KvCache, block_table: torch.Tensor, kv_
     lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if return_lse else None
     args = _attn_fields(q, out, lse, cache, block_table, kv_lens, query_start, max_q_len, max_kv_len, scale, mask_block,
                         workspace, stream)
-    _check(load_library().bdkv_attention(_cache_fields(cache), args), "bdkv_attention")
+    fields = _cache_fields(cache)
+    _same_gpu(q, out, block_table, kv_lens, query_start, *cache, *(() if workspace is None else (workspace,)))
+    _check(load_library().bdkv_attention(fields, args), "bdkv_attention")
     return (out, lse) if return_lse else out
 
 

@@ -64,3 +64,14 @@ def test_tables_of_one_row_and_wide_ones_keep_their_stride(library, call):
         name, args = library.calls[-1]
         fields = K.TABLES_FIELDS.unpack(args[0]) if call is tables else K.ATTN_FIELDS.unpack(args[1])
         assert (fields[4] if call is tables else fields[10]) == stride
+
+
+def test_tensors_of_the_host_are_refused(monkeypatch):
+    lib = Library()
+    monkeypatch.setattr(K, "load_library", lambda: lib)
+    monkeypatch.setattr(K, "_stream_handle", lambda stream: stream or 0)
+    x = torch.zeros(4, 2, 32, dtype=torch.bfloat16)
+    for call in (attention, tables, lambda: K.kv_write(x, x, ints(4, dtype=torch.int64), K.kv_cache(5, 16, 2, 32, device="cpu"))):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
+    assert not lib.calls
