@@ -65,7 +65,9 @@ typedef struct {
 } bdkv_cache;
 
 /* Rows [token, head, head_dim], head_dim contiguous; strides in elements,
- * multiples of 8; pointer 16-byte aligned. */
+ * multiples of 8; pointer 16-byte aligned. Rows that are read may share memory
+ * (a stride of 0); rows that are written must not (BD_ERR_ARG where the
+ * strides show that they do). */
 typedef struct {
   void* data;
   int32_t dtype; /* bdkv_dtype */

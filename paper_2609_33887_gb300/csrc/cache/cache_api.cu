@@ -71,6 +71,15 @@ int check_rows(const bdkv_rows& r) {
   return aligned(r.data, 16) ? BD_OK : BD_ERR_ALIGN;
 }
 
+// Rows that are written must not lie on one another, as far as strides show it: the number of tokens is not known here,
+// so where a head's tokens lie closer than its heads, the heads' distance is not checked.
+int check_rows_apart(const bdkv_rows& r, int64_t heads, int64_t dim, bool many_tokens) {
+  if ((heads > 1 && r.stride_head < dim) || (many_tokens && r.stride_token < dim)) return BD_ERR_ARG;
+  if (heads > 1 && many_tokens && r.stride_token >= r.stride_head && r.stride_token < (heads - 1) * r.stride_head + dim)
+    return BD_ERR_ARG;
+  return BD_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -139,6 +148,7 @@ int check_attention(const bdkv_cache* cache, const bdkv_attention_args* args) {
     if (!aligned(a.kv_lens, 4) || !aligned(a.query_start, 4) || !aligned(a.block_table, 4) || !aligned(a.lse, 4) ||
         !aligned(a.workspace, 256))
       return BD_ERR_ALIGN;
+    return check_rows_apart(a.out, a.n_q_heads, c.head_dim, a.n_seq > 1 || a.max_q_len > 1);
   }
   return BD_OK;
 }

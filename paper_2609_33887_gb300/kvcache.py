@@ -132,6 +132,17 @@ def _rows_fields(x: torch.Tensor, name: str) -> tuple:
     return x.data_ptr(), dtype, strides[0], strides[1]
 
 
+def _out_fields(x: torch.Tensor) -> tuple:
+    """_rows_fields of rows that are written."""
+    data, dtype, token, head = _rows_fields(x, "out")
+    tokens, heads, dim = x.shape
+    if tokens <= 1:
+        token = heads * head + dim  # a single token's stride says nothing
+    elif heads > 1 and head > token and head < (tokens - 1) * token + dim:  # (else the library sees it)
+        raise ValueError("the rows of out must not overlap")
+    return data, dtype, token, head
+
+
 def _vector(t: torch.Tensor, dtype, n: Optional[int], name: str) -> int:
     if t.dtype is not dtype or not t.is_contiguous() or (n is not None and t.numel() != n):
         raise ValueError(f"{name} must be a contiguous {dtype} tensor" + ("" if n is None else f" of {n}"))
@@ -195,7 +206,7 @@ def _attn_fields(q, out, lse, cache, block_table, kv_lens, query_start, max_q_le
     table, stride, cols = _table(block_table, n_seq)
     ws, ws_bytes = (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
     return ATTN_FIELDS.pack(
-        *_rows_fields(q, "q"), *_rows_fields(out, "out"), 0 if lse is None else lse.data_ptr(), table, stride, cols,
+        *_rows_fields(q, "q"), *out, 0 if lse is None else lse.data_ptr(), table, stride, cols,
         _vector(kv_lens, torch.int32, n_seq, "kv_lens"), _vector(query_start, torch.int32, n_seq + 1, "query_start"),
         n_seq, q.shape[1], max_q_len, max_kv_len, mask_block,
         q.shape[2] ** -0.5 if scale is None else scale, ws, ws_bytes, _stream_handle(stream) or 0)
@@ -203,7 +214,8 @@ def _attn_fields(q, out, lse, cache, block_table, kv_lens, query_start, max_q_le
 
 def kv_attention_workspace(q, cache, block_table, kv_lens, query_start, *, max_q_len, max_kv_len, mask_block=1) -> int:
     """Bytes of workspace kv_attention needs for these arguments."""
-    args = _attn_fields(q, q, None, cache, block_table, kv_lens, query_start, max_q_len, max_kv_len, None, mask_block,
+    out = (q.data_ptr(), _DT.get(q.dtype), q.shape[1] * q.shape[2], q.shape[2])
+    args = _attn_fields(q, out, None, cache, block_table, kv_lens, query_start, max_q_len, max_kv_len, None, mask_block,
                         None, 0)
     return int(load_library().bdkv_attention_workspace(_cache_fields(cache), args))
 
@@ -222,7 +234,7 @@ def kv_attention(q: torch.Tensor, cache: KvCache, block_table: torch.Tensor, kv_
     elif out.shape != q.shape or out.dtype != q.dtype:
         raise ValueError("out must have q's shape and type")
     lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if return_lse else None
-    args = _attn_fields(q, out, lse, cache, block_table, kv_lens, query_start, max_q_len, max_kv_len, scale, mask_block,
+    args = _attn_fields(q, _out_fields(out), lse, cache, block_table, kv_lens, query_start, max_q_len, max_kv_len, scale, mask_block,
                         workspace, stream)
     fields = _cache_fields(cache)
     _same_gpu(q, out, block_table, kv_lens, query_start, *cache, *(() if workspace is None else (workspace,)))

@@ -1,10 +1,14 @@
 """The checks of kvcache.py on the tensors that it turns into pointers, without a GPU: the library is replaced by a
 record of the calls that reach it, so a call that should be refused and is not is seen and nothing runs."""
 
+import os
+import shutil
+
 import pytest
 import torch
 
 from paper_2609_33887_gb300 import kvcache as K
+from paper_2609_33887_gb300.bdcommit import BD_ERR_ARG, BD_OK, BdError
 
 
 class Library:
@@ -75,3 +79,74 @@ def test_tensors_of_the_host_are_refused(monkeypatch):
         with pytest.raises(ValueError, match="GPU"):
             call()
     assert not lib.calls
+
+
+# ------------------------------------------------------- rows on top of each other --
+@pytest.fixture(scope="module")
+def checks():
+    """The library itself: its argument checks come before any CUDA call."""
+    if shutil.which("nvcc") is None and not os.path.exists("/usr/local/cuda/bin/nvcc"):
+        pytest.skip("no CUDA toolkit")
+    import __graft_entry__
+
+    __graft_entry__.build()
+    return K.load_library()
+
+
+FAKE = 1 << 20  # a non-null, aligned address that is never dereferenced
+
+
+def cache_fields(**kw):
+    f = dict(n_pages=4, page=16, heads=2, dim=32, k=(1024, 64, 32), v=(1024, 64, 32), ks=2, vs=2)
+    f.update(kw)
+    return K.CACHE_FIELDS.pack(FAKE, FAKE, FAKE, FAKE, f["n_pages"], f["page"], f["heads"], f["dim"], *f["k"], *f["v"],
+                               f["ks"], f["vs"])
+
+
+def attn_fields(token, head, n_q=4, n_seq=2, max_q=3):
+    return K.ATTN_FIELDS.pack(FAKE, K.BDKV_BF16, 0, 0, FAKE, K.BDKV_BF16, token, head, 0, FAKE, 8, 8, FAKE, FAKE, n_seq, n_q,
+                              max_q, 100, 1, 0.5, 0, 0, 0)
+
+
+OVERLAP = [dict(token=0, head=32), dict(token=128, head=0), dict(token=128, head=16), dict(token=120, head=32),
+           dict(token=32, head=32), dict(token=16, head=400), dict(token=0, head=0, n_seq=1, max_q=1)]
+APART = [dict(token=128, head=32), dict(token=32, head=96), dict(token=200, head=48), dict(token=0, head=32, n_seq=1, max_q=1)]
+
+
+@pytest.mark.parametrize("kw", OVERLAP, ids=str)
+def test_outputs_on_top_of_each_other_are_refused(checks, kw):
+    assert checks.bdkv_attention(cache_fields(), attn_fields(**kw)) == BD_ERR_ARG
+
+
+@pytest.mark.parametrize("kw", APART, ids=str)
+def test_outputs_apart_in_any_order_are_not(checks, kw):
+    if torch.cuda.is_available():
+        pytest.skip("the call would run")
+    assert checks.bdkv_attention(cache_fields(), attn_fields(**kw)) not in (BD_ERR_ARG, BD_OK)  # no device
+
+
+def test_the_binding_refuses_an_out_whose_rows_overlap(library, checks, monkeypatch):
+    x = torch.zeros(4, 4, 32, dtype=torch.bfloat16)
+    base = torch.zeros(4000, dtype=torch.bfloat16)
+    good = [x, x.transpose(0, 1).contiguous().transpose(0, 1), base.as_strided((4, 4, 32), (48, 192, 1))]
+    for out in good:
+        attention(out=out)
+    assert len(library.calls) == len(good)
+    attention(q=x[:1], out=base.as_strided((1, 4, 32), (0, 32, 1)))  # one token: its stride says nothing
+    assert K.ATTN_FIELDS.unpack(library.calls[-1][1][1])[6] >= 4 * 32
+    with pytest.raises(ValueError, match="overlap"):
+        attention(out=base.as_strided((4, 4, 32), (32, 96, 1)))
+    monkeypatch.setattr(K, "load_library", lambda: checks)
+    for out in (x[:1].expand(4, 4, 32), x[:, :1].expand(4, 4, 32)):
+        with pytest.raises(BdError) as e:
+            attention(out=out)
+        assert e.value.status == BD_ERR_ARG
+
+
+def test_queries_may_share_memory(library):
+    """Queries are only read: also where the workspace's size is asked for, which takes no outputs."""
+    q = torch.zeros(1, 4, 32, dtype=torch.bfloat16).expand(4, 4, 32)
+    args = (q, K.kv_cache(5, 16, 2, 32, device="cpu"), ints(4, 3), ints(4), ints(5))
+    K.kv_attention_workspace(*args, max_q_len=1, max_kv_len=48)
+    fields = K.ATTN_FIELDS.unpack(library.calls[-1][1][1])
+    assert fields[2] == 0 and fields[6:8] == (128, 32)
