@@ -40,7 +40,10 @@ typedef enum {
  *   k, v            E4M3 codes (OCP "fn"); element (page, token, head, i) of k
  *                   is k[page * k_stride[0] + token * k_stride[1] +
  *                   head * k_stride[2] + i], of v alike. Pointers 16-byte
- *                   aligned, strides non-negative multiples of 16.
+ *                   aligned, strides non-negative multiples of 16. A cache that
+ *                   is only read may share memory between pages, tokens or
+ *                   heads (a stride of 0); bdkv_write refuses it (BD_ERR_ARG),
+ *                   and scales of pages that share memory.
  *   k_scale, v_scale  one E8M0 byte e for each page and head, at
  *                   [page * stride + head]: the element's value is
  *                   code * 2^(e - 127). A power of two decodes exactly, and a

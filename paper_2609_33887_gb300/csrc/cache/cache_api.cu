@@ -5,6 +5,7 @@
 #include <climits>
 #include <cmath>
 #include <mutex>
+#include <utility>
 
 #include "cache.h"
 #include "trace.h"
@@ -71,6 +72,22 @@ int check_rows(const bdkv_rows& r) {
   return aligned(r.data, 16) ? BD_OK : BD_ERR_ALIGN;
 }
 
+// A cache that is written: its codes, and its scales, must not lie on one another. (Keys and values may be the same
+// memory, if a user stores the same in both.)
+int check_cache_apart(const bdkv_cache& c) {
+  for (const int64_t* s : {c.k_stride, c.v_stride}) {
+    std::pair<int64_t, int64_t> d[3] = {{s[0], c.n_pages}, {s[1], c.page_size}, {s[2], c.n_heads}};  // stride, extent
+    std::sort(d, d + 3);
+    __int128 span = c.head_dim;  // of what the smaller strides reach
+    for (const auto& [stride, extent] : d) {
+      if (extent <= 1) continue;
+      if (stride < span) return BD_ERR_ARG;
+      span += static_cast<__int128>(stride) * (extent - 1);
+    }
+  }
+  return c.n_pages > 1 && std::min(c.k_scale_stride, c.v_scale_stride) < c.n_heads ? BD_ERR_ARG : BD_OK;
+}
+
 // Rows that are written must not lie on one another, as far as strides show it: the number of tokens is not known here,
 // so where a head's tokens lie closer than its heads, the heads' distance is not checked.
 int check_rows_apart(const bdkv_rows& r, int64_t heads, int64_t dim, bool many_tokens) {
@@ -113,6 +130,7 @@ int bdkv_write(const bdkv_cache* cache, const bdkv_rows* k, const bdkv_rows* v, 
   if (int rc = check_rows(*k)) return rc;
   if (int rc = check_rows(*v)) return rc;
   if (k->dtype != v->dtype) return BD_ERR_DTYPE;
+  if (int rc = check_cache_apart(*cache)) return rc;
   if (n_tokens < 0 || n_tokens > INT_MAX) return BD_ERR_SHAPE;
   if (n_tokens == 0) return BD_OK;
   if (!k->data || !v->data || !slot_map) return BD_ERR_NULL;

@@ -150,3 +150,28 @@ def test_queries_may_share_memory(library):
     K.kv_attention_workspace(*args, max_q_len=1, max_kv_len=48)
     fields = K.ATTN_FIELDS.unpack(library.calls[-1][1][1])
     assert fields[2] == 0 and fields[6:8] == (128, 32)
+
+
+@pytest.mark.parametrize("kw", [dict(k=(0, 64, 32)), dict(v=(1024, 0, 32)), dict(k=(1024, 64, 0)), dict(k=(1024, 64, 16)),
+                                dict(v=(1024, 32, 32)), dict(k=(1008, 64, 32)), dict(v=(1024, 32, 496)), dict(ks=1),
+                                dict(vs=0), dict(n_pages=2 ** 31 - 1, v=(2 ** 40, 2 ** 40, 2 ** 40))], ids=str)
+def test_writes_into_shared_memory_are_refused(checks, kw):
+    rows = K.ROWS_FIELDS.pack(FAKE, K.BDKV_BF16, 64, 32)
+    assert checks.bdkv_write(cache_fields(**kw), rows, rows, FAKE, 3, None) == BD_ERR_ARG
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(k=(1024, 32, 512)), dict(v=(2048, 128, 64)), dict(k=(64, 256, 32)),
+                                dict(n_pages=1, k=(0, 64, 32), ks=0), dict(heads=1, v=(1024, 64, 0)),
+                                dict(n_pages=2 ** 31 - 1, v=(2 ** 40, 64, 32))], ids=str)
+def test_writes_into_any_layout_are_not(checks, kw):
+    if torch.cuda.is_available():
+        pytest.skip("the call would run")
+    rows = K.ROWS_FIELDS.pack(FAKE, K.BDKV_BF16, 64, 32)
+    assert checks.bdkv_write(cache_fields(**kw), rows, rows, FAKE, 3, None) not in (BD_ERR_ARG, BD_OK)  # no device
+
+
+def test_attention_reads_a_cache_that_shares_memory(checks):
+    if torch.cuda.is_available():
+        pytest.skip("the call would run")
+    for kw in (dict(k=(1024, 64, 0)), dict(v=(0, 64, 32)), dict(ks=0)):
+        assert checks.bdkv_attention(cache_fields(**kw), attn_fields(128, 32)) not in (BD_ERR_ARG, BD_OK)
