@@ -173,7 +173,8 @@ int bdkv_write(const bdkv_cache* cache, const bdkv_rows* k, const bdkv_rows* v, 
  *                   (not inside graph capture). One workspace must not be used
  *                   by calls that can run at the same time.
  * Limits: n_q_heads a multiple of n_heads, at most 64 times it; n_seq at most
- * 65535. Rows of `out` past query_start[n_seq] are left alone. */
+ * 65535; max_kv_len at most 2^30. Rows of `out` past query_start[n_seq] are
+ * left alone. */
 typedef struct {
   bdkv_rows q;
   bdkv_rows out; /* dtype = q.dtype */

@@ -43,6 +43,7 @@ bool aligned(const void* p, uintptr_t a) { return reinterpret_cast<uintptr_t>(p)
 bool page_size_ok(int p) { return p == 16 || p == 32 || p == 64 || p == 128 || p == 256; }
 
 constexpr int64_t MAX_STRIDE = int64_t(1) << 40;
+constexpr int MAX_KV = 1 << 30;  // the kernels count a part's end, and tokens a few tiles behind it, in 32 bits
 
 int check_strides(const int64_t* s, int n, int64_t multiple) {
   for (int i = 0; i < n; ++i) {
@@ -154,7 +155,7 @@ int check_attention(const bdkv_cache* cache, const bdkv_attention_args* args) {
   if (int rc = check_rows(a.out)) return rc;
   if (a.out.dtype != a.q.dtype) return BD_ERR_DTYPE;
   if (a.n_seq < 0 || a.n_seq > 65535 || a.n_q_heads < 1 || a.n_q_heads % c.n_heads != 0 ||
-      a.n_q_heads / c.n_heads > 64 || a.max_q_len < 0 || a.max_kv_len < 0 || a.max_blocks < 0 ||
+      a.n_q_heads / c.n_heads > 64 || a.max_q_len < 0 || a.max_kv_len < 0 || a.max_kv_len > MAX_KV || a.max_blocks < 0 ||
       a.table_stride < a.max_blocks || a.table_stride > MAX_STRIDE ||
       a.max_kv_len > int64_t(a.max_blocks) * c.page_size ||
       int64_t(a.max_q_len) * (a.n_q_heads / c.n_heads) > (1 << 26))

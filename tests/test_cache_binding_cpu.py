@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from paper_2609_33887_gb300 import kvcache as K
-from paper_2609_33887_gb300.bdcommit import BD_ERR_ARG, BD_OK, BdError
+from paper_2609_33887_gb300.bdcommit import BD_ERR_ARG, BD_ERR_SHAPE, BD_OK, BdError
 
 
 class Library:
@@ -175,3 +175,19 @@ def test_attention_reads_a_cache_that_shares_memory(checks):
         pytest.skip("the call would run")
     for kw in (dict(k=(1024, 64, 0)), dict(v=(0, 64, 32)), dict(ks=0)):
         assert checks.bdkv_attention(cache_fields(**kw), attn_fields(128, 32)) not in (BD_ERR_ARG, BD_OK)
+
+
+# --------------------------------------------------------------- very long caches --
+def test_lengths_that_32_bits_do_not_count_are_refused(checks):
+    """A part's last token is begin + chunk, and its kernels look a few tiles further: past 2^31 those sums turn negative,
+    which passes for a token inside the cache."""
+    def call(max_kv):
+        fields = list(K.ATTN_FIELDS.unpack(attn_fields(128, 32)))
+        fields[10:12] = 2 ** 27, 2 ** 27  # the table's stride and columns: 2^31 tokens
+        fields[17] = max_kv
+        return checks.bdkv_attention(cache_fields(), K.ATTN_FIELDS.pack(*fields))
+
+    for max_kv in (2 ** 30 + 1, 2 ** 31 - 200, 2 ** 31 - 1):
+        assert call(max_kv) == BD_ERR_SHAPE
+    if not torch.cuda.is_available():
+        assert call(2 ** 30) not in (BD_ERR_SHAPE, BD_OK)  # no device
