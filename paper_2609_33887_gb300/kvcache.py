@@ -159,6 +159,23 @@ def _table(t: torch.Tensor, n_seq: int) -> tuple:
     return t.data_ptr(), strides[0] if n_seq > 1 else max(strides[0], shape[1]), shape[1]
 
 
+def _allocate_on(stream, allocate):
+    """The tensors of allocate(), for a call on `stream` (None: the current one). Memory comes from that stream's pool: of
+    the current one's it could still be in use there. The current stream is noted as a reader, for when it is freed."""
+    if stream is None:
+        return allocate()
+    reader = torch.cuda.current_stream()
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream)
+    if stream == reader:
+        return allocate()
+    with torch.cuda.stream(stream):
+        tensors = allocate()
+    for t in tensors:
+        t.record_stream(reader)
+    return tensors
+
+
 def kv_tables(lens: torch.Tensor, new_tokens: torch.Tensor, block_table: torch.Tensor, free_pages: torch.Tensor,
               pool: torch.Tensor, *, page_size: int, max_tokens: int, stream=None) -> KvTables:
     """Pages, slots and positions for the tokens each request adds (or, where negative, gives back).
@@ -167,12 +184,9 @@ def kv_tables(lens: torch.Tensor, new_tokens: torch.Tensor, block_table: torch.T
     place; pool int64 [2] is the ring's (head, tail), not written. max_tokens: entries of slot_map and positions, at
     least the tokens added (entries behind them are -1)."""
     n_seq, i32, i64 = lens.numel(), torch.int32, torch.int64
-    kv_lens = lens.new_empty(n_seq)
-    query_start = lens.new_empty(n_seq + 1)
-    slot_map = pool.new_empty(max_tokens)
-    positions = lens.new_empty(max_tokens)
-    status = lens.new_empty(n_seq)
-    pool_out = pool.new_empty(2)
+    kv_lens, query_start, slot_map, positions, status, pool_out = _allocate_on(stream, lambda: (
+        lens.new_empty(n_seq), lens.new_empty(n_seq + 1), pool.new_empty(max_tokens), lens.new_empty(max_tokens),
+        lens.new_empty(n_seq), pool.new_empty(2)))
     table, stride, cols = _table(block_table, n_seq)
     args = TABLES_FIELDS.pack(
         n_seq, page_size, cols, max_tokens, stride, free_pages.numel(), _vector(lens, i32, n_seq, "lens"),
@@ -230,12 +244,13 @@ def kv_attention(q: torch.Tensor, cache: KvCache, block_table: torch.Tensor, kv_
     mask_block: 0 = no mask, 1 = causal, B = causal by blocks of B queries (a window of block slots). scale defaults to
     head_dim^-0.5. Returns out (q's shape and type), or (out, lse float32 [tokens, n_q_heads])."""
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        out, = _allocate_on(stream, lambda: (torch.empty_like(q, memory_format=torch.contiguous_format),))
     elif out.shape != q.shape or out.dtype != q.dtype:
         raise ValueError("out must have q's shape and type")
-    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if return_lse else None
-    args = _attn_fields(q, _out_fields(out), lse, cache, block_table, kv_lens, query_start, max_q_len, max_kv_len, scale, mask_block,
-                        workspace, stream)
+    lse, = _allocate_on(stream, lambda: (torch.empty(q.shape[:2], dtype=torch.float32, device=q.device),)) \
+        if return_lse else (None,)
+    args = _attn_fields(q, _out_fields(out), lse, cache, block_table, kv_lens, query_start, max_q_len, max_kv_len, scale,
+                        mask_block, workspace, stream)
     fields = _cache_fields(cache)
     _same_gpu(q, out, block_table, kv_lens, query_start, *cache, *(() if workspace is None else (workspace,)))
     _check(load_library().bdkv_attention(fields, args), "bdkv_attention")

@@ -98,3 +98,50 @@ def test_threads_on_their_own_default_streams_share_the_workspace():
     assert not failed
     for (_, _, ref, _), out in zip(cases, outs):
         assert all(torch.equal(o, ref) for o in out)
+
+
+# ------------------------------------------------------------------ outputs of a call on another stream --
+@pytest.mark.parametrize("handle", [False, True], ids=["stream", "handle"])
+def test_outputs_of_a_call_on_another_stream_are_that_streams_memory(handle):
+    """Memory that the current stream has freed may still be in use there: a call on another stream must not get it."""
+    args, bounds, ref, _ = case(80, 20, 4, 700)
+    _, ref_lse = bdc.kv_attention(*args, **bounds, return_lse=True)
+    other = torch.cuda.Stream()
+    stream = other.cuda_stream if handle else other
+    torch.cuda.synchronize()
+    freed = [torch.zeros_like(ref) for _ in range(8)] + [torch.zeros_like(ref_lse) for _ in range(8)]
+    blocks = {t.data_ptr() for t in freed}
+    del freed
+    kept = []
+    for _ in range(4):
+        out, lse = bdc.kv_attention(*args, **bounds, return_lse=True, stream=stream)
+        assert not {out.data_ptr(), lse.data_ptr()} & blocks
+        kept.append((out, lse))
+    other.synchronize()
+    for out, lse in kept:
+        assert torch.equal(out, ref) and torch.equal(lse, ref_lse)
+    # and what such a call returned goes back to its own stream's memory
+    ptrs = {out.data_ptr() for out, _ in kept}
+    del kept, out, lse
+    assert not {torch.empty_like(ref).data_ptr() for _ in range(8)} & ptrs
+
+
+def test_tables_of_a_call_on_another_stream_are_that_streams_memory():
+    lens = torch.tensor([5, 40, 0], dtype=torch.int32, device="cuda")
+    new = torch.tensor([3, 20, 9], dtype=torch.int32, device="cuda")
+    ring = torch.arange(40, dtype=torch.int32, device="cuda")
+    pool = torch.tensor([10, 40], dtype=torch.int64, device="cuda")
+    table = torch.arange(30, dtype=torch.int32, device="cuda").view(3, 10) % 10
+    n = 1000
+    kw = dict(page_size=16, max_tokens=n)
+    ref = bdc.kv_tables(lens, new, table.clone(), ring.clone(), pool, **kw)
+    other, mine, his = torch.cuda.Stream(), table.clone(), ring.clone()
+    torch.cuda.synchronize()
+    freed = [torch.zeros(n, dtype=d, device="cuda") for d in (torch.int64, torch.int32) for _ in range(8)]
+    blocks = {t.data_ptr() for t in freed}
+    del freed
+    got = bdc.kv_tables(lens, new, mine, his, pool, **kw, stream=other)
+    assert not {t.data_ptr() for t in got} & blocks
+    other.synchronize()
+    for a, b in zip(got, ref):
+        assert torch.equal(a, b)
