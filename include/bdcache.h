@@ -139,7 +139,13 @@ int bdkv_tables(const bdkv_tables_args* args, void* stream);
  *     is the larger of the page's and the run's own, and where it grows those
  *     tokens' codes are scaled by the (power of two) ratio, to the nearest
  *     code, ties to even.
- *   Tokens of the page behind the run hold nothing afterwards.
+ *   Tokens of the page behind the run hold nothing afterwards. What they and
+ *   tokens before them have done to the page's scale stays: a window that is
+ *   written and taken back leaves a page that is not begun afresh with the
+ *   largest scale it has needed. With E4M3's four bits an element is then off
+ *   by at most 2^-4 of it and 2^-9 * 2^(e - 127), e the page's scale: only
+ *   elements below 2^-13 of the largest that the page has held are coarser
+ *   than 2^-4.
  *   - code = e4m3(x * 2^(127 - e)), to nearest, ties to even.
  *   - A token with an infinity or NaN in its key or value of a head is stored,
  *     for that head, as a key of NaN codes and a value of zeros, and does not

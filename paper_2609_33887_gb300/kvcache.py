@@ -202,7 +202,8 @@ def kv_tables(lens: torch.Tensor, new_tokens: torch.Tensor, block_table: torch.T
 
 def kv_write(k: torch.Tensor, v: torch.Tensor, slot_map: torch.Tensor, cache: KvCache, *, stream=None) -> None:
     """Quantise keys and values [tokens, n_heads, head_dim] into the cache at slot_map int64 [tokens] (negative: not
-    stored). The rows of a page must be consecutive, as kv_tables lays them out."""
+    stored). The rows of a page must be consecutive, as kv_tables lays them out. A page keeps the largest scale that its
+    tokens have needed since it was begun, also of tokens taken back."""
     n = slot_map.numel()
     if k.shape != v.shape or k.shape[2:] != cache.k.shape[3:] or k.shape[1] != cache.k.shape[2] or k.shape[0] < n:
         raise ValueError("k and v must be [tokens, n_heads, head_dim] of the cache, a row for each slot")
