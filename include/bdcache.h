@@ -49,7 +49,9 @@ typedef enum {
  *                   code * 2^(e - 127). A power of two decodes exactly, and a
  *                   page whose scale grows is scaled again without a second
  *                   rounding (but for codes that become subnormal). bdkv_write
- *                   stores e in 27..247; the attention takes 27..227.
+ *                   stores e in 27..247; the attention takes 27..227, and
+ *                   values that are not NaN (bdkv_write stores none: one in a
+ *                   token may reach queries of the call that do not see it).
  *   page_size       16, 32, 64, 128 or 256
  *   head_dim        a multiple of 16, 16..128 */
 typedef struct {
@@ -92,6 +94,11 @@ typedef struct {
  * pool_in is not written, so a call repeated on the same inputs gives the same
  * outputs. The ring must have room for every page of the cache.
  *
+ * A request that is not served adds nothing, but its added tokens count in
+ * query_start all the same (so that rows keep their places): what an attention
+ * computes for those rows, whose tokens are not in the cache, means nothing and
+ * must not be used.
+ *
  * status[s]: 0 = served; 1 = too few free pages (the request, and every later
  * one that needs a page, keeps its length); 2 = it would need more than
  * max_blocks pages (it keeps its length and takes no page).
@@ -102,7 +109,8 @@ typedef struct {
  *   positions[i]    its position in the request; -1 behind the last
  *   block_table     entries of pages taken are written, others left alone
  * slot_map and positions have max_tokens entries, all written; tokens past
- * them are not (their pages are taken all the same).
+ * them are not (their pages are taken all the same). query_start counts them: an
+ * attention of such a forward needs rows for all of them.
  * Limits: n_seq 0..8192; page_size as in bdkv_cache; sums of lengths below 2^31. */
 typedef struct {
   int32_t n_seq;
@@ -159,6 +167,8 @@ int bdkv_write(const bdkv_cache* cache, const bdkv_rows* k, const bdkv_rows* v, 
  * reads key/value head h / (n_q_heads / n_heads):
  *     out = sum_t softmax_t(scale * q . k_t) v_t    over t < visible(i)
  *     lse = ln sum_t exp(scale * q . k_t)           (optional)
+ * query_start is ascending, from 0 or more, and q, out and lse have at least
+ * query_start[n_seq] rows (it is on the device: nothing checks it).
  *   mask_block 0: visible(i) = kv_len
  *   mask_block B >= 1: causal by blocks of B queries,
  *       visible(i) = kv_len - q_len + min(q_len, (i / B + 1) * B);

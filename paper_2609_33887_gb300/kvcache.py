@@ -182,7 +182,8 @@ def kv_tables(lens: torch.Tensor, new_tokens: torch.Tensor, block_table: torch.T
 
     lens, new_tokens int32 [n_seq]; block_table int32 [n_seq, max_blocks] and free_pages int32 [ring] are updated in
     place; pool int64 [2] is the ring's (head, tail), not written. max_tokens: entries of slot_map and positions, at
-    least the tokens added (entries behind them are -1)."""
+    least the tokens added (entries behind them are -1). A request whose status is not 0 keeps its length; query_start
+    has rows for its tokens all the same, whose attention means nothing."""
     n_seq, i32, i64 = lens.numel(), torch.int32, torch.int64
     kv_lens, query_start, slot_map, positions, status, pool_out = _allocate_on(stream, lambda: (
         lens.new_empty(n_seq), lens.new_empty(n_seq + 1), pool.new_empty(max_tokens), lens.new_empty(max_tokens),
@@ -241,7 +242,8 @@ def kv_attention(q: torch.Tensor, cache: KvCache, block_table: torch.Tensor, kv_
                  stream=None):
     """Attention of q [tokens, n_q_heads, head_dim] over the cached tokens of each request.
 
-    Request s holds queries query_start[s] .. query_start[s + 1], the last of its kv_lens[s] cached tokens.
+    Request s holds queries query_start[s] .. query_start[s + 1], the last of its kv_lens[s] cached tokens; q has at
+    least query_start[-1] rows, and rows of the result behind those are not written.
     mask_block: 0 = no mask, 1 = causal, B = causal by blocks of B queries (a window of block slots). scale defaults to
     head_dim^-0.5. Returns out (q's shape and type), or (out, lse float32 [tokens, n_q_heads])."""
     if out is None:
