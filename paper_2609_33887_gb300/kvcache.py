@@ -219,6 +219,8 @@ def _attn_fields(q, out, lse, cache, block_table, kv_lens, query_start, max_q_le
     n_seq = kv_lens.numel()
     if q.shape[2:] != cache.k.shape[3:]:
         raise ValueError("q must be [tokens, n_q_heads, head_dim] of the cache")
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
     table, stride, cols = _table(block_table, n_seq)
     ws, ws_bytes = (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
     return ATTN_FIELDS.pack(

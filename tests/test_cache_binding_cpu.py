@@ -191,3 +191,15 @@ def test_lengths_that_32_bits_do_not_count_are_refused(checks):
         assert call(max_kv) == BD_ERR_SHAPE
     if not torch.cuda.is_available():
         assert call(2 ** 30) not in (BD_ERR_SHAPE, BD_OK)  # no device
+
+
+def test_a_workspace_has_to_be_one_piece(library):
+    """Its bytes are counted from its elements: an expanded tensor has more of them than memory."""
+    whole = torch.zeros(4096, dtype=torch.uint8)
+    attention(workspace=whole)
+    fields = K.ATTN_FIELDS.unpack(library.calls[-1][1][1])
+    assert fields[20:22] == (whole.data_ptr(), 4096)
+    for ws in (whole[:1].expand(4096), whole[::2], whole.view(64, 64)[:, :32]):
+        with pytest.raises(ValueError, match="workspace"):
+            attention(workspace=ws)
+    assert len(library.calls) == 1
