@@ -205,17 +205,20 @@ struct Plan {
 };
 
 // The kernel: up to 32 rows per key/value head (queries times the group) are one or two tiles of the row kernel (64
-// requests of 300 to 4001 tokens: 20 rows 56 us, 64 in the tile kernel; 32 rows 56 and 62; 48 rows 82 and 66).
+// requests of 300 to 4001 tokens, 4 heads: 20 rows 56 us, 60 in the tile kernel; 28 rows 56 and 61; 32 rows 57 and 51; 48
+// rows 86 and 61. 8 requests, 8 heads: 32 rows 28 and 30).
 // Two tiles of 128 rows to a CTA read the cache once for both; one where that still runs in one wave and the
-// caches are too short to fill the device by a split (8 x 512 rows over 200 to 1400 tokens 23 us, 31 with two; 32 x 256
-// rows, two waves, 129 and 82; 2 x 256 rows over 20000 to 30000 tokens 108 and 76).
+// caches are too short to fill the device by a split (4 heads, 8 x 512 rows over 200 to 1400 tokens 21 us, 29 with two; 8
+// heads, two waves of 32 x 256 rows over 700 to 4096 111 and 82; 2 x 256 rows over 20000 to 30000 84 and 71).
 // The split along the cache. The host does not know how the lengths differ: one or two requests are split into one wave of
 // CTAs (two to an SM for the row kernel, one for the other), more requests into finer parts, which even out. Row kernel:
-// two caches of 131071 tokens 49 us in one wave, 68 in four; 16 requests of 57 to 60000 tokens 192 us in parts for 2 CTAs
-// per SM, 161 for 3, 207 for 4. Tile kernel, parts of 2048 tokens or more (a part costs its rows' fp32 results): 2 x 64
-// queries over 20000 to 30000 tokens 72 us in one wave, 92 in three; 8 x 9 queries over 300 to 30001 tokens 151 and 127.
-// More CTAs than run at once take the requests longest first: 64 requests x 35 rows over 300 to 4001 tokens 92 us in the
-// requests' order and 65 so; 512 CTAs of equal lengths, where the order is for nothing, 232 and 234.
+// two caches of 131071 tokens 48 us in one wave, 69 in four; 16 requests of 57 to 60000 tokens 193 us in parts for 2 CTAs
+// per SM, 159 for 3, 197 for 4. Tile kernel, parts of 2048 tokens or more (a part costs its rows' fp32 results): 2 x 64
+// queries over 20000 to 30000 tokens 45 us in one wave, 61 in three; 8 x 9 queries over 300 to 30001 tokens 99 and 73.
+// The parts follow the call's bound, not the lengths: one request of 1531 tokens takes 7.0 us under its own length, 14.1
+// under a bound of 131072.
+// More CTAs than run at once take the requests longest first: 64 requests x 35 rows over 300 to 4001 tokens 83 us in the
+// requests' order and 60 so; 512 CTAs of equal lengths, where the order is for nothing, 261 and 262.
 Plan make_plan(const bdkv_cache& c, const bdkv_attention_args& a, int sms) {
   Plan p = {};
   const int64_t rows = int64_t(a.max_q_len) * (a.n_q_heads / c.n_heads);

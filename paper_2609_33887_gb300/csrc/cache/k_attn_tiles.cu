@@ -4,8 +4,9 @@
 // A CTA walks a request's key/value head (whose cache is read once for all of
 // the group's heads) in tiles of 64 tokens, with two streams of products:
 //   NM = 2   256 rows (queries x heads): each half of them sees every tile
-//   NM = 1   up to 128 rows: one stream takes the even tiles, one the odd ones,
-//            and the two results are joined at the end
+//   NM = 1   128 rows (all that there are, or where one tile of rows to a CTA
+//            runs in one wave over short caches): one stream takes the even
+//            tiles, one the odd ones, and the two results are joined at the end
 // and with warps for each part of the work:
 //   converter warps   codes from global memory to f16 (exact), into shared
 //                     memory in the 128-byte swizzle, in stages; a request's
@@ -23,11 +24,13 @@
 // O's in two parts, a score and an exponent, so that scores of any size leave
 // the exponent its bits.
 //
-// 32 windows of 512 queries, 32 heads on 8, over 700 to 4096 tokens take 507 us:
-// 1150 TFLOP/s, 0.61 of a library product's rate. Bound by the softmax warps'
+// 32 windows of 512 queries, 32 heads on 8, over 700 to 4096 tokens take 513 us:
+// 1140 TFLOP/s, 0.60 of a library product's rate. Bound by the softmax warps'
 // chain from scores to weights (about 1600 cycles a tile of 2 x 128 x 64 scores,
 // 1080 of them under products), and by each CTA's start and end (a fifth of it),
-// during which nothing is multiplied.
+// during which nothing is multiplied. Few rows (64 x 5 drafts on 4 heads, 61 us,
+// 2.4 TB/s) are bound by latency: DRAM 28% busy, the tensor pipe 23%, issue slots
+// 37%, with two tiles of codes of a CTA on their way.
 #include "cache.h"
 
 namespace bdkv {
@@ -44,8 +47,8 @@ constexpr float LARGE = 256;
 constexpr int stages(int nm) { return nm == 2 ? 4 : 6; }  // tiles of keys and of values in shared memory
 // Warps of a CTA: 4 for each stream's softmax, the converters, and 4 of which one issues the MMAs and one looks up page
 // scales: warpgroups, so that registers can be moved between them (a row's 64 scores and their weights stay in 128 or more).
-// 256 rows leave few issue slots, and four converter warps disturb their softmax least (32 windows of 8 x 64 tokens 524 us,
-// 540 with eight): 512 threads start with 128 registers, 256 x 144 + 128 x 112 + 128 x 56 <= 65536. Few rows wait for the
+// 256 rows leave few issue slots, and four converter warps disturb their softmax least (32 windows of 8 x 64 tokens, when it
+// was chosen: 524 us, 540 with eight): 512 threads start with 128 registers, 256 x 144 + 128 x 112 + 128 x 56 <= 65536. Few rows wait for the
 // codes: eight converter warps, 640 threads with 96, 256 x 128 + 256 x 80 + 128 x 56 <= 61440.
 constexpr int conv_warps(int nm) { return nm == 2 ? 4 : 8; }
 constexpr int threads(int nm) { return (8 + conv_warps(nm) + 4) * 32; }

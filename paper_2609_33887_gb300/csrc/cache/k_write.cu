@@ -9,7 +9,7 @@
 // slots alone: row r0 + t does if its slot is the first one's plus t. Bound by
 // the bytes moved; few registers (one tensor's pointers to a thread) keep four
 // CTAs' loads on their way on an SM. 131072 tokens of 8 heads of 128 take 157 us,
-// 5.1 TB/s (0.76 of a copy); 64 tokens 6.6 us, latency.
+// 5.1 TB/s (0.76 of a copy); 64 tokens 5.4 us (replayed from a graph), latency.
 #include "cache.h"
 
 namespace bdkv {
