@@ -166,7 +166,7 @@ def _allocate_on(stream, allocate):
         return allocate()
     reader = torch.cuda.current_stream()
     if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(stream)
+        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()  # (0 would be a new one)
     if stream == reader:
         return allocate()
     with torch.cuda.stream(stream):

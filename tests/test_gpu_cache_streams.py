@@ -145,3 +145,15 @@ def test_tables_of_a_call_on_another_stream_are_that_streams_memory():
     other.synchronize()
     for a, b in zip(got, ref):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("current", ["default", "other"])
+def test_outputs_of_a_call_on_handle_0_are_the_default_streams_memory(current):
+    args, bounds, ref, _ = case(81, 20, 4, 700)
+    with torch.cuda.stream(torch.cuda.default_stream() if current == "default" else torch.cuda.Stream()):
+        torch.cuda.synchronize()
+        out = bdc.kv_attention(*args, **bounds, stream=0)
+    torch.cuda.synchronize()
+    home = [seg["stream"] for seg in torch.cuda.memory_snapshot()
+            if seg["address"] <= out.data_ptr() < seg["address"] + seg["total_size"]]
+    assert home == [0] and torch.equal(out, ref)
