@@ -1,7 +1,8 @@
-"""Build libbdcommit.so and libbdcache.so in-tree with nvcc for sm_103a.
+"""Build libbdcommit.so, libbdcache.so and libbdrotary.so in-tree with nvcc for sm_103a.
 
-libbdcommit.so holds the sources of csrc/, libbdcache.so those of csrc/cache/;
-each exports the C ABI of its headers under include/ only.
+libbdcommit.so holds the sources of csrc/, libbdcache.so those of csrc/cache/,
+libbdrotary.so those of csrc/rotary/; each exports the C ABI of its headers
+under include/ only.
 Each translation unit (CUDA .cu, host-only C++ .cpp) is compiled in
 parallel, then linked into its shared library (static CUDA runtime, no
 link-time dependency on libcuda: the tensor-map encoder is fetched through the
@@ -27,6 +28,8 @@ LIB = os.path.join(PKG, "libbdcommit.so")
 LIB_CHECKS = os.path.join(PKG, "libbdcommit_checks.so")
 CSRC_CACHE = os.path.join(CSRC, "cache")
 LIB_CACHE = os.path.join(PKG, "libbdcache.so")
+CSRC_ROTARY = os.path.join(CSRC, "rotary")
+LIB_ROTARY = os.path.join(PKG, "libbdrotary.so")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ARCH + [
@@ -50,7 +53,7 @@ def _stamp(nvcc: str, extra, src_dir=CSRC) -> str:
     h = hashlib.sha256()
     h.update(" ".join([nvcc] + NVCC_FLAGS + list(extra)).encode())
     files = _sources(src_dir) + sorted(
-        os.path.join(d, f) for d in {CSRC, src_dir} for f in os.listdir(d) if f.endswith((".cuh", ".h"))
+        os.path.join(d, f) for d in (CSRC, CSRC_CACHE, CSRC_ROTARY) for f in os.listdir(d) if f.endswith((".cuh", ".h"))
     ) + sorted(os.path.join(INCLUDE, f) for f in os.listdir(INCLUDE) if f.endswith(".h"))
     for f in files:
         h.update(f.encode())
@@ -60,18 +63,20 @@ def _stamp(nvcc: str, extra, src_dir=CSRC) -> str:
 
 
 def build(verbose: bool = False, force: bool = False, extra_flags=(), checks: bool = False) -> str:
-    """Compile every source and link libbdcommit.so and libbdcache.so; returns the path of libbdcommit.so.
+    """Compile every source and link the libraries; returns the path of libbdcommit.so.
 
     checks=True builds the bounds-checked variant instead (-DBD_CHECKS:
     device-side index checks that set a status bit rather than access out of
     range) as libbdcommit_checks.so, in its own build directory
-    (libbdcache.so has no such variant: it checks the page numbers it is given in every build)."""
+    (the other libraries have no such variant: they check the page numbers they are given in every build)."""
     extra_flags = list(extra_flags)
     if checks:
         return _build_one(CSRC, BUILD + "_checks", LIB_CHECKS, "bd_*", verbose, force, extra_flags + ["-DBD_CHECKS"])
-    with ThreadPoolExecutor(max_workers=2) as ex:
+    with ThreadPoolExecutor(max_workers=3) as ex:
         libs = [ex.submit(_build_one, CSRC, BUILD, LIB, "bd_*", verbose, force, extra_flags),
                 ex.submit(_build_one, CSRC_CACHE, os.path.join(BUILD, "cache"), LIB_CACHE, "bdkv_*", verbose, force,
+                          extra_flags),
+                ex.submit(_build_one, CSRC_ROTARY, os.path.join(BUILD, "rotary"), LIB_ROTARY, "bdrot_*", verbose, force,
                           extra_flags)]
         return [f.result() for f in libs][0]
 

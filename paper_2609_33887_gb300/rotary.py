@@ -1,0 +1,287 @@
+"""ctypes binding of libbdrotary (include/bdrotary.h): rotary positions on the way into the caches, and the latent cache.
+
+Argument marshalling only, as in kvcache.py, whose conventions hold here. There is no fallback: without the shared library
+every call raises.
+"""
+
+from __future__ import annotations
+
+import ctypes
+import math
+import os
+import struct
+from ctypes import c_int, c_int32, c_int64, c_size_t, c_void_p
+from fractions import Fraction
+from typing import NamedTuple, Optional
+
+import torch
+
+from .bdcommit import _stream_handle
+from .kvcache import (_DT, ROWS_FIELDS, KvCache, _allocate_on, _cache_fields, _check, _out_fields, _rows_fields, _same_gpu,
+                      _table, _vector)
+
+_PKG = os.path.dirname(os.path.abspath(__file__))
+LIB_PATH = os.path.join(_PKG, "libbdrotary.so")
+
+# bdrot_rotary, bdrot_latent, bdrot_latent_attention_args as laid out in include/bdrotary.h
+ROTARY_FIELDS = struct.Struct("Piid")
+LATENT_FIELDS = struct.Struct("PPiiqiiqqqq")
+LATENT_ATTN_FIELDS = struct.Struct("Pi4xqqPi4xqqPPqi4xPPiiiiifPNP")
+
+_TURN = 2 * Fraction(3141592653589793238462643383279502884197, 10 ** 39)  # 2 pi
+
+_lib = None
+
+
+def load_library() -> ctypes.CDLL:
+    """Load libbdrotary.so (built in-tree by paper_2609_33887_gb300/build.py)."""
+    global _lib
+    if _lib is None:
+        if not os.path.exists(LIB_PATH):
+            raise RuntimeError(f"libbdrotary.so not found at {LIB_PATH}: build it first "
+                               "(python -c 'import __graft_entry__ as g; g.build()')")
+        lib = ctypes.CDLL(LIB_PATH)
+        p = c_void_p
+        for name, res, args in (
+                ("bdrot_rotate", c_int, [p, p, p, c_int32, c_int32, p, c_int64, c_int32, p]),
+                ("bdrot_write", c_int, [p, p, p, p, p, p, c_int64, p, p, c_int32, p]),
+                ("bdrot_latent_write", c_int, [p, p, p, p, p, p, c_int64, p]),
+                ("bdrot_latent_attention", c_int, [p, p]),
+                ("bdrot_latent_attention_workspace", c_size_t, [p, p]),
+                ("bdrot_get_device_status", c_int, [p]),
+                ("bdrot_shutdown", c_int, [])):
+            fn = getattr(lib, name)
+            fn.restype, fn.argtypes = res, args
+        _lib = lib
+    return _lib
+
+
+class KvRotary(NamedTuple):
+    """A rotation by positions, as kv_rotary makes it. turns: int64 [dim / 2], the angle a position of each pair as a
+    fraction of a turn, times 2^64 (modulo 2^64); scale: what cosines and sines are multiplied by; interleaved: pairs are
+    elements 2p and 2p + 1, else p and p + dim / 2, of a row's first dim elements."""
+
+    turns: torch.Tensor
+    scale: float = 1.0
+    interleaved: bool = False
+
+
+class KvLatent(NamedTuple):
+    """The latent cache of one layer. latent: bfloat16 or float16 [n_pages, page_size, latent_dim], rope: [n_pages,
+    page_size, rope_dim] of the same type, each in any strides with its last dimension contiguous (multiples of 8)."""
+
+    latent: torch.Tensor
+    rope: torch.Tensor
+
+
+def kv_rotary(dim: int, *, base: float = 10000.0, frequencies=None, factor: float = 1.0, original_len: Optional[int] = None,
+              slow: float = 1.0, fast: float = 32.0, scale: float = 1.0, interleaved: bool = False,
+              device="cuda") -> KvRotary:
+    """The rotation of a row's first `dim` elements (a multiple of 16) with frequencies base^(-2p / dim), or the given
+    ones (radians a position, dim / 2 of them).
+
+    factor: contexts stretched by it. Without original_len all frequencies are divided by it. With original_len (the
+    length that the model was trained on) only those that turn at most `slow` times in it; those that turn `fast` times or
+    more are kept, and in between the two are blended linearly. scale: what the rotated elements are multiplied by, 1 or
+    the amplitude that goes with the stretch."""
+    if dim < 16 or dim % 16:
+        raise ValueError("dim must be a positive multiple of 16")
+    if frequencies is None:
+        f = [float(base) ** (-2.0 * p / dim) for p in range(dim // 2)]
+    else:
+        f = [float(x) for x in (frequencies.tolist() if isinstance(frequencies, torch.Tensor) else frequencies)]
+        if len(f) != dim // 2:
+            raise ValueError(f"frequencies must be {dim // 2} numbers")
+    if not (factor > 0 and math.isfinite(factor) and all(map(math.isfinite, f))):
+        raise ValueError("factor must be positive, frequencies finite")
+    if original_len is None:
+        f = [x / factor for x in f]
+    else:
+        if not 0 <= slow < fast:
+            raise ValueError("slow must be below fast")
+        kept = [min(max((original_len * abs(x) / (2 * math.pi) - slow) / (fast - slow), 0.0), 1.0) for x in f]
+        f = [x * k + x / factor * (1 - k) for x, k in zip(f, kept)]
+    turns = [round(Fraction(x) / _TURN * (1 << 64)) % (1 << 64) for x in f]
+    turns = torch.tensor([t - (1 << 64) if t >> 63 else t for t in turns], dtype=torch.int64, device=device)
+    return KvRotary(turns, float(scale), bool(interleaved))
+
+
+def kv_latent_cache(n_pages: int, page_size: int, latent_dim: int, rope_dim: int, *, dtype=torch.bfloat16,
+                    device="cuda") -> KvLatent:
+    """An empty latent cache in the layout that reads fastest: a token's latent and key part next to each other."""
+    rows = torch.zeros(n_pages, page_size, latent_dim + rope_dim, dtype=dtype, device=device)
+    return KvLatent(*rows.split([latent_dim, rope_dim], 2))
+
+
+def _rotary_fields(r: KvRotary) -> bytes:
+    turns, scale, interleaved = r
+    return ROTARY_FIELDS.pack(_vector(turns, torch.int64, None, "turns"), 2 * turns.numel(), bool(interleaved), scale)
+
+
+def _latent_fields(c: KvLatent) -> bytes:
+    latent, rope = c
+    n_pages, page_size, dim = latent.shape
+    if rope.dim() != 3 or rope.shape[:2] != latent.shape[:2] or rope.dtype != latent.dtype or latent.dtype not in _DT:
+        raise ValueError("latent and rope must be bfloat16 or float16, [n_pages, page_size, latent_dim] and "
+                         "[n_pages, page_size, rope_dim]")
+    lp, lt, l1 = latent.stride()
+    rp, rt, r1 = rope.stride()
+    if l1 != 1 or r1 != 1:
+        raise ValueError("the last dimension of latent and rope must be contiguous")
+    return LATENT_FIELDS.pack(latent.data_ptr(), rope.data_ptr(), _DT[latent.dtype], page_size, n_pages, dim,
+                              rope.shape[2], lp, lt, rp, rt)
+
+
+def _turned_fields(x, out, name):
+    """Rows and where they go turned. The stride of a single token says nothing."""
+    if out.shape != x.shape or out.dtype != x.dtype:
+        raise ValueError(f"out must have {name}'s shape and type")
+    if x.shape[0] == 0 and x.dtype in _DT:  # (nor do any strides where there is none)
+        return ROWS_FIELDS.pack(0, _DT[x.dtype], 0, 0), ROWS_FIELDS.pack(0, _DT[x.dtype], 0, 0)
+    data, dtype, token, head = _rows_fields(x, name)
+    if x.shape[0] <= 1:
+        token = 0
+    o_data, _, o_token, o_head = _rows_fields(out, "out")
+    if x.shape[0] <= 1:
+        o_token = 0
+    if x.shape[1] <= 1:
+        head = o_head = 0
+    return ROWS_FIELDS.pack(data, dtype, token, head), ROWS_FIELDS.pack(o_data, dtype, o_token, o_head)
+
+
+def _like(x, stream):
+    out, = _allocate_on(stream, lambda: (torch.empty_like(x, memory_format=torch.contiguous_format),))
+    return out
+
+
+def kv_rotate(x: torch.Tensor, positions: torch.Tensor, rotary: KvRotary, *, inverse: bool = False,
+              out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """x [tokens, heads, head_dim] with the first elements of each head turned by positions int32 [tokens].
+
+    inverse: turned back, with the same scale (the adjoint: gradients of the result to gradients of x). out may be x; to
+    turn the last elements of a head, pass x[..., first:] for both. Returns out."""
+    if x.dim() != 3:
+        raise ValueError("x must be [tokens, heads, head_dim] with head_dim contiguous")
+    if out is None:
+        out = _like(x, stream)
+    fields, (xf, of) = _rotary_fields(rotary), _turned_fields(x, out, "x")
+    n, heads, dim = x.shape
+    pos = _vector(positions, torch.int32, n, "positions")
+    _same_gpu(x, positions, rotary.turns, out)
+    _check(load_library().bdrot_rotate(fields, xf, of, heads, dim, pos, n, bool(inverse), _stream_handle(stream)),
+           "bdrot_rotate")
+    return out
+
+
+def kv_write_rotated(k: torch.Tensor, v: torch.Tensor, slot_map: torch.Tensor, cache: KvCache, positions: torch.Tensor,
+                     rotary: KvRotary, *, q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                     stream=None) -> Optional[torch.Tensor]:
+    """kv_write of keys turned by positions int32 (a position for each slot), and queries turned in the same call.
+
+    The cache gets the codes and scales of kv_write(kv_rotate(k), v). q: [tokens, n_q_heads, head_dim], a row for each
+    slot; q_out may be q. Returns the turned queries (None without q)."""
+    n = slot_map.numel()
+    if k.shape != v.shape or k.shape[2:] != cache.k.shape[3:] or k.shape[1] != cache.k.shape[2] or k.shape[0] < n:
+        raise ValueError("k and v must be [tokens, n_heads, head_dim] of the cache, a row for each slot")
+    kf, vf = ROWS_FIELDS.pack(*_rows_fields(k, "k")), ROWS_FIELDS.pack(*_rows_fields(v, "v"))
+    qf = of = None
+    tensors = ()
+    if q is not None:
+        if q.dim() != 3 or q.shape[0] != n or q.shape[2] != k.shape[2]:
+            raise ValueError("q must be [tokens, n_q_heads, head_dim] of the cache, a row for each slot")
+        if q_out is None:
+            q_out = _like(q, stream)
+        qf, of = _turned_fields(q, q_out, "q")
+        tensors = (q, q_out)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    fields, slots = _cache_fields(cache), _vector(slot_map, torch.int64, None, "slot_map")
+    pos, rf = _vector(positions, torch.int32, n, "positions"), _rotary_fields(rotary)
+    _same_gpu(k, v, slot_map, positions, rotary.turns, *cache, *tensors)
+    _check(load_library().bdrot_write(rf, fields, kf, vf, slots, pos, n, qf, of, 0 if q is None else q.shape[1],
+                                      _stream_handle(stream)), "bdrot_write")
+    return q_out
+
+
+def _vectors_fields(x, dim, n, cache, name):
+    if x.dim() != 2 or x.shape[0] < n or x.shape[1] != dim or (x.shape[0] and x.stride(1) != 1) or x.dtype != cache.latent.dtype:
+        raise ValueError(f"{name} must be [tokens, {dim}] of the cache's type, a contiguous row for each slot")
+    return ROWS_FIELDS.pack(x.data_ptr(), _DT[x.dtype], x.stride(0) if x.shape[0] > 1 else 0, 0)
+
+
+def kv_latent_write(latent: torch.Tensor, rope: torch.Tensor, slot_map: torch.Tensor, cache: KvLatent, *,
+                    positions: Optional[torch.Tensor] = None, rotary: Optional[KvRotary] = None, stream=None) -> None:
+    """Latents [tokens, latent_dim] and key parts [tokens, rope_dim] into the cache at slot_map int64 [tokens] (negative:
+    not stored; no slot twice). With rotary (of rope_dim elements), key parts are turned by positions int32 [tokens].
+    Without it they are stored as they are."""
+    n = slot_map.numel()
+    fields = _latent_fields(cache)
+    lf = _vectors_fields(latent, cache.latent.shape[2], n, cache, "latent")
+    rf = _vectors_fields(rope, cache.rope.shape[2], n, cache, "rope")
+    slots, turn, pos, tensors = _vector(slot_map, torch.int64, None, "slot_map"), None, None, ()
+    if (positions is None) != (rotary is None):
+        raise ValueError("positions and rotary go together")
+    if rotary is not None:
+        turn, pos = _rotary_fields(rotary), _vector(positions, torch.int32, n, "positions")
+        tensors = (positions, rotary.turns)
+    _same_gpu(latent, rope, slot_map, *cache, *tensors)
+    _check(load_library().bdrot_latent_write(turn, fields, lf, rf, slots, pos, n, _stream_handle(stream)),
+           "bdrot_latent_write")
+
+
+def _latent_attn_fields(q, out, lse, cache, block_table, kv_lens, query_start, max_q_len, max_kv_len, scale, mask_block,
+                        workspace, stream) -> bytes:
+    n_seq = kv_lens.numel()
+    if q.dim() != 3 or q.shape[2] != cache.latent.shape[2] + cache.rope.shape[2] or q.dtype != cache.latent.dtype:
+        raise ValueError("q must be [tokens, heads, latent_dim + rope_dim] of the cache's type")
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    table, stride, cols = _table(block_table, n_seq)
+    ws, ws_bytes = (0, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    return LATENT_ATTN_FIELDS.pack(
+        *_rows_fields(q, "q"), *out, 0 if lse is None else lse.data_ptr(), table, stride, cols,
+        _vector(kv_lens, torch.int32, n_seq, "kv_lens"), _vector(query_start, torch.int32, n_seq + 1, "query_start"),
+        n_seq, q.shape[1], max_q_len, max_kv_len, mask_block, scale, ws, ws_bytes, _stream_handle(stream) or 0)
+
+
+def kv_latent_attention_workspace(q, cache, block_table, kv_lens, query_start, *, max_q_len, max_kv_len) -> int:
+    """Bytes of workspace kv_latent_attention needs for these arguments."""
+    dim = cache.latent.shape[2]
+    out = (q.data_ptr(), _DT.get(q.dtype), q.shape[1] * dim, dim)
+    args = _latent_attn_fields(q, out, None, cache, block_table, kv_lens, query_start, max_q_len, max_kv_len, 1.0, 0, None,
+                               0)
+    return int(load_library().bdrot_latent_attention_workspace(_latent_fields(cache), args))
+
+
+def kv_latent_attention(q: torch.Tensor, cache: KvLatent, block_table: torch.Tensor, kv_lens: torch.Tensor,
+                        query_start: torch.Tensor, *, scale: float, max_q_len: int, max_kv_len: int, mask_block: int = 1,
+                        return_lse: bool = False, out: Optional[torch.Tensor] = None, workspace=None, stream=None):
+    """Attention of q [tokens, heads, latent_dim + rope_dim] over the cached latents of each request: every head's keys
+    are the cached latents and key parts, its values the latents.
+
+    Requests, masks, bounds, workspace and rows behind the last query are as in kv_attention. scale has no default: it is
+    the one of the heads before their projection into the latent's space. Returns out [tokens, heads, latent_dim] of q's
+    type, or (out, lse float32 [tokens, heads])."""
+    shape = (*q.shape[:2], cache.latent.shape[2])
+    if out is None:
+        out, = _allocate_on(stream, lambda: (torch.empty(shape, dtype=q.dtype, device=q.device),))
+    elif out.shape != shape or out.dtype != q.dtype:
+        raise ValueError("out must be [tokens, heads, latent_dim] of q's type")
+    lse, = _allocate_on(stream, lambda: (torch.empty(q.shape[:2], dtype=torch.float32, device=q.device),)) \
+        if return_lse else (None,)
+    _same_gpu(q, out, block_table, kv_lens, query_start, *cache, *(() if workspace is None else (workspace,)))
+    args = _latent_attn_fields(q, _out_fields(out), lse, cache, block_table, kv_lens, query_start, max_q_len, max_kv_len,
+                               scale, mask_block, workspace, stream)
+    fields = _latent_fields(cache)
+    _check(load_library().bdrot_latent_attention(fields, args), "bdrot_latent_attention")
+    return (out, lse) if return_lse else out
+
+
+def kv_latent_device_status(stream=None) -> int:
+    """Synchronise `stream`, then read and clear the library's device status (BD_OK, or BD_ERR_TIMEOUT)."""
+    return int(load_library().bdrot_get_device_status(_stream_handle(stream)))
+
+
+def kv_latent_shutdown() -> int:
+    """Free the library-owned workspaces."""
+    return int(load_library().bdrot_shutdown())
