@@ -1,17 +1,22 @@
-// bdrot_latent_attention: tcgen05 products of 64 rows (queries x heads) with
-// tiles of 128 cached tokens, the tokens along the instruction's 128 rows.
+// bdrot_latent_attention: tcgen05 products of up to 64 rows (queries x heads)
+// with tiles of 64 cached tokens, the tokens along the instruction's rows.
 //
-//   S^T [tokens, rows] = C Q^T     C the tile: 128 tokens x (latent, key part),
-//                                  in 128-byte columns as the TMA loads it
+//   S^T [tokens, rows] = C Q^T     C the tile: 64 tokens x (latent, key part), in
+//                                  128-byte columns as the TMA loads it
 //   O^T [dims, rows] += C_l^T P    the same bytes, read with the token index
 //                                  along K: a latent is loaded once for both
 // Rows as columns of the accumulators keep O in half of tensor memory (512 dims
 // x 64 rows are 4 x 64 columns), where rows as its rows would fill all of it,
-// and cost a few rows no more products than they fill columns.
-// Warps: one loads, one issues the products, eight hold the softmax: a thread
-// has one token and 32 rows, so maxima over tokens are taken across threads, and
-// only when some score exceeds its row's reference by more than 2^7; sums stay
-// with the threads until the end.
+// and cost a few rows no more than they fill columns.
+// Tiles of 64 tokens, 73.7 KB of 512 + 64 elements, so that two of them fit next
+// to 64 rows of queries and nearly three next to 16: the scores of a tile are
+// under way before the weights of the one before it are. A tile's weights take
+// the place of its key parts, which its scores have used up.
+// Warps: one loads, one issues the scores' products and one the values', four or
+// eight hold the softmax: a
+// thread has one token and 8 or 16 rows, so maxima over tokens are taken across
+// threads, and only when some score exceeds its row's reference by more than
+// 2^15; sums stay with the threads until the end.
 #include "rotary/latent.h"
 
 namespace bdrot {
@@ -19,45 +24,78 @@ namespace {
 
 using bdkv::Seq;
 
-constexpr int SOFT_WARPS = 8, THREADS = (SOFT_WARPS + 2) * 32;
-constexpr int SOFT = SOFT_WARPS * 32;
+constexpr int MAX_STAGES = 6, MAX_TILES = 3;  // in shared memory: of latents, and of key parts
 constexpr uint32_t CHUNK = TOKENS * 128, PAIR = 2 * CHUNK;  // bytes of 64 and of 128 elements of a tile
-constexpr uint32_t Q_CHUNK = ROWS * 128;
-constexpr int S_COL = 0, O_COL = 64;  // tensor memory: scores, then O's dims by 128
-constexpr int MAX_PAIRS = 4;
-// Weights are held times 2^8 and may exceed that by 2^7 before O is rescaled: 2^15 at most, which f16 holds, with 11 bits
-// down to 2^-22 of the reference.
-constexpr float P_SHIFT = 8, P_SLACK = 7;
+// A row's weights are 2^(score - reference). The reference is 2^8 below the largest score seen when it was set, and scores
+// may exceed it by 2^15 before it is set again and O rescaled: weights of 2^15 at most, which f16 holds, with 11 bits down
+// to 2^-22 of that largest score's.
+constexpr float P_SHIFT = 8, P_MOST = 15;
+constexpr float NO_REF = -3.0e38f;  // no score has been seen
 
 __device__ uint32_t g_status;  // bd::DEV_* bits
 
+template <int N>
 struct Ctl {
-  uint64_t q_full, pair_full[MAX_PAIRS], pair_empty[MAX_PAIRS], rope_full, rope_empty;
-  uint64_t s_full, p_full, o_done, drain;
-  alignas(16) float ref[ROWS];    // a row's weights are 2^(score - ref)
-  alignas(16) float limit[ROWS];  // scores above it make the reference grow
-  alignas(16) float factor[ROWS];
-  float part[4][ROWS];            // of the warps of a token quarter: maxima, at the end sums
-  float scale[ROWS];
-  int visible[ROWS];
-  uint64_t out[ROWS];             // where a row goes (0: nowhere); lowest bit: fp32 parts
+  uint64_t q_full, full[MAX_STAGES], empty[MAX_STAGES];
+  uint64_t s_full[2], p_full[2], o_done[2], s_drain, o_drain;  // (pairs: by parity of the tile)
+  alignas(16) float ref[N];
+  alignas(16) float factor[N];
+  alignas(16) float scale[N];
+  float part[4][N];  // of the warps of a token quarter: maxima, at the end sums
+  int visible[N];
+  uint64_t out[N];   // where a row goes (0: nowhere); lowest bit: fp32 parts
   uint32_t tmem_base;
   int abort_flag;
 };
 
-// Shared memory: the queries' columns, pairs of columns of a tile's latents in a ring of n_pairs, and one place for the
-// tile's key parts, which the weights take over once the scores are done.
-__host__ __device__ constexpr size_t smem_bytes(int n_pairs) {
-  return size_t(2 * n_pairs + 1) * Q_CHUNK + size_t(n_pairs) * PAIR + CHUNK + sizeof(Ctl) + 1024;
+// A tile comes in stages of one or two pairs of 64 columns of its latents, its key parts with the last: the warps that load
+// and multiply spend some 400 cycles a stage on barriers whatever is in it (with a stage for each pair and one for the key
+// parts, 64 rows took 2630 cycles a tile). Shared memory: the queries' columns, a ring of stages, and one of key parts (and
+// weights) for as many tiles as those hold, the last maybe in part, so that a stage that is free says that its tile's key
+// parts have a place.
+struct Layout {
+  int n_pairs, per_stage, per_tile;  // pairs of a tile and of a stage, stages of a tile
+  int stages, tiles;
+  size_t bytes;
+};
+__host__ __device__ constexpr int pairs_per_stage(int n_pairs) { return n_pairs < 2 ? 1 : 2; }
+template <int N>
+Layout layout(int dim) {
+  Layout l;
+  l.n_pairs = (dim + 127) / 128;
+  l.per_stage = pairs_per_stage(l.n_pairs);
+  l.per_tile = (l.n_pairs + l.per_stage - 1) / l.per_stage;
+  const size_t fixed = 1024 + sizeof(Ctl<N>) + (2 * l.n_pairs + 1) * N * 128, stage = l.per_stage * PAIR;
+  const auto bytes = [&](int stages) { return fixed + stages * stage + (stages + l.per_tile - 1) / l.per_tile * CHUNK; };
+  l.stages = std::min(MAX_STAGES, MAX_TILES * l.per_tile);
+  while (bytes(l.stages) > 232448) --l.stages;  // (two tiles at least)
+  l.tiles = (l.stages + l.per_tile - 1) / l.per_tile;
+  l.bytes = bytes(l.stages);
+  return l;
 }
-// (a power of two; CTAs of small latents share an SM, and none waits for another's columns)
-__device__ constexpr uint32_t tmem_columns(int n_pairs) { return n_pairs == 1 ? 128 : n_pairs < 4 ? 256 : 512; }
-static_assert(smem_bytes(MAX_PAIRS) <= 232448, "shared memory of a CTA");
+// (a power of two)
+template <int N>
+__host__ __device__ constexpr uint32_t tmem_columns(int n_pairs) {
+  const int n = (2 + n_pairs) * N;
+  return n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : 512;
+}
 
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
+// By predicate in the elected lane, with operands that are the same in all lanes: a branch, or a lane's own coordinates,
+// costs hundreds of cycles a copy.
+__device__ __forceinline__ void tma_load_3d(uint32_t issue, uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y,
+                                            int z) {
   asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
-      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %6, 0;\n\t"
+      "@q cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n\t}" ::"r"(
+          dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar), "r"(issue)
+      : "memory");
+}
+__device__ __forceinline__ void expect_bytes(uint32_t issue, uint32_t bar, uint32_t bytes) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t"
+      "@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar),
+      "r"(bytes), "r"(issue)
       : "memory");
 }
 
@@ -91,63 +129,135 @@ __device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.
 __device__ __forceinline__ void st_shared_v4(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
-// The 128 threads that share the tile's rows 32 h .. 32 h + 31: a barrier, and one that says whether any of them has `some`.
-__device__ __forceinline__ void half_sync(int h) { bd::named_barrier_sync(1 + h, SOFT / 2); }
-__device__ __forceinline__ bool half_any(int h, bool some) {
+// The 128 threads that have the same rows: a barrier, and one that says whether any of them has `some`.
+__device__ __forceinline__ void group_sync(int g) { bd::named_barrier_sync(1 + g, 128); }
+__device__ __forceinline__ bool group_any(int g, bool some) {
   uint32_t r;
   asm volatile(
       "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\t"
       "barrier.cta.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
       : "=r"(r)
-      : "r"(static_cast<uint32_t>(some)), "r"(1 + h), "r"(SOFT / 2)
+      : "r"(static_cast<uint32_t>(some)), "r"(1 + g), "r"(128)
       : "memory");
   return r != 0;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 r;
+  asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+      "mul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "=f"(r.x), "=f"(r.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return r;
+}
+// 16 columns of this thread's lane, and back.
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, float (&v)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]),
+        "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+      "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+      : "memory");
+}
+template <int COLS>
+__device__ __forceinline__ void tmem_load(uint32_t at, float (&v)[COLS]) {
+  if constexpr (COLS == 16)
+    tmem_ld16(at, v);
+  else
+    bd::tmem_ld32(at, v);
+}
+template <int COLS>
+__device__ __forceinline__ void tmem_store(uint32_t at, const uint32_t (&v)[COLS]) {
+  if constexpr (COLS == 16)
+    tmem_st16(at, v);
+  else
+    bd::tmem_st32(at, v);
+}
+// An accumulator of 64 rows lies in the first 16 lanes of each warp's quarter: threads 0..15 get COLS columns of them,
+// threads 16..31 of the same lanes the next COLS.
+template <int COLS>
+__device__ __forceinline__ void tmem_load_halves(uint32_t at, float (&v)[COLS]) {
+  if constexpr (COLS == 16)
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x32bx2.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16], 16;\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]),
+          "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15])
+        : "r"(at)
+        : "memory");
+  else
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x32bx2.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8], 8;\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+        : "r"(at)
+        : "memory");
+}
+// 16 bytes from global to shared memory, asynchronously; zeros where there is nothing to read.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool live) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
 }
 
 // A row's reference for a largest score of `most`: scores so large that 8 is about a rounding of theirs go without the shift.
 __device__ __forceinline__ float reference(float most) { return fabsf(most) < 1048576.f ? most - P_SHIFT : most; }
 
-// v[c] of all lanes combined: lane l returns column l's.
-template <class Op>
-__device__ __forceinline__ float across_lanes(const float (&v)[32], int lane, Op op) {
-  float w[16];
-  const auto step = [&](auto width, const auto& from) {
+// v[c] combined over the 16 lanes of a half warp: column c % COLS is lane c's.
+template <int COLS, class Op>
+__device__ __forceinline__ float across_lanes(const float (&v)[COLS], int lane, Op op) {
+  float w[COLS];
+#pragma unroll
+  for (int c = 0; c < COLS; ++c) w[c] = COLS == 16 ? v[c] : op(v[c], __shfl_xor_sync(~0u, v[c], 8));
+  const auto step = [&](auto width) {
     constexpr int H = decltype(width)::value;
     const bool upper = lane & H;
 #pragma unroll
     for (int u = 0; u < H; ++u) {
-      const float lo = from[u], hi = from[u + H];
-      const float other = __shfl_xor_sync(~0u, upper ? lo : hi, H);
-      w[u] = op(upper ? hi : lo, other);
+      const float other = __shfl_xor_sync(~0u, upper ? w[u] : w[u + H], H);
+      w[u] = op(upper ? w[u + H] : w[u], other);
     }
   };
-  step(std::integral_constant<int, 16>(), v);
-  step(std::integral_constant<int, 8>(), w);
-  step(std::integral_constant<int, 4>(), w);
-  step(std::integral_constant<int, 2>(), w);
-  step(std::integral_constant<int, 1>(), w);
+  if constexpr (COLS == 16) step(std::integral_constant<int, 8>());
+  step(std::integral_constant<int, 4>());
+  step(std::integral_constant<int, 2>());
+  step(std::integral_constant<int, 1>());
   return w[0];
 }
 
-__global__ void __launch_bounds__(THREADS, 1)
-    latent_attn_kernel(const LatentArgs p, const __grid_constant__ CUtensorMap latent_map,
+// N: rows of a CTA.
+template <int N>
+__global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
+    latent_attn_kernel(const LatentArgs p, const int stages, const int tiles, const __grid_constant__ CUtensorMap latent_map,
                        const __grid_constant__ CUtensorMap rope_map) {
+  constexpr int SOFT_WARPS = N == 64 ? 8 : 4, SOFT = SOFT_WARPS * 32, THREADS = SOFT + 96;
+  constexpr int WIDE = N / (SOFT_WARPS / 4), COLS = WIDE / 2;  // rows of a softmax warp, and of a thread
+  constexpr uint32_t Q_CHUNK = N * 128, O_COL = 2 * N;  // tensor memory: two tiles' scores, then O's dims by 128
   const bdkv::AttnArgs& a = p.a;
   extern __shared__ __align__(16) uint8_t raw[];
-  const int n_pairs = (a.dim + 127) / 128;
+  const int n_pairs = (a.dim + 127) / 128, per_stage = pairs_per_stage(n_pairs);
+  const uint32_t stage_bytes = per_stage * PAIR;
   const uint32_t base = (bd::smem_u32(raw) + 1023u) & ~1023u;
-  const uint32_t q_at = base, kv_at = q_at + (2 * n_pairs + 1) * Q_CHUNK, rope_at = kv_at + n_pairs * PAIR;
-  Ctl* ctl = reinterpret_cast<Ctl*>(raw + (rope_at + CHUNK - bd::smem_u32(raw)));
+  const uint32_t kv_at = base, rope_at = kv_at + stages * stage_bytes, q_at = rope_at + tiles * CHUNK;
+  Ctl<N>* ctl = reinterpret_cast<Ctl<N>*>(raw + (q_at + (2 * n_pairs + 1) * Q_CHUNK - bd::smem_u32(raw)));
   const int tid = threadIdx.x, lane = tid & 31, warp = static_cast<int>(bd::warp_uniform(tid >> 5));
 
   int seq = blockIdx.z;
   const Seq sq = a.longest_first ? bdkv::ranked_seq<THREADS>(a, blockIdx.z, reinterpret_cast<int*>(raw), seq)
                                  : bdkv::load_seq(a, seq);
   // the last rows first: under a causal mask they see the most
-  const int row0 = (gridDim.x - 1 - blockIdx.x) * ROWS, part = blockIdx.y, rows = sq.q_len * a.group;
+  const int row0 = (gridDim.x - 1 - blockIdx.x) * N, part = blockIdx.y, rows = sq.q_len * a.group;
   if (row0 >= rows) return;
   // later queries see at least as much: the CTA's last row bounds it, and all of its rows see what its first one does
-  const int i_first = row0 / a.group, i_last = (min(rows, row0 + ROWS) - 1) / a.group;
+  const int i_first = row0 / a.group, i_last = (min(rows, row0 + N) - 1) / a.group;
   const int begin = part * a.chunk, end = min(bdkv::visible(a, sq, i_last), begin + a.chunk);
   if (part > 0 && end <= begin) return;
   const int n = end > begin ? (end - begin + TOKENS - 1) / TOKENS : 0;
@@ -155,25 +265,25 @@ __global__ void __launch_bounds__(THREADS, 1)
 
   if (tid == 0) {
     bd::mbar_init(bd::smem_u32(&ctl->q_full), SOFT);
-    for (int i = 0; i < MAX_PAIRS; ++i) {
-      bd::mbar_init(bd::smem_u32(&ctl->pair_full[i]), 1);
-      bd::mbar_init(bd::smem_u32(&ctl->pair_empty[i]), 1);
+    for (int i = 0; i < stages; ++i) {
+      bd::mbar_init(bd::smem_u32(&ctl->full[i]), 1);
+      bd::mbar_init(bd::smem_u32(&ctl->empty[i]), 1);
     }
-    bd::mbar_init(bd::smem_u32(&ctl->rope_full), 1);
-    bd::mbar_init(bd::smem_u32(&ctl->rope_empty), 1);
-    bd::mbar_init(bd::smem_u32(&ctl->s_full), 1);
-    bd::mbar_init(bd::smem_u32(&ctl->p_full), SOFT);
-    bd::mbar_init(bd::smem_u32(&ctl->o_done), 1);
-    bd::mbar_init(bd::smem_u32(&ctl->drain), 1);
+    for (int i = 0; i < 2; ++i) {
+      bd::mbar_init(bd::smem_u32(&ctl->s_full[i]), 1);
+      bd::mbar_init(bd::smem_u32(&ctl->p_full[i]), SOFT_WARPS);
+      bd::mbar_init(bd::smem_u32(&ctl->o_done[i]), 1);
+    }
+    bd::mbar_init(bd::smem_u32(&ctl->s_drain), 1);
+    bd::mbar_init(bd::smem_u32(&ctl->o_drain), 1);
     ctl->abort_flag = 0;
     bd::fence_mbar_init();
   }
-  if (tid < ROWS) {
-    ctl->ref[tid] = -P_SHIFT;
-    ctl->limit[tid] = -INFINITY;
+  if (tid < N) {
+    ctl->ref[tid] = NO_REF;
     const int row = row0 + tid, i = row / a.group, h = row - i * a.group;
     const int vis = row < rows ? bdkv::visible(a, sq, i) : 0;
-    ctl->visible[tid] = row < rows ? min(vis, end) : 0;
+    ctl->visible[tid] = min(vis, end);
     uint64_t to = 0;
     if (row < rows) {
       const bdkv::RowOut o = bdkv::row_out(a, sq, seq, part, i, h, vis);
@@ -181,9 +291,9 @@ __global__ void __launch_bounds__(THREADS, 1)
     }
     ctl->out[tid] = to;
   }
-  constexpr int LOAD_WARP = SOFT_WARPS, MMA_WARP = SOFT_WARPS + 1;
-  if (warp == MMA_WARP) {
-    bd::tmem_alloc(bd::smem_u32(&ctl->tmem_base), tmem_columns(n_pairs));
+  constexpr int LOAD_WARP = SOFT_WARPS, SCORE_WARP = SOFT_WARPS + 1, VALUE_WARP = SOFT_WARPS + 2;
+  if (warp == VALUE_WARP) {
+    bd::tmem_alloc(bd::smem_u32(&ctl->tmem_base), tmem_columns<N>(n_pairs));
     bd::tmem_relinquish();
   }
   bd::tc_fence_before();
@@ -198,199 +308,265 @@ __global__ void __launch_bounds__(THREADS, 1)
 
   if (warp == LOAD_WARP) {
     // ---------------------------------------------------------------- loads
-    // Lane b has box b of a tile: a page's tokens, or 128 tokens of a larger page. What is not there (a column behind the
-    // table, a page outside the cache, tokens that no row sees) is read from behind the cache's last page, as zeros.
+    // Box b of a tile: a page's tokens, or 64 tokens of a larger page; lane b finds its page. What is not there (a column
+    // behind the table, a page outside the cache, tokens that no row sees) is read from behind the cache's last page, as zeros.
     const int page_size = 1 << a.page_shift, step = min(page_size, TOKENS), boxes = TOKENS / step;
     const int32_t* table = a.table + seq * a.table_stride;
     const int outside = static_cast<int>(max(a.n_pages, static_cast<int64_t>(1)));
-    const auto find = [&](int j) {
+    const auto find = [&](int j) {  // the page as the table has it: a tile ahead, and not looked at until it is needed
       const int t = begin + j * TOKENS + lane * step, col = t >> a.page_shift;
-      int page = lane < boxes && t < end && col < a.max_blocks ? table[col] : -1;
-      return page >= 0 && page < a.n_pages ? page : outside;
+      return lane < boxes && t < end && col < a.max_blocks ? table[col] : -1;
     };
-    int page = n > 0 ? find(0) : 0, issued = 0, ropes = 0;
+    if (lane == 0) {
+      bd::prefetch_tmap(&latent_map);
+      bd::prefetch_tmap(&rope_map);
+    }
+    int found = find(0), following = find(1);
+    int stage = 0, round = 0, tile = 0;  // of the next load: its places, and how often the stage's was used
     bool ok = true;
+    const uint32_t issue = bd::elect_one();
+    const auto load = [&](const CUtensorMap* map, uint32_t dst, uint32_t bar, int x, int y, int page) {
+      for (int b = 0; b < boxes; ++b)  // (more than one: whole pages)
+        tma_load_3d(issue, bd::warp_uniform(dst + b * step * 128), map, bar, x, y, __shfl_sync(~0u, page, b));
+    };
     for (int j = 0; ok && j < n; ++j) {
-      const int y = (begin + j * TOKENS + lane * step) & (page_size - 1);
-      for (int s = 0; s < n_pairs; ++s) {
-        if (!(ok = wait(ctl->pair_empty[s], j + 1))) break;
-        const uint32_t bar = bd::smem_u32(&ctl->pair_full[s]), dst = kv_at + s * PAIR + lane * step * 128;
-        if (lane == 0) bd::mbar_expect_tx(bar, PAIR);
-        __syncwarp();
-        if (lane < boxes) {
-          tma_load_3d(dst, &latent_map, bar, s * 128, y, page);
-          tma_load_3d(dst + CHUNK, &latent_map, bar, s * 128 + 64, y, page);
-        }
-        ++issued;
+      const int y = static_cast<int>(bd::warp_uniform((begin + j * TOKENS) & (page_size - 1)));
+      const int page = found >= 0 && found < a.n_pages ? found : outside;
+      found = following;
+      following = find(j + 2);
+      for (int s = 0; s < n_pairs; s += per_stage) {
+        if (!(ok = wait(ctl->empty[stage], round + 1))) break;
+        const int pairs = min(per_stage, n_pairs - s);
+        const bool last = s + per_stage >= n_pairs;
+        const uint32_t bar = bd::warp_uniform(bd::smem_u32(&ctl->full[stage])), dst = kv_at + stage * stage_bytes;
+        expect_bytes(issue, bar, pairs * PAIR + (last ? CHUNK : 0));
+        for (int c = 0; c < 2 * pairs; ++c) load(&latent_map, dst + c * CHUNK, bar, (2 * s + c) * 64, y, page);
+        if (last) load(&rope_map, rope_at + tile * CHUNK, bar, 0, y, page);
+        if (++stage == stages) stage = 0, ++round;
       }
-      if (!ok || !(ok = wait(ctl->rope_empty, j + 1))) break;
-      const uint32_t bar = bd::smem_u32(&ctl->rope_full);
-      if (lane == 0) bd::mbar_expect_tx(bar, CHUNK);
-      __syncwarp();
-      if (lane < boxes) tma_load_3d(rope_at + lane * step * 128, &rope_map, bar, 0, y, page);
-      ++ropes;
-      if (j + 1 < n) page = find(j + 1);
+      if (++tile == tiles) tile = 0;
     }
     // nothing is on its way when the CTA ends (all of it has been waited for, unless a wait gave up)
     __syncwarp();
-    for (int s = 0; s < n_pairs; ++s) {
-      const int loads = (issued - s + n_pairs - 1) / n_pairs;
-      if (loads > 0) bd::mbar_drain(bd::smem_u32(&ctl->pair_full[s]), (loads - 1) & 1);
+    for (int i = 0; i < stages; ++i) {
+      const int loads = round + (i < stage);
+      if (loads > 0) bd::mbar_drain(bd::smem_u32(&ctl->full[i]), (loads - 1) & 1);
     }
-    if (ropes > 0) bd::mbar_drain(bd::smem_u32(&ctl->rope_full), (ropes - 1) & 1);
     __syncwarp();
-  } else if (warp == MMA_WARP) {
+  } else if (warp == SCORE_WARP) {
     // ------------------------------------------------------------- products
+    // Two warps issue them: what one spends on barriers and descriptors between products, the other's fill. (One for both,
+    // whichever was ready: 2960 cycles a tile of 64 rows, of which the products take 1920.)
     const uint32_t issue = bd::elect_one();
-    const uint32_t type = a.f16 ? 0u : (1u << 7) | (1u << 10);
-    const uint32_t idesc_s = bd::warp_uniform(bd::idesc_f16_f32(TOKENS, ROWS) | type);
-    const uint32_t idesc_o = bd::warp_uniform(bd::idesc_f16_f32(128, ROWS) | type | A_MN_MAJOR | B_MN_MAJOR);
+    const uint32_t idesc = bd::warp_uniform(bd::idesc_f16_f32(TOKENS, N) | (a.f16 ? 0u : (1u << 7) | (1u << 10)));
     const uint32_t q_lo = bd::warp_uniform(static_cast<uint32_t>(bd::sw128_kmajor_desc(q_at)));
     const uint32_t k_lo = bd::warp_uniform(static_cast<uint32_t>(bd::sw128_kmajor_desc(kv_at)));
     const uint32_t r_lo = bd::warp_uniform(static_cast<uint32_t>(bd::sw128_kmajor_desc(rope_at)));
-    const uint32_t v_lo = bd::warp_uniform(mn_low(kv_at, CHUNK)), p_lo = bd::warp_uniform(mn_low(rope_at, CHUNK));
-    const uint32_t s_at = tmem + S_COL;
+    int stage = 0, round = 0, tile = 0;
     bool ok = n > 0 && wait(ctl->q_full, 0);
     for (int j = 0; ok && j < n; ++j) {
-      for (int s = 0; s < n_pairs; ++s) {
-        if (!(ok = wait(ctl->pair_full[s], j))) break;
+      // over the scores of two tiles before, which have become weights
+      if (j >= 2 && !(ok = wait(ctl->p_full[j & 1], (j - 2) >> 1))) break;
+      const uint32_t s_at = bd::warp_uniform(tmem + (j & 1) * N);
+      for (int s = 0; s < n_pairs; s += per_stage) {
+        if (!(ok = wait(ctl->full[stage], round))) break;
         bd::tc_fence_after();
-        const uint32_t kd = bd::warp_uniform(k_lo + s * (PAIR >> 4)), qd = bd::warp_uniform(q_lo + s * (2 * Q_CHUNK >> 4));
+        for (int u = 0; u < per_stage && s + u < n_pairs; ++u) {
+          const uint32_t kd = bd::warp_uniform(k_lo + ((stage * stage_bytes + u * PAIR) >> 4));
+          const uint32_t qd = bd::warp_uniform(q_lo + (s + u) * (2 * Q_CHUNK >> 4));
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          mma(issue, s_at, kd + (k / 4) * (CHUNK >> 4) + 2u * (k % 4), qd + (k / 4) * (Q_CHUNK >> 4) + 2u * (k % 4), DESC_HI,
-              DESC_HI, idesc_s, (s | k) != 0);
+          for (int k = 0; k < 8; ++k)
+            mma(issue, s_at, kd + (k / 4) * (CHUNK >> 4) + 2u * (k % 4), qd + (k / 4) * (Q_CHUNK >> 4) + 2u * (k % 4), DESC_HI,
+                DESC_HI, idesc, (s | u | k) != 0);
+        }
+        if (++stage == stages) stage = 0, ++round;
       }
-      if (!ok || !(ok = wait(ctl->rope_full, j))) break;
-      bd::tc_fence_after();
-      const uint32_t qr = bd::warp_uniform(q_lo + n_pairs * (2 * Q_CHUNK >> 4));
+      if (!ok) break;
+      const uint32_t rd = bd::warp_uniform(r_lo + tile * (CHUNK >> 4)), qr = bd::warp_uniform(q_lo + n_pairs * (2 * Q_CHUNK >> 4));
 #pragma unroll
-      for (int k = 0; k < 4; ++k) mma(issue, s_at, r_lo + 2u * k, qr + 2u * k, DESC_HI, DESC_HI, idesc_s, 1);
-      mma_commit(issue, bd::smem_u32(&ctl->s_full));
-      if (!(ok = wait(ctl->p_full, j))) break;
-      bd::tc_fence_after();
-      for (int s = 0; s < n_pairs; ++s) {
-        const uint32_t vd = bd::warp_uniform(v_lo + s * (PAIR >> 4)), od = bd::warp_uniform(tmem + O_COL + s * ROWS);
-#pragma unroll
-        for (int k = 0; k < TOKENS / 16; ++k)
-          mma(issue, od, vd + k * (2048u >> 4), p_lo + k * (2048u >> 4), DESC_HI, DESC_HI, idesc_o, (j | k) != 0);
-        mma_commit(issue, bd::smem_u32(&ctl->pair_empty[s]));
-      }
-      mma_commit(issue, bd::smem_u32(&ctl->rope_empty));
+      for (int k = 0; k < 4; ++k) mma(issue, s_at, rd + 2u * k, qr + 2u * k, DESC_HI, DESC_HI, idesc, 1);
+      mma_commit(issue, bd::smem_u32(&ctl->s_full[j & 1]));
+      if (++tile == tiles) tile = 0;
     }
-    mma_commit(issue, bd::smem_u32(&ctl->o_done));
-    mma_commit(issue, bd::smem_u32(&ctl->drain));  // all MMAs issued have completed once it flips
+    mma_commit(issue, bd::smem_u32(&ctl->s_drain));  // all of its products have completed once it flips
     __syncwarp();
-    bd::mbar_drain(bd::smem_u32(&ctl->drain), 0);
+    bd::mbar_drain(bd::smem_u32(&ctl->s_drain), 0);
+    __syncwarp();
+  } else if (warp == VALUE_WARP) {
+    const uint32_t issue = bd::elect_one();
+    const uint32_t idesc = bd::warp_uniform(bd::idesc_f16_f32(128, N) | (a.f16 ? 0u : (1u << 7) | (1u << 10)) | A_MN_MAJOR | B_MN_MAJOR);
+    const uint32_t v_lo = bd::warp_uniform(mn_low(kv_at, CHUNK)), p_lo = bd::warp_uniform(mn_low(rope_at, CHUNK));
+    int stage = 0, tile = 0;
+    for (int j = 0; j < n && wait(ctl->p_full[j & 1], j >> 1); ++j) {
+      bd::tc_fence_after();
+      const uint32_t pd = bd::warp_uniform(p_lo + tile * (CHUNK >> 4));
+      for (int s = 0; s < n_pairs; s += per_stage) {
+        for (int u = 0; u < per_stage && s + u < n_pairs; ++u) {
+          const uint32_t vd = bd::warp_uniform(v_lo + ((stage * stage_bytes + u * PAIR) >> 4));
+          const uint32_t od = bd::warp_uniform(tmem + O_COL + (s + u) * N);
+#pragma unroll
+          for (int k = 0; k < TOKENS / 16; ++k)
+            mma(issue, od, vd + k * (2048u >> 4), pd + k * (2048u >> 4), DESC_HI, DESC_HI, idesc, (j | k) != 0);
+        }
+        mma_commit(issue, bd::smem_u32(&ctl->empty[stage]));
+        if (++stage == stages) stage = 0;
+      }
+      mma_commit(issue, bd::smem_u32(&ctl->o_done[j & 1]));
+      if (++tile == tiles) tile = 0;
+    }
+    mma_commit(issue, bd::smem_u32(&ctl->o_drain));
+    __syncwarp();
+    bd::mbar_drain(bd::smem_u32(&ctl->o_drain), 0);
     __syncwarp();
   } else {
     // -------------------------------------------------------------- softmax
     // A wait that gives up (`ok`) ends no warp's loop: the barriers below count all of them.
-    const int quarter = warp & 3, half = warp >> 2;  // tokens and rows, by 32
+    const int quarter = warp & 3, group = warp >> 2, col0 = group * WIDE + (lane >> 4) * COLS;
     if (n > 0) {
-      const int wide = a.dim + p.rope_dim, units = (2 * n_pairs + 1) * 8;  // units of eight elements
-      const uint16_t* q = static_cast<const uint16_t*>(a.q);
-      for (int x = tid; x < ROWS * units; x += SOFT) {
-        const int r = x / units, u = x - r * units, row = row0 + r;
-        // the key part's columns begin behind the padded latents'
-        const int e = u < 16 * n_pairs ? (u * 8 < a.dim ? u * 8 : wide) : a.dim + (u - 16 * n_pairs) * 8;
-        uint4 w = {0, 0, 0, 0};
-        if (row < rows && e < wide) {
-          const int i = row / a.group, h = row - i * a.group;
-          w = *reinterpret_cast<const uint4*>(q + static_cast<int64_t>(sq.q0 + i) * a.q_tok + h * a.q_head + e);
-        }
-        st_shared_v4(q_at + (u / 8) * Q_CHUNK + r * 128 + (((u % 8) ^ (r & 7)) << 4), w.x, w.y, w.z, w.w);
+      // a lane has up to three units of eight elements of every row; the key part's columns begin behind the padded latents'
+      const int wide = a.dim + p.rope_dim, units = (2 * n_pairs + 1) * 8;
+      int from[3];
+#pragma unroll
+      for (int x = 0; x < 3; ++x) {
+        const int u = lane + 32 * x;
+        from[x] = u < 16 * n_pairs ? (u * 8 < a.dim ? u * 8 : wide) : a.dim + (u - 16 * n_pairs) * 8;
       }
+      const uint16_t* q = static_cast<const uint16_t*>(a.q) + static_cast<int64_t>(sq.q0) * a.q_tok;
+      int i = (row0 + warp) / a.group, h = row0 + warp - i * a.group;
+#pragma unroll 2
+      for (int r = warp; r < N; r += SOFT_WARPS) {
+        const uint16_t* src = q + i * a.q_tok + h * a.q_head;
+        const uint32_t dst = q_at + r * 128;
+#pragma unroll
+        for (int x = 0; x < 3; ++x) {
+          const int u = lane + 32 * x;
+          const bool live = row0 + r < rows && from[x] < wide;
+          if (u < units) copy16(dst + (u / 8) * Q_CHUNK + (((u % 8) ^ (r & 7)) << 4), live ? src + from[x] : q, live);
+        }
+        for (h += SOFT_WARPS; h >= a.group; h -= a.group) ++i;
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
       fence_proxy_async();
       bd::mbar_arrive(bd::smem_u32(&ctl->q_full));
     }
     const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
-    const uint32_t s_at = tmem + lanes + S_COL + half * 32, o_at = tmem + lanes + O_COL + half * 32;
-    const int token = quarter * 32 + lane;
-    // the weights of a token, its row of the second operand: 64 rows contiguous
-    const uint32_t p_at = rope_at + (token / 8) * 1024 + (token % 8) * 128;
-    float L[32];
+    const uint32_t s_at = tmem + lanes + group * WIDE, o_at = tmem + lanes + O_COL + group * WIDE;
+    const int token = quarter * 16 + (lane & 15);
+    // the weights of a token, its row of the second operand: the tile's rows contiguous
+    const uint32_t w_at = rope_at + (token / 8) * 1024 + (token % 8) * 128;
+    float2 L[COLS / 2];
 #pragma unroll
-    for (int c = 0; c < 32; ++c) L[c] = 0.f;
+    for (int c = 0; c < COLS / 2; ++c) L[c] = make_float2(0.f, 0.f);
     bool ok = true;
+    int stage = 0, tile = 0;
     for (int j = 0; j < n; ++j) {
       const int t0 = begin + j * TOKENS;
-      if (ok) ok = wait(ctl->s_full, j);
+      if (ok) ok = wait(ctl->s_full[j & 1], j >> 1);
       bd::tc_fence_after();
-      float v[32];
+      float v[COLS];
       __syncwarp();
-      bd::tmem_ld32(s_at, v);
-      const bool cut = t0 + TOKENS > min(all_see, end);  // some row does not see all of the tile
+      tmem_load_halves<COLS>(s_at + (j & 1) * N, v);
 #pragma unroll
-      for (int c = 0; c < 32; ++c) v[c] = __fmul_rn(v[c], a.coef);
-      if (cut) {
-#pragma unroll
-        for (int c = 0; c < 32; ++c)
-          if (t0 + token >= ctl->visible[half * 32 + c]) v[c] = -INFINITY;
+      for (int c = 0; c < COLS; c += 2) {
+        const float2 x = mul2(make_float2(v[c], v[c + 1]), make_float2(a.coef, a.coef));
+        v[c] = x.x, v[c + 1] = x.y;
       }
-      bool grow = false;
+      if (t0 + TOKENS > min(all_see, end)) {  // some row does not see all of the tile
 #pragma unroll
-      for (int c = 0; c < 32; ++c) grow |= v[c] > ctl->limit[half * 32 + c];
-      if (half_any(half, grow)) {
-        const float top = across_lanes(v, lane, [](float x, float y) { return fmaxf(x, y); });
-        const int col = half * 32 + lane;
-        ctl->part[quarter][col] = top;
-        half_sync(half);
-        const float most = fmaxf(fmaxf(ctl->part[0][col], ctl->part[1][col]), fmaxf(ctl->part[2][col], ctl->part[3][col]));
-        const float limit = ctl->limit[col], before = ctl->ref[col];
-        half_sync(half);
-        if (quarter == 0) {
-          const bool up = most > limit;  // (a limit of -inf: there is no reference yet)
-          ctl->factor[col] = !up ? 1.f : limit == -INFINITY ? 0.f : bd::ex2_approx(before - reference(most));
-          if (up) ctl->ref[col] = reference(most), ctl->limit[col] = most + P_SLACK;
+        for (int c = 0; c < COLS; ++c)
+          if (t0 + token >= ctl->visible[col0 + c]) v[c] = -INFINITY;
+      }
+      float2 x[COLS / 2];
+      const auto subtract = [&] {
+#pragma unroll
+        for (int c = 0; c < COLS; c += 4) {
+          const float4 r = *reinterpret_cast<const float4*>(&ctl->ref[col0 + c]);
+          x[c / 2] = bd::add2(make_float2(v[c], v[c + 1]), make_float2(-r.x, -r.y));
+          x[c / 2 + 1] = bd::add2(make_float2(v[c + 2], v[c + 3]), make_float2(-r.z, -r.w));
         }
-        half_sync(half);
-        float f[32];
+      };
+      subtract();
+      float top = -INFINITY;
 #pragma unroll
-        for (int c = 0; c < 32; ++c) f[c] = ctl->factor[half * 32 + c], L[c] *= f[c];
-        if (j > 0) {  // the products of the tile before came before this tile's scores: O is at rest
+      for (int c = 0; c < COLS / 2; ++c) top = bd::max3(top, x[c].x, x[c].y);
+      if (group_any(group, top > P_MOST)) {
+        const int col = col0 + (lane & (COLS - 1));
+        const bool first = (lane & 15) < COLS;  // of the lanes that have this column
+        const float most_here = across_lanes<COLS>(v, lane, [](float x, float y) { return fmaxf(x, y); });
+        if (first) ctl->part[quarter][col] = most_here;
+        group_sync(group);
+        const float most = fmaxf(fmaxf(ctl->part[0][col], ctl->part[1][col]), fmaxf(ctl->part[2][col], ctl->part[3][col]));
+        const float before = ctl->ref[col];
+        group_sync(group);
+        if (quarter == 0 && first) {
+          const bool up = most - before > P_MOST;
+          ctl->factor[col] = up ? bd::ex2_approx(before - reference(most)) : 1.f;
+          if (up) ctl->ref[col] = reference(most);
+        }
+        group_sync(group);
+        subtract();
+#pragma unroll
+        for (int c = 0; c < COLS; c += 2)
+          L[c / 2] = mul2(L[c / 2], make_float2(ctl->factor[col0 + c], ctl->factor[col0 + c + 1]));
+        if (j > 0) {
+          // (of the last tile with its parity, three before this one, the products have ended: this one's key parts, or those
+          // of the tile before it, came in their place)
+          if (ok) ok = wait(ctl->o_done[(j - 1) & 1], (j - 1) >> 1);
+          bd::tc_fence_after();
           for (int s = 0; s < n_pairs; ++s) {
-            float o[32];
-            uint32_t y[32];
+            float o[WIDE];
+            uint32_t y[WIDE];
             __syncwarp();
-            bd::tmem_ld32(o_at + s * ROWS, o);
+            tmem_load<WIDE>(o_at + s * N, o);
 #pragma unroll
-            for (int c = 0; c < 32; ++c) y[c] = __float_as_uint(o[c] * f[c]);
-            bd::tmem_st32(o_at + s * ROWS, y);
+            for (int c = 0; c < WIDE; ++c) y[c] = __float_as_uint(o[c] * ctl->factor[group * WIDE + c]);
+            tmem_store<WIDE>(o_at + s * N, y);
           }
           bd::tmem_st_wait();
         }
       }
-      uint32_t w[16];
+      uint32_t w[COLS / 2];
 #pragma unroll
-      for (int c = 0; c < 32; c += 2) {
-        const float2 ref = *reinterpret_cast<const float2*>(&ctl->ref[half * 32 + c]);
-        const float2 x = make_float2(bd::ex2_approx(v[c] - ref.x), bd::ex2_approx(v[c + 1] - ref.y));
-        L[c] += x.x, L[c + 1] += x.y;
-        w[c / 2] = a.f16 ? F16::from_float2(x) : Bf16::from_float2(x);
+      for (int c = 0; c < COLS / 2; ++c) {
+        const float2 e = make_float2(bd::ex2_approx(x[c].x), bd::ex2_approx(x[c].y));
+        L[c] = bd::add2(L[c], e);
+        w[c] = a.f16 ? F16::from_float2(e) : Bf16::from_float2(e);
       }
-      // (the scores are done, so the key parts that lay here have been read)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        st_shared_v4(p_at + (((half * 4 + i) ^ (token & 7)) << 4), w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+      for (int i = 0; i < COLS / 8; ++i)
+        st_shared_v4(w_at + tile * CHUNK + (((col0 / 8 + i) ^ (token & 7)) << 4), w[4 * i], w[4 * i + 1], w[4 * i + 2],
+                     w[4 * i + 3]);
+      if (++tile == tiles) tile = 0;
       if (t0 + TOKENS > end) {
         // What a page holds behind the last token may be anything, and zero times it NaN: its latents become zeros.
-        const int from = end - t0, units = (TOKENS - from) * n_pairs * 16;
-        for (int x = tid; x < units; x += SOFT) {
-          const int r = from + x / (n_pairs * 16), u = x % (n_pairs * 16);
-          st_shared_v4(kv_at + (u / 8) * CHUNK + r * 128 + ((u % 8) << 4), 0, 0, 0, 0);
+        const int from = end - t0, units = (TOKENS - from) * 16;
+        for (int s = 0; s < n_pairs; ++s) {
+          int place = stage + s / per_stage;
+          if (place >= stages) place -= stages;
+          const uint32_t at = kv_at + place * stage_bytes + s % per_stage * PAIR;
+          for (int x = tid; x < units; x += SOFT)
+            st_shared_v4(at + (x % 16 / 8) * CHUNK + (from + x / 16) * 128 + ((x % 8) << 4), 0, 0, 0, 0);
         }
       }
+      stage += (n_pairs + per_stage - 1) / per_stage;
+      if (stage >= stages) stage -= stages;
       fence_proxy_async();
       bd::tc_fence_before();
-      bd::mbar_arrive(bd::smem_u32(&ctl->p_full));
+      __syncwarp();
+      if (lane == 0) bd::mbar_arrive(bd::smem_u32(&ctl->p_full[j & 1]));
     }
 
     // a row's sum: over the lanes, then over the four warps that have its tokens
-    ctl->part[quarter][half * 32 + lane] = across_lanes(L, lane, [](float x, float y) { return x + y; });
-    half_sync(half);
-    if (quarter == 0) {
-      const int col = half * 32 + lane, row = row0 + col;
+    float sums[COLS];
+#pragma unroll
+    for (int c = 0; c < COLS; ++c) sums[c] = c & 1 ? L[c / 2].y : L[c / 2].x;
+    const float sum_here = across_lanes<COLS>(sums, lane, [](float x, float y) { return x + y; });
+    const int col = col0 + (lane & (COLS - 1));
+    const bool first = (lane & 15) < COLS;
+    if (first) ctl->part[quarter][col] = sum_here;
+    group_sync(group);
+    if (quarter == 0 && first) {
+      const int row = row0 + col;
       const float sum = (ctl->part[0][col] + ctl->part[1][col]) + (ctl->part[2][col] + ctl->part[3][col]);
       const uint64_t to = ctl->out[col];
       // a whole row is 0 where it sees nothing, NaN where all of its scores are -inf (a part may well hold nothing)
@@ -404,28 +580,28 @@ __global__ void __launch_bounds__(THREADS, 1)
           bdkv::store_lse(o, sum == 0.f ? -INFINITY : ctl->ref[col] + log2f(sum));
       }
     }
-    half_sync(half);
-    if (n > 0 && ok) ok = wait(ctl->o_done, 0);
+    group_sync(group);
+    if (n > 0 && ok) wait(ctl->o_drain, 0);
     bd::tc_fence_after();
     for (int s = 0; s < n_pairs; ++s) {
-      float o[32];
+      float o[WIDE];
       __syncwarp();
       if (n > 0)
-        bd::tmem_ld32(o_at + s * ROWS, o);
+        tmem_load<WIDE>(o_at + s * N, o);
       else
 #pragma unroll
-        for (int c = 0; c < 32; ++c) o[c] = 0.f;
-      const int d = s * 128 + token;
+        for (int c = 0; c < WIDE; ++c) o[c] = 0.f;
+      const int d = s * 128 + quarter * 32 + lane;
       if (d < a.dim)
 #pragma unroll
-        for (int c = 0; c < 32; ++c) {
-          const uint64_t to = ctl->out[half * 32 + c];
-          const float x = o[c] * ctl->scale[half * 32 + c];
+        for (int c = 0; c < WIDE; ++c) {
+          const uint64_t to = ctl->out[group * WIDE + c];
+          const float y = o[c] * ctl->scale[group * WIDE + c];
           if (to & 1)
-            reinterpret_cast<float*>(to & ~uint64_t(1))[d] = x;
+            reinterpret_cast<float*>(to & ~uint64_t(1))[d] = y;
           else if (to != 0)
-            reinterpret_cast<uint16_t*>(to)[d] = static_cast<uint16_t>(a.f16 ? F16::from_float2(make_float2(x, 0.f))
-                                                                            : Bf16::from_float2(make_float2(x, 0.f)));
+            reinterpret_cast<uint16_t*>(to)[d] = static_cast<uint16_t>(a.f16 ? F16::from_float2(make_float2(y, 0.f))
+                                                                            : Bf16::from_float2(make_float2(y, 0.f)));
         }
     }
   }
@@ -434,17 +610,24 @@ __global__ void __launch_bounds__(THREADS, 1)
   bd::tc_fence_before();
   __syncthreads();
   bd::tc_fence_after();
-  if (warp == MMA_WARP) bd::tmem_dealloc(tmem, tmem_columns(n_pairs));
+  if (warp == VALUE_WARP) bd::tmem_dealloc(tmem, tmem_columns<N>(n_pairs));
+}
+
+template <int N>
+cudaError_t launch(const LatentArgs& p, const CUtensorMap& latent, const CUtensorMap& rope, cudaStream_t st) {
+  static std::atomic<bool> ready[64];  // by device
+  if (cudaError_t e = bdkv::allow_smem(latent_attn_kernel<N>, 232448, ready); e != cudaSuccess) return e;
+  const Layout l = layout<N>(p.a.dim);
+  const dim3 grid((p.a.max_q * p.a.group + N - 1) / N, p.a.n_split, p.a.n_seq);
+  latent_attn_kernel<N><<<grid, N == 64 ? 352 : 224, l.bytes, st>>>(p, l.stages, l.tiles, latent, rope);
+  return cudaGetLastError();
 }
 
 }  // namespace
 
 cudaError_t launch_latent_attn(const LatentArgs& p, const CUtensorMap& latent, const CUtensorMap& rope, cudaStream_t st) {
-  static std::atomic<bool> ready[64];  // by device
-  if (cudaError_t e = bdkv::allow_smem(latent_attn_kernel, smem_bytes(MAX_PAIRS), ready); e != cudaSuccess) return e;
-  const dim3 grid((p.a.max_q * p.a.group + ROWS - 1) / ROWS, p.a.n_split, p.a.n_seq);
-  latent_attn_kernel<<<grid, THREADS, smem_bytes((p.a.dim + 127) / 128), st>>>(p, latent, rope);
-  return cudaGetLastError();
+  return p.rows == 16 ? launch<16>(p, latent, rope, st) : p.rows == 32 ? launch<32>(p, latent, rope, st)
+                                                                       : launch<64>(p, latent, rope, st);
 }
 
 cudaError_t latent_status(cudaStream_t st, uint32_t* bits) {

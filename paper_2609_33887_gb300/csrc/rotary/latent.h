@@ -17,9 +17,9 @@ cudaError_t launch_latent_write(const bdrot_latent& c, const bdkv_rows& latent, 
 struct LatentArgs {
   bdkv::AttnArgs a;
   int rope_dim;
+  int rows;  // (queries x heads) of a CTA: 16, 32 or 64
 };
-constexpr int ROWS = 64;     // rows (queries x heads) of a CTA
-constexpr int TOKENS = 128;  // cached tokens of a tile
+constexpr int TOKENS = 64;  // cached tokens of a tile
 cudaError_t launch_latent_attn(const LatentArgs& p, const CUtensorMap& latent, const CUtensorMap& rope, cudaStream_t st);
 cudaError_t launch_latent_join(const LatentArgs& p, cudaStream_t st);
 cudaError_t latent_status(cudaStream_t st, uint32_t* bits);

@@ -129,7 +129,7 @@ int check_attention(const bdrot_latent* cache, const bdrot_latent_attention_args
 // How a call is split along the cache.
 struct Plan {
   bool longest_first;
-  int chunk, n_split;
+  int rows, chunk, n_split;
   int64_t part_rows;  // rows of partial results
   size_t bytes;       // of workspace
 };
@@ -139,7 +139,8 @@ struct Plan {
 Plan make_plan(const bdrot_latent& c, const bdrot_latent_attention_args& a, int sms) {
   Plan p = {};
   const int64_t rows = int64_t(a.max_q_len) * a.n_heads;
-  const int64_t ctas = (rows + bdrot::ROWS - 1) / bdrot::ROWS * a.n_seq;
+  p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  const int64_t ctas = (rows + p.rows - 1) / p.rows * a.n_seq;
   const bool few = a.n_seq <= 2;
   const int64_t finer = std::min<int64_t>((3 * int64_t(sms) + ctas - 1) / ctas, a.max_kv_len / 1024);
   const int64_t parts = few || ctas >= sms ? sms / ctas : std::max<int64_t>(sms / ctas, finer);
@@ -192,7 +193,7 @@ bdrot::LatentArgs latent_args(const bdrot_latent& c, const bdrot_latent_attentio
   r.n_pages = c.n_pages;
   while ((1 << r.page_shift) < c.page_size) ++r.page_shift;
   r.dim = c.latent_dim, r.n_kv = 1, r.group = a.n_heads;
-  p.rope_dim = c.rope_dim;
+  p.rope_dim = c.rope_dim, p.rows = plan.rows;
   r.q = a.q.data, r.q_tok = a.q.stride_token, r.q_head = a.q.stride_head;
   r.out = a.out.data, r.o_tok = a.out.stride_token, r.o_head = a.out.stride_head;
   r.lse = a.lse;
