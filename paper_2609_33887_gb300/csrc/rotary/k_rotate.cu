@@ -9,7 +9,7 @@ namespace {
 
 template <class T>
 __global__ void __launch_bounds__(ROTATE_THREADS) rotate_kernel(RotateArgs a) {
-  rotate_rows<T, 4>(a, blockIdx.x);
+  rotate_rows<T, 4>(a, blockIdx.x, threadIdx.x);
 }
 
 }  // namespace

@@ -1,9 +1,14 @@
 // bdrot_write: keys turned on their way into the 8-bit cache, and the queries of the same tokens turned by further CTAs
 // of the same launch.
 //
-// The write is that of the cache library (cache/write_rows.cuh), whose key rows are turned as they are read and rounded
-// to their type, so that its scales and codes are those of rows turned before. A thread reads the eight elements that
-// its own are paired with as well (they are in L1 then: their own thread reads them at the same time).
+// A CTA takes a few rows (a chunk) and some heads, one head after another, and does every run that starts among them, as
+// the cache library's write does (cache/write_rows.cuh: runs, scales, tokens that are not finite). A thread has one or
+// two pieces of a row, 16 elements each: of keys, the eight pairs that are turned together, whose sines and cosines it
+// keeps for all heads. Turned keys are rounded to their type before their magnitudes and codes are taken, so that scales
+// and codes are those of rows turned before. The next head's rows are on their way while a head's scales are agreed on.
+// Bound by instructions and bytes. (Threads that compute sines and cosines for each head, or read them from shared memory
+// with a thread to eight elements: 823 and 683 us for 131072 tokens of 32 + 2 x 8 heads.)
+// Pages of 256 tokens go the cache library's way, with keys turned as they are read.
 #include "cache/write_rows.cuh"
 #include "rotary/rotary.cuh"
 
@@ -11,13 +16,16 @@ namespace bdrot {
 namespace {
 
 using bdkv::WRITE_THREADS;
+// Threads for which a run's rows, of up to eight pieces each, are two pieces to a thread.
+constexpr int threads_for(int page_size) { return page_size <= 64 ? 256 : 512; }
 static_assert(WRITE_THREADS == ROTATE_THREADS, "CTAs of both kinds in one launch");
 
+// ---------------------------------------------------------------------------------------------------- large pages --
 template <class T>
 struct TurnedRows {
   Turn turn;
   __device__ __forceinline__ uint4 operator()(const uint16_t* p, int64_t row, int sub, int w) const {
-    uint4 x = *reinterpret_cast<const uint4*>(p);
+    const uint4 x = *reinterpret_cast<const uint4*>(p);
     const int e = sub * 8, half = turn.dim / 2;
     if (w != 0 || e >= turn.dim) return x;
     const int position = turn.positions[row];
@@ -26,9 +34,8 @@ struct TurnedRows {
 #pragma unroll
       for (int i = 0; i < 4; i += 2) {
         const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(turn.turns + sub * 4 + i);
-        const float2 s = cos_sin(turn, f.x, position), t = cos_sin(turn, f.y, position);
-        u[i] = T::from_float2(turn_pair(T::to_float2(u[i]), s));
-        u[i + 1] = T::from_float2(turn_pair(T::to_float2(u[i + 1]), t));
+        u[i] = T::from_float2(turn_pair(T::to_float2(u[i]), cos_sin(turn, f.x, position)));
+        u[i + 1] = T::from_float2(turn_pair(T::to_float2(u[i + 1]), cos_sin(turn, f.y, position)));
       }
     } else {
       const bool second = e >= half;
@@ -47,12 +54,202 @@ struct TurnedRows {
   }
 };
 
+// ---------------------------------------------------------------------------------------------------- small pages --
+// A piece: 16 elements of a row, in two groups of eight.
+struct Piece {
+  uint4 a, b;
+};
+__device__ __forceinline__ uint32_t top_of(const Piece& x) {
+  const uint32_t t = __vmaxu2(bdkv::top_of(x.a), bdkv::top_of(x.b));
+  return max(t & 0xffffu, t >> 16);
+}
 template <class T>
-__global__ void __launch_bounds__(WRITE_THREADS, 3) write_turned_kernel(bdkv::WriteArgs a, Turn turn, int64_t writes, RotateArgs q) {
-  if (blockIdx.x < writes)
-    bdkv::write_rows<T>(a, TurnedRows<T>{turn}, blockIdx.x);
+__device__ __forceinline__ uint2 codes_of(uint4 x, float f) {
+  using namespace bdkv;
+  return make_uint2(e4m3x4(scaled(T::to_float2(x.x), f), scaled(T::to_float2(x.y), f)),
+                    e4m3x4(scaled(T::to_float2(x.z), f), scaled(T::to_float2(x.w), f)));
+}
+// Codes held under one scale, under a larger one.
+__device__ __forceinline__ uint32_t rescaled(uint32_t x, float g) {
+  using namespace bdkv;
+  uint32_t lo, hi;
+  decode4(x, lo, hi);
+  return e4m3x4(scaled(bdkv::F16::to_float2(lo), g), scaled(bdkv::F16::to_float2(hi), g));
+}
+
+template <class T, bool INTER, int THREADS>
+__device__ __forceinline__ void write_turned(const bdkv::WriteArgs& a, const Turn& turn, int heads, uint32_t block) {
+  using namespace bdkv;
+  constexpr uint32_t INF = std::is_same<T, bdkv::Bf16>::value ? 0x7f80u : 0x7c00u;
+  constexpr int WARPS = THREADS / 32, PAGE = THREADS / 4;
+  __shared__ int64_t sl[2 * PAGE + 64];   // slots, from page_size rows before the chunk to as many behind
+  __shared__ uint32_t top[2][2][WARPS];   // of the heads in turn: keys' and values' largest patterns
+  __shared__ uint8_t bad[PAGE];      // a run's rows with something that is not finite
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, page_size = a.c.page_size;
+  const int groups = (a.c.n_heads + heads - 1) / heads;
+  const int h0 = static_cast<int>(block % groups) * heads, h_end = min(h0 + heads, a.c.n_heads);
+  const int64_t r0 = static_cast<int64_t>(block / groups) * a.chunk, first = r0 - page_size;
+  for (int i = tid; i < 2 * page_size + a.chunk; i += THREADS) {
+    const int64_t r = first + i;
+    const int64_t s = r >= 0 && r < a.n_tokens ? a.slots[r] : -1;
+    sl[i] = s < a.n_slots ? s : -1;
+  }
+  __syncthreads();
+  uint64_t starts = 0;  // rows of the chunk that start a run
+#pragma unroll
+  for (int part = 0; part < 2; ++part) {
+    const int t = part * 32 + lane;
+    const int64_t s = t < a.chunk ? sl[page_size + t] : -1;
+    bool begins = s >= 0;
+    if (begins) {
+      const int off = static_cast<int>(s & (page_size - 1));
+      int d = 1;  // to the row before that is stored at all
+      while (d <= off && sl[page_size + t - d] < 0) ++d;
+      begins = d > off || sl[page_size + t - d] != s - d;
+    }
+    starts |= static_cast<uint64_t>(__ballot_sync(~0u, begins)) << (part * 32);
+  }
+
+  const int units = a.c.head_dim / 16;
+  int t_of[2], u_of[2], e0[2], e1[2];  // a piece's row of the run and place in it; where keys' two groups begin
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    t_of[i] = (tid + i * THREADS) / units, u_of[i] = tid + i * THREADS - t_of[i] * units;
+    const bool halves = !INTER && u_of[i] * 16 < turn.dim;
+    e0[i] = halves ? u_of[i] * 8 : u_of[i] * 16, e1[i] = halves ? turn.dim / 2 + u_of[i] * 8 : u_of[i] * 16 + 8;
+  }
+  int buf = 0;
+  for (; starts != 0; starts &= starts - 1) {
+    const int at = page_size + __ffsll(static_cast<long long>(starts)) - 1;
+    const int64_t slot = sl[at], page = slot >> a.shift, row = first + at;
+    const int off = static_cast<int>(slot & (page_size - 1)), n = page_size - off;
+    bool live[2];
+    Piece k[2], v[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) live[i] = t_of[i] < n && sl[at + t_of[i]] == slot + t_of[i];
+    const auto load = [&](int h) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        k[i].a = k[i].b = v[i].a = v[i].b = make_uint4(0, 0, 0, 0);
+        if (!live[i]) continue;
+        const uint16_t* p = a.k + (row + t_of[i]) * a.k_tok + h * a.k_head;
+        const uint16_t* q = a.v + (row + t_of[i]) * a.v_tok + h * a.v_head + u_of[i] * 16;
+        k[i].a = *reinterpret_cast<const uint4*>(p + e0[i]), k[i].b = *reinterpret_cast<const uint4*>(p + e1[i]);
+        v[i].a = *reinterpret_cast<const uint4*>(q), v[i].b = *reinterpret_cast<const uint4*>(q + 8);
+      }
+    };
+    load(h0);
+    float2 cs[2][8];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (live[i] && u_of[i] * 16 < turn.dim) {
+        const int position = turn.positions[row + t_of[i]];
+#pragma unroll
+        for (int x = 0; x < 8; x += 2) {
+          const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(turn.turns + u_of[i] * 8 + x);
+          cs[i][x] = cos_sin(turn, f.x, position);
+          cs[i][x + 1] = cos_sin(turn, f.y, position);
+        }
+      } else {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) cs[i][x] = make_float2(1.f, 0.f);
+      }
+    for (int h = h0; h < h_end; ++h, buf ^= 1) {
+      uint8_t* k_scale = a.c.k_scale + page * a.c.k_scale_stride + h;
+      uint8_t* v_scale = a.c.v_scale + page * a.c.v_scale_stride + h;
+      const int k_before = off != 0 ? *k_scale : 0, v_before = off != 0 ? *v_scale : 0;
+      Piece x[2], y[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        x[i] = k[i], y[i] = v[i];
+        if (u_of[i] * 16 < turn.dim) turn8<T, INTER>(x[i].a, x[i].b, cs[i]);
+      }
+      uint32_t k_top = max(top_of(x[0]), top_of(x[1])), v_top = max(top_of(y[0]), top_of(y[1]));
+      const auto agree = [&](uint32_t k_most, uint32_t v_most) {
+        const uint32_t k_warp = __reduce_max_sync(~0u, k_most), v_warp = __reduce_max_sync(~0u, v_most);
+        if (lane == 0) top[buf][0][warp] = k_warp, top[buf][1][warp] = v_warp;
+      };
+      agree(k_top, v_top);
+      if (h + 1 < h_end) load(h + 1);
+      const bool some_bad = __syncthreads_or(k_top >= INF || v_top >= INF);
+      if (some_bad) {  // such rows do not count for either tensor's scale: find them, and the largest of the others
+        if (tid < page_size) bad[tid] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (top_of(x[i]) >= INF || top_of(y[i]) >= INF) bad[t_of[i]] = 1;
+        __syncthreads();
+        k_top = v_top = 0;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (live[i] && !bad[t_of[i]]) k_top = max(k_top, top_of(x[i])), v_top = max(v_top, top_of(y[i]));
+        agree(k_top, v_top);
+        __syncthreads();
+      }
+      uint32_t k_most = 0, v_most = 0;
+#pragma unroll
+      for (int i = 0; i < WARPS; ++i) k_most = max(k_most, top[buf][0][i]), v_most = max(v_most, top[buf][1][i]);
+      const int k_e = max(scale_byte(T::to_float2(k_most).x), k_before), v_e = max(scale_byte(T::to_float2(v_most).x), v_before);
+      const float k_f = pow2i(127 - k_e), v_f = pow2i(127 - v_e);
+      uint8_t* k_codes = a.c.k + page * a.c.k_stride[0] + h * a.c.k_stride[2];
+      uint8_t* v_codes = a.c.v + page * a.c.v_stride[0] + h * a.c.v_stride[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (!live[i]) continue;
+        uint2 ka = codes_of<T>(x[i].a, k_f), kb = codes_of<T>(x[i].b, k_f);
+        uint2 va = codes_of<T>(y[i].a, v_f), vb = codes_of<T>(y[i].b, v_f);
+        if (some_bad && bad[t_of[i]]) {
+          ka.x = ka.y = kb.x = kb.y = 0x7f7f7f7fu;
+          va.x = va.y = vb.x = vb.y = 0u;
+        }
+        uint8_t* p = k_codes + (off + t_of[i]) * a.c.k_stride[1];
+        if (INTER) {
+          *reinterpret_cast<uint4*>(p + u_of[i] * 16) = make_uint4(ka.x, ka.y, kb.x, kb.y);
+        } else {
+          *reinterpret_cast<uint2*>(p + e0[i]) = ka;
+          *reinterpret_cast<uint2*>(p + e1[i]) = kb;
+        }
+        *reinterpret_cast<uint4*>(v_codes + (off + t_of[i]) * a.c.v_stride[1] + u_of[i] * 16) = make_uint4(va.x, va.y, vb.x, vb.y);
+      }
+      // the tokens that the page holds already
+      const auto again = [&](uint8_t* codes, int64_t cell, int before, int e) {
+        const float g = before - e < -126 ? 0.f : pow2i(before - e);
+        for (int i = tid; i < off * units; i += THREADS) {
+          uint4* p = reinterpret_cast<uint4*>(codes + i / units * cell + i % units * 16);
+          const uint4 w = *p;
+          *p = make_uint4(rescaled(w.x, g), rescaled(w.y, g), rescaled(w.z, g), rescaled(w.w, g));
+        }
+      };
+      if (off != 0 && k_e > k_before) again(k_codes, a.c.k_stride[1], k_before, k_e);
+      if (off != 0 && v_e > v_before) again(v_codes, a.c.v_stride[1], v_before, v_e);
+      if (tid == 0) {  // (read by all before the barrier above)
+        if (k_e != k_before) *k_scale = static_cast<uint8_t>(k_e);
+        if (v_e != v_before) *v_scale = static_cast<uint8_t>(v_e);
+      }
+      if (some_bad) __syncthreads();  // `bad` is free again; `top` alternates
+    }
+  }
+}
+
+template <class T, int THREADS>
+__global__ void __launch_bounds__(THREADS, 512 / THREADS)
+    write_turned_kernel(bdkv::WriteArgs a, Turn turn, int heads, uint32_t writes, RotateArgs q) {
+  constexpr uint32_t PER = THREADS / ROTATE_THREADS;  // blocks of rows of queries
+  if (blockIdx.x >= writes)
+    rotate_rows<T, 4>(q, (blockIdx.x - writes) * PER + threadIdx.x / ROTATE_THREADS, threadIdx.x % ROTATE_THREADS);
+  else if (turn.inter)
+    write_turned<T, true, THREADS>(a, turn, heads, blockIdx.x);
   else
-    rotate_rows<T, 2>(q, blockIdx.x - static_cast<uint32_t>(writes));
+    write_turned<T, false, THREADS>(a, turn, heads, blockIdx.x);
+}
+
+template <class T>
+__global__ void __launch_bounds__(WRITE_THREADS, 3)
+    write_turned_large_kernel(bdkv::WriteArgs a, Turn turn, uint32_t writes, RotateArgs q) {
+  if (blockIdx.x >= writes)
+    rotate_rows<T, 2>(q, blockIdx.x - writes, threadIdx.x);
+  else
+    bdkv::write_rows<T>(a, TurnedRows<T>{turn}, blockIdx.x);
 }
 
 }  // namespace
@@ -62,13 +259,25 @@ cudaError_t launch_write(const bdkv_cache& c, const bdkv_rows& k, const bdkv_row
                          cudaStream_t st) {
   int64_t writes = 0;
   const bdkv::WriteArgs a = bdkv::write_args(c, k, v, slot_map, n_tokens, sm_count, &writes);
-  const int64_t grid = writes + q_blocks;
-  if (grid > INT32_MAX) return cudaErrorInvalidValue;
   const RotateArgs r = q != nullptr ? *q : RotateArgs{};
-  if (k.dtype == BDKV_BF16)
-    write_turned_kernel<Bf16><<<static_cast<unsigned>(grid), WRITE_THREADS, 0, st>>>(a, turn, writes, r);
-  else
-    write_turned_kernel<F16><<<static_cast<unsigned>(grid), WRITE_THREADS, 0, st>>>(a, turn, writes, r);
+  const bool bf16 = k.dtype == BDKV_BF16;
+  if (c.page_size > 128) {
+    if (writes + q_blocks > INT32_MAX) return cudaErrorInvalidValue;
+    const auto kernel = bf16 ? write_turned_large_kernel<Bf16> : write_turned_large_kernel<F16>;
+    kernel<<<static_cast<unsigned>(writes + q_blocks), WRITE_THREADS, 0, st>>>(a, turn, static_cast<uint32_t>(writes), r);
+    return cudaGetLastError();
+  }
+  // heads of a CTA: as many as leave eight CTAs to each SM
+  const int64_t chunks = writes / c.n_heads;
+  int heads = c.n_heads;
+  while (heads > 1 && chunks * ((c.n_heads + heads - 1) / heads) < 8 * sm_count) heads = (heads + 1) / 2;
+  writes = chunks * ((c.n_heads + heads - 1) / heads);
+  const int threads = threads_for(c.page_size), per = threads / ROTATE_THREADS;
+  const int64_t grid = writes + (q_blocks + per - 1) / per;
+  if (grid > INT32_MAX) return cudaErrorInvalidValue;
+  const auto kernel = threads == 256 ? (bf16 ? write_turned_kernel<Bf16, 256> : write_turned_kernel<F16, 256>)
+                                     : (bf16 ? write_turned_kernel<Bf16, 512> : write_turned_kernel<F16, 512>);
+  kernel<<<static_cast<unsigned>(grid), threads, 0, st>>>(a, turn, heads, static_cast<uint32_t>(writes), r);
   return cudaGetLastError();
 }
 

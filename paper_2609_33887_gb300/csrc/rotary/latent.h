@@ -9,7 +9,8 @@
 namespace bdrot {
 
 cudaError_t launch_latent_write(const bdrot_latent& c, const bdkv_rows& latent, const bdkv_rows& rope,
-                                const int64_t* slot_map, int64_t n_tokens, const Turn* turn, cudaStream_t st);
+                                const int64_t* slot_map, int64_t n_tokens, const Turn* turn, int sm_count,
+                                cudaStream_t st);
 
 // What the attention kernels read of one call: lengths, masks, outputs and the split as the 8-bit cache's kernels have
 // them (one key/value head, dim = latent_dim; part_l

@@ -119,8 +119,8 @@ __device__ __forceinline__ void rotate_heads(const RotateArgs& a, int64_t token,
 }
 
 template <class T, int AHEAD>
-__device__ __forceinline__ void rotate_rows(const RotateArgs& a, uint32_t block) {
-  const int tokens = ROTATE_THREADS / a.units, local = threadIdx.x / a.units, u = threadIdx.x - local * a.units;
+__device__ __forceinline__ void rotate_rows(const RotateArgs& a, uint32_t block, int thread) {
+  const int tokens = ROTATE_THREADS / a.units, local = thread / a.units, u = thread - local * a.units;
   const uint32_t at = block / a.groups, group = block - at * a.groups;
   const int64_t token = static_cast<int64_t>(at) * tokens + local;
   if (local >= tokens || token >= a.n_tokens) return;

@@ -287,7 +287,7 @@ int bdrot_latent_write(const bdrot_rotary* rotary, const bdrot_latent* cache, co
   bdrot::Turn turn = {};
   if (rotary) turn = turn_of(*rotary, positions, false);
   return cuda_status(bdrot::launch_latent_write(*cache, *latent, *rope, slot_map, n_tokens, rotary ? &turn : nullptr,
-                                                static_cast<cudaStream_t>(stream)));
+                                                sms, static_cast<cudaStream_t>(stream)));
 }
 
 size_t bdrot_latent_attention_workspace(const bdrot_latent* cache, const bdrot_latent_attention_args* args) {

@@ -16,7 +16,7 @@ from typing import NamedTuple, Optional
 
 import torch
 
-from .bdcommit import _stream_handle
+from .bdcommit import BD_OK, BdError, _stream_handle
 from .kvcache import (_DT, ROWS_FIELDS, KvCache, _allocate_on, _cache_fields, _check, _out_fields, _rows_fields, _same_gpu,
                       _table, _vector)
 
@@ -115,43 +115,50 @@ def kv_latent_cache(n_pages: int, page_size: int, latent_dim: int, rope_dim: int
 
 def _rotary_fields(r: KvRotary) -> bytes:
     turns, scale, interleaved = r
-    return ROTARY_FIELDS.pack(_vector(turns, torch.int64, None, "turns"), 2 * turns.numel(), bool(interleaved), scale)
+    if turns.dtype is not torch.int64 or not turns.is_contiguous():
+        raise ValueError("turns must be a contiguous torch.int64 tensor")
+    return ROTARY_FIELDS.pack(turns.data_ptr(), 2 * turns.numel(), bool(interleaved), scale)
 
 
 def _latent_fields(c: KvLatent) -> bytes:
     latent, rope = c
-    n_pages, page_size, dim = latent.shape
-    if rope.dim() != 3 or rope.shape[:2] != latent.shape[:2] or rope.dtype != latent.dtype or latent.dtype not in _DT:
+    shape, rope_shape, dtype = latent.shape, rope.shape, _DT.get(latent.dtype)
+    if len(shape) != 3 or len(rope_shape) != 3 or rope_shape[:2] != shape[:2] or rope.dtype is not latent.dtype or dtype is None:
         raise ValueError("latent and rope must be bfloat16 or float16, [n_pages, page_size, latent_dim] and "
                          "[n_pages, page_size, rope_dim]")
     lp, lt, l1 = latent.stride()
     rp, rt, r1 = rope.stride()
     if l1 != 1 or r1 != 1:
         raise ValueError("the last dimension of latent and rope must be contiguous")
-    return LATENT_FIELDS.pack(latent.data_ptr(), rope.data_ptr(), _DT[latent.dtype], page_size, n_pages, dim,
-                              rope.shape[2], lp, lt, rp, rt)
+    n_pages, page_size, dim = shape
+    return LATENT_FIELDS.pack(latent.data_ptr(), rope.data_ptr(), dtype, page_size, n_pages, dim, rope_shape[2], lp, lt, rp,
+                              rt)
 
 
-def _turned_fields(x, out, name):
-    """Rows and where they go turned. The stride of a single token says nothing."""
-    if out.shape != x.shape or out.dtype != x.dtype:
+def _turned_fields(x, shape, out, name, stream):
+    """Rows and where they go turned (allocated where out is None): their fields and the output."""
+    if out is None:
+        if stream is None:
+            out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        else:
+            out, = _allocate_on(stream, lambda: (torch.empty_like(x, memory_format=torch.contiguous_format),))
+    elif out.shape != shape or out.dtype is not x.dtype:
         raise ValueError(f"out must have {name}'s shape and type")
-    if x.shape[0] == 0 and x.dtype in _DT:  # (nor do any strides where there is none)
-        return ROWS_FIELDS.pack(0, _DT[x.dtype], 0, 0), ROWS_FIELDS.pack(0, _DT[x.dtype], 0, 0)
-    data, dtype, token, head = _rows_fields(x, name)
-    if x.shape[0] <= 1:
-        token = 0
-    o_data, _, o_token, o_head = _rows_fields(out, "out")
-    if x.shape[0] <= 1:
-        o_token = 0
-    if x.shape[1] <= 1:
+    dtype, n = _DT.get(x.dtype), shape[0]
+    if dtype is None:
+        raise ValueError(f"{name} must be bfloat16 or float16")
+    if n == 0:
+        none = ROWS_FIELDS.pack(0, dtype, 0, 0)
+        return none, none, out
+    (token, head, one), (o_token, o_head, o_one) = x.stride(), out.stride()
+    if one != 1 or o_one != 1:
+        raise ValueError(f"{name} and out must be [tokens, heads, head_dim] with head_dim contiguous")
+    if n == 1:  # (the strides of a single token, or head, say nothing)
+        token = o_token = 0
+    if shape[1] == 1:
         head = o_head = 0
-    return ROWS_FIELDS.pack(data, dtype, token, head), ROWS_FIELDS.pack(o_data, dtype, o_token, o_head)
-
-
-def _like(x, stream):
-    out, = _allocate_on(stream, lambda: (torch.empty_like(x, memory_format=torch.contiguous_format),))
-    return out
+    return (ROWS_FIELDS.pack(x.data_ptr(), dtype, token, head), ROWS_FIELDS.pack(out.data_ptr(), dtype, o_token, o_head),
+            out)
 
 
 def kv_rotate(x: torch.Tensor, positions: torch.Tensor, rotary: KvRotary, *, inverse: bool = False,
@@ -160,16 +167,16 @@ def kv_rotate(x: torch.Tensor, positions: torch.Tensor, rotary: KvRotary, *, inv
 
     inverse: turned back, with the same scale (the adjoint: gradients of the result to gradients of x). out may be x; to
     turn the last elements of a head, pass x[..., first:] for both. Returns out."""
-    if x.dim() != 3:
+    shape = x.shape
+    if len(shape) != 3:
         raise ValueError("x must be [tokens, heads, head_dim] with head_dim contiguous")
-    if out is None:
-        out = _like(x, stream)
-    fields, (xf, of) = _rotary_fields(rotary), _turned_fields(x, out, "x")
-    n, heads, dim = x.shape
-    pos = _vector(positions, torch.int32, n, "positions")
-    _same_gpu(x, positions, rotary.turns, out)
-    _check(load_library().bdrot_rotate(fields, xf, of, heads, dim, pos, n, bool(inverse), _stream_handle(stream)),
-           "bdrot_rotate")
+    n, heads, dim = shape
+    xf, of, out = _turned_fields(x, shape, out, "x", stream)
+    fields, pos = _rotary_fields(rotary), _vector(positions, torch.int32, n, "positions")
+    _same_gpu(x, positions, rotary[0], out)
+    rc = load_library().bdrot_rotate(fields, xf, of, heads, dim, pos, n, bool(inverse), _stream_handle(stream))
+    if rc != BD_OK:
+        raise BdError(rc, "bdrot_rotate")
     return out
 
 
@@ -180,33 +187,38 @@ def kv_write_rotated(k: torch.Tensor, v: torch.Tensor, slot_map: torch.Tensor, c
 
     The cache gets the codes and scales of kv_write(kv_rotate(k), v). q: [tokens, n_q_heads, head_dim], a row for each
     slot; q_out may be q. Returns the turned queries (None without q)."""
-    n = slot_map.numel()
-    if k.shape != v.shape or k.shape[2:] != cache.k.shape[3:] or k.shape[1] != cache.k.shape[2] or k.shape[0] < n:
+    n, shape, (_, _, heads, dim) = slot_map.numel(), k.shape, cache.k.shape
+    if len(shape) != 3 or shape != v.shape or shape[2] != dim or shape[1] != heads or shape[0] < n:
         raise ValueError("k and v must be [tokens, n_heads, head_dim] of the cache, a row for each slot")
     kf, vf = ROWS_FIELDS.pack(*_rows_fields(k, "k")), ROWS_FIELDS.pack(*_rows_fields(v, "v"))
-    qf = of = None
-    tensors = ()
-    if q is not None:
-        if q.dim() != 3 or q.shape[0] != n or q.shape[2] != k.shape[2]:
-            raise ValueError("q must be [tokens, n_q_heads, head_dim] of the cache, a row for each slot")
-        if q_out is None:
-            q_out = _like(q, stream)
-        qf, of = _turned_fields(q, q_out, "q")
-        tensors = (q, q_out)
-    elif q_out is not None:
-        raise ValueError("q_out without q")
     fields, slots = _cache_fields(cache), _vector(slot_map, torch.int64, None, "slot_map")
     pos, rf = _vector(positions, torch.int32, n, "positions"), _rotary_fields(rotary)
-    _same_gpu(k, v, slot_map, positions, rotary.turns, *cache, *tensors)
-    _check(load_library().bdrot_write(rf, fields, kf, vf, slots, pos, n, qf, of, 0 if q is None else q.shape[1],
-                                      _stream_handle(stream)), "bdrot_write")
+    if q is None:
+        if q_out is not None:
+            raise ValueError("q_out without q")
+        qf, of, n_q = None, None, 0
+        _same_gpu(k, v, slot_map, positions, rotary[0], *cache)
+    else:
+        q_shape = q.shape
+        if len(q_shape) != 3 or q_shape[0] != n or q_shape[2] != dim:
+            raise ValueError("q must be [tokens, n_q_heads, head_dim] of the cache, a row for each slot")
+        qf, of, q_out = _turned_fields(q, q_shape, q_out, "q", stream)
+        n_q = q_shape[1]
+        _same_gpu(k, v, slot_map, positions, rotary[0], q, q_out, *cache)
+    rc = load_library().bdrot_write(rf, fields, kf, vf, slots, pos, n, qf, of, n_q, _stream_handle(stream))
+    if rc != BD_OK:
+        raise BdError(rc, "bdrot_write")
     return q_out
 
 
-def _vectors_fields(x, dim, n, cache, name):
-    if x.dim() != 2 or x.shape[0] < n or x.shape[1] != dim or (x.shape[0] and x.stride(1) != 1) or x.dtype != cache.latent.dtype:
-        raise ValueError(f"{name} must be [tokens, {dim}] of the cache's type, a contiguous row for each slot")
-    return ROWS_FIELDS.pack(x.data_ptr(), _DT[x.dtype], x.stride(0) if x.shape[0] > 1 else 0, 0)
+def _vectors_fields(x, dim, n, dtype, name):
+    shape = x.shape
+    if len(shape) != 2 or shape[0] < n or shape[1] != dim or x.dtype is not dtype:
+        raise ValueError(f"{name} must be [tokens, {dim}] of the cache's type, a row for each slot")
+    token, one = x.stride()
+    if one != 1 and shape[0]:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    return ROWS_FIELDS.pack(x.data_ptr(), _DT[dtype], token if shape[0] > 1 else 0, 0)
 
 
 def kv_latent_write(latent: torch.Tensor, rope: torch.Tensor, slot_map: torch.Tensor, cache: KvLatent, *,
@@ -214,26 +226,26 @@ def kv_latent_write(latent: torch.Tensor, rope: torch.Tensor, slot_map: torch.Te
     """Latents [tokens, latent_dim] and key parts [tokens, rope_dim] into the cache at slot_map int64 [tokens] (negative:
     not stored; no slot twice). With rotary (of rope_dim elements), key parts are turned by positions int32 [tokens].
     Without it they are stored as they are."""
-    n = slot_map.numel()
+    n, dtype = slot_map.numel(), cache[0].dtype
     fields = _latent_fields(cache)
-    lf = _vectors_fields(latent, cache.latent.shape[2], n, cache, "latent")
-    rf = _vectors_fields(rope, cache.rope.shape[2], n, cache, "rope")
-    slots, turn, pos, tensors = _vector(slot_map, torch.int64, None, "slot_map"), None, None, ()
+    lf = _vectors_fields(latent, cache[0].shape[2], n, dtype, "latent")
+    rf = _vectors_fields(rope, cache[1].shape[2], n, dtype, "rope")
+    slots = _vector(slot_map, torch.int64, None, "slot_map")
     if (positions is None) != (rotary is None):
         raise ValueError("positions and rotary go together")
-    if rotary is not None:
+    if rotary is None:
+        turn = pos = None
+        _same_gpu(latent, rope, slot_map, *cache)
+    else:
         turn, pos = _rotary_fields(rotary), _vector(positions, torch.int32, n, "positions")
-        tensors = (positions, rotary.turns)
-    _same_gpu(latent, rope, slot_map, *cache, *tensors)
+        _same_gpu(latent, rope, slot_map, positions, rotary[0], *cache)
     _check(load_library().bdrot_latent_write(turn, fields, lf, rf, slots, pos, n, _stream_handle(stream)),
            "bdrot_latent_write")
 
 
-def _latent_attn_fields(q, out, lse, cache, block_table, kv_lens, query_start, max_q_len, max_kv_len, scale, mask_block,
-                        workspace, stream) -> bytes:
+def _latent_attn_fields(q, shape, out, lse, cache, block_table, kv_lens, query_start, max_q_len, max_kv_len, scale,
+                        mask_block, workspace, stream) -> bytes:
     n_seq = kv_lens.numel()
-    if q.dim() != 3 or q.shape[2] != cache.latent.shape[2] + cache.rope.shape[2] or q.dtype != cache.latent.dtype:
-        raise ValueError("q must be [tokens, heads, latent_dim + rope_dim] of the cache's type")
     if workspace is not None and not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous")
     table, stride, cols = _table(block_table, n_seq)
@@ -241,15 +253,23 @@ def _latent_attn_fields(q, out, lse, cache, block_table, kv_lens, query_start, m
     return LATENT_ATTN_FIELDS.pack(
         *_rows_fields(q, "q"), *out, 0 if lse is None else lse.data_ptr(), table, stride, cols,
         _vector(kv_lens, torch.int32, n_seq, "kv_lens"), _vector(query_start, torch.int32, n_seq + 1, "query_start"),
-        n_seq, q.shape[1], max_q_len, max_kv_len, mask_block, scale, ws, ws_bytes, _stream_handle(stream) or 0)
+        n_seq, shape[1], max_q_len, max_kv_len, mask_block, scale, ws, ws_bytes, _stream_handle(stream) or 0)
+
+
+def _latent_q(q, cache):
+    """(q's shape, latent_dim)."""
+    shape, dim = q.shape, cache[0].shape[2]
+    if len(shape) != 3 or shape[2] != dim + cache[1].shape[2] or q.dtype is not cache[0].dtype:
+        raise ValueError("q must be [tokens, heads, latent_dim + rope_dim] of the cache's type")
+    return shape, dim
 
 
 def kv_latent_attention_workspace(q, cache, block_table, kv_lens, query_start, *, max_q_len, max_kv_len) -> int:
     """Bytes of workspace kv_latent_attention needs for these arguments."""
-    dim = cache.latent.shape[2]
-    out = (q.data_ptr(), _DT.get(q.dtype), q.shape[1] * dim, dim)
-    args = _latent_attn_fields(q, out, None, cache, block_table, kv_lens, query_start, max_q_len, max_kv_len, 1.0, 0, None,
-                               0)
+    shape, dim = _latent_q(q, cache)
+    out = (q.data_ptr(), _DT.get(q.dtype), shape[1] * dim, dim)
+    args = _latent_attn_fields(q, shape, out, None, cache, block_table, kv_lens, query_start, max_q_len, max_kv_len, 1.0, 0,
+                               None, 0)
     return int(load_library().bdrot_latent_attention_workspace(_latent_fields(cache), args))
 
 
@@ -262,18 +282,22 @@ def kv_latent_attention(q: torch.Tensor, cache: KvLatent, block_table: torch.Ten
     Requests, masks, bounds, workspace and rows behind the last query are as in kv_attention. scale has no default: it is
     the one of the heads before their projection into the latent's space. Returns out [tokens, heads, latent_dim] of q's
     type, or (out, lse float32 [tokens, heads])."""
-    shape = (*q.shape[:2], cache.latent.shape[2])
+    shape, dim = _latent_q(q, cache)
+    n, heads, _ = shape
     if out is None:
-        out, = _allocate_on(stream, lambda: (torch.empty(shape, dtype=q.dtype, device=q.device),))
-    elif out.shape != shape or out.dtype != q.dtype:
+        if stream is None:
+            out = q.new_empty((n, heads, dim))
+        else:
+            out, = _allocate_on(stream, lambda: (q.new_empty((n, heads, dim)),))
+    elif out.shape != (n, heads, dim) or out.dtype != q.dtype:
         raise ValueError("out must be [tokens, heads, latent_dim] of q's type")
-    lse, = _allocate_on(stream, lambda: (torch.empty(q.shape[:2], dtype=torch.float32, device=q.device),)) \
-        if return_lse else (None,)
+    lse, = _allocate_on(stream, lambda: (q.new_empty((n, heads), dtype=torch.float32),)) if return_lse else (None,)
     _same_gpu(q, out, block_table, kv_lens, query_start, *cache, *(() if workspace is None else (workspace,)))
-    args = _latent_attn_fields(q, _out_fields(out), lse, cache, block_table, kv_lens, query_start, max_q_len, max_kv_len,
-                               scale, mask_block, workspace, stream)
-    fields = _latent_fields(cache)
-    _check(load_library().bdrot_latent_attention(fields, args), "bdrot_latent_attention")
+    args = _latent_attn_fields(q, shape, _out_fields(out), lse, cache, block_table, kv_lens, query_start, max_q_len,
+                               max_kv_len, scale, mask_block, workspace, stream)
+    rc = load_library().bdrot_latent_attention(_latent_fields(cache), args)
+    if rc != BD_OK:
+        raise BdError(rc, "bdrot_latent_attention")
     return (out, lse) if return_lse else out
 
 
