@@ -17,6 +17,12 @@
 // thread has one token and 8 or 16 rows, so maxima over tokens are taken across
 // threads, and only when some score exceeds its row's reference by more than
 // 2^15; sums stay with the threads until the end.
+// Work: a unit is a request's 64 rows (or 32, 16) and the tiles that the last of
+// them sees. Each CTA takes an equal share of all units' tiles, laid one behind
+// another: the end of a unit, whole units, the beginning of another (a segment
+// each). Only the device knows the lengths, so every CTA adds them up itself. Of
+// a unit in several CTAs each leaves its part, which k_latent_join.cu joins. Too
+// many units to add up: a CTA to each.
 #include "rotary/latent.h"
 
 namespace bdrot {
@@ -37,13 +43,15 @@ __device__ uint32_t g_status;  // bd::DEV_* bits
 template <int N>
 struct Ctl {
   uint64_t q_full, full[MAX_STAGES], empty[MAX_STAGES];
-  uint64_t s_full[2], p_full[2], o_done[2], s_drain, o_drain;  // (pairs: by parity of the tile)
+  uint64_t s_full[2], p_full[2], o_done[2], segment_done, s_drain, o_drain;  // (pairs: by parity of the tile)
   alignas(16) float ref[N];
   alignas(16) float factor[N];
   alignas(16) float scale[N];
   float part[4][N];  // of the warps of a token quarter: maxima, at the end sums
   int visible[N];
-  uint64_t out[N];   // where a row goes (0: nowhere); lowest bit: fp32 parts
+  uint64_t out[N];   // where a row goes (0: nowhere)
+  int starts[MAX_SHARED_SEQ + 1];  // tiles of the requests before
+  int sums[16];
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -58,7 +66,6 @@ struct Layout {
   int stages, tiles;
   size_t bytes;
 };
-__host__ __device__ constexpr int pairs_per_stage(int n_pairs) { return n_pairs < 2 ? 1 : 2; }
 template <int N>
 Layout layout(int dim) {
   Layout l;
@@ -89,6 +96,16 @@ __device__ __forceinline__ void tma_load_3d(uint32_t issue, uint32_t dst, const 
       "@q cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n\t}" ::"r"(
           dst),
       "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar), "r"(issue)
+      : "memory");
+}
+// The same of several columns of 64 elements at once: [64 elements, tokens, column, page].
+__device__ __forceinline__ void tma_load_4d(uint32_t issue, uint32_t dst, const CUtensorMap* map, uint32_t bar, int y, int column,
+                                            int page) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %6, 0;\n\t"
+      "@q cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {0, %2, %3, %4}], [%5];\n\t}" ::"r"(
+          dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(y), "r"(column), "r"(page), "r"(bar), "r"(issue)
       : "memory");
 }
 __device__ __forceinline__ void expect_bytes(uint32_t issue, uint32_t bar, uint32_t bytes) {
@@ -250,18 +267,131 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
   Ctl<N>* ctl = reinterpret_cast<Ctl<N>*>(raw + (q_at + (2 * n_pairs + 1) * Q_CHUNK - bd::smem_u32(raw)));
   const int tid = threadIdx.x, lane = tid & 31, warp = static_cast<int>(bd::warp_uniform(tid >> 5));
 
-  int seq = blockIdx.z;
-  const Seq sq = a.longest_first ? bdkv::ranked_seq<THREADS>(a, blockIdx.z, reinterpret_cast<int*>(raw), seq)
-                                 : bdkv::load_seq(a, seq);
-  // the last rows first: under a causal mask they see the most
-  const int row0 = (gridDim.x - 1 - blockIdx.x) * N, part = blockIdx.y, rows = sq.q_len * a.group;
-  if (row0 >= rows) return;
-  // later queries see at least as much: the CTA's last row bounds it, and all of its rows see what its first one does
-  const int i_first = row0 / a.group, i_last = (min(rows, row0 + N) - 1) / a.group;
-  const int begin = part * a.chunk, end = min(bdkv::visible(a, sq, i_last), begin + a.chunk);
-  if (part > 0 && end <= begin) return;
-  const int n = end > begin ? (end - begin + TOKENS - 1) / TOKENS : 0;
-  const int all_see = bdkv::visible(a, sq, i_first);
+  // ------------------------------------------------------------------ work
+  // A unit's rows and tiles; one with rows that see nothing counts as a tile, in which its zeros are written.
+  const auto rows_end = [&](const Seq& sq, int tile) { return min(sq.q_len * a.group, tile * N + N); };
+  const auto unit_sees = [&](const Seq& sq, int tile) { return bdkv::visible(a, sq, (rows_end(sq, tile) - 1) / a.group); };
+  const auto unit_tiles = [&](const Seq& sq, int tile) {
+    return tile * N >= sq.q_len * a.group ? 0 : max(1, (unit_sees(sq, tile) + TOKENS - 1) / TOKENS);
+  };
+  struct Segment {
+    Seq sq;
+    int seq, row0, begin, end, n;  // rows from row0 on; tokens; tiles
+    bool whole, first;             // of its unit; of its CTA
+  };
+  int from = 0, to = 0;  // the CTA's share
+  // the same in all lanes, and known to be: loops and products behind it then run from uniform registers
+  const auto uniform = [](int x) { return static_cast<int>(bd::warp_uniform(static_cast<uint32_t>(x))); };
+  Segment only;
+  if (p.shared) {
+    if (p.row_tiles <= 16) {
+      for (int x = tid; x < a.n_seq; x += THREADS) {
+        const Seq sq = bdkv::load_seq(a, x);
+        int sum = 0;
+        for (int t = 0; t < p.row_tiles; ++t) sum += unit_tiles(sq, t);
+        ctl->starts[x + 1] = sum;
+      }
+    } else {
+      for (int x = warp; x < a.n_seq; x += THREADS / 32) {
+        const Seq sq = bdkv::load_seq(a, x);
+        int sum = 0;
+        for (int t = lane; t < p.row_tiles; t += 32) sum += unit_tiles(sq, t);
+        sum = __reduce_add_sync(~0u, sum);
+        if (lane == 0) ctl->starts[x + 1] = sum;
+      }
+    }
+    __syncthreads();
+    if (warp == 0) {
+      constexpr int PER = MAX_SHARED_SEQ / 32;
+      int v[PER], sum = 0;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int x = lane * PER + i;
+        sum += x < a.n_seq ? ctl->starts[x + 1] : 0;
+        v[i] = sum;
+      }
+      int before = sum;
+#pragma unroll
+      for (int d = 1; d < 32; d *= 2) {
+        const int other = __shfl_up_sync(~0u, before, d);
+        if (lane >= d) before += other;
+      }
+      before -= sum;
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (lane * PER + i < a.n_seq) ctl->starts[lane * PER + i + 1] = before + v[i];
+      if (lane == 0) ctl->starts[0] = 0;
+    }
+    __syncthreads();
+    // (two tiles to a CTA where there are few)
+    const int64_t total = ctl->starts[a.n_seq], ctas = min(static_cast<int64_t>(gridDim.x), (total + 1) / 2);
+    if (static_cast<int64_t>(blockIdx.x) >= ctas) return;
+    from = static_cast<int>(blockIdx.x * total / ctas), to = static_cast<int>((blockIdx.x + 1) * total / ctas);
+  } else {
+    only.seq = blockIdx.y;
+    only.sq = a.longest_first ? bdkv::ranked_seq<THREADS>(a, blockIdx.y, reinterpret_cast<int*>(raw), only.seq)
+                              : bdkv::load_seq(a, only.seq);
+    // the last rows first: under a causal mask they see the most
+    const int tile = gridDim.x - 1 - blockIdx.x;
+    to = unit_tiles(only.sq, tile);
+    if (to == 0) return;
+    only.row0 = tile * N, only.begin = 0, only.end = unit_sees(only.sq, tile), only.n = (only.end + TOKENS - 1) / TOKENS;
+    only.whole = only.first = true;
+  }
+  from = uniform(from), to = uniform(to);
+  // The segment that begins at tile `at` of the share, which `seq` (0 at first) keeps the request of; by whole warps.
+  const auto segment = [&](int& at, int& seq) {
+    Segment g = only;
+    if (!p.shared) {
+      at = to;
+    } else {
+      g.first = at == from;
+      if (g.first) {
+        int hi = a.n_seq - 1;  // the last request that begins at `at` or before
+        while (seq < hi) {
+          const int mid = (seq + hi + 1) / 2;
+          if (ctl->starts[mid] <= at)
+            seq = mid;
+          else
+            hi = mid - 1;
+        }
+      }
+      while (ctl->starts[seq + 1] <= at) ++seq;
+      g.seq = seq, g.sq = bdkv::load_seq(a, seq);
+      int start = ctl->starts[seq], tile = 0, tiles = 0;
+      for (int t0 = 0;; t0 += 32) {  // the unit
+        const int mine = t0 + lane < p.row_tiles ? unit_tiles(g.sq, t0 + lane) : 0;
+        int upto = mine;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+          const int other = __shfl_up_sync(~0u, upto, d);
+          if (lane >= d) upto += other;
+        }
+        const uint32_t past = __ballot_sync(~0u, start + upto > at);
+        if (past != 0 || t0 + 32 >= p.row_tiles) {  // (it is there: the request ends behind `at`)
+          const int l = past != 0 ? __ffs(past) - 1 : 31;
+          tile = t0 + l, tiles = __shfl_sync(~0u, mine, l);
+          start += __shfl_sync(~0u, upto, l) - tiles;
+          break;
+        }
+        start += __shfl_sync(~0u, upto, 31);
+      }
+      const int stop = min(to, start + tiles);
+      g.row0 = tile * N;
+      g.begin = (at - start) * TOKENS, g.end = min(unit_sees(g.sq, tile), (stop - start) * TOKENS);
+      g.n = g.end > g.begin ? (g.end - g.begin + TOKENS - 1) / TOKENS : 0;
+      g.whole = at == start && stop == start + tiles;
+      if (warp == 0 && lane == 0 && at == start) {  // for the join: a split unit's first part and last CTA
+        const int64_t total = ctl->starts[a.n_seq], ctas = min(static_cast<int64_t>(gridDim.x), (total + 1) / 2);
+        p.plan[seq * p.row_tiles + tile] =
+            g.whole ? make_int2(-1, -1)
+                    : make_int2(2 * blockIdx.x + !g.first, static_cast<int>(((start + tiles) * ctas + total - 1) / total) - 1);
+      }
+      at = uniform(stop);
+    }
+    g.seq = uniform(g.seq), g.row0 = uniform(g.row0), g.begin = uniform(g.begin), g.end = uniform(g.end), g.n = uniform(g.n);
+    return g;
+  };
 
   if (tid == 0) {
     bd::mbar_init(bd::smem_u32(&ctl->q_full), SOFT);
@@ -274,22 +404,11 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
       bd::mbar_init(bd::smem_u32(&ctl->p_full[i]), SOFT_WARPS);
       bd::mbar_init(bd::smem_u32(&ctl->o_done[i]), 1);
     }
+    bd::mbar_init(bd::smem_u32(&ctl->segment_done), 1);
     bd::mbar_init(bd::smem_u32(&ctl->s_drain), 1);
     bd::mbar_init(bd::smem_u32(&ctl->o_drain), 1);
     ctl->abort_flag = 0;
     bd::fence_mbar_init();
-  }
-  if (tid < N) {
-    ctl->ref[tid] = NO_REF;
-    const int row = row0 + tid, i = row / a.group, h = row - i * a.group;
-    const int vis = row < rows ? bdkv::visible(a, sq, i) : 0;
-    ctl->visible[tid] = min(vis, end);
-    uint64_t to = 0;
-    if (row < rows) {
-      const bdkv::RowOut o = bdkv::row_out(a, sq, seq, part, i, h, vis);
-      to = o.out != nullptr ? reinterpret_cast<uint64_t>(o.out) : o.o != nullptr ? reinterpret_cast<uint64_t>(o.o) | 1u : 0u;
-    }
-    ctl->out[tid] = to;
   }
   constexpr int LOAD_WARP = SOFT_WARPS, SCORE_WARP = SOFT_WARPS + 1, VALUE_WARP = SOFT_WARPS + 2;
   if (warp == VALUE_WARP) {
@@ -311,17 +430,11 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
     // Box b of a tile: a page's tokens, or 64 tokens of a larger page; lane b finds its page. What is not there (a column
     // behind the table, a page outside the cache, tokens that no row sees) is read from behind the cache's last page, as zeros.
     const int page_size = 1 << a.page_shift, step = min(page_size, TOKENS), boxes = TOKENS / step;
-    const int32_t* table = a.table + seq * a.table_stride;
     const int outside = static_cast<int>(max(a.n_pages, static_cast<int64_t>(1)));
-    const auto find = [&](int j) {  // the page as the table has it: a tile ahead, and not looked at until it is needed
-      const int t = begin + j * TOKENS + lane * step, col = t >> a.page_shift;
-      return lane < boxes && t < end && col < a.max_blocks ? table[col] : -1;
-    };
     if (lane == 0) {
       bd::prefetch_tmap(&latent_map);
       bd::prefetch_tmap(&rope_map);
     }
-    int found = find(0), following = find(1);
     int stage = 0, round = 0, tile = 0;  // of the next load: its places, and how often the stage's was used
     bool ok = true;
     const uint32_t issue = bd::elect_one();
@@ -329,22 +442,35 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
       for (int b = 0; b < boxes; ++b)  // (more than one: whole pages)
         tma_load_3d(issue, bd::warp_uniform(dst + b * step * 128), map, bar, x, y, __shfl_sync(~0u, page, b));
     };
-    for (int j = 0; ok && j < n; ++j) {
-      const int y = static_cast<int>(bd::warp_uniform((begin + j * TOKENS) & (page_size - 1)));
-      const int page = found >= 0 && found < a.n_pages ? found : outside;
-      found = following;
-      following = find(j + 2);
-      for (int s = 0; s < n_pairs; s += per_stage) {
-        if (!(ok = wait(ctl->empty[stage], round + 1))) break;
-        const int pairs = min(per_stage, n_pairs - s);
-        const bool last = s + per_stage >= n_pairs;
-        const uint32_t bar = bd::warp_uniform(bd::smem_u32(&ctl->full[stage])), dst = kv_at + stage * stage_bytes;
-        expect_bytes(issue, bar, pairs * PAIR + (last ? CHUNK : 0));
-        for (int c = 0; c < 2 * pairs; ++c) load(&latent_map, dst + c * CHUNK, bar, (2 * s + c) * 64, y, page);
-        if (last) load(&rope_map, rope_at + tile * CHUNK, bar, 0, y, page);
-        if (++stage == stages) stage = 0, ++round;
+    for (int at = from, seq = 0; ok && at < to;) {
+      const Segment g = segment(at, seq);
+      const int32_t* table = a.table + g.seq * a.table_stride;
+      const auto find = [&](int j) {  // the page as the table has it: a tile ahead, and not looked at until it is needed
+        const int t = g.begin + j * TOKENS + lane * step, col = t >> a.page_shift;
+        return lane < boxes && t < g.end && col < a.max_blocks ? table[col] : -1;
+      };
+      int found = find(0), following = find(1);
+      for (int j = 0; ok && j < g.n; ++j) {
+        const int y = static_cast<int>(bd::warp_uniform((g.begin + j * TOKENS) & (page_size - 1)));
+        const int page = found >= 0 && found < a.n_pages ? found : outside;
+        found = following;
+        following = find(j + 2);
+        for (int s = 0; s < n_pairs; s += per_stage) {
+          if (!(ok = wait(ctl->empty[stage], round + 1))) break;
+          const bool last = s + per_stage >= n_pairs;
+          const uint32_t bar = bd::warp_uniform(bd::smem_u32(&ctl->full[stage])), dst = bd::warp_uniform(kv_at + stage * stage_bytes);
+          const int pairs = min(per_stage, n_pairs - s);
+          // (columns behind the latents' last are read as zeros)
+          expect_bytes(issue, bar, (p.columns ? stage_bytes : pairs * PAIR) + (last ? CHUNK : 0));
+          if (p.columns)
+            tma_load_4d(issue, dst, &latent_map, bar, y, 2 * s, __shfl_sync(~0u, page, 0));
+          else
+            for (int c = 0; c < 2 * pairs; ++c) load(&latent_map, dst + c * CHUNK, bar, (2 * s + c) * 64, y, page);
+          if (last) load(&rope_map, rope_at + tile * CHUNK, bar, 0, y, page);
+          if (++stage == stages) stage = 0, ++round;
+        }
+        if (++tile == tiles) tile = 0;
       }
-      if (++tile == tiles) tile = 0;
     }
     // nothing is on its way when the CTA ends (all of it has been waited for, unless a wait gave up)
     __syncwarp();
@@ -362,31 +488,35 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
     const uint32_t q_lo = bd::warp_uniform(static_cast<uint32_t>(bd::sw128_kmajor_desc(q_at)));
     const uint32_t k_lo = bd::warp_uniform(static_cast<uint32_t>(bd::sw128_kmajor_desc(kv_at)));
     const uint32_t r_lo = bd::warp_uniform(static_cast<uint32_t>(bd::sw128_kmajor_desc(rope_at)));
-    int stage = 0, round = 0, tile = 0;
-    bool ok = n > 0 && wait(ctl->q_full, 0);
-    for (int j = 0; ok && j < n; ++j) {
-      // over the scores of two tiles before, which have become weights
-      if (j >= 2 && !(ok = wait(ctl->p_full[j & 1], (j - 2) >> 1))) break;
-      const uint32_t s_at = bd::warp_uniform(tmem + (j & 1) * N);
-      for (int s = 0; s < n_pairs; s += per_stage) {
-        if (!(ok = wait(ctl->full[stage], round))) break;
-        bd::tc_fence_after();
-        for (int u = 0; u < per_stage && s + u < n_pairs; ++u) {
-          const uint32_t kd = bd::warp_uniform(k_lo + ((stage * stage_bytes + u * PAIR) >> 4));
-          const uint32_t qd = bd::warp_uniform(q_lo + (s + u) * (2 * Q_CHUNK >> 4));
+    int stage = 0, round = 0, tile = 0, t = 0, segments = 0;  // (t: the CTA's tile)
+    bool ok = true;
+    for (int at = from, seq = 0; ok && at < to;) {
+      const Segment g = segment(at, seq);
+      if (g.n > 0) ok = wait(ctl->q_full, segments++);
+      for (int j = 0; ok && j < g.n; ++j, ++t) {
+        // over the scores of two tiles before, which have become weights
+        if (t >= 2 && !(ok = wait(ctl->p_full[t & 1], (t - 2) >> 1))) break;
+        const uint32_t s_at = bd::warp_uniform(tmem + (t & 1) * N);
+        for (int s = 0; s < n_pairs; s += per_stage) {
+          if (!(ok = wait(ctl->full[stage], round))) break;
+          bd::tc_fence_after();
+          for (int u = 0; u < per_stage && s + u < n_pairs; ++u) {
+            const uint32_t kd = bd::warp_uniform(k_lo + ((stage * stage_bytes + u * PAIR) >> 4));
+            const uint32_t qd = bd::warp_uniform(q_lo + (s + u) * (2 * Q_CHUNK >> 4));
 #pragma unroll
-          for (int k = 0; k < 8; ++k)
-            mma(issue, s_at, kd + (k / 4) * (CHUNK >> 4) + 2u * (k % 4), qd + (k / 4) * (Q_CHUNK >> 4) + 2u * (k % 4), DESC_HI,
-                DESC_HI, idesc, (s | u | k) != 0);
+            for (int k = 0; k < 8; ++k)
+              mma(issue, s_at, kd + (k / 4) * (CHUNK >> 4) + 2u * (k % 4), qd + (k / 4) * (Q_CHUNK >> 4) + 2u * (k % 4), DESC_HI,
+                  DESC_HI, idesc, (s | u | k) != 0);
+          }
+          if (++stage == stages) stage = 0, ++round;
         }
-        if (++stage == stages) stage = 0, ++round;
-      }
-      if (!ok) break;
-      const uint32_t rd = bd::warp_uniform(r_lo + tile * (CHUNK >> 4)), qr = bd::warp_uniform(q_lo + n_pairs * (2 * Q_CHUNK >> 4));
+        if (!ok) break;
+        const uint32_t rd = bd::warp_uniform(r_lo + tile * (CHUNK >> 4)), qr = bd::warp_uniform(q_lo + n_pairs * (2 * Q_CHUNK >> 4));
 #pragma unroll
-      for (int k = 0; k < 4; ++k) mma(issue, s_at, rd + 2u * k, qr + 2u * k, DESC_HI, DESC_HI, idesc, 1);
-      mma_commit(issue, bd::smem_u32(&ctl->s_full[j & 1]));
-      if (++tile == tiles) tile = 0;
+        for (int k = 0; k < 4; ++k) mma(issue, s_at, rd + 2u * k, qr + 2u * k, DESC_HI, DESC_HI, idesc, 1);
+        mma_commit(issue, bd::smem_u32(&ctl->s_full[t & 1]));
+        if (++tile == tiles) tile = 0;
+      }
     }
     mma_commit(issue, bd::smem_u32(&ctl->s_drain));  // all of its products have completed once it flips
     __syncwarp();
@@ -396,23 +526,29 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
     const uint32_t issue = bd::elect_one();
     const uint32_t idesc = bd::warp_uniform(bd::idesc_f16_f32(128, N) | (a.f16 ? 0u : (1u << 7) | (1u << 10)) | A_MN_MAJOR | B_MN_MAJOR);
     const uint32_t v_lo = bd::warp_uniform(mn_low(kv_at, CHUNK)), p_lo = bd::warp_uniform(mn_low(rope_at, CHUNK));
-    int stage = 0, tile = 0;
-    for (int j = 0; j < n && wait(ctl->p_full[j & 1], j >> 1); ++j) {
-      bd::tc_fence_after();
-      const uint32_t pd = bd::warp_uniform(p_lo + tile * (CHUNK >> 4));
-      for (int s = 0; s < n_pairs; s += per_stage) {
-        for (int u = 0; u < per_stage && s + u < n_pairs; ++u) {
-          const uint32_t vd = bd::warp_uniform(v_lo + ((stage * stage_bytes + u * PAIR) >> 4));
-          const uint32_t od = bd::warp_uniform(tmem + O_COL + (s + u) * N);
+    int stage = 0, tile = 0, t = 0;
+    bool ok = true;
+    for (int at = from, seq = 0; ok && at < to;) {
+      const Segment g = segment(at, seq);
+      for (int j = 0; j < g.n; ++j, ++t) {
+        if (!(ok = wait(ctl->p_full[t & 1], t >> 1))) break;
+        bd::tc_fence_after();
+        const uint32_t pd = bd::warp_uniform(p_lo + tile * (CHUNK >> 4));
+        for (int s = 0; s < n_pairs; s += per_stage) {
+          for (int u = 0; u < per_stage && s + u < n_pairs; ++u) {
+            const uint32_t vd = bd::warp_uniform(v_lo + ((stage * stage_bytes + u * PAIR) >> 4));
+            const uint32_t od = bd::warp_uniform(tmem + O_COL + (s + u) * N);
 #pragma unroll
-          for (int k = 0; k < TOKENS / 16; ++k)
-            mma(issue, od, vd + k * (2048u >> 4), pd + k * (2048u >> 4), DESC_HI, DESC_HI, idesc, (j | k) != 0);
+            for (int k = 0; k < TOKENS / 16; ++k)
+              mma(issue, od, vd + k * (2048u >> 4), pd + k * (2048u >> 4), DESC_HI, DESC_HI, idesc, (j | k) != 0);
+          }
+          mma_commit(issue, bd::smem_u32(&ctl->empty[stage]));
+          if (++stage == stages) stage = 0;
         }
-        mma_commit(issue, bd::smem_u32(&ctl->empty[stage]));
-        if (++stage == stages) stage = 0;
+        mma_commit(issue, bd::smem_u32(&ctl->o_done[t & 1]));
+        if (++tile == tiles) tile = 0;
       }
-      mma_commit(issue, bd::smem_u32(&ctl->o_done[j & 1]));
-      if (++tile == tiles) tile = 0;
+      if (g.n > 0) mma_commit(issue, bd::smem_u32(&ctl->segment_done));
     }
     mma_commit(issue, bd::smem_u32(&ctl->o_drain));
     __syncwarp();
@@ -420,19 +556,26 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
     __syncwarp();
   } else {
     // -------------------------------------------------------------- softmax
+    const auto soft_sync = [] { bd::named_barrier_sync(3, SOFT); };
     // A wait that gives up (`ok`) ends no warp's loop: the barriers below count all of them.
     const int quarter = warp & 3, group = warp >> 2, col0 = group * WIDE + (lane >> 4) * COLS;
-    if (n > 0) {
+    const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
+    const uint32_t s_at = tmem + lanes + group * WIDE, o_at = tmem + lanes + O_COL + group * WIDE;
+    const int token = quarter * 16 + (lane & 15);
+    // the weights of a token, its row of the second operand: the tile's rows contiguous
+    const uint32_t w_at = rope_at + (token / 8) * 1024 + (token % 8) * 128;
+    // A segment's queries: copies begun, once no product reads those of the segment before any more; and handed over.
+    const auto begin_queries = [&](const Segment& g) {
       // a lane has up to three units of eight elements of every row; the key part's columns begin behind the padded latents'
-      const int wide = a.dim + p.rope_dim, units = (2 * n_pairs + 1) * 8;
-      int from[3];
+      const int wide = a.dim + p.rope_dim, units = (2 * n_pairs + 1) * 8, rows = g.sq.q_len * a.group;
+      int piece[3];
 #pragma unroll
       for (int x = 0; x < 3; ++x) {
         const int u = lane + 32 * x;
-        from[x] = u < 16 * n_pairs ? (u * 8 < a.dim ? u * 8 : wide) : a.dim + (u - 16 * n_pairs) * 8;
+        piece[x] = u < 16 * n_pairs ? (u * 8 < a.dim ? u * 8 : wide) : a.dim + (u - 16 * n_pairs) * 8;
       }
-      const uint16_t* q = static_cast<const uint16_t*>(a.q) + static_cast<int64_t>(sq.q0) * a.q_tok;
-      int i = (row0 + warp) / a.group, h = row0 + warp - i * a.group;
+      const uint16_t* q = static_cast<const uint16_t*>(a.q) + static_cast<int64_t>(g.sq.q0) * a.q_tok;
+      int i = (g.row0 + warp) / a.group, h = g.row0 + warp - i * a.group;
 #pragma unroll 2
       for (int r = warp; r < N; r += SOFT_WARPS) {
         const uint16_t* src = q + i * a.q_tok + h * a.q_head;
@@ -440,169 +583,219 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
 #pragma unroll
         for (int x = 0; x < 3; ++x) {
           const int u = lane + 32 * x;
-          const bool live = row0 + r < rows && from[x] < wide;
-          if (u < units) copy16(dst + (u / 8) * Q_CHUNK + (((u % 8) ^ (r & 7)) << 4), live ? src + from[x] : q, live);
+          const bool live = g.row0 + r < rows && piece[x] < wide;
+          if (u < units) copy16(dst + (u / 8) * Q_CHUNK + (((u % 8) ^ (r & 7)) << 4), live ? src + piece[x] : q, live);
         }
         for (h += SOFT_WARPS; h >= a.group; h -= a.group) ++i;
       }
+    };
+    const auto end_queries = [&] {
       asm volatile("cp.async.wait_all;" ::: "memory");
       fence_proxy_async();
       bd::mbar_arrive(bd::smem_u32(&ctl->q_full));
-    }
-    const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
-    const uint32_t s_at = tmem + lanes + group * WIDE, o_at = tmem + lanes + O_COL + group * WIDE;
-    const int token = quarter * 16 + (lane & 15);
-    // the weights of a token, its row of the second operand: the tile's rows contiguous
-    const uint32_t w_at = rope_at + (token / 8) * 1024 + (token % 8) * 128;
-    float2 L[COLS / 2];
-#pragma unroll
-    for (int c = 0; c < COLS / 2; ++c) L[c] = make_float2(0.f, 0.f);
+    };
     bool ok = true;
-    int stage = 0, tile = 0;
-    for (int j = 0; j < n; ++j) {
-      const int t0 = begin + j * TOKENS;
-      if (ok) ok = wait(ctl->s_full[j & 1], j >> 1);
-      bd::tc_fence_after();
-      float v[COLS];
-      __syncwarp();
-      tmem_load_halves<COLS>(s_at + (j & 1) * N, v);
-#pragma unroll
-      for (int c = 0; c < COLS; c += 2) {
-        const float2 x = mul2(make_float2(v[c], v[c + 1]), make_float2(a.coef, a.coef));
-        v[c] = x.x, v[c + 1] = x.y;
+    int stage = 0, tile = 0, t = 0, segments = 0;
+    int at = from, seq = 0;
+    Segment g = segment(at, seq), next = g;
+    if (g.n > 0) {
+      begin_queries(g);
+      end_queries();
+    }
+    for (bool more = true; more;) {
+      const int rows = g.sq.q_len * a.group;
+      const int all_see = bdkv::visible(a, g.sq, g.row0 / a.group);  // its first row, and so all of them
+      const int64_t part_row = static_cast<int64_t>(2 * blockIdx.x + !g.first) * N;
+      if (tid < N) {
+        const int row = g.row0 + tid, i = row / a.group, h = row - i * a.group;
+        ctl->ref[tid] = NO_REF;
+        ctl->visible[tid] = row < rows ? min(bdkv::visible(a, g.sq, i), g.end) : 0;
+        ctl->out[tid] = row >= rows ? 0u
+                        : g.whole   ? reinterpret_cast<uint64_t>(static_cast<uint16_t*>(a.out) +
+                                                                 (static_cast<int64_t>(g.sq.q0) + i) * a.o_tok + h * a.o_head)
+                                    : reinterpret_cast<uint64_t>(a.part_o + (part_row + tid) * a.dim);
       }
-      if (t0 + TOKENS > min(all_see, end)) {  // some row does not see all of the tile
+      soft_sync();
+      more = at < to;
+      if (more) next = segment(at, seq);
+      float2 L[COLS / 2];
 #pragma unroll
-        for (int c = 0; c < COLS; ++c)
-          if (t0 + token >= ctl->visible[col0 + c]) v[c] = -INFINITY;
-      }
-      float2 x[COLS / 2];
-      const auto subtract = [&] {
+      for (int c = 0; c < COLS / 2; ++c) L[c] = make_float2(0.f, 0.f);
+      for (int j = 0; j < g.n; ++j, ++t) {
+        const int t0 = g.begin + j * TOKENS;
+        if (ok) ok = wait(ctl->s_full[t & 1], t >> 1);
+        bd::tc_fence_after();
+        float v[COLS];
+        __syncwarp();
+        tmem_load_halves<COLS>(s_at + (t & 1) * N, v);
 #pragma unroll
-        for (int c = 0; c < COLS; c += 4) {
-          const float4 r = *reinterpret_cast<const float4*>(&ctl->ref[col0 + c]);
-          x[c / 2] = bd::add2(make_float2(v[c], v[c + 1]), make_float2(-r.x, -r.y));
-          x[c / 2 + 1] = bd::add2(make_float2(v[c + 2], v[c + 3]), make_float2(-r.z, -r.w));
+        for (int c = 0; c < COLS; c += 2) {
+          const float2 x = mul2(make_float2(v[c], v[c + 1]), make_float2(a.coef, a.coef));
+          v[c] = x.x, v[c + 1] = x.y;
         }
-      };
-      subtract();
-      float top = -INFINITY;
+        if (t0 + TOKENS > min(all_see, g.end)) {  // some row does not see all of the tile
 #pragma unroll
-      for (int c = 0; c < COLS / 2; ++c) top = bd::max3(top, x[c].x, x[c].y);
-      if (group_any(group, top > P_MOST)) {
-        const int col = col0 + (lane & (COLS - 1));
-        const bool first = (lane & 15) < COLS;  // of the lanes that have this column
-        const float most_here = across_lanes<COLS>(v, lane, [](float x, float y) { return fmaxf(x, y); });
-        if (first) ctl->part[quarter][col] = most_here;
-        group_sync(group);
-        const float most = fmaxf(fmaxf(ctl->part[0][col], ctl->part[1][col]), fmaxf(ctl->part[2][col], ctl->part[3][col]));
-        const float before = ctl->ref[col];
-        group_sync(group);
-        if (quarter == 0 && first) {
-          const bool up = most - before > P_MOST;
-          ctl->factor[col] = up ? bd::ex2_approx(before - reference(most)) : 1.f;
-          if (up) ctl->ref[col] = reference(most);
+          for (int c = 0; c < COLS; ++c)
+            if (t0 + token >= ctl->visible[col0 + c]) v[c] = -INFINITY;
         }
-        group_sync(group);
-        subtract();
+        float2 x[COLS / 2];
+        const auto subtract = [&] {
 #pragma unroll
-        for (int c = 0; c < COLS; c += 2)
-          L[c / 2] = mul2(L[c / 2], make_float2(ctl->factor[col0 + c], ctl->factor[col0 + c + 1]));
-        if (j > 0) {
-          // (of the last tile with its parity, three before this one, the products have ended: this one's key parts, or those
-          // of the tile before it, came in their place)
-          if (ok) ok = wait(ctl->o_done[(j - 1) & 1], (j - 1) >> 1);
-          bd::tc_fence_after();
-          for (int s = 0; s < n_pairs; ++s) {
-            float o[WIDE];
-            uint32_t y[WIDE];
-            __syncwarp();
-            tmem_load<WIDE>(o_at + s * N, o);
-#pragma unroll
-            for (int c = 0; c < WIDE; ++c) y[c] = __float_as_uint(o[c] * ctl->factor[group * WIDE + c]);
-            tmem_store<WIDE>(o_at + s * N, y);
+          for (int c = 0; c < COLS; c += 4) {
+            const float4 r = *reinterpret_cast<const float4*>(&ctl->ref[col0 + c]);
+            x[c / 2] = bd::add2(make_float2(v[c], v[c + 1]), make_float2(-r.x, -r.y));
+            x[c / 2 + 1] = bd::add2(make_float2(v[c + 2], v[c + 3]), make_float2(-r.z, -r.w));
           }
-          bd::tmem_st_wait();
-        }
-      }
-      uint32_t w[COLS / 2];
+        };
+        subtract();
+        float top = -INFINITY;
 #pragma unroll
-      for (int c = 0; c < COLS / 2; ++c) {
-        const float2 e = make_float2(bd::ex2_approx(x[c].x), bd::ex2_approx(x[c].y));
-        L[c] = bd::add2(L[c], e);
-        w[c] = a.f16 ? F16::from_float2(e) : Bf16::from_float2(e);
-      }
+        for (int c = 0; c < COLS / 2; ++c) top = bd::max3(top, x[c].x, x[c].y);
+        if (group_any(group, top > P_MOST)) {
+          const int col = col0 + (lane & (COLS - 1));
+          const bool first = (lane & 15) < COLS;  // of the lanes that have this column
+          const float most_here = across_lanes<COLS>(v, lane, [](float x, float y) { return fmaxf(x, y); });
+          if (first) ctl->part[quarter][col] = most_here;
+          group_sync(group);
+          const float most = fmaxf(fmaxf(ctl->part[0][col], ctl->part[1][col]), fmaxf(ctl->part[2][col], ctl->part[3][col]));
+          const float before = ctl->ref[col];
+          group_sync(group);
+          if (quarter == 0 && first) {
+            const bool up = most - before > P_MOST;
+            ctl->factor[col] = up ? bd::ex2_approx(before - reference(most)) : 1.f;
+            if (up) ctl->ref[col] = reference(most);
+          }
+          group_sync(group);
+          subtract();
 #pragma unroll
-      for (int i = 0; i < COLS / 8; ++i)
-        st_shared_v4(w_at + tile * CHUNK + (((col0 / 8 + i) ^ (token & 7)) << 4), w[4 * i], w[4 * i + 1], w[4 * i + 2],
-                     w[4 * i + 3]);
-      if (++tile == tiles) tile = 0;
-      if (t0 + TOKENS > end) {
-        // What a page holds behind the last token may be anything, and zero times it NaN: its latents become zeros.
-        const int from = end - t0, units = (TOKENS - from) * 16;
-        for (int s = 0; s < n_pairs; ++s) {
-          int place = stage + s / per_stage;
-          if (place >= stages) place -= stages;
-          const uint32_t at = kv_at + place * stage_bytes + s % per_stage * PAIR;
-          for (int x = tid; x < units; x += SOFT)
-            st_shared_v4(at + (x % 16 / 8) * CHUNK + (from + x / 16) * 128 + ((x % 8) << 4), 0, 0, 0, 0);
+          for (int c = 0; c < COLS; c += 2)
+            L[c / 2] = mul2(L[c / 2], make_float2(ctl->factor[col0 + c], ctl->factor[col0 + c + 1]));
+          if (j > 0) {
+            // (of the last tile with its parity, three before this one, the products have ended: this one's key parts, or those
+            // of the tile before it, came in their place)
+            if (ok) ok = wait(ctl->o_done[(t - 1) & 1], (t - 1) >> 1);
+            bd::tc_fence_after();
+            for (int s = 0; s < n_pairs; ++s) {
+              float o[WIDE];
+              uint32_t y[WIDE];
+              __syncwarp();
+              tmem_load<WIDE>(o_at + s * N, o);
+#pragma unroll
+              for (int c = 0; c < WIDE; ++c) y[c] = __float_as_uint(o[c] * ctl->factor[group * WIDE + c]);
+              tmem_store<WIDE>(o_at + s * N, y);
+            }
+            bd::tmem_st_wait();
+          }
         }
+        uint32_t w[COLS / 2];
+#pragma unroll
+        for (int c = 0; c < COLS / 2; ++c) {
+          const float2 e = make_float2(bd::ex2_approx(x[c].x), bd::ex2_approx(x[c].y));
+          L[c] = bd::add2(L[c], e);
+          w[c] = a.f16 ? F16::from_float2(e) : Bf16::from_float2(e);
+        }
+#pragma unroll
+        for (int i = 0; i < COLS / 8; ++i)
+          st_shared_v4(w_at + tile * CHUNK + (((col0 / 8 + i) ^ (token & 7)) << 4), w[4 * i], w[4 * i + 1], w[4 * i + 2],
+                       w[4 * i + 3]);
+        if (++tile == tiles) tile = 0;
+        if (t0 + TOKENS > g.end) {
+          // What a page holds behind the last token may be anything, and zero times it NaN: its latents become zeros.
+          const int live = g.end - t0, units = (TOKENS - live) * 16;
+          for (int s = 0; s < n_pairs; ++s) {
+            int place = stage + s / per_stage;
+            if (place >= stages) place -= stages;
+            const uint32_t at = kv_at + place * stage_bytes + s % per_stage * PAIR;
+            for (int x = tid; x < units; x += SOFT)
+              st_shared_v4(at + (x % 16 / 8) * CHUNK + (live + x / 16) * 128 + ((x % 8) << 4), 0, 0, 0, 0);
+          }
+        }
+        stage += (n_pairs + per_stage - 1) / per_stage;
+        if (stage >= stages) stage -= stages;
+        fence_proxy_async();
+        bd::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) bd::mbar_arrive(bd::smem_u32(&ctl->p_full[t & 1]));
       }
-      stage += (n_pairs + per_stage - 1) / per_stage;
-      if (stage >= stages) stage -= stages;
-      fence_proxy_async();
-      bd::tc_fence_before();
-      __syncwarp();
-      if (lane == 0) bd::mbar_arrive(bd::smem_u32(&ctl->p_full[j & 1]));
-    }
 
-    // a row's sum: over the lanes, then over the four warps that have its tokens
-    float sums[COLS];
+      // all of the segment's scores are done: the next one's queries can come
+      if (more && next.n > 0) begin_queries(next);
+
+      // a row's sum: over the lanes, then over the four warps that have its tokens
+      float sums[COLS];
 #pragma unroll
-    for (int c = 0; c < COLS; ++c) sums[c] = c & 1 ? L[c / 2].y : L[c / 2].x;
-    const float sum_here = across_lanes<COLS>(sums, lane, [](float x, float y) { return x + y; });
-    const int col = col0 + (lane & (COLS - 1));
-    const bool first = (lane & 15) < COLS;
-    if (first) ctl->part[quarter][col] = sum_here;
-    group_sync(group);
-    if (quarter == 0 && first) {
-      const int row = row0 + col;
-      const float sum = (ctl->part[0][col] + ctl->part[1][col]) + (ctl->part[2][col] + ctl->part[3][col]);
-      const uint64_t to = ctl->out[col];
-      // a whole row is 0 where it sees nothing, NaN where all of its scores are -inf (a part may well hold nothing)
-      ctl->scale[col] = sum == 0.f ? (to != 0 && (to & 1) == 0 && ctl->visible[col] > 0 ? NAN : 0.f) : 1.f / sum;
-      if (row < rows) {
-        const int i = row / a.group, h = row - i * a.group;
-        const bdkv::RowOut o = bdkv::row_out(a, sq, seq, part, i, h, bdkv::visible(a, sq, i));
-        if (o.o != nullptr)  // a part's reference and sum: their log-sum-exp in one number would lose the sum of large scores
-          reinterpret_cast<float2*>(a.part_l)[o.l - a.part_l] = make_float2(sum == 0.f ? -INFINITY : ctl->ref[col], sum);
-        else
-          bdkv::store_lse(o, sum == 0.f ? -INFINITY : ctl->ref[col] + log2f(sum));
-      }
-    }
-    group_sync(group);
-    if (n > 0 && ok) wait(ctl->o_drain, 0);
-    bd::tc_fence_after();
-    for (int s = 0; s < n_pairs; ++s) {
-      float o[WIDE];
-      __syncwarp();
-      if (n > 0)
-        tmem_load<WIDE>(o_at + s * N, o);
-      else
-#pragma unroll
-        for (int c = 0; c < WIDE; ++c) o[c] = 0.f;
-      const int d = s * 128 + quarter * 32 + lane;
-      if (d < a.dim)
-#pragma unroll
-        for (int c = 0; c < WIDE; ++c) {
-          const uint64_t to = ctl->out[group * WIDE + c];
-          const float y = o[c] * ctl->scale[group * WIDE + c];
-          if (to & 1)
-            reinterpret_cast<float*>(to & ~uint64_t(1))[d] = y;
-          else if (to != 0)
-            reinterpret_cast<uint16_t*>(to)[d] = static_cast<uint16_t>(a.f16 ? F16::from_float2(make_float2(y, 0.f))
-                                                                            : Bf16::from_float2(make_float2(y, 0.f)));
+      for (int c = 0; c < COLS; ++c) sums[c] = c & 1 ? L[c / 2].y : L[c / 2].x;
+      const float sum_here = across_lanes<COLS>(sums, lane, [](float x, float y) { return x + y; });
+      const int col = col0 + (lane & (COLS - 1));
+      const bool first = (lane & 15) < COLS;
+      if (first) ctl->part[quarter][col] = sum_here;
+      group_sync(group);
+      if (quarter == 0 && first) {
+        const float sum = (ctl->part[0][col] + ctl->part[1][col]) + (ctl->part[2][col] + ctl->part[3][col]);
+        // a whole row is 0 where it sees nothing, NaN where all of its scores are -inf (a part may well hold nothing)
+        ctl->scale[col] = sum == 0.f ? (g.whole && ctl->visible[col] > 0 ? NAN : 0.f) : 1.f / sum;
+        const int row = g.row0 + col;
+        if (!g.whole) {  // a part's reference and sum: their log-sum-exp in one number would lose the sum of large scores
+          reinterpret_cast<float2*>(a.part_l)[part_row + col] = make_float2(sum == 0.f ? -INFINITY : ctl->ref[col], sum);
+        } else if (row < rows && a.lse != nullptr) {
+          const int i = row / a.group, h = row - i * a.group;
+          a.lse[(static_cast<int64_t>(g.sq.q0) + i) * a.group + h] =
+              sum == 0.f ? -INFINITY : (ctl->ref[col] + log2f(sum)) / bd::LOG2E;
         }
+      }
+      group_sync(group);
+      if (g.n > 0) {
+        if (ok) ok = wait(ctl->segment_done, segments);
+        ++segments;
+      }
+      bd::tc_fence_after();
+      if (more && next.n > 0) end_queries();
+      for (int s = 0; s < n_pairs; ++s) {
+        float o[WIDE];
+        __syncwarp();
+        if (g.n > 0)
+          tmem_load<WIDE>(o_at + s * N, o);
+        else
+#pragma unroll
+          for (int c = 0; c < WIDE; ++c) o[c] = 0.f;
+        // Four lanes exchange until each has four dims next to each other, of a row in four: their stores are wider and fewer.
+        const int d = s * 128 + quarter * 32 + (lane & ~3);
+        const bool odd = lane & 1, upper = lane & 2;
+        float2 two[WIDE / 2];
+#pragma unroll
+        for (int c = 0; c < WIDE; c += 2) {
+          const float2 f = *reinterpret_cast<const float2*>(&ctl->scale[group * WIDE + c]);
+          const float lo = o[c] * f.x, hi = o[c + 1] * f.y;
+          const float other = __shfl_xor_sync(~0u, odd ? lo : hi, 1);
+          two[c / 2] = odd ? make_float2(other, hi) : make_float2(lo, other);
+        }
+        if (g.whole) {
+#pragma unroll
+          for (int c = 0; c < WIDE; c += 4) {
+            const uint32_t lo = a.f16 ? F16::from_float2(two[c / 2]) : Bf16::from_float2(two[c / 2]);
+            const uint32_t hi = a.f16 ? F16::from_float2(two[c / 2 + 1]) : Bf16::from_float2(two[c / 2 + 1]);
+            const uint32_t other = __shfl_xor_sync(~0u, upper ? lo : hi, 2);
+            const uint64_t dst = ctl->out[group * WIDE + c + (lane & 3)];
+            if (dst != 0 && d < a.dim)
+              asm volatile("st.global.v2.b32 [%0], {%1, %2};" ::"l"(dst + d * 2), "r"(upper ? other : lo), "r"(upper ? hi : other)
+                           : "memory");
+          }
+        } else {
+#pragma unroll
+          for (int c = 0; c < WIDE; c += 4) {
+            const float2 lo = two[c / 2], hi = two[c / 2 + 1];
+            const float2 give = upper ? lo : hi;
+            const float2 other = make_float2(__shfl_xor_sync(~0u, give.x, 2), __shfl_xor_sync(~0u, give.y, 2));
+            const uint64_t dst = ctl->out[group * WIDE + c + (lane & 3)];
+            if (dst != 0 && d < a.dim)
+              asm volatile("st.global.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(dst + d * 4), "f"(upper ? other.x : lo.x),
+                           "f"(upper ? other.y : lo.y), "f"(upper ? hi.x : other.x), "f"(upper ? hi.y : other.y)
+                           : "memory");
+          }
+        }
+      }
+      soft_sync();  // the rows have left
+      g = next;
     }
   }
 
@@ -614,20 +807,21 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
 }
 
 template <int N>
-cudaError_t launch(const LatentArgs& p, const CUtensorMap& latent, const CUtensorMap& rope, cudaStream_t st) {
+cudaError_t launch(const LatentArgs& p, const CUtensorMap& latent, const CUtensorMap& rope, int sm_count, cudaStream_t st) {
   static std::atomic<bool> ready[64];  // by device
   if (cudaError_t e = bdkv::allow_smem(latent_attn_kernel<N>, 232448, ready); e != cudaSuccess) return e;
   const Layout l = layout<N>(p.a.dim);
-  const dim3 grid((p.a.max_q * p.a.group + N - 1) / N, p.a.n_split, p.a.n_seq);
+  const dim3 grid = p.shared ? dim3(sm_count) : dim3(p.row_tiles, p.a.n_seq);
   latent_attn_kernel<N><<<grid, N == 64 ? 352 : 224, l.bytes, st>>>(p, l.stages, l.tiles, latent, rope);
   return cudaGetLastError();
 }
 
 }  // namespace
 
-cudaError_t launch_latent_attn(const LatentArgs& p, const CUtensorMap& latent, const CUtensorMap& rope, cudaStream_t st) {
-  return p.rows == 16 ? launch<16>(p, latent, rope, st) : p.rows == 32 ? launch<32>(p, latent, rope, st)
-                                                                       : launch<64>(p, latent, rope, st);
+cudaError_t launch_latent_attn(const LatentArgs& p, const CUtensorMap& latent, const CUtensorMap& rope, int sm_count,
+                               cudaStream_t st) {
+  const auto run = p.rows == 16 ? launch<16> : p.rows == 32 ? launch<32> : launch<64>;
+  return run(p, latent, rope, sm_count, st);
 }
 
 cudaError_t latent_status(cudaStream_t st, uint32_t* bits) {

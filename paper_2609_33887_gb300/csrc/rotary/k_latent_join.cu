@@ -1,71 +1,140 @@
-// Joins the parts of rows whose cache was split: the parts' normalised outputs
-// weighted by their sums of weights, brought to one reference. A CTA takes a row, a thread four dims of it.
+// Joins the parts of units whose tiles went to several CTAs: the parts'
+// normalised outputs weighted by their sums of weights, brought to one reference.
+// Many units have a few parts each: a warp takes a row, all of its dims. Few
+// units have many: eight warps share the parts of a row's 128 dims.
 #include "rotary/latent.h"
 
 namespace bdrot {
 namespace {
 
-constexpr int THREADS = 128, AHEAD = 8;
+constexpr int WARPS = 8, AHEAD = 8;
 
-template <class T>
-__global__ void __launch_bounds__(THREADS) latent_join_kernel(bdkv::AttnArgs a) {
-  const int row = blockIdx.x, seq = blockIdx.y, i = row / a.group, h = row - i * a.group, lane = threadIdx.x & 31;
+template <class T, bool MANY>
+__global__ void __launch_bounds__(WARPS * 32) latent_join_kernel(const LatentArgs p) {
+  const bdkv::AttnArgs& a = p.a;
+  __shared__ float4 sums[MANY ? WARPS : 1][32];
+  __shared__ float2 totals[WARPS];  // references, sums
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int chunks = (a.dim + 127) / 128, per_unit = MANY ? p.rows * chunks : p.rows / WARPS;
+  const int unit = blockIdx.x / per_unit, rest = blockIdx.x - unit * per_unit;
+  const int seq = unit / p.row_tiles, tile = unit - seq * p.row_tiles;
+  const int in_tile = MANY ? rest / chunks : rest * WARPS + warp, row = tile * p.rows + in_tile;
+  const int i = row / a.group, h = row - i * a.group;
   const bdkv::Seq sq = bdkv::load_seq(a, seq);
-  const int vis = i < sq.q_len ? bdkv::visible(a, sq, i) : 0;
-  if (vis <= a.chunk) return;  // part 0 has written the row
-  const int n = (vis - 1) / a.chunk + 1, d = threadIdx.x * 4;
+  const bool live = i < sq.q_len;
+  const int vis = live ? bdkv::visible(a, sq, i) : 0;
   bd::griddep_wait();
+  if (tile * p.rows >= sq.q_len * a.group) return;
+  const int2 plan = p.plan[unit];
+  if (plan.x < 0 || !live) return;
+  const int first = plan.x >> 1, n = plan.y - first + 1;
+  const auto part = [&](int k) { return static_cast<int64_t>(k == 0 ? plan.x : 2 * (first + k)) * p.rows + in_tile; };
 
-  const int64_t at = (static_cast<int64_t>(seq) * a.max_q * a.group + row) * a.n_split;
-  const float2* l = reinterpret_cast<const float2*>(a.part_l) + at;  // reference, sum
-  const float* src = a.part_o + at * a.dim + d;
-  const bool in_row = d < a.dim;
-  float top = -INFINITY;
-  for (int p = lane; p < n; p += 32) top = fmaxf(top, l[p].x);
-#pragma unroll
-  for (int s = 16; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, s));
-  const float ref = top == -INFINITY ? 0.f : top;
-  float4 o = {0.f, 0.f, 0.f, 0.f};
-  float total = 0.f;
-  for (int p0 = 0; p0 < n; p0 += AHEAD) {
-    float4 x[AHEAD];
-    float2 w[AHEAD];
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      const int p = p0 + u;
-      x[u] = p < n && in_row ? *reinterpret_cast<const float4*>(src + static_cast<int64_t>(p) * a.dim)
-                             : make_float4(0.f, 0.f, 0.f, 0.f);
-      w[u] = p < n ? l[p] : make_float2(-INFINITY, 0.f);
-    }
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      const float f = w[u].y * bd::ex2_approx(w[u].x - ref);
-      total += f;
-      o.x = fmaf(f, x[u].x, o.x), o.y = fmaf(f, x[u].y, o.y), o.z = fmaf(f, x[u].z, o.z), o.w = fmaf(f, x[u].w, o.w);
-    }
-  }
-  const float f = 1.f / total;  // (0 * inf, NaN, where all scores of the row are -inf)
+  const float2* l = reinterpret_cast<const float2*>(a.part_l);  // reference, sum
   const int64_t tok = static_cast<int64_t>(sq.q0) + i;
   const bdkv::RowOut dst = {static_cast<uint16_t*>(a.out) + tok * a.o_tok + h * a.o_head, nullptr,
                             a.lse == nullptr ? nullptr : a.lse + tok * a.group + h};
-  if (in_row) bdkv::store4<T>(dst, d, make_float4(o.x * f, o.y * f, o.z * f, o.w * f));
-  if (threadIdx.x == 0) bdkv::store_lse(dst, total == 0.f ? -INFINITY : ref + log2f(total));
+  const float4 zero = {0.f, 0.f, 0.f, 0.f};
+  const auto scaled = [](float4 x, float f) { return make_float4(x.x * f, x.y * f, x.z * f, x.w * f); };
+  const auto add = [](float4& o, float f, float4 x) {
+    o.x = fmaf(f, x.x, o.x), o.y = fmaf(f, x.y, o.y), o.z = fmaf(f, x.z, o.z), o.w = fmaf(f, x.w, o.w);
+  };
+  // Sums under the largest reference so far (-inf: nothing yet), as in the attention itself; `by` brings what is held to a
+  // new one.
+  float ref = -INFINITY, total = 0.f;
+  const auto raise = [&](float to) {
+    const float most = fmaxf(ref, to), by = most == ref ? 1.f : bd::ex2_approx(ref - most);
+    ref = most;
+    total *= by;
+    return by;
+  };
+  const auto weight = [&](float2 w) { return ref == -INFINITY ? w.y : w.y * bd::ex2_approx(w.x - ref); };  // (w.y: 0 or NaN)
+  const auto store = [&](int c, float4 o) {
+    // (0 * inf, NaN, where all scores of the row are -inf; 0 where it sees nothing)
+    const int d = c * 128 + lane * 4;
+    if (d < a.dim) bdkv::store4<T>(dst, d, scaled(o, vis > 0 ? 1.f / total : 0.f));
+    if (c == 0 && lane == 0) bdkv::store_lse(dst, total == 0.f ? -INFINITY : ref + log2f(total));
+  };
+  if constexpr (MANY) {
+    const int c = rest % chunks, d = c * 128 + lane * 4;
+    float4 o = zero;
+    for (int k0 = warp; k0 < n; k0 += AHEAD * WARPS) {
+      float4 x[AHEAD];
+      float2 w[AHEAD];
+      float most = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int k = k0 + u * WARPS;
+        x[u] = k < n && d < a.dim ? *reinterpret_cast<const float4*>(a.part_o + part(k) * a.dim + d) : zero;
+        w[u] = k < n ? l[part(k)] : make_float2(-INFINITY, 0.f);
+        most = fmaxf(most, w[u].x);
+      }
+      o = scaled(o, raise(most));
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const float f = weight(w[u]);
+        total += f;
+        add(o, f, x[u]);
+      }
+    }
+    sums[warp][lane] = o;
+    if (lane == 0) totals[warp] = make_float2(ref, total);
+    __syncthreads();
+    if (warp != 0) return;
+    for (int s = 1; s < WARPS; ++s) {
+      const float2 w = totals[s];
+      o = scaled(o, raise(w.x));
+      const float f = ref == -INFINITY ? 1.f : bd::ex2_approx(w.x - ref);
+      total += w.y * f;
+      add(o, f, sums[s][lane]);
+    }
+    store(c, o);
+  } else {
+    float4 o[4] = {zero, zero, zero, zero};  // of up to 4 x 128 dims
+    for (int k0 = 0; k0 < n; k0 += 2) {
+      float4 x[2][4];
+      float2 w[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const bool there = k0 + u < n;
+        w[u] = there ? l[part(k0 + u)] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const int d = c * 128 + lane * 4;
+          x[u][c] = there && d < a.dim ? *reinterpret_cast<const float4*>(a.part_o + part(k0 + u) * a.dim + d) : zero;
+        }
+      }
+      const float by = raise(fmaxf(w[0].x, w[1].x)), f[2] = {weight(w[0]), weight(w[1])};
+      total += f[0] + f[1];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        o[c] = scaled(o[c], by);
+        add(o[c], f[0], x[0][c]);
+        add(o[c], f[1], x[1][c]);
+      }
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) store(c, o[c]);
+  }
 }
 
 }  // namespace
 
-cudaError_t launch_latent_join(const LatentArgs& p, cudaStream_t st) {
+cudaError_t launch_latent_join(const LatentArgs& p, int sm_count, cudaStream_t st) {
+  const int units = p.a.n_seq * p.row_tiles;
+  const bool many = sm_count >= 8 * units;  // parts of a unit, on average
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(p.a.max_q) * p.a.group, p.a.n_seq);
-  cfg.blockDim = dim3(THREADS);
+  cfg.gridDim = dim3(static_cast<unsigned>(units) * (many ? p.rows * ((p.a.dim + 127) / 128) : p.rows / WARPS));
+  cfg.blockDim = dim3(WARPS * 32);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];  // scheduled while the parts still run; it waits for them before it reads
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return p.a.f16 ? cudaLaunchKernelEx(&cfg, latent_join_kernel<F16>, p.a)
-                 : cudaLaunchKernelEx(&cfg, latent_join_kernel<Bf16>, p.a);
+  const auto kernel = p.a.f16 ? (many ? latent_join_kernel<F16, true> : latent_join_kernel<F16, false>)
+                              : (many ? latent_join_kernel<Bf16, true> : latent_join_kernel<Bf16, false>);
+  return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
 }  // namespace bdrot

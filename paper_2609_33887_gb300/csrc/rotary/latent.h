@@ -12,17 +12,23 @@ cudaError_t launch_latent_write(const bdrot_latent& c, const bdkv_rows& latent, 
                                 const int64_t* slot_map, int64_t n_tokens, const Turn* turn, int sm_count,
                                 cudaStream_t st);
 
-// What the attention kernels read of one call: lengths, masks, outputs and the split as the 8-bit cache's kernels have
-// them (one key/value head, dim = latent_dim; part_l
-// holds two floats a row and part, its reference and sum of weights); latents and key parts come through the tensor maps.
+// What the attention kernels read of one call: lengths, masks and outputs as the 8-bit cache's kernels have them (one
+// key/value head, dim = latent_dim); latents and key parts come through the tensor maps.
 struct LatentArgs {
-  bdkv::AttnArgs a;
+  bdkv::AttnArgs a;  // part_o [2 CTAs, rows, dim], part_l [2 CTAs, rows, 2]: parts of units that begin (0) or end in a CTA
   int rope_dim;
-  int rows;  // (queries x heads) of a CTA: 16, 32 or 64
+  int rows;       // (queries x heads) of a unit: 16, 32 or 64
+  int row_tiles;  // units of a request, at most
+  bool shared;    // the units' tiles shared out equally (else a CTA to each unit)
+  bool columns;   // the latents' map is [64 elements, token, column, page], its boxes a stage's columns of 64 tokens
+  int2* plan;     // [n_seq, row_tiles], of units that have rows: the first part of a split one (-1: it is whole) and its last CTA
 };
-constexpr int TOKENS = 64;  // cached tokens of a tile
-cudaError_t launch_latent_attn(const LatentArgs& p, const CUtensorMap& latent, const CUtensorMap& rope, cudaStream_t st);
-cudaError_t launch_latent_join(const LatentArgs& p, cudaStream_t st);
+constexpr int TOKENS = 64;           // cached tokens of a tile
+__host__ __device__ constexpr int pairs_per_stage(int n_pairs) { return n_pairs < 2 ? 1 : 2; }  // of columns of 64
+constexpr int MAX_SHARED_SEQ = 256;  // requests whose tiles are shared out, at most
+cudaError_t launch_latent_attn(const LatentArgs& p, const CUtensorMap& latent, const CUtensorMap& rope, int sm_count,
+                               cudaStream_t st);
+cudaError_t launch_latent_join(const LatentArgs& p, int sm_count, cudaStream_t st);
 cudaError_t latent_status(cudaStream_t st, uint32_t* bits);
 
 }  // namespace bdrot

@@ -126,37 +126,29 @@ int check_attention(const bdrot_latent* cache, const bdrot_latent_attention_args
   return check_rows_apart(a.out, a.n_heads, c.latent_dim, a.n_seq > 1 || a.max_q_len > 1);
 }
 
-// How a call is split along the cache.
+// How a call's work is shared out.
 struct Plan {
-  bool longest_first;
-  int rows, chunk, n_split;
-  int64_t part_rows;  // rows of partial results
-  size_t bytes;       // of workspace
+  int rows, row_tiles;
+  bool shared, longest_first;
+  int64_t part_rows;  // rows of partial results, two units to each CTA
+  size_t bytes;       // of workspace: those, with a reference and a sum each, and two words for each unit
 };
 
-// One or two requests are split into one wave of CTAs, more requests into finer parts, which even out lengths that the
-// host does not know.
+// Equal shares of all units' tiles, which each CTA adds up itself, up to one unit for each SM: lengths that the host does
+// not know then make no CTA wait for another (64 units of 57 to 8189 tokens 65 us, 75 in parts of equal lengths, two to an
+// SM). With more units a CTA to each, the longest requests first (320 units of 300 to 4001 tokens 129 us, 165 in shares,
+// whose CTAs change units more often and read less of what others read at the same time).
 Plan make_plan(const bdrot_latent& c, const bdrot_latent_attention_args& a, int sms) {
   Plan p = {};
   const int64_t rows = int64_t(a.max_q_len) * a.n_heads;
   p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
-  const int64_t ctas = (rows + p.rows - 1) / p.rows * a.n_seq;
-  const bool few = a.n_seq <= 2;
-  const int64_t finer = std::min<int64_t>((3 * int64_t(sms) + ctas - 1) / ctas, a.max_kv_len / 1024);
-  const int64_t parts = few || ctas >= sms ? sms / ctas : std::max<int64_t>(sms / ctas, finer);
-  constexpr int64_t TILE = bdrot::TOKENS;
-  int64_t chunk = parts > 1 ? ((a.max_kv_len + parts - 1) / parts + TILE - 1) / TILE * TILE : a.max_kv_len;
-  if (chunk < TILE) chunk = TILE;
-  p.n_split = static_cast<int>((a.max_kv_len + chunk - 1) / chunk);
-  p.longest_first = !few && a.n_seq <= bdkv::MAX_ORDERED && ctas * p.n_split > sms;
-  if (p.n_split <= 1) {
-    p.n_split = 1;
-    p.chunk = INT_MAX;
-    return p;
-  }
-  p.chunk = static_cast<int>(chunk);
-  p.part_rows = int64_t(a.n_seq) * rows * p.n_split;
-  p.bytes = static_cast<size_t>(p.part_rows) * (c.latent_dim + 2) * sizeof(float);
+  p.row_tiles = static_cast<int>((rows + p.rows - 1) / p.rows);
+  const int64_t units = int64_t(p.row_tiles) * a.n_seq, tiles = a.max_kv_len / bdrot::TOKENS + 1;
+  p.shared = units <= sms && a.n_seq <= bdrot::MAX_SHARED_SEQ && units * tiles < (int64_t(1) << 30);
+  p.longest_first = !p.shared && a.n_seq > 2 && a.n_seq <= bdkv::MAX_ORDERED && units > sms;
+  if (!p.shared) return p;
+  p.part_rows = 2 * int64_t(sms) * p.rows;
+  p.bytes = static_cast<size_t>(p.part_rows) * (c.latent_dim + 2) * sizeof(float) + static_cast<size_t>(units) * 8;
   return p;
 }
 
@@ -172,19 +164,24 @@ PFN_cuTensorMapEncodeTiled_v12000 encoder() {
   return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
 }
 
-// Boxes of 64 elements by a page's tokens (or a tile's, of larger pages). A cache without pages gets a map of one page
-// over `any`, which no box reads: page numbers outside the cache are taken to the coordinate behind its last page.
-bool encode(CUtensorMap* m, const bdrot_latent& c, const void* data, const int64_t* stride, int dim, const void* any) {
+// Boxes of 64 elements by a page's tokens (or a tile's, of larger pages), or of as many columns of 64 elements as a stage of
+// the attention kernel holds, by a tile's tokens. A cache without pages gets a map of one page over `any`, which no box
+// reads: page numbers outside the cache are taken to the coordinate behind its last page.
+bool encode(CUtensorMap* m, const bdrot_latent& c, const void* data, const int64_t* stride, int dim, int columns,
+            const void* any) {
   const auto f = encoder();
   if (f == nullptr) return false;
-  const int64_t tok = c.n_pages > 0 ? stride[1] : dim, page = c.n_pages > 1 ? stride[0] : tok * c.page_size;
-  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(dim), static_cast<cuuint64_t>(c.page_size),
-                              static_cast<cuuint64_t>(std::max<int64_t>(c.n_pages, 1))};
-  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(tok * 2), static_cast<cuuint64_t>(page * 2)};
-  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(std::min(c.page_size, bdrot::TOKENS)), 1}, step[3] = {1, 1, 1};
-  return f(m, c.dtype == BDKV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
-           const_cast<void*>(c.n_pages > 0 ? data : any), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  const cuuint64_t tok = (c.n_pages > 0 ? stride[1] : dim) * 2, page = c.n_pages > 1 ? stride[0] * 2 : tok * c.page_size;
+  const cuuint64_t tokens = c.page_size, pages = std::max<int64_t>(c.n_pages, 1);
+  const cuuint64_t dims[2][4] = {{static_cast<cuuint64_t>(dim), tokens, pages}, {64, tokens, static_cast<cuuint64_t>(dim / 64), pages}};
+  const cuuint64_t strides[2][3] = {{tok, page}, {tok, 128, page}};
+  const cuuint32_t most = std::min(c.page_size, bdrot::TOKENS);
+  const cuuint32_t box[2][4] = {{64, most, 1}, {64, most, static_cast<cuuint32_t>(columns), 1}}, step[4] = {1, 1, 1, 1};
+  const int kind = columns > 0;
+  return f(m, c.dtype == BDKV_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3 + kind,
+           const_cast<void*>(c.n_pages > 0 ? data : any), dims[kind], strides[kind], box[kind], step,
+           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 bdrot::LatentArgs latent_args(const bdrot_latent& c, const bdrot_latent_attention_args& a, const Plan& plan) {
@@ -193,7 +190,7 @@ bdrot::LatentArgs latent_args(const bdrot_latent& c, const bdrot_latent_attentio
   r.n_pages = c.n_pages;
   while ((1 << r.page_shift) < c.page_size) ++r.page_shift;
   r.dim = c.latent_dim, r.n_kv = 1, r.group = a.n_heads;
-  p.rope_dim = c.rope_dim, p.rows = plan.rows;
+  p.rope_dim = c.rope_dim, p.rows = plan.rows, p.row_tiles = plan.row_tiles, p.shared = plan.shared;
   r.q = a.q.data, r.q_tok = a.q.stride_token, r.q_head = a.q.stride_head;
   r.out = a.out.data, r.o_tok = a.out.stride_token, r.o_head = a.out.stride_head;
   r.lse = a.lse;
@@ -202,7 +199,7 @@ bdrot::LatentArgs latent_args(const bdrot_latent& c, const bdrot_latent_attentio
   r.n_seq = a.n_seq, r.max_q = a.max_q_len, r.max_kv = a.max_kv_len, r.mask_block = a.mask_block;
   r.coef = a.scale * bd::LOG2E;
   r.f16 = a.q.dtype == BDKV_F16;
-  r.chunk = plan.chunk, r.n_split = plan.n_split, r.longest_first = plan.longest_first;
+  r.longest_first = plan.longest_first;
   return p;
 }
 
@@ -307,14 +304,17 @@ int bdrot_latent_attention(const bdrot_latent* cache, const bdrot_latent_attenti
   const Plan plan = make_plan(*cache, *args, sms);
   bdrot::LatentArgs p = latent_args(*cache, *args, plan);
   CUtensorMap latent, rope;
-  if (!encode(&latent, *cache, cache->latent, cache->latent_stride, cache->latent_dim, args->q.data) ||
-      !encode(&rope, *cache, cache->rope, cache->rope_stride, cache->rope_dim, args->q.data))
+  p.columns = cache->page_size >= bdrot::TOKENS && cache->latent_dim % 64 == 0;
+  const int columns = p.columns ? 2 * bdrot::pairs_per_stage((cache->latent_dim + 127) / 128) : 0;
+  if (!encode(&latent, *cache, cache->latent, cache->latent_stride, cache->latent_dim, columns, args->q.data) ||
+      !encode(&rope, *cache, cache->rope, cache->rope_stride, cache->rope_dim, 0, args->q.data))
     return BD_ERR_CUDA;
   const auto run = [&](void* ws) {
     p.a.part_o = static_cast<float*>(ws);
     p.a.part_l = p.a.part_o + plan.part_rows * cache->latent_dim;
-    cudaError_t e = bdrot::launch_latent_attn(p, latent, rope, st);
-    if (e == cudaSuccess && plan.n_split > 1) e = bdrot::launch_latent_join(p, st);
+    p.plan = reinterpret_cast<int2*>(p.a.part_l + plan.part_rows * 2);
+    cudaError_t e = bdrot::launch_latent_attn(p, latent, rope, sms, st);
+    if (e == cudaSuccess && plan.shared) e = bdrot::launch_latent_join(p, sms, st);
     return cuda_status(e);
   };
   if (plan.bytes == 0) return run(nullptr);
