@@ -438,9 +438,11 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
     int stage = 0, round = 0, tile = 0;  // of the next load: its places, and how often the stage's was used
     bool ok = true;
     const uint32_t issue = bd::elect_one();
-    const auto load = [&](const CUtensorMap* map, uint32_t dst, uint32_t bar, int x, int y, int page) {
-      for (int b = 0; b < boxes; ++b)  // (more than one: whole pages)
-        tma_load_3d(issue, bd::warp_uniform(dst + b * step * 128), map, bar, x, y, __shfl_sync(~0u, page, b));
+    int pages[TOKENS / 16];  // of a tile's boxes
+    const auto load = [&](const CUtensorMap* map, uint32_t dst, uint32_t bar, int x, int y) {
+#pragma unroll
+      for (int b = 0; b < TOKENS / 16; ++b)  // (more than one: whole pages)
+        if (b < boxes) tma_load_3d(issue, dst + b * step * 128, map, bar, x, y, pages[b]);
     };
     for (int at = from, seq = 0; ok && at < to;) {
       const Segment g = segment(at, seq);
@@ -455,6 +457,8 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
         const int page = found >= 0 && found < a.n_pages ? found : outside;
         found = following;
         following = find(j + 2);
+#pragma unroll
+        for (int b = 0; b < TOKENS / 16; ++b) pages[b] = __shfl_sync(~0u, page, b);
         for (int s = 0; s < n_pairs; s += per_stage) {
           if (!(ok = wait(ctl->empty[stage], round + 1))) break;
           const bool last = s + per_stage >= n_pairs;
@@ -463,10 +467,10 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
           // (columns behind the latents' last are read as zeros)
           expect_bytes(issue, bar, (p.columns ? stage_bytes : pairs * PAIR) + (last ? CHUNK : 0));
           if (p.columns)
-            tma_load_4d(issue, dst, &latent_map, bar, y, 2 * s, __shfl_sync(~0u, page, 0));
+            tma_load_4d(issue, dst, &latent_map, bar, y, 2 * s, pages[0]);
           else
-            for (int c = 0; c < 2 * pairs; ++c) load(&latent_map, dst + c * CHUNK, bar, (2 * s + c) * 64, y, page);
-          if (last) load(&rope_map, rope_at + tile * CHUNK, bar, 0, y, page);
+            for (int c = 0; c < 2 * pairs; ++c) load(&latent_map, dst + c * CHUNK, bar, (2 * s + c) * 64, y);
+          if (last) load(&rope_map, bd::warp_uniform(rope_at + tile * CHUNK), bar, 0, y);
           if (++stage == stages) stage = 0, ++round;
         }
         if (++tile == tiles) tile = 0;

@@ -1,7 +1,7 @@
 // Joins the parts of units whose tiles went to several CTAs: the parts'
 // normalised outputs weighted by their sums of weights, brought to one reference.
-// Many units have a few parts each: a warp takes a row, all of its dims. Few
-// units have many: eight warps share the parts of a row's 128 dims.
+// A warp takes 128 dims of a row where units have a few parts each; where they
+// have many, eight warps share the parts.
 #include "rotary/latent.h"
 
 namespace bdrot {
@@ -13,12 +13,13 @@ template <class T, bool MANY>
 __global__ void __launch_bounds__(WARPS * 32) latent_join_kernel(const LatentArgs p) {
   const bdkv::AttnArgs& a = p.a;
   __shared__ float4 sums[MANY ? WARPS : 1][32];
+  constexpr int STEP = MANY ? WARPS : 1;
   __shared__ float2 totals[WARPS];  // references, sums
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int chunks = (a.dim + 127) / 128, per_unit = MANY ? p.rows * chunks : p.rows / WARPS;
-  const int unit = blockIdx.x / per_unit, rest = blockIdx.x - unit * per_unit;
+  const int chunks = (a.dim + 127) / 128, per_unit = MANY ? p.rows * chunks : p.rows * chunks / WARPS;
+  const int unit = blockIdx.x / per_unit, rest = blockIdx.x - unit * per_unit, item = MANY ? rest : rest * WARPS + warp;
   const int seq = unit / p.row_tiles, tile = unit - seq * p.row_tiles;
-  const int in_tile = MANY ? rest / chunks : rest * WARPS + warp, row = tile * p.rows + in_tile;
+  const int in_tile = item / chunks, c = item - in_tile * chunks, row = tile * p.rows + in_tile;
   const int i = row / a.group, h = row - i * a.group;
   const bdkv::Seq sq = bdkv::load_seq(a, seq);
   const bool live = i < sq.q_len;
@@ -49,34 +50,28 @@ __global__ void __launch_bounds__(WARPS * 32) latent_join_kernel(const LatentArg
     return by;
   };
   const auto weight = [&](float2 w) { return ref == -INFINITY ? w.y : w.y * bd::ex2_approx(w.x - ref); };  // (w.y: 0 or NaN)
-  const auto store = [&](int c, float4 o) {
-    // (0 * inf, NaN, where all scores of the row are -inf; 0 where it sees nothing)
-    const int d = c * 128 + lane * 4;
-    if (d < a.dim) bdkv::store4<T>(dst, d, scaled(o, vis > 0 ? 1.f / total : 0.f));
-    if (c == 0 && lane == 0) bdkv::store_lse(dst, total == 0.f ? -INFINITY : ref + log2f(total));
-  };
-  if constexpr (MANY) {
-    const int c = rest % chunks, d = c * 128 + lane * 4;
-    float4 o = zero;
-    for (int k0 = warp; k0 < n; k0 += AHEAD * WARPS) {
-      float4 x[AHEAD];
-      float2 w[AHEAD];
-      float most = -INFINITY;
+  const int d = c * 128 + lane * 4;
+  float4 o = zero;
+  for (int k0 = MANY ? warp : 0; k0 < n; k0 += AHEAD * STEP) {
+    float4 x[AHEAD];
+    float2 w[AHEAD];
+    float most = -INFINITY;
 #pragma unroll
-      for (int u = 0; u < AHEAD; ++u) {
-        const int k = k0 + u * WARPS;
-        x[u] = k < n && d < a.dim ? *reinterpret_cast<const float4*>(a.part_o + part(k) * a.dim + d) : zero;
-        w[u] = k < n ? l[part(k)] : make_float2(-INFINITY, 0.f);
-        most = fmaxf(most, w[u].x);
-      }
-      o = scaled(o, raise(most));
-#pragma unroll
-      for (int u = 0; u < AHEAD; ++u) {
-        const float f = weight(w[u]);
-        total += f;
-        add(o, f, x[u]);
-      }
+    for (int u = 0; u < AHEAD; ++u) {
+      const int k = k0 + u * STEP;
+      x[u] = k < n && d < a.dim ? *reinterpret_cast<const float4*>(a.part_o + part(k) * a.dim + d) : zero;
+      w[u] = k < n ? l[part(k)] : make_float2(-INFINITY, 0.f);
+      most = fmaxf(most, w[u].x);
     }
+    o = scaled(o, raise(most));
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const float f = weight(w[u]);
+      total += f;
+      add(o, f, x[u]);
+    }
+  }
+  if constexpr (MANY) {
     sums[warp][lane] = o;
     if (lane == 0) totals[warp] = make_float2(ref, total);
     __syncthreads();
@@ -88,34 +83,10 @@ __global__ void __launch_bounds__(WARPS * 32) latent_join_kernel(const LatentArg
       total += w.y * f;
       add(o, f, sums[s][lane]);
     }
-    store(c, o);
-  } else {
-    float4 o[4] = {zero, zero, zero, zero};  // of up to 4 x 128 dims
-    for (int k0 = 0; k0 < n; k0 += 2) {
-      float4 x[2][4];
-      float2 w[2];
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const bool there = k0 + u < n;
-        w[u] = there ? l[part(k0 + u)] : make_float2(-INFINITY, 0.f);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const int d = c * 128 + lane * 4;
-          x[u][c] = there && d < a.dim ? *reinterpret_cast<const float4*>(a.part_o + part(k0 + u) * a.dim + d) : zero;
-        }
-      }
-      const float by = raise(fmaxf(w[0].x, w[1].x)), f[2] = {weight(w[0]), weight(w[1])};
-      total += f[0] + f[1];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        o[c] = scaled(o[c], by);
-        add(o[c], f[0], x[0][c]);
-        add(o[c], f[1], x[1][c]);
-      }
-    }
-#pragma unroll
-    for (int c = 0; c < 4; ++c) store(c, o[c]);
   }
+  // (0 * inf, NaN, where all scores of the row are -inf; 0 where it sees nothing)
+  if (d < a.dim) bdkv::store4<T>(dst, d, scaled(o, vis > 0 ? 1.f / total : 0.f));
+  if (c == 0 && lane == 0) bdkv::store_lse(dst, total == 0.f ? -INFINITY : ref + log2f(total));
 }
 
 }  // namespace
@@ -124,7 +95,7 @@ cudaError_t launch_latent_join(const LatentArgs& p, int sm_count, cudaStream_t s
   const int units = p.a.n_seq * p.row_tiles;
   const bool many = sm_count >= 8 * units;  // parts of a unit, on average
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(units) * (many ? p.rows * ((p.a.dim + 127) / 128) : p.rows / WARPS));
+  cfg.gridDim = dim3(static_cast<unsigned>(units) * (p.rows * ((p.a.dim + 127) / 128) / (many ? 1 : WARPS)));
   cfg.blockDim = dim3(WARPS * 32);
   cfg.stream = st;
   cudaLaunchAttribute attr[1];  // scheduled while the parts still run; it waits for them before it reads
