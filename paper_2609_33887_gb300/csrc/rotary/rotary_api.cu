@@ -70,6 +70,9 @@ int check_turned(const bdkv_rows& x, const bdkv_rows& out, int64_t heads, int64_
   if (n == 0) return BD_OK;
   if (!x.data || !out.data) return BD_ERR_NULL;
   if (int rc = check_rows_apart(out, heads, head_dim, n > 1)) return rc;
+  if (heads > 1 && n > 1 && out.stride_head > out.stride_token &&
+      out.stride_head < static_cast<__int128>(n - 1) * out.stride_token + head_dim)
+    return BD_ERR_ARG;  // a head's tokens reach into the next head's
   return same_rows(x, out, heads, n) || !rows_meet(x, heads, head_dim, out, heads, head_dim, n) ? BD_OK : BD_ERR_ARG;
 }
 
@@ -171,7 +174,7 @@ bool encode(CUtensorMap* m, const bdrot_latent& c, const void* data, const int64
             const void* any) {
   const auto f = encoder();
   if (f == nullptr) return false;
-  const cuuint64_t tok = (c.n_pages > 0 ? stride[1] : dim) * 2, page = c.n_pages > 1 ? stride[0] * 2 : tok * c.page_size;
+  const cuuint64_t tok = (c.n_pages > 0 ? stride[1] : dim) * 2, page = c.n_pages > 1 ? stride[0] * 2 : tok;  // (one page's stride says nothing)
   const cuuint64_t tokens = c.page_size, pages = std::max<int64_t>(c.n_pages, 1);
   const cuuint64_t dims[2][4] = {{static_cast<cuuint64_t>(dim), tokens, pages}, {64, tokens, static_cast<cuuint64_t>(dim / 64), pages}};
   const cuuint64_t strides[2][3] = {{tok, page}, {tok, 128, page}};

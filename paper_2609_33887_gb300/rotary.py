@@ -273,6 +273,25 @@ def kv_latent_attention_workspace(q, cache, block_table, kv_lens, query_start, *
     return int(load_library().bdrot_latent_attention_workspace(_latent_fields(cache), args))
 
 
+def _apart(q, out) -> None:
+    """Refuses an output that lies on the queries, which other rows' work still reads: exact where the two have the same
+    strides, else whether their addresses meet."""
+    (n, heads, wide), dim, (token, head, _) = q.shape, out.shape[2], q.stride()
+    if not q.numel() or not out.numel():
+        return
+
+    def end(t):
+        return t.data_ptr() + 2 * (1 + sum((s - 1) * x for s, x in zip(t.shape, t.stride())))
+
+    if q.data_ptr() >= end(out) or out.data_ptr() >= end(q):
+        return
+    if out.stride() == q.stride() and head > 0 and token % head == 0:
+        gap = (out.data_ptr() - q.data_ptr()) // 2 % head
+        if gap >= wide and gap + dim <= head:
+            return
+    raise ValueError("out must not lie on q")
+
+
 def kv_latent_attention(q: torch.Tensor, cache: KvLatent, block_table: torch.Tensor, kv_lens: torch.Tensor,
                         query_start: torch.Tensor, *, scale: float, max_q_len: int, max_kv_len: int, mask_block: int = 1,
                         return_lse: bool = False, out: Optional[torch.Tensor] = None, workspace=None, stream=None):
@@ -289,11 +308,15 @@ def kv_latent_attention(q: torch.Tensor, cache: KvLatent, block_table: torch.Ten
             out = q.new_empty((n, heads, dim))
         else:
             out, = _allocate_on(stream, lambda: (q.new_empty((n, heads, dim)),))
-    elif out.shape != (n, heads, dim) or out.dtype != q.dtype:
-        raise ValueError("out must be [tokens, heads, latent_dim] of q's type")
+        out_fields = out.data_ptr(), _DT.get(q.dtype), heads * dim, dim
+    else:
+        if out.shape != (n, heads, dim) or out.dtype != q.dtype:
+            raise ValueError("out must be [tokens, heads, latent_dim] of q's type")
+        out_fields = _out_fields(out)
+        _apart(q, out)
     lse, = _allocate_on(stream, lambda: (q.new_empty((n, heads), dtype=torch.float32),)) if return_lse else (None,)
     _same_gpu(q, out, block_table, kv_lens, query_start, *cache, *(() if workspace is None else (workspace,)))
-    args = _latent_attn_fields(q, shape, _out_fields(out), lse, cache, block_table, kv_lens, query_start, max_q_len,
+    args = _latent_attn_fields(q, shape, out_fields, lse, cache, block_table, kv_lens, query_start, max_q_len,
                                max_kv_len, scale, mask_block, workspace, stream)
     rc = load_library().bdrot_latent_attention(_latent_fields(cache), args)
     if rc != BD_OK:

@@ -125,7 +125,8 @@ def check(c, q_lens, heads, *, mask_block=1, scale=0.05, seed=0, q_mag=1.0, rows
 # --------------------------------------------------------------- attention --
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("page,heads,dim,rope", [(32, 16, 512, 64), (16, 1, 16, 16), (64, 64, 128, 32), (128, 20, 256, 48),
-                                                 (256, 128, 512, 64), (16, 7, 144, 64), (64, 33, 448, 16), (32, 65, 64, 64)])
+                                                 (256, 128, 512, 64), (16, 7, 144, 64), (64, 33, 448, 16), (32, 65, 64, 64),
+                                                 (64, 3, 64, 48), (128, 12, 192, 32)])
 def test_single_tokens(page, heads, dim, rope, dtype):
     lens = [1, 2, 15, 16, 17, 63, 64, 127, 128, 129, 255, 256, 300, 1025]
     check(Cache(lens, page, dim, rope, dtype, seed=heads), [1] * len(lens), heads, mask_block=0)
@@ -173,6 +174,37 @@ def test_caches_in_parts(q_len, total, heads):
     c = Cache([total, total // 3, 130], 64, 128, 64, "bf16", seed=6)
     check(c, [q_len] * 3, heads)
     check(Cache([total], 64, 512, 64, "f16", seed=7), [q_len], heads, mask_block=0)
+
+
+@pytest.mark.parametrize("mask_block", [0, 1, 32])
+@pytest.mark.parametrize("n_seq,q_len,heads", [(1, 90, 64), (2, 150, 16), (7, 33, 40), (19, 64, 8), (150, 1, 3), (153, 1, 3),
+                                               (31, 5, 64)])
+def test_units_in_shares(n_seq, q_len, heads, mask_block):
+    """Up to one unit of rows to an SM, whose tiles are shared out: whole units, parts that begin and end in a CTA, units over
+    many CTAs, requests without rows or without tokens between them."""
+    rng = np.random.default_rng(n_seq + q_len)
+    lens, q_lens = rng.integers(0, 1500 if n_seq < 20 else 300, n_seq), rng.integers(0, q_len + 1, n_seq)
+    lens[n_seq // 2], q_lens[n_seq // 3] = 1400, q_len
+    check(Cache(lens, 32, 64, 16, "bf16", seed=23), q_lens.tolist(), heads, mask_block=mask_block, max_q=q_len)
+
+
+def test_replayed_with_other_lengths():
+    c = Cache([900, 40, 1300, 0], 32, 128, 16, "bf16", seed=24)
+    q = torch.randn(4, 8, 144, device="cuda").to(torch.bfloat16)
+    cache, table, lens, starts = c.gpu(), ints(c.table), ints(c.lens), ints([0, 1, 2, 3, 4])
+    limits = dict(max_q_len=1, max_kv_len=1300)
+    ws = torch.empty(bdc.kv_latent_attention_workspace(q, cache, table, lens, starts, **limits), dtype=torch.uint8, device="cuda")
+    out = torch.empty(4, 8, 128, dtype=torch.bfloat16, device="cuda")
+    args = dict(scale=0.1, workspace=ws, out=out, **limits)
+    bdc.kv_latent_attention(q, cache, table, lens, starts, **args)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        bdc.kv_latent_attention(q, cache, table, lens, starts, **args)
+    for other in ([900, 40, 1300, 0], [1, 0, 64, 0], [0, 0, 0, 0], [899, 33, 65, 0]):
+        lens.copy_(ints(other))
+        graph.replay()
+        got = out.clone()
+        assert torch.equal(got, bdc.kv_latent_attention(q, cache, table, lens, starts, scale=0.1, **limits)), other
 
 
 @pytest.mark.parametrize("q_len", [1, 100])

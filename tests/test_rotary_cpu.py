@@ -151,7 +151,7 @@ def test_bad_rotations_are_refused(lib, kw, want):
     (dict(x=rows(dtype=2)), BD_ERR_DTYPE), (dict(x=rows(dtype=F16)), BD_ERR_DTYPE), (dict(x=rows(0)), BD_ERR_NULL),
     (dict(out=rows(0)), BD_ERR_NULL), (dict(pos=0), BD_ERR_NULL), (dict(pos=FAKE + 2), BD_ERR_ALIGN),
     (dict(x=rows(FAKE + 8)), BD_ERR_ALIGN), (dict(x=rows(tok=132)), BD_ERR_ALIGN), (dict(out=rows(OUT, tok=-128)), BD_ERR_SHAPE),
-    (dict(out=rows(OUT, tok=0)), BD_ERR_ARG), (dict(out=rows(OUT, head=16)), BD_ERR_ARG), (dict(out=rows(OUT, tok=120)), BD_ERR_ARG),
+    (dict(out=rows(OUT, tok=32, head=64)), BD_ERR_ARG), (dict(out=rows(OUT, tok=0)), BD_ERR_ARG), (dict(out=rows(OUT, head=16)), BD_ERR_ARG), (dict(out=rows(OUT, tok=120)), BD_ERR_ARG),
     # on x otherwise than in place
     (dict(out=rows(FAKE + 16)), BD_ERR_ARG), (dict(out=rows(FAKE + 256)), BD_ERR_ARG), (dict(out=rows(FAKE + 512)), BD_ERR_ARG),
     (dict(out=rows(FAKE - 512)), BD_ERR_ARG), (dict(out=rows(FAKE, tok=256)), BD_ERR_ARG), (dict(x=rows(tok=0), out=rows(FAKE)), BD_ERR_ARG)],
@@ -162,7 +162,7 @@ def test_rotate_refusals(lib, kw, want):
 
 def test_rotations_that_are_apart_or_in_place_reach_the_device(lib):
     refused = (BD_ERR_ARG, BD_ERR_SHAPE, BD_ERR_ALIGN, BD_ERR_NULL, BD_ERR_DTYPE, BD_OK)
-    for kw in (dict(), dict(out=rows(FAKE)), dict(x=rows(tok=0)), dict(x=rows(head=0)), dict(out=rows(FAKE + 768)),
+    for kw in (dict(), dict(out=rows(OUT, tok=32, head=96)), dict(out=rows(FAKE)), dict(x=rows(tok=0)), dict(x=rows(head=0)), dict(out=rows(FAKE + 768)),
                dict(x=rows(tok=256), out=rows(FAKE + 256, tok=256)),  # other heads of the same rows
                dict(x=rows(tok=512, head=64), out=rows(FAKE + 64, tok=512, head=64)),  # other elements of the same heads
                dict(x=rows(tok=0, head=0), out=rows(FAKE, tok=0, head=0), heads=1, n=1)):
@@ -323,6 +323,14 @@ def test_binding_checks_tensors_before_the_library(monkeypatch):
                dict(table=table.long()), dict(workspace=zeros(8, 8).t()[:, :4]), dict(cache=lat._replace(rope=lat.rope.half()))):
         with pytest.raises(ValueError):
             attend(**kw)
+    wide = zeros(4, 5, 160)
+    for out in (q[..., :64], wide[..., 32:96], zeros(8, 5, 96)[4:, :, :64]):
+        attended = wide[..., :96] if out.data_ptr() == wide[..., 32:].data_ptr() else q
+        if out.data_ptr() in (q.data_ptr(), wide[..., 32:].data_ptr()):
+            with pytest.raises(ValueError, match="lie on"):
+                attend(q=attended, out=out)
+    monkeypatch.setattr(R, "load_library", lambda: type("Library", (), {"bdrot_latent_attention": lambda *a: 0}))
+    assert attend(q=wide[..., :96], out=wide[..., 96:]).shape == (4, 5, 64)  # between the rows of the queries
     for bad in (dict(dim=24), dict(dim=0), dict(dim=32, frequencies=[1.0]), dict(dim=16, frequencies=[math.nan] * 8),
                 dict(dim=32, factor=0.0), dict(dim=32, factor=2.0, original_len=128, slow=4.0, fast=4.0)):
         with pytest.raises(ValueError):
