@@ -151,7 +151,7 @@ typedef struct {
 int bdrot_latent_attention(const bdrot_latent* cache, const bdrot_latent_attention_args* args);
 
 /* Bytes of workspace a call with these arguments needs (0 where it needs none,
- * or the arguments are invalid). Depends on sizes only. */
+ * or the arguments are invalid). Depends on sizes and the device only. */
 size_t bdrot_latent_attention_workspace(const bdrot_latent* cache, const bdrot_latent_attention_args* args);
 
 /* As bdkv_get_device_status and bdkv_shutdown, for this library. */
