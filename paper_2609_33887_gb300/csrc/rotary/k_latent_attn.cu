@@ -59,8 +59,9 @@ struct Ctl {
   float part[4][N];  // of the warps of a token quarter: maxima, at the end sums
   int visible[N];
   uint64_t out[N];   // where a row goes (0: nowhere)
-  int starts[MAX_SHARED_SEQ + 1];  // tiles of the requests before
-  int sums[16];
+  int starts[MAX_SHARED_UNITS + 1];  // tiles of the requests before
+  int first[MAX_SHARED_UNITS + 1], length[MAX_SHARED_UNITS];  // the requests' first queries and cached tokens
+  int most;                                              // tiles of a unit
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -288,30 +289,44 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
     int seq, row0, begin, end, n;  // rows from row0 on; tokens; tiles
     bool whole, first;             // of its unit; of its CTA
   };
+  const auto sequence = [&](int x) { return bdkv::make_seq(a, ctl->first[x], ctl->first[x + 1], ctl->length[x]); };
   int from = 0, to = 0;  // the CTA's share
   // the same in all lanes, and known to be: loops and products behind it then run from uniform registers
   const auto uniform = [](int x) { return static_cast<int>(bd::warp_uniform(static_cast<uint32_t>(x))); };
   Segment only;
   if (p.shared) {
+    if (tid == 0) ctl->most = 0;
+    for (int x = tid; x <= a.n_seq; x += THREADS) {
+      ctl->first[x] = a.q_start[x];
+      if (x < a.n_seq) ctl->length[x] = a.kv_lens[x];
+    }
+    __syncthreads();
     if (p.row_tiles <= 16) {
       for (int x = tid; x < a.n_seq; x += THREADS) {
-        const Seq sq = bdkv::load_seq(a, x);
-        int sum = 0;
-        for (int t = 0; t < p.row_tiles; ++t) sum += unit_tiles(sq, t);
+        const Seq sq = sequence(x);
+        int sum = 0, most = 0;
+        for (int t = 0; t < p.row_tiles; ++t) {
+          const int n = unit_tiles(sq, t);
+          sum += n, most = max(most, n);
+        }
         ctl->starts[x + 1] = sum;
+        atomicMax(&ctl->most, most);
       }
     } else {
       for (int x = warp; x < a.n_seq; x += THREADS / 32) {
-        const Seq sq = bdkv::load_seq(a, x);
-        int sum = 0;
-        for (int t = lane; t < p.row_tiles; t += 32) sum += unit_tiles(sq, t);
-        sum = __reduce_add_sync(~0u, sum);
-        if (lane == 0) ctl->starts[x + 1] = sum;
+        const Seq sq = sequence(x);
+        int sum = 0, most = 0;
+        for (int t = lane; t < p.row_tiles; t += 32) {
+          const int n = unit_tiles(sq, t);
+          sum += n, most = max(most, n);
+        }
+        sum = __reduce_add_sync(~0u, sum), most = __reduce_max_sync(~0u, most);
+        if (lane == 0) ctl->starts[x + 1] = sum, atomicMax(&ctl->most, most);
       }
     }
     __syncthreads();
     if (warp == 0) {
-      constexpr int PER = MAX_SHARED_SEQ / 32;
+      constexpr int PER = MAX_SHARED_UNITS / 32;
       int v[PER], sum = 0;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
@@ -334,8 +349,25 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
     __syncthreads();
     // (two tiles to a CTA where there are few)
     const int64_t total = ctl->starts[a.n_seq], ctas = min(static_cast<int64_t>(gridDim.x), (total + 1) / 2);
-    if (static_cast<int64_t>(blockIdx.x) >= ctas) return;
-    from = static_cast<int>(blockIdx.x * total / ctas), to = static_cast<int>((blockIdx.x + 1) * total / ctas);
+    // Parts cost their rows' results in fp32, written and read, and the join's time: a CTA to each unit (there are no more
+    // units than CTAs) where the longest has but a few tiles more than an equal share. With units of 64 rows: 150 of 2000
+    // tokens 55 us, 86 in shares; 140 of 1000 to 2000 tokens 63 and 80, but 80 of them 57 and 53; 16 of 4000 tokens 92 and
+    // 37. Of 16 rows: 140 of 1000 to 1500 tokens 49 us, 57 in shares; 60 of them 37 and 29.
+    const int64_t share = ctas > 0 ? total / ctas : 0;
+    const bool whole = ctl->most <= share + share / 4 + (N == 64 ? 8 : 3);
+    if (blockIdx.x == 0 && tid == 0) p.plan[a.n_seq * p.row_tiles] = make_int2(whole ? -1 : 0, 0);
+    if (whole) {
+      const int x = blockIdx.x / p.row_tiles, tile = blockIdx.x - x * p.row_tiles;
+      if (x >= a.n_seq) return;
+      const Seq sq = sequence(x);
+      int before = 0;
+      for (int t = lane; t < tile; t += 32) before += unit_tiles(sq, t);
+      from = ctl->starts[x] + __reduce_add_sync(~0u, before), to = from + unit_tiles(sq, tile);
+      if (to == from) return;
+    } else {
+      if (static_cast<int64_t>(blockIdx.x) >= ctas) return;
+      from = static_cast<int>(blockIdx.x * total / ctas), to = static_cast<int>((blockIdx.x + 1) * total / ctas);
+    }
   } else {
     only.seq = blockIdx.y;
     only.sq = a.longest_first ? bdkv::ranked_seq<THREADS>(a, blockIdx.y, reinterpret_cast<int*>(raw), only.seq)
@@ -366,7 +398,7 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
         }
       }
       while (ctl->starts[seq + 1] <= at) ++seq;
-      g.seq = seq, g.sq = bdkv::load_seq(a, seq);
+      g.seq = seq, g.sq = sequence(seq);
       int start = ctl->starts[seq], tile = 0, tiles = 0;
       for (int t0 = 0;; t0 += 32) {  // the unit
         const int mine = t0 + lane < p.row_tiles ? unit_tiles(g.sq, t0 + lane) : 0;
@@ -611,11 +643,9 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
     int stage = 0, tile = 0, t = 0, segments = 0;
     int at = from, seq = 0;
     Segment g = segment(at, seq), next = g;
-    if (g.n > 0) {
-      begin_queries(g);
-      end_queries();
-    }
-    for (bool more = true; more;) {
+    if (g.n > 0) begin_queries(g);
+    bool handed = g.n == 0, more = true;  // whether the queries of the segment have been handed over
+    while (more) {
       const int rows = g.sq.q_len * a.group;
       const int all_see = bdkv::visible(a, g.sq, g.row0 / a.group);  // its first row, and so all of them
       const int64_t part_row = static_cast<int64_t>(2 * blockIdx.x + !g.first) * N;
@@ -631,6 +661,7 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
       soft_sync();
       more = at < to;
       if (more) next = segment(at, seq);
+      if (!handed) end_queries();
       float2 L[COLS / 2];
 #pragma unroll
       for (int c = 0; c < COLS / 2; ++c) L[c] = make_float2(0.f, 0.f);
@@ -762,6 +793,7 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
         ++segments;
       }
       bd::tc_fence_after();
+      handed = true;
       if (more && next.n > 0) end_queries();
       for (int s = 0; s < n_pairs; ++s) {
         float o[WIDE];

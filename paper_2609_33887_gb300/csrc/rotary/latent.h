@@ -21,11 +21,12 @@ struct LatentArgs {
   int row_tiles;  // units of a request, at most
   bool shared;    // the units' tiles shared out equally (else a CTA to each unit)
   bool columns;   // the latents' map is [64 elements, token, column, page], its boxes a stage's columns of 64 tokens
-  int2* plan;     // [n_seq, row_tiles], of units that have rows: the first part of a split one (-1: it is whole) and its last CTA
+  int2* plan;     // [n_seq, row_tiles], of units that have rows: the first part of a split one (-1: it is whole) and its last
+                  // CTA; behind them -1 where no unit is split
 };
 constexpr int TOKENS = 64;           // cached tokens of a tile
 __host__ __device__ constexpr int pairs_per_stage(int n_pairs) { return n_pairs < 2 ? 1 : 2; }  // of columns of 64
-constexpr int MAX_SHARED_SEQ = 256;  // requests whose tiles are shared out, at most
+constexpr int MAX_SHARED_UNITS = 256;  // units whose tiles are shared out, at most
 cudaError_t launch_latent_attn(const LatentArgs& p, const CUtensorMap& latent, const CUtensorMap& rope, int sm_count,
                                cudaStream_t st);
 cudaError_t launch_latent_join(const LatentArgs& p, int sm_count, cudaStream_t st);

@@ -137,21 +137,21 @@ struct Plan {
   size_t bytes;       // of workspace: those, with a reference and a sum each, and two words for each unit
 };
 
-// Equal shares of all units' tiles, which each CTA adds up itself, up to one unit for each SM: lengths that the host does
-// not know then make no CTA wait for another (64 units of 57 to 8189 tokens 65 us, 75 in parts of equal lengths, two to an
-// SM). With more units a CTA to each, the longest requests first (320 units of 300 to 4001 tokens 129 us, 165 in shares,
-// whose CTAs change units more often and read less of what others read at the same time).
+// Up to one unit for each SM the CTAs add up the tiles of all units, of lengths that the host does not know, and take equal
+// shares of them, or a unit each where that is as good (64 units of 57 to 8189 tokens 70 us, a unit each 134, in parts of
+// equal lengths, two to an SM, 75). With more units a CTA to each, the longest requests first (320 units of 300 to 4001
+// tokens 129 us, 165 in shares, whose CTAs change units more often and read less of what others read at the same time).
 Plan make_plan(const bdrot_latent& c, const bdrot_latent_attention_args& a, int sms) {
   Plan p = {};
   const int64_t rows = int64_t(a.max_q_len) * a.n_heads;
   p.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
   p.row_tiles = static_cast<int>((rows + p.rows - 1) / p.rows);
   const int64_t units = int64_t(p.row_tiles) * a.n_seq, tiles = a.max_kv_len / bdrot::TOKENS + 1;
-  p.shared = units <= sms && a.n_seq <= bdrot::MAX_SHARED_SEQ && units * tiles < (int64_t(1) << 30);
+  p.shared = units <= std::min(sms, bdrot::MAX_SHARED_UNITS) && units * tiles < (int64_t(1) << 30);
   p.longest_first = !p.shared && a.n_seq > 2 && a.n_seq <= bdkv::MAX_ORDERED && units > sms;
   if (!p.shared) return p;
   p.part_rows = 2 * int64_t(sms) * p.rows;
-  p.bytes = static_cast<size_t>(p.part_rows) * (c.latent_dim + 2) * sizeof(float) + static_cast<size_t>(units) * 8;
+  p.bytes = static_cast<size_t>(p.part_rows) * (c.latent_dim + 2) * sizeof(float) + static_cast<size_t>(units + 1) * 8;
   return p;
 }
 
