@@ -61,7 +61,7 @@ struct Ctl {
   uint64_t out[N];   // where a row goes (0: nowhere)
   int starts[MAX_SHARED_UNITS + 1];  // tiles of the requests before
   int first[MAX_SHARED_UNITS + 1], length[MAX_SHARED_UNITS];  // the requests' first queries and cached tokens
-  int most;                                              // tiles of a unit
+  int most, from, to;  // tiles of a unit, at most; the CTA's share of all units' tiles
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -260,8 +260,8 @@ __device__ __forceinline__ float across_lanes(const float (&v)[COLS], int lane, 
   return w[0];
 }
 
-// N: rows of a CTA.
-template <int N>
+// N: rows of a CTA; SHARED: it takes its share of all units' tiles, else one unit.
+template <int N, bool SHARED>
 __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
     latent_attn_kernel(const LatentArgs p, const int stages, const int tiles, const __grid_constant__ CUtensorMap latent_map,
                        const __grid_constant__ CUtensorMap rope_map) {
@@ -294,7 +294,7 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
   // the same in all lanes, and known to be: loops and products behind it then run from uniform registers
   const auto uniform = [](int x) { return static_cast<int>(bd::warp_uniform(static_cast<uint32_t>(x))); };
   Segment only;
-  if (p.shared) {
+  if constexpr (SHARED) {
     if (tid == 0) ctl->most = 0;
     for (int x = tid; x <= a.n_seq; x += THREADS) {
       ctl->first[x] = a.q_start[x];
@@ -345,29 +345,32 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
       for (int i = 0; i < PER; ++i)
         if (lane * PER + i < a.n_seq) ctl->starts[lane * PER + i + 1] = before + v[i];
       if (lane == 0) ctl->starts[0] = 0;
+      __syncwarp();
+      // The CTA's share (two tiles or more, where there are few). Parts cost their rows' results in fp32, written and
+      // read, and the join's time: a CTA to each unit (there are no more units than CTAs) where the longest has but a few
+      // tiles more than an equal share. With units of 64 rows: 150 of 2000 tokens 55 us, 86 in shares; 140 of 1000 to 2000
+      // tokens 63 and 80, but 80 of them 57 and 53; 16 of 4000 tokens 92 and 37. Of 16 rows: 140 of 1000 to 1500 tokens
+      // 49 us, 57 in shares; 60 of them 37 and 29.
+      const int64_t total = ctl->starts[a.n_seq], ctas = min(static_cast<int64_t>(gridDim.x), (total + 1) / 2);
+      const int64_t share = ctas > 0 ? total / ctas : 0;
+      const bool whole = ctl->most <= share + share / 4 + (N == 64 ? 8 : 3);
+      const int x = blockIdx.x / p.row_tiles, tile = blockIdx.x - x * p.row_tiles;
+      if (whole && x < a.n_seq) {
+        const Seq sq = sequence(x);
+        int before = 0;
+        for (int t = lane; t < tile; t += 32) before += unit_tiles(sq, t);
+        from = ctl->starts[x] + __reduce_add_sync(~0u, before), to = from + unit_tiles(sq, tile);
+      } else if (!whole && static_cast<int64_t>(blockIdx.x) < ctas) {
+        from = static_cast<int>(blockIdx.x * total / ctas), to = static_cast<int>((blockIdx.x + 1) * total / ctas);
+      }
+      if (lane == 0) {
+        ctl->from = from, ctl->to = to;
+        if (blockIdx.x == 0) p.plan[a.n_seq * p.row_tiles] = make_int2(whole ? -1 : 0, 0);
+      }
     }
     __syncthreads();
-    // (two tiles to a CTA where there are few)
-    const int64_t total = ctl->starts[a.n_seq], ctas = min(static_cast<int64_t>(gridDim.x), (total + 1) / 2);
-    // Parts cost their rows' results in fp32, written and read, and the join's time: a CTA to each unit (there are no more
-    // units than CTAs) where the longest has but a few tiles more than an equal share. With units of 64 rows: 150 of 2000
-    // tokens 55 us, 86 in shares; 140 of 1000 to 2000 tokens 63 and 80, but 80 of them 57 and 53; 16 of 4000 tokens 92 and
-    // 37. Of 16 rows: 140 of 1000 to 1500 tokens 49 us, 57 in shares; 60 of them 37 and 29.
-    const int64_t share = ctas > 0 ? total / ctas : 0;
-    const bool whole = ctl->most <= share + share / 4 + (N == 64 ? 8 : 3);
-    if (blockIdx.x == 0 && tid == 0) p.plan[a.n_seq * p.row_tiles] = make_int2(whole ? -1 : 0, 0);
-    if (whole) {
-      const int x = blockIdx.x / p.row_tiles, tile = blockIdx.x - x * p.row_tiles;
-      if (x >= a.n_seq) return;
-      const Seq sq = sequence(x);
-      int before = 0;
-      for (int t = lane; t < tile; t += 32) before += unit_tiles(sq, t);
-      from = ctl->starts[x] + __reduce_add_sync(~0u, before), to = from + unit_tiles(sq, tile);
-      if (to == from) return;
-    } else {
-      if (static_cast<int64_t>(blockIdx.x) >= ctas) return;
-      from = static_cast<int>(blockIdx.x * total / ctas), to = static_cast<int>((blockIdx.x + 1) * total / ctas);
-    }
+    from = uniform(ctl->from), to = uniform(ctl->to);
+    if (from == to) return;
   } else {
     only.seq = blockIdx.y;
     only.sq = a.longest_first ? bdkv::ranked_seq<THREADS>(a, blockIdx.y, reinterpret_cast<int*>(raw), only.seq)
@@ -383,7 +386,7 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
   // The segment that begins at tile `at` of the share, which `seq` (0 at first) keeps the request of; by whole warps.
   const auto segment = [&](int& at, int& seq) {
     Segment g = only;
-    if (!p.shared) {
+    if constexpr (!SHARED) {
       at = to;
     } else {
       g.first = at == from;
@@ -851,13 +854,13 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
   if (warp == VALUE_WARP) bd::tmem_dealloc(tmem, tmem_columns<N>(n_pairs));
 }
 
-template <int N>
+template <int N, bool SHARED>
 cudaError_t launch(const LatentArgs& p, const CUtensorMap& latent, const CUtensorMap& rope, int sm_count, cudaStream_t st) {
   static std::atomic<bool> ready[64];  // by device
-  if (cudaError_t e = bdkv::allow_smem(latent_attn_kernel<N>, 232448, ready); e != cudaSuccess) return e;
+  if (cudaError_t e = bdkv::allow_smem(latent_attn_kernel<N, SHARED>, 232448, ready); e != cudaSuccess) return e;
   const Layout l = layout<N>(p.a.dim);
-  const dim3 grid = p.shared ? dim3(sm_count) : dim3(p.row_tiles, p.a.n_seq);
-  latent_attn_kernel<N><<<grid, N == 64 ? 352 : 224, l.bytes, st>>>(p, l.stages, l.tiles, latent, rope);
+  const dim3 grid = SHARED ? dim3(sm_count) : dim3(p.row_tiles, p.a.n_seq);
+  latent_attn_kernel<N, SHARED><<<grid, N == 64 ? 352 : 224, l.bytes, st>>>(p, l.stages, l.tiles, latent, rope);
   return cudaGetLastError();
 }
 
@@ -865,7 +868,8 @@ cudaError_t launch(const LatentArgs& p, const CUtensorMap& latent, const CUtenso
 
 cudaError_t launch_latent_attn(const LatentArgs& p, const CUtensorMap& latent, const CUtensorMap& rope, int sm_count,
                                cudaStream_t st) {
-  const auto run = p.rows == 16 ? launch<16> : p.rows == 32 ? launch<32> : launch<64>;
+  const auto run = p.shared ? (p.rows == 16 ? launch<16, true> : p.rows == 32 ? launch<32, true> : launch<64, true>)
+                            : (p.rows == 16 ? launch<16, false> : p.rows == 32 ? launch<32, false> : launch<64, false>);
   return run(p, latent, rope, sm_count, st);
 }
 
