@@ -20,14 +20,16 @@
 // Work: a unit is a request's 64 rows (or 32, 16) and the tiles that the last of
 // them sees. Each CTA takes an equal share of all units' tiles, laid one behind
 // another: the end of a unit, whole units, the beginning of another (a segment
-// each). Only the device knows the lengths, so every CTA adds them up itself. Of
-// a unit in several CTAs each leaves its part, which k_latent_join.cu joins.
-// With more than a unit to each SM a CTA takes one (see make_plan).
+// each). Only the device knows the lengths, so every CTA adds them up itself, and
+// takes one unit whole where shares would not pay. Of a unit in several CTAs each
+// leaves its part, which k_latent_join.cu joins. With more than a unit to each SM
+// a CTA takes one (see make_plan); that is a kernel of its own, as both in one
+// took 3 to 5 us longer, from the registers and the order of the code.
 //
 // 64 single tokens of 16 heads over 57 to 8189 tokens of 512 + 64 take 65 us with
 // the join: 303 MB at 6.3 TB/s between the first load and the last, 2 us before,
 // 2 after, 8 of CTAs that HBM serves later than others, 7 of the join. 32 x 5
-// drafts of 128 heads over 300 to 4001 tokens 128 us, 747 TFLOP/s (0.39 of a
+// drafts of 128 heads over 300 to 4001 tokens 125 us, 765 TFLOP/s (0.40 of a
 // library product's rate): about 2600 cycles a tile of 64 rows, of which products
 // take 1920 (64 columns leave the instructions short of shared memory: M = 64, N
 // = 64 takes 32 cycles, M = 128 48). The rest is the way round a ring of two

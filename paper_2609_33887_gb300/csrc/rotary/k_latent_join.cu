@@ -1,8 +1,10 @@
 // Joins the parts of units whose tiles went to several CTAs: the parts'
 // normalised outputs weighted by their sums of weights, brought to one reference.
-// A warp takes 128 dims of a row where units have a few parts each; where they
-// have many, eight warps share the parts. Latency: the plan, then all loads of a
-// warp at once, then the store; 512 CTAs 7 us, 64 CTAs 5 (from cold caches).
+// A warp takes 128 dims of a row; where there are so few of them that the units
+// have many parts, eight warps share the parts. Latency: the plan, then all loads
+// of a warp at once, then the store; 512 CTAs 7 us, 64 CTAs 5 (from cold caches).
+// 16 CTAs to an SM at most, each for several items: with 4, 2 us more for 80 units
+// of 64 rows; with a CTA to every eight items, 2 us more where no unit is split.
 #include <algorithm>
 
 #include "rotary/latent.h"

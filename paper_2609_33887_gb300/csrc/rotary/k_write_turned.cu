@@ -6,11 +6,13 @@
 // two pieces of a row, 16 elements each: of keys, the eight pairs that are turned together, whose sines and cosines it
 // keeps for all heads. Turned keys are rounded to their type before their magnitudes and codes are taken, so that scales
 // and codes are those of rows turned before. The next head's rows are on their way while a head's scales are agreed on.
-// 131072 tokens of 32 query heads and 2 x 8 of 128 take 507 us, 5.8 TB/s (0.86 of a copy): 206 us the keys and values alone,
-// where kv_write takes 156 and turning first 84. Few warps (two CTAs to an SM) are what bounds them. 64 tokens 10.3 us
-// (replayed from a graph), latency: slots, rows, positions and angles, the page's scale. (Threads that compute sines and cosines for each head, or read them from shared memory
-// with a thread to eight elements: 823 and 683 us for 131072 tokens of 32 + 2 x 8 heads.)
-// Pages of 256 tokens, whose runs would be four pieces to a thread, go the cache library's way, with keys turned as they are read.
+// 131072 tokens of 32 query heads and 2 x 8 of 128 take 487 us, 6.1 TB/s (0.90 of a copy): 169 us the keys and values alone,
+// where kv_write takes 152 and turning first 84; in pages of 128 and 256 tokens 192 and 276 (205 and 258). Few warps (two
+// CTAs to an SM) are what bounds them. 64 tokens 9.8 us (replayed from a graph), latency: slots, rows, positions and angles,
+// the page's scale. (Threads that compute sines and cosines for each head, or read them from shared memory with a thread to
+// eight elements: 823 and 683 us for 131072 tokens of 32 + 2 x 8 heads.)
+// A page of 256 tokens, whose runs would be four pieces to a thread, takes two CTAs, each for half of its rows, which give each
+// other their largest magnitudes (a cluster).
 #include "cache/write_rows.cuh"
 #include "rotary/rotary.cuh"
 
@@ -18,45 +20,11 @@ namespace bdrot {
 namespace {
 
 using bdkv::WRITE_THREADS;
-// Threads for which a run's rows, of up to eight pieces each, are two pieces to a thread.
+// Threads for which a run's rows, of up to eight pieces each, are two pieces to a thread, and in how many CTAs.
 constexpr int threads_for(int page_size) { return page_size <= 64 ? 256 : 512; }
+constexpr int ctas_for(int page_size) { return page_size <= 128 ? 1 : 2; }
 static_assert(WRITE_THREADS == ROTATE_THREADS, "CTAs of both kinds in one launch");
 
-// ---------------------------------------------------------------------------------------------------- large pages --
-template <class T>
-struct TurnedRows {
-  Turn turn;
-  __device__ __forceinline__ uint4 operator()(const uint16_t* p, int64_t row, int sub, int w) const {
-    const uint4 x = *reinterpret_cast<const uint4*>(p);
-    const int e = sub * 8, half = turn.dim / 2;
-    if (w != 0 || e >= turn.dim) return x;
-    const int position = turn.positions[row];
-    uint32_t u[4] = {x.x, x.y, x.z, x.w};
-    if (turn.inter) {
-#pragma unroll
-      for (int i = 0; i < 4; i += 2) {
-        const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(turn.turns + sub * 4 + i);
-        u[i] = T::from_float2(turn_pair(T::to_float2(u[i]), cos_sin(turn, f.x, position)));
-        u[i + 1] = T::from_float2(turn_pair(T::to_float2(u[i + 1]), cos_sin(turn, f.y, position)));
-      }
-    } else {
-      const bool second = e >= half;
-      const uint4 y = *reinterpret_cast<const uint4*>(second ? p - half : p + half);
-      const uint32_t v[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const ulonglong2 f = *reinterpret_cast<const ulonglong2*>(turn.turns + (second ? e - half : e) + 2 * i);
-        float2 s = cos_sin(turn, f.x, position), t = cos_sin(turn, f.y, position);
-        if (!second) s.y = -s.y, t.y = -t.y;
-        const float2 own = T::to_float2(u[i]), other = T::to_float2(v[i]);
-        u[i] = T::from_float2(make_float2(turn_one(own.x, other.x, s.x, s.y), turn_one(own.y, other.y, t.x, t.y)));
-      }
-    }
-    return make_uint4(u[0], u[1], u[2], u[3]);
-  }
-};
-
-// ---------------------------------------------------------------------------------------------------- small pages --
 // A piece: 16 elements of a row, in two groups of eight.
 struct Piece {
   uint4 a, b;
@@ -79,14 +47,21 @@ __device__ __forceinline__ uint32_t rescaled(uint32_t x, float g) {
   return e4m3x4(scaled(bdkv::F16::to_float2(lo), g), scaled(bdkv::F16::to_float2(hi), g));
 }
 
-template <class T, bool INTER, int THREADS>
+template <class T, bool INTER, int THREADS, int CTAS>
 __device__ __forceinline__ void write_turned(const bdkv::WriteArgs& a, const Turn& turn, int heads, uint32_t block) {
   using namespace bdkv;
   constexpr uint32_t INF = std::is_same<T, bdkv::Bf16>::value ? 0x7f80u : 0x7c00u;
-  constexpr int WARPS = THREADS / 32, PAGE = THREADS / 4;
+  constexpr int WARPS = THREADS / 32, PAGE = CTAS * THREADS / 4;
   __shared__ int64_t sl[2 * PAGE + 64];   // slots, from page_size rows before the chunk to as many behind
-  __shared__ uint32_t top[2][2][WARPS];   // of the heads in turn: keys' and values' largest patterns
-  __shared__ uint8_t bad[PAGE];      // a run's rows with something that is not finite
+  __shared__ uint32_t top[2][2][CTAS * WARPS];  // of the heads in turn: keys' and values' largest patterns, of all CTAs' warps
+  __shared__ uint8_t bad[PAGE];                 // a run's rows with something that is not finite
+  const int rank = CTAS == 1 ? 0 : static_cast<int>(bd::cluster_ctarank());
+  const auto sync = [] {
+    if constexpr (CTAS == 1)
+      __syncthreads();
+    else
+      bd::cluster_sync_all();
+  };
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, page_size = a.c.page_size;
   const int groups = (a.c.n_heads + heads - 1) / heads;
   const int h0 = static_cast<int>(block % groups) * heads, h_end = min(h0 + heads, a.c.n_heads);
@@ -96,7 +71,7 @@ __device__ __forceinline__ void write_turned(const bdkv::WriteArgs& a, const Tur
     const int64_t s = r >= 0 && r < a.n_tokens ? a.slots[r] : -1;
     sl[i] = s < a.n_slots ? s : -1;
   }
-  __syncthreads();
+  sync();
   uint64_t starts = 0;  // rows of the chunk that start a run
 #pragma unroll
   for (int part = 0; part < 2; ++part) {
@@ -117,6 +92,7 @@ __device__ __forceinline__ void write_turned(const bdkv::WriteArgs& a, const Tur
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     t_of[i] = (tid + i * THREADS) / units, u_of[i] = tid + i * THREADS - t_of[i] * units;
+    if (CTAS > 1) t_of[i] = t_of[i] < PAGE / CTAS ? t_of[i] + rank * (PAGE / CTAS) : PAGE;
     const bool halves = !INTER && u_of[i] * 16 < turn.dim;
     e0[i] = halves ? u_of[i] * 8 : u_of[i] * 16, e1[i] = halves ? turn.dim / 2 + u_of[i] * 8 : u_of[i] * 16 + 8;
   }
@@ -166,17 +142,31 @@ __device__ __forceinline__ void write_turned(const bdkv::WriteArgs& a, const Tur
         x[i] = k[i], y[i] = v[i];
         if (u_of[i] * 16 < turn.dim) turn8<T, INTER>(x[i].a, x[i].b, cs[i]);
       }
-      uint32_t k_top = max(top_of(x[0]), top_of(x[1])), v_top = max(top_of(y[0]), top_of(y[1]));
-      const auto agree = [&](uint32_t k_most, uint32_t v_most) {
-        const uint32_t k_warp = __reduce_max_sync(~0u, k_most), v_warp = __reduce_max_sync(~0u, v_most);
-        if (lane == 0) top[buf][0][warp] = k_warp, top[buf][1][warp] = v_warp;
+      uint32_t k_top = max(top_of(x[0]), top_of(x[1])), v_top = max(top_of(y[0]), top_of(y[1])), k_most, v_most;
+      const auto give = [&] {
+        const uint32_t k_warp = __reduce_max_sync(~0u, k_top), v_warp = __reduce_max_sync(~0u, v_top);
+        if (lane != 0) return;
+        uint32_t* mine = &top[buf][0][rank * WARPS + warp];
+        mine[0] = k_warp, mine[CTAS * WARPS] = v_warp;
+        if constexpr (CTAS > 1) {
+          const uint32_t other = bd::mapa_shared(bd::smem_u32(mine), rank ^ 1);
+          asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(other), "r"(k_warp) : "memory");
+          asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(other + CTAS * WARPS * 4), "r"(v_warp) : "memory");
+        }
       };
-      agree(k_top, v_top);
+      const auto take = [&] {
+        k_most = v_most = 0;
+#pragma unroll
+        for (int i = 0; i < CTAS * WARPS; ++i) k_most = max(k_most, top[buf][0][i]), v_most = max(v_most, top[buf][1][i]);
+      };
+      give();
       if (h + 1 < h_end) load(h + 1);
-      const bool some_bad = __syncthreads_or(k_top >= INF || v_top >= INF);
+      sync();
+      take();
+      const bool some_bad = max(k_most, v_most) >= INF;
       if (some_bad) {  // such rows do not count for either tensor's scale: find them, and the largest of the others
         if (tid < page_size) bad[tid] = 0;
-        __syncthreads();
+        sync();
 #pragma unroll
         for (int i = 0; i < 2; ++i)
           if (top_of(x[i]) >= INF || top_of(y[i]) >= INF) bad[t_of[i]] = 1;
@@ -185,12 +175,10 @@ __device__ __forceinline__ void write_turned(const bdkv::WriteArgs& a, const Tur
 #pragma unroll
         for (int i = 0; i < 2; ++i)
           if (live[i] && !bad[t_of[i]]) k_top = max(k_top, top_of(x[i])), v_top = max(v_top, top_of(y[i]));
-        agree(k_top, v_top);
-        __syncthreads();
+        give();
+        sync();
+        take();
       }
-      uint32_t k_most = 0, v_most = 0;
-#pragma unroll
-      for (int i = 0; i < WARPS; ++i) k_most = max(k_most, top[buf][0][i]), v_most = max(v_most, top[buf][1][i]);
       const int k_e = max(scale_byte(T::to_float2(k_most).x), k_before), v_e = max(scale_byte(T::to_float2(v_most).x), v_before);
       const float k_f = pow2i(127 - k_e), v_f = pow2i(127 - v_e);
       uint8_t* k_codes = a.c.k + page * a.c.k_stride[0] + h * a.c.k_stride[2];
@@ -216,7 +204,7 @@ __device__ __forceinline__ void write_turned(const bdkv::WriteArgs& a, const Tur
       // the tokens that the page holds already
       const auto again = [&](uint8_t* codes, int64_t cell, int before, int e) {
         const float g = before - e < -126 ? 0.f : pow2i(before - e);
-        for (int i = tid; i < off * units; i += THREADS) {
+        for (int i = rank * THREADS + tid; i < off * units; i += CTAS * THREADS) {
           uint4* p = reinterpret_cast<uint4*>(codes + i / units * cell + i % units * 16);
           const uint4 w = *p;
           *p = make_uint4(rescaled(w.x, g), rescaled(w.y, g), rescaled(w.z, g), rescaled(w.w, g));
@@ -224,34 +212,26 @@ __device__ __forceinline__ void write_turned(const bdkv::WriteArgs& a, const Tur
       };
       if (off != 0 && k_e > k_before) again(k_codes, a.c.k_stride[1], k_before, k_e);
       if (off != 0 && v_e > v_before) again(v_codes, a.c.v_stride[1], v_before, v_e);
-      if (tid == 0) {  // (read by all before the barrier above)
+      if (tid == 0 && rank == 0) {  // (read by all before the barrier above)
         if (k_e != k_before) *k_scale = static_cast<uint8_t>(k_e);
         if (v_e != v_before) *v_scale = static_cast<uint8_t>(v_e);
       }
       if (some_bad) __syncthreads();  // `bad` is free again; `top` alternates
     }
   }
+  if constexpr (CTAS > 1) bd::cluster_sync_all();  // (the other may still write here)
 }
 
-template <class T, int THREADS>
+template <class T, int THREADS, int CTAS>
 __global__ void __launch_bounds__(THREADS, 512 / THREADS)
     write_turned_kernel(bdkv::WriteArgs a, Turn turn, int heads, uint32_t writes, RotateArgs q) {
   constexpr uint32_t PER = THREADS / ROTATE_THREADS;  // blocks of rows of queries
   if (blockIdx.x >= writes)
     rotate_rows<T, 4>(q, (blockIdx.x - writes) * PER + threadIdx.x / ROTATE_THREADS, threadIdx.x % ROTATE_THREADS);
   else if (turn.inter)
-    write_turned<T, true, THREADS>(a, turn, heads, blockIdx.x);
+    write_turned<T, true, THREADS, CTAS>(a, turn, heads, blockIdx.x / CTAS);
   else
-    write_turned<T, false, THREADS>(a, turn, heads, blockIdx.x);
-}
-
-template <class T>
-__global__ void __launch_bounds__(WRITE_THREADS, 3)
-    write_turned_large_kernel(bdkv::WriteArgs a, Turn turn, uint32_t writes, RotateArgs q) {
-  if (blockIdx.x >= writes)
-    rotate_rows<T, 2>(q, blockIdx.x - writes, threadIdx.x);
-  else
-    bdkv::write_rows<T>(a, TurnedRows<T>{turn}, blockIdx.x);
+    write_turned<T, false, THREADS, CTAS>(a, turn, heads, blockIdx.x / CTAS);
 }
 
 }  // namespace
@@ -263,24 +243,27 @@ cudaError_t launch_write(const bdkv_cache& c, const bdkv_rows& k, const bdkv_row
   const bdkv::WriteArgs a = bdkv::write_args(c, k, v, slot_map, n_tokens, sm_count, &writes);
   const RotateArgs r = q != nullptr ? *q : RotateArgs{};
   const bool bf16 = k.dtype == BDKV_BF16;
-  if (c.page_size > 128) {
-    if (writes + q_blocks > INT32_MAX) return cudaErrorInvalidValue;
-    const auto kernel = bf16 ? write_turned_large_kernel<Bf16> : write_turned_large_kernel<F16>;
-    kernel<<<static_cast<unsigned>(writes + q_blocks), WRITE_THREADS, 0, st>>>(a, turn, static_cast<uint32_t>(writes), r);
-    return cudaGetLastError();
-  }
   // heads of a CTA: as many as leave eight CTAs to each SM
   const int64_t chunks = writes / c.n_heads;
   int heads = c.n_heads;
   while (heads > 1 && chunks * ((c.n_heads + heads - 1) / heads) < 8 * sm_count) heads = (heads + 1) / 2;
-  writes = chunks * ((c.n_heads + heads - 1) / heads);
-  const int threads = threads_for(c.page_size), per = threads / ROTATE_THREADS;
-  const int64_t grid = writes + (q_blocks + per - 1) / per;
+  const int threads = threads_for(c.page_size), per = threads / ROTATE_THREADS, ctas = ctas_for(c.page_size);
+  writes = chunks * ((c.n_heads + heads - 1) / heads) * ctas;
+  const int64_t rest = (q_blocks + per - 1) / per, grid = writes + (rest + ctas - 1) / ctas * ctas;
   if (grid > INT32_MAX) return cudaErrorInvalidValue;
-  const auto kernel = threads == 256 ? (bf16 ? write_turned_kernel<Bf16, 256> : write_turned_kernel<F16, 256>)
-                                     : (bf16 ? write_turned_kernel<Bf16, 512> : write_turned_kernel<F16, 512>);
-  kernel<<<static_cast<unsigned>(grid), threads, 0, st>>>(a, turn, heads, static_cast<uint32_t>(writes), r);
-  return cudaGetLastError();
+  const auto kernel = ctas == 2        ? (bf16 ? write_turned_kernel<Bf16, 512, 2> : write_turned_kernel<F16, 512, 2>)
+                      : threads == 512 ? (bf16 ? write_turned_kernel<Bf16, 512, 1> : write_turned_kernel<F16, 512, 1>)
+                                       : (bf16 ? write_turned_kernel<Bf16, 256, 1> : write_turned_kernel<F16, 256, 1>);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(grid));
+  cfg.blockDim = dim3(threads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = ctas, attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = ctas > 1;
+  return cudaLaunchKernelEx(&cfg, kernel, a, turn, heads, static_cast<uint32_t>(writes), r);
 }
 
 }  // namespace bdrot

@@ -188,6 +188,17 @@ def test_units_in_shares(n_seq, q_len, heads, mask_block):
     check(Cache(lens, 32, 64, 16, "bf16", seed=23), q_lens.tolist(), heads, mask_block=mask_block, max_q=q_len)
 
 
+@pytest.mark.parametrize("n_seq,q_len,heads,lo,hi", [(1, 140, 64, 3000, 3000), (1, 100, 64, 4000, 4000), (15, 5, 128, 2000, 2000),
+                                                     (15, 5, 128, 100, 4000), (140, 1, 16, 1000, 1500), (60, 1, 16, 1000, 1500),
+                                                     (3, 40, 16, 500, 5000)])
+def test_whole_units_where_lengths_are_alike_and_parts_where_not(n_seq, q_len, heads, lo, hi):
+    rng = np.random.default_rng(hi)
+    lens, q_lens = rng.integers(lo, hi + 1, n_seq), np.full(n_seq, q_len)
+    if n_seq > 1:
+        lens[n_seq // 3], q_lens[n_seq // 2] = 0, 0
+    check(Cache(lens, 64, 64, 16, "bf16", seed=25), q_lens.tolist(), heads, max_q=q_len)
+
+
 def test_replayed_with_other_lengths():
     c = Cache([900, 40, 1300, 0], 32, 128, 16, "bf16", seed=24)
     q = torch.randn(4, 8, 144, device="cuda").to(torch.bfloat16)

@@ -235,6 +235,22 @@ def test_writes_of_what_is_not_finite_and_of_what_overflows(interleaved):
     check_write(64, [100, 50], [60, 20], 2, 64, 32, 2, "bf16", interleaved, edit)
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("page,n_kv,dim,n", [(16, 8, 64, 5000), (64, 8, 128, 20000), (128, 5, 80, 40000), (256, 8, 128, 20000),
+                                             (256, 3, 48, 60000)])
+def test_many_rows_with_some_that_are_not_finite(page, n_kv, dim, n, interleaved):
+    """Calls in which a block takes several heads one after another; requests begin inside pages."""
+    def edit(qkv, slots):
+        rng = np.random.default_rng(page)
+        for value in (math.nan, math.inf, -math.inf):
+            where = torch.from_numpy(rng.integers(0, len(slots), 40))
+            qkv[where, torch.from_numpy(rng.integers(1, 1 + 2 * n_kv, 40)), torch.from_numpy(rng.integers(0, dim, 40))] = value
+        slots[rng.integers(0, len(slots), 40)] = -1
+        qkv[torch.from_numpy(rng.integers(0, len(slots), 9))] *= 1000.0
+    lens = [n // 3 + 77, n // 3 + 130, n // 3 - 1, 300]
+    check_write(page, lens, [n // 3, n // 3, n // 3 - 1, 1], n_kv, dim, dim, 1, "bf16", interleaved, edit)
+
+
 def test_queries_in_place_next_to_their_keys():
     qkv, q, k, v, slots, pos, rotary = check_write(32, [40, 70], [40, 33], 2, 64, 64, 4, "bf16", False)
     ref, keys = bdc.kv_rotate(q, pos, rotary), k.clone()
