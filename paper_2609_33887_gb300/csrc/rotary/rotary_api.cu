@@ -138,9 +138,10 @@ struct Plan {
 };
 
 // Up to one unit for each SM the CTAs add up the tiles of all units, of lengths that the host does not know, and take equal
-// shares of them, or a unit each where that is as good (64 units of 57 to 8189 tokens 70 us, a unit each 134, in parts of
+// shares of them, or a unit each where that is as good (64 units of 57 to 8189 tokens 66 us, a unit each 134, in parts of
 // equal lengths, two to an SM, 75). With more units a CTA to each, the longest requests first (320 units of 300 to 4001
-// tokens 129 us, 165 in shares, whose CTAs change units more often and read less of what others read at the same time).
+// tokens 125 us; in shares, whose CTAs change units more often and read less of what others read at the same time, 165 when
+// this took 129).
 Plan make_plan(const bdrot_latent& c, const bdrot_latent_attention_args& a, int sms) {
   Plan p = {};
   const int64_t rows = int64_t(a.max_q_len) * a.n_heads;

@@ -283,3 +283,27 @@ def test_captured_and_replayed_on_a_stream_of_its_own():
     assert all(torch.equal(a, b) for a, b in zip(cache, other))
     with torch.cuda.stream(stream):
         assert torch.equal(bdc.kv_rotate(x, positions, rotary, stream=stream), want)
+
+
+@pytest.mark.parametrize("page", [64, 256])
+def test_writes_replayed_with_other_rows_and_slots(page):
+    n, rotary = 700, bdc.kv_rotary(96, interleaved=True)
+    x, positions, slots = rows(n, 7, 96, "f16"), ints(np.arange(n)), torch.arange(n, device="cuda")
+    cache, q_out = bdc.kv_cache(2048 // page, page, 3, 96), torch.empty_like(x[:, :1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        bdc.kv_write_rotated(x[:, 1:4], x[:, 4:], slots, cache, positions, rotary, q=x[:, :1], q_out=q_out)
+    rng = np.random.default_rng(page)
+    for first in (0, 700, 1348):
+        x.copy_(rows(n, 7, 96, "f16", first))
+        positions += 311
+        slots.copy_(torch.arange(first, first + n))
+        slots[torch.from_numpy(rng.integers(0, n, 5)).cuda()] = -1
+        before = [t.clone() for t in cache]
+        graph.replay()
+        torch.cuda.synchronize()
+        other = bdc.KvCache(*before)
+        turned = bdc.kv_rotate(x, positions, rotary)
+        bdc.kv_write(turned[:, 1:4], x[:, 4:], slots, other)
+        assert torch.equal(q_out, turned[:, :1])
+        assert all(torch.equal(a, b) for a, b in zip(cache, other))
