@@ -6,13 +6,14 @@
 // two pieces of a row, 16 elements each: of keys, the eight pairs that are turned together, whose sines and cosines it
 // keeps for all heads. Turned keys are rounded to their type before their magnitudes and codes are taken, so that scales
 // and codes are those of rows turned before. The next head's rows are on their way while a head's scales are agreed on.
-// 131072 tokens of 32 query heads and 2 x 8 of 128 take 487 us, 6.1 TB/s (0.90 of a copy): 169 us the keys and values alone,
-// where kv_write takes 152 and turning first 84; in pages of 128 and 256 tokens 192 and 276 (205 and 258). Few warps (two
-// CTAs to an SM) are what bounds them. 64 tokens 9.8 us (replayed from a graph), latency: slots, rows, positions and angles,
-// the page's scale. (Threads that compute sines and cosines for each head, or read them from shared memory with a thread to
-// eight elements: 823 and 683 us for 131072 tokens of 32 + 2 x 8 heads.)
-// A page of 256 tokens, whose runs would be four pieces to a thread, takes two CTAs, each for half of its rows, which give each
-// other their largest magnitudes (a cluster).
+// 131072 tokens of 32 query heads and 2 x 8 of 128 take 477 us, 6.2 TB/s (0.91 of a copy): 158 us the keys and values alone,
+// where kv_write takes 152 and turning first 84; in pages of 16, 32, 128 and 256 tokens 174, 172, 187 and 276 (377, 225, 205
+// and 258). Few warps (two CTAs to an SM) are what bounds them. 64 tokens 8.7 us (replayed from a graph), latency: slots,
+// rows, positions and angles, the page's scale. (Threads that compute sines and cosines for each head, or read them from
+// shared memory with a thread to eight elements: 823 and 683 us for 131072 tokens of 32 + 2 x 8 heads.)
+// Runs of pages of 16 and 32 tokens are the work of a few warps each, so several are done at once (one after another: 384 and
+// 225 us). A page of 256 tokens, whose runs would be four pieces to a thread, takes two CTAs, each for half of its rows, which
+// give each other their largest magnitudes (a cluster).
 #include "cache/write_rows.cuh"
 #include "rotary/rotary.cuh"
 
@@ -47,7 +48,7 @@ __device__ __forceinline__ uint32_t rescaled(uint32_t x, float g) {
   return e4m3x4(scaled(bdkv::F16::to_float2(lo), g), scaled(bdkv::F16::to_float2(hi), g));
 }
 
-template <class T, bool INTER, int THREADS, int CTAS>
+template <class T, bool INTER, int THREADS, int CTAS, bool TEAMS>
 __device__ __forceinline__ void write_turned(const bdkv::WriteArgs& a, const Turn& turn, int heads, uint32_t block) {
   using namespace bdkv;
   constexpr uint32_t INF = std::is_same<T, bdkv::Bf16>::value ? 0x7f80u : 0x7c00u;
@@ -62,7 +63,7 @@ __device__ __forceinline__ void write_turned(const bdkv::WriteArgs& a, const Tur
     else
       bd::cluster_sync_all();
   };
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, page_size = a.c.page_size;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, page_size = TEAMS ? a.c.page_size : PAGE;
   const int groups = (a.c.n_heads + heads - 1) / heads;
   const int h0 = static_cast<int>(block % groups) * heads, h_end = min(h0 + heads, a.c.n_heads);
   const int64_t r0 = static_cast<int64_t>(block / groups) * a.chunk, first = r0 - page_size;
@@ -87,20 +88,27 @@ __device__ __forceinline__ void write_turned(const bdkv::WriteArgs& a, const Tur
     starts |= static_cast<uint64_t>(__ballot_sync(~0u, begins)) << (part * 32);
   }
 
-  const int units = a.c.head_dim / 16;
+  // A run of a small page is a few warps' work (a team): several runs at once.
+  const int units = a.c.head_dim / 16, rows = page_size / CTAS;
+  const int size = TEAMS ? ((rows * units + 1) / 2 + 31) / 32 * 32 : THREADS;
+  const int teams = TEAMS ? min(THREADS / size, PAGE / page_size) : 1, team = TEAMS ? tid / size : 0, local = tid - team * size;
   int t_of[2], u_of[2], e0[2], e1[2];  // a piece's row of the run and place in it; where keys' two groups begin
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    t_of[i] = (tid + i * THREADS) / units, u_of[i] = tid + i * THREADS - t_of[i] * units;
-    if (CTAS > 1) t_of[i] = t_of[i] < PAGE / CTAS ? t_of[i] + rank * (PAGE / CTAS) : PAGE;
+    t_of[i] = (local + i * size) / units, u_of[i] = local + i * size - t_of[i] * units;
+    t_of[i] = t_of[i] < rows ? t_of[i] + rank * rows : PAGE;  // (PAGE: of no run)
     const bool halves = !INTER && u_of[i] * 16 < turn.dim;
     e0[i] = halves ? u_of[i] * 8 : u_of[i] * 16, e1[i] = halves ? turn.dim / 2 + u_of[i] * 8 : u_of[i] * 16 + 8;
   }
   int buf = 0;
-  for (; starts != 0; starts &= starts - 1) {
-    const int at = page_size + __ffsll(static_cast<long long>(starts)) - 1;
-    const int64_t slot = sl[at], page = slot >> a.shift, row = first + at;
-    const int off = static_cast<int>(slot & (page_size - 1)), n = page_size - off;
+  while (starts != 0) {
+    uint64_t mine = team < teams ? starts : 0;
+    for (int i = 0; i < team; ++i) mine &= mine - 1;  // (of several runs, the team's)
+    for (int i = 0; i < teams; ++i) starts &= starts - 1;
+    const bool some = !TEAMS || mine != 0;
+    const int at = some ? page_size + __ffsll(static_cast<long long>(mine)) - 1 : 0;
+    const int64_t slot = some ? sl[at] : 0, page = slot >> a.shift, row = first + at;
+    const int off = static_cast<int>(slot & (page_size - 1)), n = some ? page_size - off : 0;
     bool live[2];
     Piece k[2], v[2];
 #pragma unroll
@@ -142,7 +150,7 @@ __device__ __forceinline__ void write_turned(const bdkv::WriteArgs& a, const Tur
         x[i] = k[i], y[i] = v[i];
         if (u_of[i] * 16 < turn.dim) turn8<T, INTER>(x[i].a, x[i].b, cs[i]);
       }
-      uint32_t k_top = max(top_of(x[0]), top_of(x[1])), v_top = max(top_of(y[0]), top_of(y[1])), k_most, v_most;
+      uint32_t k_top = max(top_of(x[0]), top_of(x[1])), v_top = max(top_of(y[0]), top_of(y[1])), k_most, v_most, any;
       const auto give = [&] {
         const uint32_t k_warp = __reduce_max_sync(~0u, k_top), v_warp = __reduce_max_sync(~0u, v_top);
         if (lane != 0) return;
@@ -155,26 +163,32 @@ __device__ __forceinline__ void write_turned(const bdkv::WriteArgs& a, const Tur
         }
       };
       const auto take = [&] {
-        k_most = v_most = 0;
+        k_most = v_most = any = 0;
 #pragma unroll
-        for (int i = 0; i < CTAS * WARPS; ++i) k_most = max(k_most, top[buf][0][i]), v_most = max(v_most, top[buf][1][i]);
+        for (int i = 0; i < CTAS * WARPS; ++i) {
+          const uint32_t k_warp = top[buf][0][i], v_warp = top[buf][1][i];
+          if (TEAMS) any = max(any, max(k_warp, v_warp));
+          if (!TEAMS || (i * 32 >= team * size && i * 32 < team * size + size))
+            k_most = max(k_most, k_warp), v_most = max(v_most, v_warp);
+        }
+        if (!TEAMS) any = max(k_most, v_most);
       };
       give();
       if (h + 1 < h_end) load(h + 1);
       sync();
       take();
-      const bool some_bad = max(k_most, v_most) >= INF;
+      const bool some_bad = any >= INF;
       if (some_bad) {  // such rows do not count for either tensor's scale: find them, and the largest of the others
-        if (tid < page_size) bad[tid] = 0;
+        if (tid < PAGE) bad[tid] = 0;
         sync();
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-          if (top_of(x[i]) >= INF || top_of(y[i]) >= INF) bad[t_of[i]] = 1;
+          if (top_of(x[i]) >= INF || top_of(y[i]) >= INF) bad[team * page_size + t_of[i]] = 1;
         __syncthreads();
         k_top = v_top = 0;
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-          if (live[i] && !bad[t_of[i]]) k_top = max(k_top, top_of(x[i])), v_top = max(v_top, top_of(y[i]));
+          if (live[i] && !bad[team * page_size + t_of[i]]) k_top = max(k_top, top_of(x[i])), v_top = max(v_top, top_of(y[i]));
         give();
         sync();
         take();
@@ -188,7 +202,7 @@ __device__ __forceinline__ void write_turned(const bdkv::WriteArgs& a, const Tur
         if (!live[i]) continue;
         uint2 ka = codes_of<T>(x[i].a, k_f), kb = codes_of<T>(x[i].b, k_f);
         uint2 va = codes_of<T>(y[i].a, v_f), vb = codes_of<T>(y[i].b, v_f);
-        if (some_bad && bad[t_of[i]]) {
+        if (some_bad && bad[team * page_size + t_of[i]]) {
           ka.x = ka.y = kb.x = kb.y = 0x7f7f7f7fu;
           va.x = va.y = vb.x = vb.y = 0u;
         }
@@ -204,7 +218,7 @@ __device__ __forceinline__ void write_turned(const bdkv::WriteArgs& a, const Tur
       // the tokens that the page holds already
       const auto again = [&](uint8_t* codes, int64_t cell, int before, int e) {
         const float g = before - e < -126 ? 0.f : pow2i(before - e);
-        for (int i = rank * THREADS + tid; i < off * units; i += CTAS * THREADS) {
+        for (int i = rank * size + local; i < off * units; i += CTAS * size) {
           uint4* p = reinterpret_cast<uint4*>(codes + i / units * cell + i % units * 16);
           const uint4 w = *p;
           *p = make_uint4(rescaled(w.x, g), rescaled(w.y, g), rescaled(w.z, g), rescaled(w.w, g));
@@ -212,7 +226,7 @@ __device__ __forceinline__ void write_turned(const bdkv::WriteArgs& a, const Tur
       };
       if (off != 0 && k_e > k_before) again(k_codes, a.c.k_stride[1], k_before, k_e);
       if (off != 0 && v_e > v_before) again(v_codes, a.c.v_stride[1], v_before, v_e);
-      if (tid == 0 && rank == 0) {  // (read by all before the barrier above)
+      if (some && local == 0 && rank == 0) {  // (read by all before the barrier above)
         if (k_e != k_before) *k_scale = static_cast<uint8_t>(k_e);
         if (v_e != v_before) *v_scale = static_cast<uint8_t>(v_e);
       }
@@ -222,16 +236,16 @@ __device__ __forceinline__ void write_turned(const bdkv::WriteArgs& a, const Tur
   if constexpr (CTAS > 1) bd::cluster_sync_all();  // (the other may still write here)
 }
 
-template <class T, int THREADS, int CTAS>
+template <class T, int THREADS, int CTAS, bool TEAMS>
 __global__ void __launch_bounds__(THREADS, 512 / THREADS)
     write_turned_kernel(bdkv::WriteArgs a, Turn turn, int heads, uint32_t writes, RotateArgs q) {
   constexpr uint32_t PER = THREADS / ROTATE_THREADS;  // blocks of rows of queries
   if (blockIdx.x >= writes)
     rotate_rows<T, 4>(q, (blockIdx.x - writes) * PER + threadIdx.x / ROTATE_THREADS, threadIdx.x % ROTATE_THREADS);
   else if (turn.inter)
-    write_turned<T, true, THREADS, CTAS>(a, turn, heads, blockIdx.x / CTAS);
+    write_turned<T, true, THREADS, CTAS, TEAMS>(a, turn, heads, blockIdx.x / CTAS);
   else
-    write_turned<T, false, THREADS, CTAS>(a, turn, heads, blockIdx.x / CTAS);
+    write_turned<T, false, THREADS, CTAS, TEAMS>(a, turn, heads, blockIdx.x / CTAS);
 }
 
 }  // namespace
@@ -240,20 +254,25 @@ cudaError_t launch_write(const bdkv_cache& c, const bdkv_rows& k, const bdkv_row
                          int64_t n_tokens, const Turn& turn, const RotateArgs* q, int64_t q_blocks, int sm_count,
                          cudaStream_t st) {
   int64_t writes = 0;
-  const bdkv::WriteArgs a = bdkv::write_args(c, k, v, slot_map, n_tokens, sm_count, &writes);
+  bdkv::WriteArgs a = bdkv::write_args(c, k, v, slot_map, n_tokens, sm_count, &writes);
+  // rows of a CTA: 64, so that small pages make several runs, fewer while the CTAs would not fill the SMs twice
+  a.chunk = 64;
+  while (a.chunk > 1 && (n_tokens + a.chunk - 1) / a.chunk * c.n_heads < 2 * sm_count) a.chunk /= 2;
   const RotateArgs r = q != nullptr ? *q : RotateArgs{};
   const bool bf16 = k.dtype == BDKV_BF16;
   // heads of a CTA: as many as leave eight CTAs to each SM
-  const int64_t chunks = writes / c.n_heads;
+  const int64_t chunks = (n_tokens + a.chunk - 1) / a.chunk;
   int heads = c.n_heads;
   while (heads > 1 && chunks * ((c.n_heads + heads - 1) / heads) < 8 * sm_count) heads = (heads + 1) / 2;
   const int threads = threads_for(c.page_size), per = threads / ROTATE_THREADS, ctas = ctas_for(c.page_size);
   writes = chunks * ((c.n_heads + heads - 1) / heads) * ctas;
   const int64_t rest = (q_blocks + per - 1) / per, grid = writes + (rest + ctas - 1) / ctas * ctas;
   if (grid > INT32_MAX) return cudaErrorInvalidValue;
-  const auto kernel = ctas == 2        ? (bf16 ? write_turned_kernel<Bf16, 512, 2> : write_turned_kernel<F16, 512, 2>)
-                      : threads == 512 ? (bf16 ? write_turned_kernel<Bf16, 512, 1> : write_turned_kernel<F16, 512, 1>)
-                                       : (bf16 ? write_turned_kernel<Bf16, 256, 1> : write_turned_kernel<F16, 256, 1>);
+  const auto of = [&](auto bf16_kernel, auto f16_kernel) { return bf16 ? bf16_kernel : f16_kernel; };
+  const auto kernel = c.page_size > 128  ? of(write_turned_kernel<Bf16, 512, 2, false>, write_turned_kernel<F16, 512, 2, false>)
+                      : c.page_size > 64 ? of(write_turned_kernel<Bf16, 512, 1, false>, write_turned_kernel<F16, 512, 1, false>)
+                      : c.page_size > 32 ? of(write_turned_kernel<Bf16, 256, 1, false>, write_turned_kernel<F16, 256, 1, false>)
+                                         : of(write_turned_kernel<Bf16, 256, 1, true>, write_turned_kernel<F16, 256, 1, true>);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(grid));
   cfg.blockDim = dim3(threads);

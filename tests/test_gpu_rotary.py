@@ -236,10 +236,11 @@ def test_writes_of_what_is_not_finite_and_of_what_overflows(interleaved):
 
 
 @pytest.mark.parametrize("interleaved", [False, True])
-@pytest.mark.parametrize("page,n_kv,dim,n", [(16, 8, 64, 5000), (64, 8, 128, 20000), (128, 5, 80, 40000), (256, 8, 128, 20000),
-                                             (256, 3, 48, 60000)])
+@pytest.mark.parametrize("page,n_kv,dim,n", [(16, 8, 64, 20000), (16, 3, 80, 2000), (16, 8, 128, 2000), (32, 8, 48, 20000),
+                                             (32, 2, 16, 1000), (64, 8, 128, 20000), (128, 8, 64, 20000), (256, 8, 128, 20000),
+                                             (256, 3, 48, 2000)])
 def test_many_rows_with_some_that_are_not_finite(page, n_kv, dim, n, interleaved):
-    """Calls in which a block takes several heads one after another; requests begin inside pages."""
+    """Calls in which a block takes several heads one after another, and others; requests begin inside pages."""
     def edit(qkv, slots):
         rng = np.random.default_rng(page)
         for value in (math.nan, math.inf, -math.inf):
@@ -249,6 +250,20 @@ def test_many_rows_with_some_that_are_not_finite(page, n_kv, dim, n, interleaved
         qkv[torch.from_numpy(rng.integers(0, len(slots), 9))] *= 1000.0
     lens = [n // 3 + 77, n // 3 + 130, n // 3 - 1, 300]
     check_write(page, lens, [n // 3, n // 3, n // 3 - 1, 1], n_kv, dim, dim, 1, "bf16", interleaved, edit)
+
+
+@pytest.mark.parametrize("page,dim", [(16, 128), (16, 48), (32, 80), (64, 128)])
+def test_single_tokens_of_many_requests(page, dim):
+    """Blocks with far more runs than they do at once, each behind tokens that may need a larger scale."""
+    rng = np.random.default_rng(page)
+    lens = rng.integers(1, page + 4, 700)
+
+    def edit(qkv, slots):
+        qkv[torch.from_numpy(rng.integers(0, 700, 70))] *= 64.0
+        qkv[torch.from_numpy(rng.integers(0, 700, 20)), 3] = math.inf
+        slots[rng.integers(0, len(slots), 9)] = -1
+    check_write(page, lens.tolist(), [1] * 700, 8, dim, 16, 2, "bf16", False, edit)
+    check_write(page, lens.tolist(), rng.integers(0, np.minimum(lens, 9)).tolist(), 8, dim, 16, 2, "f16", True)
 
 
 def test_queries_in_place_next_to_their_keys():
