@@ -2,7 +2,7 @@
 // of the same launch.
 //
 // A CTA takes a few rows (a chunk) and some heads, one head after another, and does every run that starts among them, as
-// the cache library's write does (cache/write_rows.cuh: runs, scales, tokens that are not finite). A thread has one or
+// the cache library's write does (cache/k_write.cu: runs, scales, tokens that are not finite). A thread has one or
 // two pieces of a row, 16 elements each: of keys, the eight pairs that are turned together, whose sines and cosines it
 // keeps for all heads. Turned keys are rounded to their type before their magnitudes and codes are taken, so that scales
 // and codes are those of rows turned before. The next head's rows are on their way while a head's scales are agreed on.
