@@ -41,7 +41,6 @@ namespace {
 
 using bdkv::Seq;
 
-constexpr int MAX_STAGES = 6, MAX_TILES = 3;  // in shared memory: of latents, and of key parts
 constexpr uint32_t CHUNK = TOKENS * 128, PAIR = 2 * CHUNK;  // bytes of 64 and of 128 elements of a tile
 // A row's weights are 2^(score - reference). The reference is 2^8 below the largest score seen when it was set, and scores
 // may exceed it by 2^15 before it is set again and O rescaled: weights of 2^15 at most, which f16 holds, with 11 bits down
@@ -54,7 +53,8 @@ __device__ uint32_t g_status;  // bd::DEV_* bits
 template <int N>
 struct Ctl {
   uint64_t q_full, full[MAX_STAGES], empty[MAX_STAGES];
-  uint64_t s_full[2], p_full[2], o_done[2], segment_done, s_drain, o_drain;  // (pairs: by parity of the tile)
+  uint64_t s_full[2], segment_done, s_drain, o_drain;    // (scores: by parity of the tile)
+  uint64_t p_full[HANDOVERS], o_done[HANDOVERS];
   alignas(16) float ref[N];
   alignas(16) float factor[N];
   alignas(16) float scale[N];
@@ -445,8 +445,8 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
       bd::mbar_init(bd::smem_u32(&ctl->full[i]), 1);
       bd::mbar_init(bd::smem_u32(&ctl->empty[i]), 1);
     }
-    for (int i = 0; i < 2; ++i) {
-      bd::mbar_init(bd::smem_u32(&ctl->s_full[i]), 1);
+    for (int i = 0; i < 2; ++i) bd::mbar_init(bd::smem_u32(&ctl->s_full[i]), 1);
+    for (int i = 0; i < HANDOVERS; ++i) {
       bd::mbar_init(bd::smem_u32(&ctl->p_full[i]), SOFT_WARPS);
       bd::mbar_init(bd::smem_u32(&ctl->o_done[i]), 1);
     }
@@ -539,13 +539,17 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
     const uint32_t k_lo = bd::warp_uniform(static_cast<uint32_t>(bd::sw128_kmajor_desc(kv_at)));
     const uint32_t r_lo = bd::warp_uniform(static_cast<uint32_t>(bd::sw128_kmajor_desc(rope_at)));
     int stage = 0, round = 0, tile = 0, t = 0, segments = 0;  // (t: the CTA's tile)
+    int done = 0, turn = 0;  // of the tile two before: its place, and how often the ring has been round
     bool ok = true;
     for (int at = from, seq = 0; ok && at < to;) {
       const Segment g = segment(at, seq);
       if (g.n > 0) ok = wait(ctl->q_full, segments++);
       for (int j = 0; ok && j < g.n; ++j, ++t) {
         // over the scores of two tiles before, which have become weights
-        if (t >= 2 && !(ok = wait(ctl->p_full[t & 1], (t - 2) >> 1))) break;
+        if (t >= 2) {
+          if (!(ok = wait(ctl->p_full[done], turn))) break;
+          if (++done == tiles) done = 0, ++turn;
+        }
         const uint32_t s_at = bd::warp_uniform(tmem + (t & 1) * N);
         for (int s = 0; s < n_pairs; s += per_stage) {
           if (!(ok = wait(ctl->full[stage], round))) break;
@@ -576,12 +580,12 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
     const uint32_t issue = bd::elect_one();
     const uint32_t idesc = bd::warp_uniform(bd::idesc_f16_f32(128, N) | (a.f16 ? 0u : (1u << 7) | (1u << 10)) | A_MN_MAJOR | B_MN_MAJOR);
     const uint32_t v_lo = bd::warp_uniform(mn_low(kv_at, CHUNK)), p_lo = bd::warp_uniform(mn_low(rope_at, CHUNK));
-    int stage = 0, tile = 0, t = 0;
+    int stage = 0, tile = 0, turn = 0;  // (how often the ring has been round)
     bool ok = true;
     for (int at = from, seq = 0; ok && at < to;) {
       const Segment g = segment(at, seq);
-      for (int j = 0; j < g.n; ++j, ++t) {
-        if (!(ok = wait(ctl->p_full[t & 1], t >> 1))) break;
+      for (int j = 0; j < g.n; ++j) {
+        if (!(ok = wait(ctl->p_full[tile], turn))) break;
         bd::tc_fence_after();
         const uint32_t pd = bd::warp_uniform(p_lo + tile * (CHUNK >> 4));
         for (int s = 0; s < n_pairs; s += per_stage) {
@@ -595,8 +599,8 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
           mma_commit(issue, bd::smem_u32(&ctl->empty[stage]));
           if (++stage == stages) stage = 0;
         }
-        mma_commit(issue, bd::smem_u32(&ctl->o_done[t & 1]));
-        if (++tile == tiles) tile = 0;
+        mma_commit(issue, bd::smem_u32(&ctl->o_done[tile]));
+        if (++tile == tiles) tile = 0, ++turn;
       }
       if (g.n > 0) mma_commit(issue, bd::smem_u32(&ctl->segment_done));
     }
@@ -645,7 +649,7 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
       bd::mbar_arrive(bd::smem_u32(&ctl->q_full));
     };
     bool ok = true;
-    int stage = 0, tile = 0, t = 0, segments = 0;
+    int stage = 0, tile = 0, turn = 0, t = 0, segments = 0;
     int at = from, seq = 0;
     Segment g = segment(at, seq), next = g;
     if (g.n > 0) begin_queries(g);
@@ -720,9 +724,8 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
           for (int c = 0; c < COLS; c += 2)
             L[c / 2] = mul2(L[c / 2], make_float2(ctl->factor[col0 + c], ctl->factor[col0 + c + 1]));
           if (j > 0) {
-            // (of the last tile with its parity, three before this one, the products have ended: this one's key parts, or those
-            // of the tile before it, came in their place)
-            if (ok) ok = wait(ctl->o_done[(t - 1) & 1], (t - 1) >> 1);
+            // the tile before, in the place before
+            if (ok) ok = tile > 0 ? wait(ctl->o_done[tile - 1], turn) : wait(ctl->o_done[tiles - 1], turn - 1);
             bd::tc_fence_after();
             for (int s = 0; s < n_pairs; ++s) {
               float o[WIDE];
@@ -747,7 +750,6 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
         for (int i = 0; i < COLS / 8; ++i)
           st_shared_v4(w_at + tile * CHUNK + (((col0 / 8 + i) ^ (token & 7)) << 4), w[4 * i], w[4 * i + 1], w[4 * i + 2],
                        w[4 * i + 3]);
-        if (++tile == tiles) tile = 0;
         if (t0 + TOKENS > g.end) {
           // What a page holds behind the last token may be anything, and zero times it NaN: its latents become zeros.
           const int live = g.end - t0, units = (TOKENS - live) * 16;
@@ -764,7 +766,8 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
         fence_proxy_async();
         bd::tc_fence_before();
         __syncwarp();
-        if (lane == 0) bd::mbar_arrive(bd::smem_u32(&ctl->p_full[t & 1]));
+        if (lane == 0) bd::mbar_arrive(bd::smem_u32(&ctl->p_full[tile]));
+        if (++tile == tiles) tile = 0, ++turn;
       }
 
       // all of the segment's scores are done: the next one's queries can come

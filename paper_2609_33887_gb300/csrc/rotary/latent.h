@@ -25,6 +25,12 @@ struct LatentArgs {
                   // CTA; behind them -1 where no unit is split
 };
 constexpr int TOKENS = 64;           // cached tokens of a tile
+constexpr int MAX_STAGES = 6, MAX_TILES = 3;  // in shared memory: of latents, and of key parts
+// Barriers by which weights are handed over and values' products say that they have ended: one for each place of the ring, in
+// turn. A wait knows a phase by its parity, so a barrier must not get two phases ahead of a warp that waits for it. The loads
+// see to that: nothing of the next tile in a place comes before the values' products have read the last. (With two, by the
+// tile's parity, scores and weights could overtake the warp that issues those products in a ring of three tiles.)
+constexpr int HANDOVERS = MAX_TILES;
 __host__ __device__ constexpr int pairs_per_stage(int n_pairs) { return n_pairs < 2 ? 1 : 2; }  // of columns of 64
 constexpr int MAX_SHARED_UNITS = 256;  // units whose tiles are shared out, at most
 cudaError_t launch_latent_attn(const LatentArgs& p, const CUtensorMap& latent, const CUtensorMap& rope, int sm_count,

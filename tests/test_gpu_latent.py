@@ -334,6 +334,30 @@ def test_repeated_calls_give_the_same_bits(q_len, heads, total):
         assert torch.equal(bdc.kv_latent_attention(*args, **limits, scale=0.05, workspace=ws if i % 2 else None), first), i
 
 
+@pytest.mark.parametrize("dim,rope", [(64, 16), (128, 64), (256, 64), (512, 64)])
+@pytest.mark.parametrize("n_seq,heads,total", [(3, 16, 9000), (40, 64, 1500), (160, 16, 1100)])
+def test_rings_of_two_and_of_three_tiles(n_seq, heads, total, dim, rope):
+    """Many tiles to a CTA, with sums that are rescaled at every tile: its scores are 16 above those of the tile before."""
+    c = Cache(np.random.default_rng(n_seq).integers(total // 2, total + 1, n_seq), 64, dim, rope, "bf16", seed=26)
+    for s in range(n_seq):
+        for j in range(int(-(-c.lens[s] // 64))):
+            c.rows[c.table[s, j], :, dim:] *= 0
+            c.rows[c.table[s, j], :, dim] += j
+
+    def edit(q):
+        q[..., dim:] = 0
+        q[..., dim] = 1.0
+
+    out, lse = check(c, [1] * n_seq, heads, mask_block=0, scale=16.0, edit=edit, q_mag=0.001)
+    args = (torch.randn(n_seq, heads, dim + rope, device="cuda").to(torch.bfloat16), c.gpu(), ints(c.table), ints(c.lens),
+            torch.arange(n_seq + 1, dtype=torch.int32, device="cuda"))
+    limits = dict(scale=0.05, max_q_len=1, max_kv_len=int(c.lens.max()))
+    first = bdc.kv_latent_attention(*args, **limits)
+    for i in range(30):
+        assert torch.equal(bdc.kv_latent_attention(*args, **limits), first), i
+    assert bdc.rotary.kv_latent_device_status() == 0
+
+
 def test_workspaces():
     c = Cache([9000], 64, 128, 16, "bf16", seed=18)
     q = torch.randn(1, 4, 144, device="cuda").to(torch.bfloat16)
