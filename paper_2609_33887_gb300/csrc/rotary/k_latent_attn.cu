@@ -34,6 +34,8 @@
 // take 1920 (64 columns leave the instructions short of shared memory: M = 64, N
 // = 64 takes 32 cycles, M = 128 48). The rest is the way round a ring of two
 // tiles: values' products, 1500 cycles of load, scores, 600 of softmax.
+#include <cfloat>
+
 #include "rotary/latent.h"
 
 namespace bdrot {
@@ -46,7 +48,7 @@ constexpr uint32_t CHUNK = TOKENS * 128, PAIR = 2 * CHUNK;  // bytes of 64 and o
 // may exceed it by 2^15 before it is set again and O rescaled: weights of 2^15 at most, which f16 holds, with 11 bits down
 // to 2^-22 of that largest score's.
 constexpr float P_SHIFT = 8, P_MOST = 15;
-constexpr float NO_REF = -3.0e38f;  // no score has been seen
+constexpr float NO_REF = -FLT_MAX;  // no score has been seen; none that is finite is smaller
 
 __device__ uint32_t g_status;  // bd::DEV_* bits
 

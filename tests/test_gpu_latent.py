@@ -249,6 +249,27 @@ def test_scores_far_beyond_the_weights_range(size, dtype):
     assert torch.allclose(out[0, 0].double().cpu(), latent.mean(0), rtol=2 * U[dtype], atol=2 * U[dtype])
 
 
+@pytest.mark.parametrize("n", [1, 70, 9000])
+@pytest.mark.parametrize("key", [-1.0, -0.9375, 1.0])
+def test_scores_at_the_end_of_the_range(n, key):
+    """Scores of up to 1.0625 * 3.2e38 as powers of two, either sign, that fp32 still holds: the largest, which are equal, share
+    the weight. Their weights are 1, so a result is off by its rounding and the n - 1 additions of either sum alone."""
+    c = Cache([n], 64, 128, 16, "bf16", seed=27)
+    at = [c.rows[c.table[0, t // 64], t % 64] for t in range(n)]
+    for t, r in enumerate(at):
+        r[128:] = 0
+        r[128] = -1.0625 if t % 7 == 3 else key
+    q = torch.zeros(1, 3, 144, dtype=torch.bfloat16, device="cuda")
+    q[..., 128] = 1.0
+    scale = 3.2e38 * math.log(2)
+    out, lse = attend(c, q, [1], 3, mask_block=0, scale=scale)
+    latent = torch.stack([r[:128].double() for t, r in enumerate(at) if t % 7 != 3])
+    want, spread = latent.mean(0), latent.abs().mean(0)
+    off = (out[0].double().cpu() - want).abs()
+    assert bool((off <= U["bf16"] * want.abs() + 2 * n * 2.0 ** -23 * spread).all()), float(off.max())
+    assert torch.allclose(lse.double().cpu(), torch.full((1, 3), key * scale, dtype=torch.float64), rtol=2.0 ** -20)
+
+
 @pytest.mark.parametrize("q_len,mask_block", [(1, 1), (6, 1), (130, 1), (130, 64)])
 def test_tokens_that_are_not_finite_reach_only_the_queries_that_see_them(q_len, mask_block):
     c = Cache([200, 300], 16, 128, 32, "bf16", seed=10)
