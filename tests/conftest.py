@@ -11,3 +11,17 @@ if ROOT not in sys.path:
 def pytest_configure(config):
     config.addinivalue_line("markers", "gpu: needs a CUDA GPU (GB300, sm_103a)")
     config.addinivalue_line("markers", "slow: long-running (full-size workloads)")
+
+
+# Host tests that take calls with made-up addresses past every check, where a machine without a GPU ends them.
+MADE_UP_ADDRESSES = {"test_rotations_that_are_apart_or_in_place_reach_the_device",
+                     "test_rows_that_meet_are_found_as_a_set_of_elements_finds_them",
+                     "test_latent_writes_that_may_run_reach_the_device"}
+
+
+def pytest_runtest_setup(item):
+    if getattr(item, "originalname", item.name) in MADE_UP_ADDRESSES:
+        import torch
+
+        if torch.cuda.is_available():
+            pytest.skip("the calls would run")
