@@ -121,7 +121,10 @@ int bdrot_latent_write(const bdrot_rotary* rotary, const bdrot_latent* cache, co
  * whose scores are all -inf, workspace and bounds are those of bdkv_attention;
  * lse is float32 [tokens, n_heads] contiguous, or NULL.
  *   q      rows [token, head, latent_dim + rope_dim] of the cache's type
- *   out    rows [token, head, latent_dim] of the same type, apart from q
+ *   out    rows [token, head, latent_dim] of the same type, apart from q: rows
+ *          of the first token that lie on its queries are refused (BD_ERR_ARG);
+ *          how many tokens there are is on the device, so for the others the
+ *          caller sees to it
  * Latents of tokens that are seen by some query of the call are finite (as
  * bdrot_latent_write stores them); what is behind a request's tokens in its last
  * page may be anything. Products of 16-bit elements are exact and summed in

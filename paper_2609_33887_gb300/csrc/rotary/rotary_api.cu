@@ -302,6 +302,9 @@ int bdrot_latent_attention(const bdrot_latent* cache, const bdrot_latent_attenti
   bd::TraceRange trace("bdrot_latent_attention");
   if (int rc = check_attention(cache, args)) return rc;
   if (args->n_seq == 0 || args->max_q_len == 0) return BD_OK;
+  // (of the first token: how many there are is on the device)
+  if (rows_meet(args->q, args->n_heads, cache->latent_dim + cache->rope_dim, args->out, args->n_heads, cache->latent_dim, 1))
+    return BD_ERR_ARG;
   int sms = 0;
   if (int rc = check_device(&sms)) return rc;
   const cudaStream_t st = static_cast<cudaStream_t>(args->stream);

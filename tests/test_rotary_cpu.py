@@ -279,6 +279,29 @@ def test_attention_refusals(lib, kw, want):
     assert lib.bdrot_latent_attention(latent(), attn(**kw)) == want
 
 
+# (q: rows of 4 heads of 64 + 32 at FAKE)
+@pytest.mark.parametrize("out,meets", [((FAKE, 256, 64), True), ((FAKE, 384, 96), True), ((FAKE + 16, 384, 96), True),
+                                       ((FAKE - 16, 384, 96), True), ((FAKE + 2 * 96, 384, 96), True), ((FAKE + 2 * 320, 384, 96), True),
+                                       ((FAKE + 2 * 384, 384, 96), False), ((FAKE - 2 * 352, 384, 96), False),
+                                       ((FAKE - 2 * 344, 384, 96), True)], ids=str)
+def test_attention_onto_its_queries_is_refused(lib, out, meets):
+    args = attn(out=(out[0], BF16, *out[1:]))
+    if meets:
+        assert lib.bdrot_latent_attention(latent(), args) == BD_ERR_ARG
+    elif not torch.cuda.is_available():
+        assert lib.bdrot_latent_attention(latent(), args) not in (BD_ERR_ARG, BD_OK)
+
+
+def test_attention_between_its_queries_is_not(lib):
+    """Rows of a head's queries and its result next to each other, 96 and 64 elements."""
+    for off in range(0, 160, 8):
+        args = attn(q=(FAKE, BF16, 640, 160), out=(FAKE + 2 * off, BF16, 640, 160))
+        if off != 96:
+            assert lib.bdrot_latent_attention(latent(), args) == BD_ERR_ARG, off
+        elif not torch.cuda.is_available():
+            assert lib.bdrot_latent_attention(latent(), args) not in (BD_ERR_ARG, BD_OK)
+
+
 def test_attention_with_nothing_to_do_queues_nothing(lib):
     assert lib.bdrot_latent_attention(latent(), attn(n_seq=0, lens=0, starts=0, table=0)) == BD_OK
     assert lib.bdrot_latent_attention(latent(), attn(max_q=0)) == BD_OK
