@@ -30,8 +30,8 @@ bdrot::Turn turn_of(const bdrot_rotary& r, const int32_t* positions, bool back) 
   return t;
 }
 
-// Whether rows a [n, heads_a, dim_a] and b [n, heads_b, dim_b] share memory: exact where they have the same strides, else
-// whether their address ranges meet.
+// Whether rows a [n, heads_a, dim_a] and b [n, heads_b, dim_b] share memory: exact where they have the same strides (those of
+// one token, or of one head on either side, aside), else whether their address ranges meet.
 bool rows_meet(const bdkv_rows& a, int64_t heads_a, int64_t dim_a, const bdkv_rows& b, int64_t heads_b, int64_t dim_b,
                int64_t n) {
   using wide = __int128;
@@ -41,8 +41,8 @@ bool rows_meet(const bdkv_rows& a, int64_t heads_a, int64_t dim_a, const bdkv_ro
     return static_cast<wide>(n - 1) * r.stride_token + static_cast<wide>(heads - 1) * r.stride_head + dim;
   };
   if (delta >= span(a, heads_a, dim_a) || -delta >= span(b, heads_b, dim_b)) return false;
-  const int64_t t = a.stride_token, h = a.stride_head;
-  if ((n > 1 && t != b.stride_token) || ((heads_a > 1 || heads_b > 1) && h != b.stride_head)) return true;
+  const int64_t t = a.stride_token, h = heads_a > 1 ? a.stride_head : b.stride_head;  // (of a single head it says nothing)
+  if ((n > 1 && t != b.stride_token) || (heads_a > 1 && heads_b > 1 && h != b.stride_head)) return true;
   const auto floor_div = [](wide x, wide d) { return x >= 0 ? x / d : -((-x + d - 1) / d); };
   for (int64_t d = 1 - heads_a; d < heads_b; ++d) {  // a head of b less one of a, and k tokens: -dim_b < x + k t < dim_a?
     const wide x = delta + static_cast<wide>(d) * h;

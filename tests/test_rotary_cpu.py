@@ -203,6 +203,43 @@ def test_write_refusals(lib, kw, want):
     assert write(lib, **kw) == want
 
 
+@pytest.mark.parametrize("n_k,n_q", [(2, 1), (1, 4), (1, 1), (2, 3)])
+@pytest.mark.parametrize("single", [0, 8, 48, 4096])
+def test_the_head_stride_of_a_single_head_says_nothing(lib, n_k, n_q, single):
+    """Queries in place at every offset from keys of the same rows, on 8-element steps: refused where an element is of both."""
+    if torch.cuda.is_available():
+        pytest.skip("the calls would run")
+    tok, dim, n = 256, 32, 3
+    k = {t * tok + h * dim + e for t in range(n) for h in range(n_k) for e in range(dim)}
+    q = {t * tok + h * dim + e for t in range(n) for h in range(n_q) for e in range(dim)}
+    k_head, q_head = (single if heads == 1 else dim for heads in (n_k, n_q))
+    for off in range(-40, 41):
+        meets = any(x + 8 * off in k for x in q)
+        at = rows(FAKE + 16 * off, tok=tok, head=q_head)
+        got = write(lib, c=cache(heads=n_k), k=rows(tok=tok, head=k_head), v=rows(OUT, tok=tok, head=k_head), q=at, q_out=at, n_q=n_q, n=n)
+        assert (got == BD_ERR_ARG) == meets and got != BD_OK, off
+
+
+def test_the_binding_takes_single_heads_next_to_others(lib, monkeypatch):
+    if torch.cuda.is_available():
+        pytest.skip("the calls would run")
+    monkeypatch.setattr(R, "_same_gpu", lambda *tensors: None)
+    monkeypatch.setattr(R, "_stream_handle", lambda stream: 0)
+    turn, pos, slots = R.kv_rotary(32, device="cpu"), zeros(6, dtype=torch.int32), zeros(6, dtype=torch.int64)
+
+    def status(q, k, v):
+        with pytest.raises(BdError) as e:  # no device here
+            R.kv_write_rotated(k, v, slots, K.kv_cache(3, 16, k.shape[1], 32, device="cpu"), pos, turn, q=q, q_out=q)
+        return e.value.status
+
+    row = zeros(6, 5, 32)
+    assert status(row[:, :1], row[:, 1:3], row[:, 3:]) != BD_ERR_ARG  # one query head, two of keys
+    flat = zeros(6, 6 * 32)  # four query heads, and one of keys as [1, tokens, dim] turned round
+    q, k, v = flat[:, :128].unflatten(1, (4, 32)), flat[None, :, 128:160].transpose(0, 1), flat[None, :, 160:].transpose(0, 1)
+    assert k.stride(1) == 6 * 192 and status(q, k, v) != BD_ERR_ARG
+    assert status(q, flat[None, :, 96:128].transpose(0, 1), v) == BD_ERR_ARG
+
+
 def test_a_write_of_nothing_queues_nothing(lib):
     assert write(lib, n=0, slots=0, pos=0) == BD_OK
     assert lib.bdrot_write(None, cache(), rows(), rows(), FAKE, FAKE, 3, None, None, 0, None) == BD_ERR_NULL
