@@ -277,6 +277,20 @@ def test_queries_in_place_next_to_their_keys():
             bdc.kv_write_rotated(k, v, slots, cache, pos, rotary, q=q, q_out=out)
 
 
+@pytest.mark.parametrize("n_q,n_kv", [(1, 2), (4, 1), (1, 1)])
+def test_single_heads_in_place_next_to_others(n_q, n_kv):
+    n, dim, rotary = 50, 64, bdc.kv_rotary(64)
+    x, pos, slots = rows(n, n_q + 2 * n_kv, dim, "bf16"), ints(np.arange(n) + 7), torch.arange(n, device="cuda")
+    q, k, v = x.split([n_q, n_kv, n_kv], 1)
+    if n_kv == 1:  # a head's stride as that of a [1, tokens, dim] tensor turned round
+        k, v = (t.squeeze(1)[None].transpose(0, 1) for t in (k, v))
+    keys, ref = k.clone(), bdc.kv_rotate(q, pos, rotary)
+    one, two = bdc.kv_cache(5, 16, n_kv, dim), bdc.kv_cache(5, 16, n_kv, dim)
+    bdc.kv_write(bdc.kv_rotate(k, pos, rotary), v, slots, two)
+    assert bdc.kv_write_rotated(k, v, slots, one, pos, rotary, q=q, q_out=q) is q
+    assert torch.equal(q, ref) and torch.equal(k, keys) and all(torch.equal(a, b) for a, b in zip(one, two))
+
+
 def test_captured_and_replayed_on_a_stream_of_its_own():
     x, positions, rotary = rows(64, 8, 128, "bf16"), ints(np.arange(64)), bdc.kv_rotary(128)
     cache, slots = bdc.kv_cache(8, 16, 4, 128), torch.arange(64, device="cuda")
