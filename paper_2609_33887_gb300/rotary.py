@@ -275,8 +275,8 @@ def kv_latent_attention_workspace(q, cache, block_table, kv_lens, query_start, *
 
 def _apart(q, out) -> None:
     """Refuses an output that lies on the queries, which other rows' work still reads: exact where the two have the same
-    strides, else whether their addresses meet."""
-    (n, heads, wide), dim, (token, head, _) = q.shape, out.shape[2], q.stride()
+    strides (those of one token or one head aside), else whether their addresses meet."""
+    (n, heads, wide), dim, (token, head, _), (o_token, o_head, _) = q.shape, out.shape[2], q.stride(), out.stride()
     if not q.numel() or not out.numel():
         return
 
@@ -285,9 +285,16 @@ def _apart(q, out) -> None:
 
     if q.data_ptr() >= end(out) or out.data_ptr() >= end(q):
         return
-    if out.stride() == q.stride() and head > 0 and token % head == 0:
-        gap = (out.data_ptr() - q.data_ptr()) // 2 % head
-        if gap >= wide and gap + dim <= head:
+    if (n == 1 or token == o_token) and (heads == 1 or head == o_head):
+        gap = (out.data_ptr() - q.data_ptr()) // 2
+        if heads > 1 and head > 0 and (n == 1 or token % head == 0) and wide <= gap % head <= head - dim:
+            return  # each head's result behind its queries
+        step, most = (token, n - 1) if n > 1 and token > 0 else (1 << 62, 0)
+        for d in range(1 - heads, heads):  # a head of out less one of q, and k tokens: -dim < x + k * step < wide?
+            x = gap + d * head
+            if max(-((x + dim - 1) // step), -most) <= min((wide - 1 - x) // step, most):
+                break
+        else:
             return
     raise ValueError("out must not lie on q")
 

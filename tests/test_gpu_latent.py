@@ -324,6 +324,19 @@ def test_bounds_above_and_below_the_lengths(q_len):
     assert torch.equal(cut, attend(c, q, [q_len] * 3, 4, mask_block=0, max_kv=64)[0])
 
 
+@pytest.mark.parametrize("heads,pad", [(1, 0), (3, 24)])
+def test_results_next_to_their_queries(heads, pad):
+    c = Cache([300, 70, 129], 64, 64, 32, "bf16", seed=28)
+    rows = torch.randn(3, heads * 160 + pad, device="cuda").to(torch.bfloat16)
+    q, out = rows[:, :heads * 160].unflatten(1, (heads, 160)).split([96, 64], 2)
+    if heads == 1:
+        q, out = rows[:, :96].unsqueeze(1), rows[:, 96:].unsqueeze(1)  # a single head's stride is its width
+    kept = q.clone()
+    want, _ = attend(c, kept, [1] * 3, heads)
+    got, _ = attend(c, q, [1] * 3, heads, out=out)
+    assert got is out and torch.equal(out, want) and torch.equal(q, kept)
+
+
 def test_rows_behind_the_last_sequence_stay_as_they_are():
     c = Cache([50, 60], 16, 64, 16, "bf16", seed=15)
     q = torch.randn(10, 3, 80, device="cuda").to(torch.bfloat16)

@@ -397,6 +397,37 @@ def test_binding_checks_tensors_before_the_library(monkeypatch):
             R.kv_rotary(**bad, device="cpu")
 
 
+@pytest.mark.parametrize("n,heads,token,head", [(3, 2, 100, 40), (3, 2, 104, 52), (3, 1, 40, 24), (1, 3, 0, 44), (1, 1, 8, 8), (2, 3, 48, 200),
+                                                (4, 2, 30, 120), (3, 2, 0, 60), (3, 3, 40, 0), (5, 1, 33, 7)])
+@pytest.mark.parametrize("o_single", [None, 0, 72])
+def test_results_are_apart_from_queries_where_no_element_is_of_both(n, heads, token, head, o_single):
+    """Every offset of results of 16 elements from queries of 24. Strides that are of a single token or head are arbitrary."""
+    base = zeros(2048)
+
+    def view(at, wide, token, head):
+        return base.as_strided((n, heads, wide), (token, head, 1), at)
+
+    def elements(at, wide):
+        return {at + t * token + h * head + e for t in range(n) for h in range(heads) for e in range(wide)}
+
+    o_token, o_head = (x if o_single is None or size > 1 else o_single for x, size in ((token, n), (head, heads)))
+    for at in range(1024 - 300, 1024 + 300):
+        meets = bool(elements(1024, 24) & elements(at, 16))
+        try:
+            R._apart(view(1024, 24, token, head), view(at, 16, o_token, o_head))
+            refused = False
+        except ValueError:
+            refused = True
+        assert refused == meets, at
+
+
+def test_results_next_to_the_queries_of_a_single_head():
+    row = zeros(5, 160)
+    R._apart(row[:, :96].unsqueeze(1), row[:, 96:].unsqueeze(1))
+    with pytest.raises(ValueError, match="lie on"):
+        R._apart(row[:, :96].unsqueeze(1), row[:, 32:96].unsqueeze(1))
+
+
 def test_turns_are_the_frequencies_to_the_last_bit():
     f = [1.0, 0.5, 1e-4, 6.25, -0.25, 0.0, 1e-9, 2.0]
     turns = R.kv_rotary(16, frequencies=f, device="cpu").turns.tolist()
