@@ -82,8 +82,10 @@ def kv_rotary(dim: int, *, base: float = 10000.0, frequencies=None, factor: floa
 
     factor: contexts stretched by it. Without original_len all frequencies are divided by it. With original_len (the
     length that the model was trained on) only those that turn at most `slow` times in it; those that turn `fast` times or
-    more are kept, and in between the two are blended linearly. scale: what the rotated elements are multiplied by, 1 or
-    the amplitude that goes with the stretch."""
+    more are kept, and in between the kept share grows linearly with the number of turns: (turns - slow) / (fast - slow).
+    Models that blend by the pair's index between the two bounds instead (linearly in the logarithm of the turns) have other
+    frequencies there with the same numbers: pass theirs as `frequencies`, with factor 1. scale: what the rotated elements
+    are multiplied by, 1 or the amplitude that goes with the stretch."""
     if dim < 16 or dim % 16:
         raise ValueError("dim must be a positive multiple of 16")
     if frequencies is None:

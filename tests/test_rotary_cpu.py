@@ -397,6 +397,29 @@ def test_binding_checks_tensors_before_the_library(monkeypatch):
             R.kv_rotary(**bad, device="cpu")
 
 
+@pytest.mark.parametrize("dim,base,factor,length,slow,fast", [(64, 10000.0, 8.0, 4096, 1.0, 32.0), (128, 5e5, 40.0, 8192, 1.0, 4.0),
+                                                              (96, 10000.0, 0.5, 100, 0.0, 7.5)])
+def test_the_kept_share_of_a_band_grows_linearly_with_its_turns(dim, base, factor, length, slow, fast):
+    """Each frequency from the definition; in the middle bands far from those of a blend by the pair's index."""
+    got = R.kv_rotary(dim, base=base, factor=factor, original_len=length, slow=slow, fast=fast, device="cpu").turns.tolist()
+    middle = 0
+    for p, turns in enumerate(got):
+        f = base ** (-2 * p / dim)
+        n = length * f / (2 * math.pi)
+        kept = 0.0 if n <= slow else 1.0 if n >= fast else (n - slow) / (fast - slow)
+        want = (kept * f + (1 - kept) * f / factor) / (2 * math.pi) * 2.0 ** 64
+        assert abs(turns % 2 ** 64 - want) <= 1e-13 * want + 0.5  # (turns are whole numbers)
+        if slow > 0 and 0.05 < kept < 0.95:
+            middle += 1
+            by_index = math.log(n / slow) / math.log(fast / slow)
+            other = (by_index * f + (1 - by_index) * f / factor) / (2 * math.pi) * 2.0 ** 64
+            assert other > 1.01 * want
+            # the frequencies of such a model, given as they are
+            own = R.kv_rotary(16, frequencies=[other / 2.0 ** 64 * 2 * math.pi] * 8, device="cpu").turns[0].item()
+            assert abs(own % 2 ** 64 - other) <= 1e-13 * other + 0.5
+    assert middle >= 3 or slow == 0
+
+
 @pytest.mark.parametrize("n,heads,token,head", [(3, 2, 100, 40), (3, 2, 104, 52), (3, 1, 40, 24), (1, 3, 0, 44), (1, 1, 8, 8), (2, 3, 48, 200),
                                                 (4, 2, 30, 120), (3, 2, 0, 60), (3, 3, 40, 0), (5, 1, 33, 7)])
 @pytest.mark.parametrize("o_single", [None, 0, 72])
