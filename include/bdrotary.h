@@ -38,8 +38,9 @@ extern "C" {
  *                radians a position). position * turns modulo 2^64 is then the
  *                angle without its whole turns, exact at any position.
  *   dim          a multiple of 16, 16..256
- *   scale        finite in fp32; cosines and sines are multiplied by it (1, or the
- *                amplitude of a rotation stretched for long contexts)
+ *   scale        0, or from 2^-96 to what fp32 holds in magnitude; cosines and
+ *                sines are multiplied by it (1, or the amplitude of a rotation
+ *                stretched for long contexts)
  * Positions are int32 of any sign (one behind the last token, -1, turns its row
  * as any other). Sines and cosines are fp32, results rounded once. */
 typedef struct {

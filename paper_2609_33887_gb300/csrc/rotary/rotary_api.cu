@@ -9,12 +9,14 @@
 
 namespace {
 
+constexpr double MIN_SCALE = 0x1p-96;  // below it the sines' factor, scale * 2 pi / 2^32, leaves fp32's normal numbers
 constexpr int64_t MAX_TMA_STRIDE = int64_t(1) << 38;  // elements of 16 bits: below 2^40 bytes
 
 int check_rotary(const bdrot_rotary& r, int64_t head_dim) {
   if (r.dim < 16 || r.dim > 256 || r.dim % 16 != 0 || r.dim > head_dim) return BD_ERR_SHAPE;
   if ((r.interleaved != 0 && r.interleaved != 1) || !std::isfinite(static_cast<float>(r.scale)))
     return BD_ERR_ARG;
+  if (r.scale != 0 && std::fabs(r.scale) < MIN_SCALE) return BD_ERR_ARG;
   if (!r.turns) return BD_ERR_NULL;
   return aligned(r.turns, 16) ? BD_OK : BD_ERR_ALIGN;
 }

@@ -83,6 +83,11 @@ def test_far_and_negative_positions(scale, base, interleaved):
     check(rows(len(positions), 4, 64, "f16"), positions, 64, "f16", scale=scale, base=base, interleaved=interleaved)
 
 
+@pytest.mark.parametrize("scale", [2.0 ** -96, -1.37 * 2.0 ** -95, 1e30])
+def test_smallest_and_large_scales(scale):
+    check(rows(40, 3, 64, "bf16"), list(range(40)), 64, "bf16", scale=scale)
+
+
 def test_position_zero_leaves_rows_as_they_are():
     x = rows(9, 3, 64, "bf16")
     for inter in (False, True):

@@ -145,6 +145,17 @@ def test_bad_rotations_are_refused(lib, kw, want):
     assert latent_write(lib, rot=rotary(**kw)) == want
 
 
+@pytest.mark.parametrize("scale", [2.0 ** -97, -2.0 ** -97, 1e-37, -5e-324])
+def test_scales_whose_sines_fp32_does_not_hold_are_refused(lib, scale):
+    """A sine is its angle in 2^-32 turns times scale * 2 pi / 2^32, in two fp32 terms, which lose their bits below 2^-126."""
+    assert rotate(lib, rot=rotary(scale=scale)) == BD_ERR_ARG
+    assert write(lib, rot=rotary(scale=scale)) == BD_ERR_ARG
+    assert latent_write(lib, rot=rotary(scale=scale)) == BD_ERR_ARG
+    if not torch.cuda.is_available():
+        for fine in (0.0, 2.0 ** -96, -2.0 ** -96, 3e38):
+            assert rotate(lib, rot=rotary(scale=fine)) not in (BD_ERR_ARG, BD_OK)
+
+
 @pytest.mark.parametrize("kw,want", [
     (dict(heads=0), BD_ERR_SHAPE), (dict(heads=1025), BD_ERR_SHAPE), (dict(dim=40), BD_ERR_SHAPE), (dict(dim=1040), BD_ERR_SHAPE),
     (dict(dim=16), BD_ERR_SHAPE), (dict(n=-1), BD_ERR_SHAPE), (dict(n=1 << 31), BD_ERR_SHAPE), (dict(inverse=2), BD_ERR_ARG),
