@@ -130,6 +130,9 @@ int bdrot_latent_write(const bdrot_rotary* rotary, const bdrot_latent* cache, co
  * bdrot_latent_write stores them); what is behind a request's tokens in its last
  * page may be anything. Products of 16-bit elements are exact and summed in
  * fp32; statistics are fp32; softmax weights are rounded to the cache's type.
+ * Scores are held times log2 e, so they are infinite from 2.35e38 on, and scale
+ * times log2 e must be finite (BD_ERR_ARG). Weights are up to 2^15 before they
+ * are divided by their sum: bf16 latents of 2^113 / kv_len and more can overflow.
  * Limits: n_heads 1..1024, n_seq at most 65535, max_kv_len at most 2^30,
  * max_q_len * n_heads at most 2^26. */
 typedef struct {

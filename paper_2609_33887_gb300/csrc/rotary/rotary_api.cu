@@ -122,7 +122,7 @@ int check_attention(const bdrot_latent* cache, const bdrot_latent_attention_args
       a.max_kv_len > MAX_KV || a.max_blocks < 0 || a.table_stride < a.max_blocks || a.table_stride > MAX_STRIDE ||
       a.max_kv_len > int64_t(a.max_blocks) * c.page_size || int64_t(a.max_q_len) * a.n_heads > (1 << 26))
     return BD_ERR_SHAPE;
-  if (a.mask_block < 0 || !std::isfinite(a.scale)) return BD_ERR_ARG;
+  if (a.mask_block < 0 || !std::isfinite(a.scale * bd::LOG2E)) return BD_ERR_ARG;
   if (a.n_seq == 0 || a.max_q_len == 0) return BD_OK;
   if (!a.q.data || !a.out.data || !a.kv_lens || !a.query_start || (a.max_blocks > 0 && !a.block_table)) return BD_ERR_NULL;
   if (!aligned(a.kv_lens, 4) || !aligned(a.query_start, 4) || !aligned(a.block_table, 4) || !aligned(a.lse, 4) ||

@@ -350,6 +350,13 @@ def test_attention_between_its_queries_is_not(lib):
             assert lib.bdrot_latent_attention(latent(), args) not in (BD_ERR_ARG, BD_OK)
 
 
+@pytest.mark.parametrize("scale", [2.4e38, -3.4e38])
+def test_attention_scales_that_are_infinite_as_powers_of_two_are_refused(lib, scale):
+    assert lib.bdrot_latent_attention(latent(), attn(scale=scale)) == BD_ERR_ARG
+    if not torch.cuda.is_available():
+        assert lib.bdrot_latent_attention(latent(), attn(scale=math.copysign(2.3e38, scale))) not in (BD_ERR_ARG, BD_OK)
+
+
 def test_attention_with_nothing_to_do_queues_nothing(lib):
     assert lib.bdrot_latent_attention(latent(), attn(n_seq=0, lens=0, starts=0, table=0)) == BD_OK
     assert lib.bdrot_latent_attention(latent(), attn(max_q=0)) == BD_OK
