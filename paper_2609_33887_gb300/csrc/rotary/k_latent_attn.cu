@@ -26,10 +26,11 @@
 // a CTA takes one (see make_plan); that is a kernel of its own, as both in one
 // took 3 to 5 us longer, from the registers and the order of the code.
 //
-// 64 single tokens of 16 heads over 57 to 8189 tokens of 512 + 64 take 65 us with
-// the join: 303 MB at 6.3 TB/s between the first load and the last, 2 us before,
-// 2 after, 8 of CTAs that HBM serves later than others, 7 of the join. 32 x 5
-// drafts of 128 heads over 300 to 4001 tokens 125 us, 765 TFLOP/s (0.40 of a
+// 64 single tokens of 16 heads over 57 to 8189 tokens of 512 + 64 take 66 us with
+// the join, one behind another: 3.5 us to the first load, 46 until half of the CTAs
+// have their last tile (304 MB at 6.6 TB/s), 4 of CTAs that HBM serves later than
+// others, 2.5 of results, 5.5 of the join, 4 to the next call's start. 32 x 5
+// drafts of 128 heads over 300 to 4001 tokens 126 us, 760 TFLOP/s (0.40 of a
 // library product's rate): about 2600 cycles a tile of 64 rows, of which products
 // take 1920 (64 columns leave the instructions short of shared memory: M = 64, N
 // = 64 takes 32 cycles, M = 128 48). The rest is the way round a ring of two
@@ -354,7 +355,8 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
       // read, and the join's time: a CTA to each unit (there are no more units than CTAs) where the longest has but a few
       // tiles more than an equal share. With units of 64 rows: 150 of 2000 tokens 55 us, 86 in shares; 140 of 1000 to 2000
       // tokens 63 and 80, but 80 of them 57 and 53; 16 of 4000 tokens 92 and 37. Of 16 rows: 140 of 1000 to 1500 tokens
-      // 49 us, 57 in shares; 60 of them 37 and 29.
+      // 49 us, 57 in shares; 60 of them 37 and 29. Of 32 rows: 140 of 1000 to 1500 tokens 51 and 62, 60 of them 40 and 35, 80 of
+      // 1000 to 2000 50 and 49; but 140 of 1000 to 2000 61 and 71, and 100 of 800 to 1200 39 and 46, which this takes in shares.
       const int64_t total = ctl->starts[a.n_seq], ctas = min(static_cast<int64_t>(gridDim.x), (total + 1) / 2);
       const int64_t share = ctas > 0 ? total / ctas : 0;
       const bool whole = ctl->most <= share + share / 4 + (N == 64 ? 8 : 3);
@@ -746,6 +748,10 @@ __global__ void __launch_bounds__(N == 64 ? 352 : 224, 1)
         for (int c = 0; c < COLS / 2; ++c) {
           const float2 e = make_float2(bd::ex2_approx(x[c].x), bd::ex2_approx(x[c].y));
           L[c] = bd::add2(L[c], e);
+          // The product takes one type for both operands, so weights get the latents': 11 bits in f16, 8 in bf16, each off by half
+          // a step at most, as independent errors of a sum's terms. bf16 results, which are rounded to 8 bits anyway, are off by
+          // 2.0e-3 in the 2-norm, 1.7e-3 with weights in fp32 (f16 2.1e-4 to 2.5e-4, 2.1e-4). A second product, of what the
+          // rounding left, would bring that back for nearly half more of the products' time. The row's sum has them in fp32.
           w[c] = a.f16 ? F16::from_float2(e) : Bf16::from_float2(e);
         }
 #pragma unroll

@@ -6,11 +6,13 @@
 // two pieces of a row, 16 elements each: of keys, the eight pairs that are turned together, whose sines and cosines it
 // keeps for all heads. Turned keys are rounded to their type before their magnitudes and codes are taken, so that scales
 // and codes are those of rows turned before. The next head's rows are on their way while a head's scales are agreed on.
-// 131072 tokens of 32 query heads and 2 x 8 of 128 take 477 us, 6.2 TB/s (0.91 of a copy): 158 us the keys and values alone,
-// where kv_write takes 152 and turning first 84; in pages of 16, 32, 128 and 256 tokens 174, 172, 187 and 276 (377, 225, 205
-// and 258). Few warps (two CTAs to an SM) are what bounds them. 64 tokens 8.7 us (replayed from a graph), latency: slots,
-// rows, positions and angles, the page's scale. (Threads that compute sines and cosines for each head, or read them from
-// shared memory with a thread to eight elements: 823 and 683 us for 131072 tokens of 32 + 2 x 8 heads.)
+// 131072 tokens of 32 query heads and 2 x 8 of 128 take 477 us, 6.2 TB/s (0.91 of a copy): 158 us the keys and values alone in
+// whole pages, where kv_write takes 152 (157 from 256 requests that begin inside pages) and turning first 84; in pages of 16,
+// 32, 128 and 256 tokens 174, 172, 187 and 276 (377, 226, 205 and 258). Few warps are what bounds them: 512 threads to an SM,
+// with 128 registers each that do not quite do (48 to 56 bytes a thread are spilled, 160 where several runs are done at
+// once). 64 tokens 8.3 to 8.7 us (replayed from a graph), latency: slots, rows, positions and angles, the page's scale.
+// (Threads that compute sines and cosines for each head, or read them from shared memory with a thread to eight elements: 823
+// and 683 us for 131072 tokens of 32 + 2 x 8 heads.)
 // Runs of pages of 16 and 32 tokens are the work of a few warps each, so several are done at once (one after another: 384 and
 // 225 us). A page of 256 tokens, whose runs would be four pieces to a thread, takes two CTAs, each for half of its rows, which
 // give each other their largest magnitudes (a cluster).
